@@ -11,7 +11,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libhqmq.so")
 
 SOURCES = ["hqmq_api.hip", "hqmq_median.hip", "hqmq_search.hip", "hqmq_decode.hip", "hqmq_attend.hip",
-           "hqmq_codebook.cpp"]
+           "hqmq_shared.hip", "hqmq_mass.hip", "hqmq_evict.hip", "hqmq_codebook.cpp"]
 
 FLAGS = [
     "--offload-arch=gfx950",

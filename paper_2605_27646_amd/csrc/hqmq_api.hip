@@ -7,6 +7,7 @@
 #include <mutex>
 
 #include "hqmq_device.h"
+#include "hqmq_serve_device.h"
 
 namespace hqmq {
 
@@ -797,6 +798,19 @@ extern "C" uint64_t hqmq_attend_workspace_bytes(const hqmq_params *params, int32
         .total_bytes;
 }
 
+static AttendSide attend_side(const hqmq_encoded *e, const float *sec, uint64_t cap)
+{
+    AttendSide s;
+    s.codes = e->codes;
+    s.sigma = e->sigma;
+    s.flags = e->flags;
+    s.row_off = e->row_off;
+    s.outliers = e->outliers;
+    s.sec = sec;
+    s.outlier_capacity = cap;
+    return s;
+}
+
 static int32_t attend_impl(const hqmq_params *params, int32_t n_q_heads, const void *q_dev,
                            float scale, const hqmq_encoded *enc_k, uint64_t cap_k,
                            const float *sec_k_dev, const hqmq_encoded *enc_v, uint64_t cap_v,
@@ -827,20 +841,9 @@ static int32_t attend_impl(const hqmq_params *params, int32_t n_q_heads, const v
             return hip_failed(ready);
     }
 
-    auto side = [](const hqmq_encoded *e, const float *sec, uint64_t cap) {
-        AttendSide s;
-        s.codes = e->codes;
-        s.sigma = e->sigma;
-        s.flags = e->flags;
-        s.row_off = e->row_off;
-        s.outliers = e->outliers;
-        s.sec = sec;
-        s.outlier_capacity = cap;
-        return s;
-    };
     AttendArgs a;
-    a.k = side(enc_k, sec_k_dev, cap_k);
-    a.v = side(enc_v, sec_v_dev, cap_v);
+    a.k = attend_side(enc_k, sec_k_dev, cap_k);
+    a.v = attend_side(enc_v, sec_v_dev, cap_v);
     a.q = static_cast<const _Float16 *>(q_dev);
     a.out = static_cast<_Float16 *>(out_dev);
     a.lse = lse_dev;
@@ -850,10 +853,13 @@ static int32_t attend_impl(const hqmq_params *params, int32_t n_q_heads, const v
     a.qscale = scale * 1.44269504088896340736f;
     a.G = G;
     a.D = params->D;
-    a.n_splits = plan.n_splits;
+    a.n_splits = a.part_pitch = plan.n_splits;
+    a.split0 = 0;
     a.rows_per_split = plan.rows_per_split;
     a.joint = plan.joint;
-    hipError_t err = launch_attend(g, a, static_cast<hipStream_t>(stream));
+    hipError_t err = launch_attend_partials(g, a, static_cast<hipStream_t>(stream));
+    if (err == hipSuccess)
+        err = launch_attend_merge((int64_t)g.B * g.H * G, a, static_cast<hipStream_t>(stream));
     if (err != hipSuccess)
         return hip_failed(err);
     return HQMQ_OK;
@@ -891,4 +897,309 @@ extern "C" int32_t hqmq_attend_masked(const hqmq_params *params, int32_t n_q_hea
         return HQMQ_ERR_INVALID_ARG;
     return attend_impl(params, n_q_heads, q_dev, scale, enc_k, cap_k, sec_k_dev, enc_v, cap_v, sec_v_dev, out_dev,
                        lse_dev, visible_dev, workspace_dev, workspace_bytes, stream);
+}
+
+// ---- serving a batch from packed caches (include/hqmq_serve.h) ---------------------------------------------------------
+
+static int32_t check_share(const hqmq_params *params, int32_t n_share, int32_t n_q_heads)
+{
+    const int32_t rc = check_attend(params, n_q_heads);
+    if (rc != HQMQ_OK)
+        return rc;
+    if (n_share < 1 || n_share > HQMQ_MAX_SHARE)
+        return HQMQ_ERR_INVALID_ARG;
+    if ((int64_t)params->B * n_share * params->H > 65535)
+        return HQMQ_ERR_UNSUPPORTED;  // grid.y of the own tokens
+    return HQMQ_OK;
+}
+
+static int32_t check_own(const hqmq_params *params, int32_t n_share, const hqmq_params *own)
+{
+    const int32_t rc = check_params(own);
+    if (rc != HQMQ_OK)
+        return rc;
+    if (own->B != params->B * n_share || own->H != params->H || own->D != params->D || own->S != params->S || own->b_r != params->b_r)
+        return HQMQ_ERR_INVALID_ARG;
+    return HQMQ_OK;
+}
+
+// The partial sums of the prefix's shares, then of the own tokens': [query head][splits of both].
+struct SharedLayout {
+    SharedPlan prefix;
+    AttendPlan own;
+    uint64_t ml_bytes, total;
+    int32_t parts;
+};
+static SharedLayout shared_layout(const Geometry &g, int G, int n_share, const hqmq_params *own)
+{
+    SharedLayout l;
+    l.prefix = plan_shared(g, G, n_share);
+    l.own.n_splits = 0;
+    if (own)
+        l.own = plan_attend(make_geometry(own), G, false);
+    l.parts = l.prefix.n_splits + l.own.n_splits;
+    const uint64_t parts = (uint64_t)g.B * n_share * g.H * G * l.parts;
+    l.ml_bytes = align_up(parts * 2 * sizeof(float), 256);
+    l.total = l.ml_bytes + align_up(parts * 128 * sizeof(float), 256);
+    return l;
+}
+
+extern "C" uint64_t hqmq_attend_shared_workspace_bytes(const hqmq_params *params, int32_t n_share, int32_t n_q_heads,
+                                                       const hqmq_params *own_params)
+{
+    if (check_share(params, n_share, n_q_heads) != HQMQ_OK || (own_params && check_own(params, n_share, own_params) != HQMQ_OK))
+        return 0;
+    return shared_layout(make_geometry(params), n_q_heads / params->H, n_share, own_params).total;
+}
+
+extern "C" int32_t hqmq_attend_shared(const hqmq_params *params, int32_t n_share, int32_t n_q_heads, const void *q_dev, float scale,
+                                      const hqmq_encoded *enc_k, uint64_t cap_k, const float *sec_k_dev,
+                                      const hqmq_encoded *enc_v, uint64_t cap_v, const float *sec_v_dev,
+                                      const int32_t *visible_dev, const hqmq_own_tokens *own, void *out_dev, float *lse_dev,
+                                      void *workspace_dev, uint64_t workspace_bytes, void *stream)
+{
+    int32_t rc = check_share(params, n_share, n_q_heads);
+    if (rc != HQMQ_OK)
+        return rc;
+    if (!q_dev || !out_dev || !sec_k_dev || !sec_v_dev || !workspace_dev || !std::isfinite(scale))
+        return HQMQ_ERR_INVALID_ARG;
+    if (misaligned(q_dev, 16) || misaligned(out_dev, 16) || misaligned(sec_k_dev, 16) || misaligned(sec_v_dev, 16) ||
+        misaligned(workspace_dev, 256) || misaligned(visible_dev, 4) || misaligned(lse_dev, 4))
+        return HQMQ_ERR_INVALID_ARG;
+    rc = check_encoded(enc_k, false, cap_k);
+    if (rc == HQMQ_OK)
+        rc = check_encoded(enc_v, false, cap_v);
+    if (rc == HQMQ_OK && own) {
+        rc = check_own(params, n_share, own->params);
+        if (rc == HQMQ_OK)
+            rc = check_encoded(own->enc_k, false, own->cap_k);
+        if (rc == HQMQ_OK)
+            rc = check_encoded(own->enc_v, false, own->cap_v);
+        if (rc == HQMQ_OK && misaligned(own->visible_dev, 4))
+            rc = HQMQ_ERR_INVALID_ARG;
+    }
+    if (rc != HQMQ_OK)
+        return rc;
+    const Geometry g = make_geometry(params);
+    const int G = n_q_heads / params->H;
+    const SharedLayout l = shared_layout(g, G, n_share, own ? own->params : nullptr);
+    if (workspace_bytes < l.total)
+        return HQMQ_ERR_BUFFER_TOO_SMALL;
+    const hipError_t ready = ensure_device_setup();
+    if (ready != hipSuccess)
+        return hip_failed(ready);
+
+    float *part_ml = reinterpret_cast<float *>(workspace_dev);
+    float *part_acc = reinterpret_cast<float *>(static_cast<char *>(workspace_dev) + l.ml_bytes);
+    SharedArgs a;
+    a.k = attend_side(enc_k, sec_k_dev, cap_k);
+    a.v = attend_side(enc_v, sec_v_dev, cap_v);
+    a.q = static_cast<const _Float16 *>(q_dev);
+    a.visible = visible_dev;
+    a.part_ml = part_ml;
+    a.part_acc = part_acc;
+    a.qscale = scale * 1.44269504088896340736f;
+    a.G = G;
+    a.n_share = n_share;
+    a.n_splits = l.prefix.n_splits;
+    a.rows_per_split = l.prefix.rows_per_split;
+    a.part_pitch = l.parts;
+    hipError_t err = launch_shared(g, a, static_cast<hipStream_t>(stream));
+    if (err != hipSuccess)
+        return hip_failed(err);
+
+    AttendArgs o;
+    std::memset(&o, 0, sizeof(o));
+    o.q = a.q;
+    o.out = static_cast<_Float16 *>(out_dev);
+    o.lse = lse_dev;
+    o.part_ml = part_ml;
+    o.part_acc = part_acc;
+    o.qscale = a.qscale;
+    o.G = G;
+    o.D = params->D;
+    o.part_pitch = l.parts;
+    if (own) {
+        o.k = attend_side(own->enc_k, sec_k_dev, own->cap_k);
+        o.v = attend_side(own->enc_v, sec_v_dev, own->cap_v);
+        o.visible = own->visible_dev;
+        o.n_splits = l.own.n_splits;
+        o.split0 = l.prefix.n_splits;
+        o.rows_per_split = l.own.rows_per_split;
+        o.joint = l.own.joint;
+        err = launch_attend_partials(make_geometry(own->params), o, static_cast<hipStream_t>(stream));
+        if (err != hipSuccess)
+            return hip_failed(err);
+    }
+    err = launch_attend_merge((int64_t)g.B * n_share * g.H * G, o, static_cast<hipStream_t>(stream));
+    return err == hipSuccess ? HQMQ_OK : hip_failed(err);
+}
+
+extern "C" int32_t hqmq_attend_mass(const hqmq_params *params, int32_t n_share, int32_t n_q_heads, const void *q_dev, float scale,
+                                    const hqmq_encoded *enc_k, uint64_t cap_k, const float *sec_k_dev, const float *lse_dev,
+                                    const int32_t *visible_dev, const float *mass_in_dev, float decay, float *mass_out_dev,
+                                    void *stream)
+{
+    int32_t rc = check_share(params, n_share, n_q_heads);
+    if (rc != HQMQ_OK)
+        return rc;
+    if (!q_dev || !sec_k_dev || !lse_dev || !mass_out_dev || !std::isfinite(scale) || !std::isfinite(decay) ||
+        (decay != 0.f && !mass_in_dev))
+        return HQMQ_ERR_INVALID_ARG;
+    if (misaligned(q_dev, 16) || misaligned(sec_k_dev, 16) || misaligned(lse_dev, 4) || misaligned(visible_dev, 4) ||
+        misaligned(mass_in_dev, 4) || misaligned(mass_out_dev, 4))
+        return HQMQ_ERR_INVALID_ARG;
+    rc = check_encoded(enc_k, false, cap_k);
+    if (rc != HQMQ_OK)
+        return rc;
+    const hipError_t ready = ensure_device_setup();
+    if (ready != hipSuccess)
+        return hip_failed(ready);
+    MassArgs a;
+    a.k = attend_side(enc_k, sec_k_dev, cap_k);
+    a.q = static_cast<const _Float16 *>(q_dev);
+    a.lse = lse_dev;
+    a.visible = visible_dev;
+    a.mass_in = decay != 0.f ? mass_in_dev : nullptr;
+    a.mass_out = mass_out_dev;
+    a.qscale = scale * 1.44269504088896340736f;
+    a.decay = decay;
+    a.G = n_q_heads / params->H;
+    a.n_share = n_share;
+    const hipError_t err = launch_mass(make_geometry(params), a, static_cast<hipStream_t>(stream));
+    return err == hipSuccess ? HQMQ_OK : hip_failed(err);
+}
+
+static int32_t check_select(int32_t B, int32_t H, int32_t T, int32_t n_keep)
+{
+    if (B <= 0 || H <= 0 || T <= 0 || n_keep <= 0 || n_keep > T)
+        return HQMQ_ERR_INVALID_ARG;
+    if ((int64_t)B * H > 65535 || (uint64_t)B * H * T >= (1ull << 32))
+        return HQMQ_ERR_UNSUPPORTED;
+    return HQMQ_OK;
+}
+
+extern "C" uint64_t hqmq_evict_select_workspace_bytes(int32_t B, int32_t H, int32_t T, int32_t n_keep)
+{
+    if (check_select(B, H, T, n_keep) != HQMQ_OK)
+        return 0;
+    return 0;
+}
+
+extern "C" int32_t hqmq_evict_select(int32_t B, int32_t H, int32_t T, const float *mass_dev, const int32_t *length_dev,
+                                     int32_t n_sink, int32_t n_recent, int32_t n_keep, int32_t *keep_dev, int32_t *n_kept_dev,
+                                     float *kept_mass_dev, void *workspace_dev, uint64_t workspace_bytes, void *stream)
+{
+    const int32_t rc = check_select(B, H, T, n_keep);
+    if (rc != HQMQ_OK)
+        return rc;
+    if (n_sink < 0 || n_recent < 0 || n_sink > n_keep || n_recent > n_keep - n_sink || !mass_dev || !keep_dev || !n_kept_dev)
+        return HQMQ_ERR_INVALID_ARG;
+    if (misaligned(mass_dev, 4) || misaligned(length_dev, 4) || misaligned(keep_dev, 4) || misaligned(n_kept_dev, 4) ||
+        misaligned(kept_mass_dev, 4) || misaligned(workspace_dev, 256))
+        return HQMQ_ERR_INVALID_ARG;
+    const uint64_t need = hqmq_evict_select_workspace_bytes(B, H, T, n_keep);
+    if (need > 0 && !workspace_dev)
+        return HQMQ_ERR_INVALID_ARG;
+    if (workspace_bytes < need)
+        return HQMQ_ERR_BUFFER_TOO_SMALL;
+    SelectArgs a;
+    a.mass = mass_dev;
+    a.length = length_dev;
+    a.keep = keep_dev;
+    a.n_kept = n_kept_dev;
+    a.kept_mass = kept_mass_dev;
+    a.B = B;
+    a.H = H;
+    a.T = T;
+    a.n_sink = n_sink;
+    a.n_recent = n_recent;
+    a.n_keep = n_keep;
+    const hipError_t err = launch_evict_select(a, static_cast<hipStream_t>(stream));
+    return err == hipSuccess ? HQMQ_OK : hip_failed(err);
+}
+
+static int32_t check_compact(const hqmq_params *params, int32_t n_keep, int32_t n_tensors)
+{
+    const int32_t rc = check_params(params);
+    if (rc != HQMQ_OK)
+        return rc;
+    if (n_keep <= 0 || n_tensors <= 0)
+        return HQMQ_ERR_INVALID_ARG;
+    if ((uint64_t)params->B * params->H * n_keep * kChunksPerRow >= (1ull << 32))
+        return HQMQ_ERR_UNSUPPORTED;  // 32-bit outlier offsets of the new tensor
+    return HQMQ_OK;
+}
+
+static CompactShape compact_shape(const hqmq_params *params, int32_t n_keep)
+{
+    const Geometry g = make_geometry(params);
+    CompactShape s;
+    s.B = g.B;
+    s.H = g.H;
+    s.T = g.T;
+    s.n_keep = n_keep;
+    s.row_words = g.row_words;
+    s.blocks_per_seg = (n_keep + kCompactRows - 1) / kCompactRows;
+    s.totals = nullptr;
+    s.totals_stride = align_up((uint64_t)g.B * g.H * s.blocks_per_seg, 64);
+    return s;
+}
+
+extern "C" uint64_t hqmq_evict_compact_workspace_bytes(const hqmq_params *params, int32_t n_keep, int32_t n_tensors)
+{
+    if (check_compact(params, n_keep, n_tensors) != HQMQ_OK)
+        return 0;
+    return compact_shape(params, n_keep).totals_stride * sizeof(uint32_t) * (uint64_t)std::min(n_tensors, kMaxCompactBatch);
+}
+
+extern "C" int32_t hqmq_evict_compact(const hqmq_params *params, int32_t n_keep, int32_t n_tensors, const hqmq_encoded *enc,
+                                      const uint64_t *outlier_capacity, const int32_t *const *keep_dev, const hqmq_encoded *out,
+                                      const uint64_t *out_capacity, void *workspace_dev, uint64_t workspace_bytes, void *stream)
+{
+    int32_t rc = check_compact(params, n_keep, n_tensors);
+    if (rc != HQMQ_OK)
+        return rc;
+    if (!enc || !outlier_capacity || !keep_dev || !out || !out_capacity || !workspace_dev || misaligned(workspace_dev, 256))
+        return HQMQ_ERR_INVALID_ARG;
+    for (int32_t i = 0; i < n_tensors; ++i) {
+        rc = check_encoded(&enc[i], false, outlier_capacity[i]);
+        if (rc == HQMQ_OK)
+            rc = check_encoded(&out[i], true, out_capacity[i]);
+        if (rc == HQMQ_OK && (!enc[i].status || misaligned(enc[i].status, 4) || !keep_dev[i] || misaligned(keep_dev[i], 4)))
+            rc = HQMQ_ERR_INVALID_ARG;
+        if (rc != HQMQ_OK)
+            return rc;
+    }
+    // rows move to other places while others are still read: no new tensor on top of a given one or of another new one
+    for (int32_t i = 0; i < n_tensors; ++i)
+        for (int32_t j = 0; j < n_tensors; ++j)
+            if (out[i].codes == enc[j].codes || out[i].sigma == enc[j].sigma || out[i].flags == enc[j].flags ||
+                out[i].row_off == enc[j].row_off || (out_capacity[i] > 0 && out[i].outliers == enc[j].outliers) ||
+                out[i].status == enc[j].status ||
+                (i != j && (out[i].codes == out[j].codes || out[i].sigma == out[j].sigma || out[i].flags == out[j].flags ||
+                            out[i].row_off == out[j].row_off || (out_capacity[i] > 0 && out[i].outliers == out[j].outliers) ||
+                            out[i].n_outliers == out[j].n_outliers || out[i].status == out[j].status)))
+                return HQMQ_ERR_INVALID_ARG;
+    CompactShape s = compact_shape(params, n_keep);
+    if (workspace_bytes < s.totals_stride * sizeof(uint32_t) * (uint64_t)std::min(n_tensors, kMaxCompactBatch))
+        return HQMQ_ERR_BUFFER_TOO_SMALL;
+    s.totals = static_cast<uint32_t *>(workspace_dev);
+    for (int32_t first = 0; first < n_tensors; first += kMaxCompactBatch) {
+        const int n = std::min(n_tensors - first, kMaxCompactBatch);
+        CompactBatch batch;
+        std::memset(&batch, 0, sizeof(batch));
+        for (int i = 0; i < n; ++i) {
+            CompactTensor &t = batch.t[i];
+            t.in = to_ptrs(&enc[first + i]);
+            t.out = to_ptrs(&out[first + i]);
+            t.keep = keep_dev[first + i];
+            t.in_capacity = outlier_capacity[first + i];
+            t.out_capacity = out_capacity[first + i];
+        }
+        const hipError_t err = launch_evict_compact(s, batch, n, static_cast<hipStream_t>(stream));
+        if (err != hipSuccess)
+            return hip_failed(err);
+    }
+    return HQMQ_OK;
 }

@@ -43,7 +43,7 @@ constexpr int kPaySlots = 128;                      // outlier payloads of a wav
 constexpr int kSideWords = kStageWords + 3 * kStageRows + 2 * kPaySlots;  // one side (K or V) of one wave
 constexpr float kNegBig = -1.0e30f;                 // "no row seen yet" (finite, so differences stay finite)
 constexpr int kRedStride = 2 + 128;                 // one partial state: maximum, sum, 128 weighted values
-constexpr int kAttendTargetBlocks = 512;            // two resident workgroups per compute unit
+constexpr int kAttendTargetBlocks = 512;            // two resident workgroups per compute unit; no more splits than that
 constexpr uint32_t kHalfOfMaxHalf = 0x77ffu;        // 32752 = 65504 / 2 as fp16 bits
 constexpr float kWeightScale = 16384.f;             // softmax weights enter the value products times 2^14
 
@@ -565,10 +565,11 @@ __global__ __launch_bounds__(kAttThreads, 2) void k_attend_partial(Geometry g, A
             oo = fmaf(src[2 + d], c, oo);
         }
         const size_t head = (size_t)seg * G + gq;  // = b * (H G) + h * G + gq
-        a.part_acc[(head * a.n_splits + split) * 128 + d] = oo * (1.0f / kWeightScale);
+        const size_t part = head * a.part_pitch + a.split0 + split;
+        a.part_acc[part * 128 + d] = oo * (1.0f / kWeightScale);
         if (d == 0) {
-            a.part_ml[(head * a.n_splits + split) * 2 + 0] = mm;
-            a.part_ml[(head * a.n_splits + split) * 2 + 1] = ll;
+            a.part_ml[part * 2 + 0] = mm;
+            a.part_ml[part * 2 + 1] = ll;
         }
     }
 }
@@ -1050,10 +1051,11 @@ __global__ __launch_bounds__(kJointThreads, 1) void k_attend_joint(Geometry g, A
             oo = fmaf(src[2 + d], c, oo);
         }
         const size_t head = (size_t)seg * G + gq;  // = b * (H G) + h * G + gq
-        a.part_acc[(head * a.n_splits + split) * 128 + d] = oo * (1.0f / kWeightScale);
+        const size_t part = head * a.part_pitch + a.split0 + split;
+        a.part_acc[part * 128 + d] = oo * (1.0f / kWeightScale);
         if (d == 0) {
-            a.part_ml[(head * a.n_splits + split) * 2 + 0] = mm;
-            a.part_ml[(head * a.n_splits + split) * 2 + 1] = ll;
+            a.part_ml[part * 2 + 0] = mm;
+            a.part_ml[part * 2 + 1] = ll;
         }
     }
 }
@@ -1090,7 +1092,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_attend_merge(AttendArgs a)
     const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
     const size_t head = blockIdx.x;
     const int d = blockIdx.y * kMergeDims + lane;
-    const int n = a.n_splits;
+    const int n = a.part_pitch;
     const float2 *ml = reinterpret_cast<const float2 *>(a.part_ml) + head * n;
     const float *pa = a.part_acc + head * n * 128 + d;  // a pitch of 128: dimensions past D are read and not used
     const int per = (n + kWaves - 1) / kWaves, first = wv * per, end = min(n, first + per);
@@ -1104,7 +1106,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_attend_merge(AttendArgs a)
     for (int s = lane; s < n; s += 64)
         mx = fmaxf(mx, ml[s].x);
     mx = reduce_wave(mx, [](float x, float y) { return fmaxf(x, y); });
-    const int here = end - first;  // at most 64 (launch_attend)
+    const int here = end - first;  // at most 64 (launch_attend_merge)
     const float wgt = lane < here ? __builtin_amdgcn_exp2f(st.x - mx) : 0.f;
     float o = 0.f, lsum = st.y * wgt;
     for (int j0 = 0; j0 < here; j0 += kEarly) {
@@ -1199,7 +1201,7 @@ hipError_t prepare_attend_kernels()
     return err;
 }
 
-hipError_t launch_attend(const Geometry &g, const AttendArgs &a, hipStream_t stream)
+hipError_t launch_attend_partials(const Geometry &g, const AttendArgs &a, hipStream_t stream)
 {
     if (a.G < 1 || a.G > kMaxGroup)
         return hipErrorInvalidValue;
@@ -1248,12 +1250,16 @@ hipError_t launch_attend(const Geometry &g, const AttendArgs &a, hipStream_t str
             return hipErrorInvalidValue;
 #undef HQMQ_LAUNCH_ATTEND
     }
-    hipError_t err = hipGetLastError();
-    if (err != hipSuccess)
-        return err;
-    const dim3 outputs((unsigned)(g.B * g.H * a.G), (unsigned)((g.D + kMergeDims - 1) / kMergeDims));
-    static_assert(kAttendTargetBlocks <= 64 * 16 && kJointTargetBlocks <= 64 * 16, "a lane per split of a wave's share");
-    if (a.n_splits <= kMergeFew)
+    return hipGetLastError();
+}
+
+hipError_t launch_attend_merge(int64_t heads, const AttendArgs &a, hipStream_t stream)
+{
+    const dim3 outputs((unsigned)heads, (unsigned)((a.D + kMergeDims - 1) / kMergeDims));
+    static_assert(kMostParts <= 64 * 16, "a lane per split of a wave's share");
+    if (a.part_pitch > kMostParts)
+        return hipErrorInvalidValue;
+    if (a.part_pitch <= kMergeFew)
         hipLaunchKernelGGL(k_attend_merge<4>, outputs, dim3(64 * 4), 0, stream, a);
     else
         hipLaunchKernelGGL(k_attend_merge<16>, outputs, dim3(64 * 16), 0, stream, a);

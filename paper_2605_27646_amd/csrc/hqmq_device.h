@@ -274,12 +274,14 @@ struct AttendArgs {
     _Float16 *out;         // [B][H * G][D]
     float *lse;            // [B][H * G] natural-log sum of exp(score) over the cached tokens, or null
     const int32_t *visible;  // [B][H * G] number of leading cached tokens each query head may see, or null (all)
-    float *part_ml;        // [B * H * G][n_splits][2]: running maximum (log2 domain) and weight sum
-    float *part_acc;       // [B * H * G][n_splits][128]: weighted value sum
+    float *part_ml;        // [B * H * G][part_pitch][2]: running maximum (log2 domain) and weight sum
+    float *part_acc;       // [B * H * G][part_pitch][128]: weighted value sum
     float qscale;          // softmax scale * log2(e), folded into the query
     int32_t G;             // query heads per kv head
     int32_t D;             // head dimension: 64, 96 or 128 (q and out rows; the partial sums keep a pitch of 128)
     int32_t n_splits;      // workgroups along the sequence
+    int32_t split0, part_pitch;  // the first one's place in the partial arrays, and how many there are to merge: n_splits, or with
+                           // those of a shared prefix
     int32_t rows_per_split;  // multiple of kAttendTile (of the table form's tile of 128 rows when joint)
     int32_t joint;           // the form that reads the reconstruction from half tables in LDS
 };
@@ -397,6 +399,8 @@ hipError_t launch_outlier_list(const Geometry &g, const WorkspaceOffsets &wo, co
                                hipStream_t stream);
 hipError_t launch_decode(const Geometry &g, const DecodeBatch &batch, int n_tensors, hipStream_t stream);
 hipError_t prepare_attend_kernels();  // once per device, before the first launch_attend on it
-hipError_t launch_attend(const Geometry &g, const AttendArgs &args, hipStream_t stream);
+hipError_t launch_attend_partials(const Geometry &g, const AttendArgs &args, hipStream_t stream);
+hipError_t launch_attend_merge(int64_t heads, const AttendArgs &args, hipStream_t stream);  // uses what describes the partial sums and the results
+constexpr int kMostParts = 1024;  // that launch_attend_merge merges
 
 }  // namespace hqmq
