@@ -23,6 +23,7 @@ struct SharedPlan {
     int32_t n_splits, rows_per_split;
 };
 SharedPlan plan_shared(const Geometry &g, int G, int n_share);
+hipError_t prepare_shared_kernels();  // once per device, before the first launch_shared on it
 hipError_t launch_shared(const Geometry &g, const SharedArgs &a, hipStream_t stream);
 
 struct MassArgs {
