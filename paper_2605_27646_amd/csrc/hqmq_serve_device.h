@@ -19,6 +19,7 @@ struct SharedArgs {
     int32_t n_splits, rows_per_split;  // workgroups along the prefix and its tokens per workgroup
     int32_t part_pitch;      // splits of the partial arrays, the own tokens' included
 };
+constexpr int kMostSharedSplits = 512;  // and as many of the own tokens: kMostParts in all
 struct SharedPlan {
     int32_t n_splits, rows_per_split;
 };

@@ -8,8 +8,8 @@ namespace hqmq {
 
 namespace {
 
-constexpr int kThreadsShared = 512;
-constexpr int kGroupThreads = 256;  // a group of four waves works on tiles of its own
+constexpr int kSideThreads = 256;   // that fetch and reconstruct a side (K or V) of a tile; workgroups of four waves do both sides
+constexpr int kLoads = 3;           // code words of a tile and side per thread
 constexpr int kPay = 128;           // outlier payloads of a tile and side kept in LDS
 constexpr float kNoToken = -1.0e30f;
 constexpr float kTop = 10.f;        // weights are taken relative to 2^-kTop of the largest score,
@@ -20,7 +20,7 @@ typedef _Float16 half8_t __attribute__((ext_vector_type(8)));
 typedef float float16_t __attribute__((ext_vector_type(16)));
 typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
 
-// Tokens of a tile: 2048 chunks of K and V together, eight for each of a group's threads (24 chunks per row: 1536).
+// Tokens of a tile: 1024 chunks of K and of V (24 chunks per row: 768), four for each of a side's threads.
 template <int kNc>
 constexpr int tile_tokens() { return kNc == 16 ? 64 : 32; }
 template <int kNc>
@@ -28,102 +28,138 @@ constexpr int key_pitch() { return 4 * kNc + 8; }  // halves; an odd number of 1
 template <int kNc>
 constexpr int value_pitch() { return tile_tokens<kNc>() + 8; }
 
-// LDS of a group, in 32-bit words: keys [tokens][key_pitch] halves | values [D rows][value_pitch] halves | code words of K, of V |
-// flags, scales, offsets of K, of V | payloads of K, of V
+// A tile in LDS, in 32-bit words: keys [tokens][key_pitch] halves | values [D rows][value_pitch] halves
 template <int kNc>
-struct GroupLds {
-    static constexpr int kTok = tile_tokens<kNc>();
-    static constexpr int keys = kTok * key_pitch<kNc>() / 2;
-    static constexpr int values = 4 * kNc * value_pitch<kNc>() / 2;
-    static constexpr int rows = 3 * kTok;
-    static constexpr int pay = 2 * kPay + 4;  // and a slot past the last that is read and not used
-    __host__ __device__ static constexpr int words(int row_words) { return (kTok * row_words + 2 + 3) / 4 * 4; }  // + a word read past the last
-    __host__ __device__ static constexpr int total(int row_words) { return keys + values + 2 * (words(row_words) + rows + pay); }
+struct TileLds {
+    static constexpr int keys = tile_tokens<kNc>() * key_pitch<kNc>() / 2;
+    static constexpr int total = keys + 4 * kNc * value_pitch<kNc>() / 2;
+    static_assert(keys % 4 == 0 && total % 4 == 0, "16-byte accesses");
 };
-static_assert(GroupLds<32>::keys % 4 == 0 && GroupLds<24>::keys % 4 == 0 && GroupLds<16>::keys % 4 == 0, "16-byte reads of what follows");
-static_assert(GroupLds<32>::values % 4 == 0 && GroupLds<24>::values % 4 == 0 && GroupLds<16>::values % 4 == 0, "16-byte reads of what follows");
+// A tile's packed rows of one side: code words (room for the largest w) | flags, scales, offsets | payloads, with a slot past the last
+// that is read and not used | two words that say whether the tile wants care, the window's first entry
+template <int kNc>
+struct StageLds {
+    static constexpr int kTok = tile_tokens<kNc>();
+    static constexpr int words = kLoads * kSideThreads;
+    static_assert(kTok * (kNc * 24 / 32) <= words, "w <= 24");
+    static constexpr int pays = words + 3 * kTok;
+    static constexpr int about = pays + 2 * kPay + 4;
+    static constexpr int total = about + 4;
+    static_assert(words % 4 == 0 && kTok % 4 == 0 && about % 4 == 0, "16-byte reads");
+};
 
-// Codeword directions divided by the radius codes' range L, so that a chunk is (radius code * scale, exact in fp32) times an
-// entry, rounded once.  kTable: per side 13 S entries (12 primaries with a positive first non-zero component, then zeros for
-// primaries past the 24), else the S secondaries and the 24 primaries.
-template <bool kTable>
-__host__ __device__ constexpr size_t side_floats(int S) { return (size_t)(kTable ? 13 : 1) * S * 4; }
+// The 24 primaries are +-u w^m with u one of 1, i, j, k, w = (1 + i + j + k) / 2 and m = 0, 1, 2.  A product with u reorders the
+// components (e takes that of e ^ u) and flips signs, which costs nothing on the packed fp16 result, rounding being symmetric: two
+// byte permutes and two exclusive ors.  So a table of three entries per secondary, w^m (x) q_s, serves all 24.
+struct Primary {
+    uint32_t m, select, flip_lo, flip_hi;  // select: of the result's first dword; the second's is select ^ 0x04040404
+};
+struct Primaries {
+    Primary p[32];
+};
+constexpr Primaries make_primaries()
+{
+    Primaries out{};
+    const int w[3][4] = {{2, 0, 0, 0}, {1, 1, 1, 1}, {-1, 1, 1, 1}};                               // twice w^m
+    const int sign[4][4] = {{1, 1, 1, 1}, {-1, 1, -1, 1}, {-1, 1, 1, -1}, {-1, -1, 1, 1}};  // of component e ^ u in u (x) x
+    for (int p = 0; p < 32; ++p) {
+        int P[4] = {0, 0, 0, 0};  // twice the primary
+        if (p < 8)
+            P[p >> 1] = (p & 1) ? -2 : 2;
+        else if (p < 24)
+            for (int e = 0; e < 4; ++e)
+                P[e] = ((p - 8) >> (3 - e)) & 1 ? -1 : 1;
+        out.p[p] = Primary{0u, 0x03020100u, 0u, 0u};  // past the 24: any that stays in the table
+        for (int u = 0; p < 24 && u < 4; ++u)
+            for (int m = 0; m < 3; ++m)
+                for (int s = -1; s < 2; s += 2) {
+                    bool same = true;
+                    for (int e = 0; e < 4; ++e)
+                        same = same && P[e] == s * sign[u][e] * w[m][e ^ u];
+                    if (!same)
+                        continue;
+                    const uint32_t lo = 2u * (0u ^ u), hi = 2u * (1u ^ u);
+                    uint32_t flip[2] = {0u, 0u};
+                    for (int e = 0; e < 4; ++e)
+                        if (s * sign[u][e] < 0)
+                            flip[e >> 1] |= 0x8000u << (16 * (e & 1));
+                    out.p[p] = Primary{(uint32_t)m, lo | (lo + 1u) << 8 | hi << 16 | (hi + 1u) << 24, flip[0], flip[1]};
+                }
+    }
+    return out;
+}
+__constant__ const Primaries kPrimaries = make_primaries();
 
 // Row of V^T in LDS for component e of chunk c: blocks of 32 rows are the operands of one product; in a product's result a lane
 // then holds all four components of a chunk.
 __device__ __forceinline__ int value_row(int c, int e) { return 32 * (c >> 3) + 8 * e + (c & 7); }
 
-__device__ __forceinline__ float4_t product(const float P[4], float4_t q)
+// A barrier for what goes through LDS: loads from memory stay in flight across it.
+__device__ __forceinline__ void lds_barrier()
 {
-    float4_t d;
-    d[0] = fmaf(-P[3], q[3], fmaf(-P[2], q[2], fmaf(-P[1], q[1], P[0] * q[0])));
-    d[1] = fmaf(-P[3], q[2], fmaf(P[2], q[3], fmaf(P[1], q[0], P[0] * q[1])));
-    d[2] = fmaf(P[3], q[1], fmaf(P[2], q[0], fmaf(-P[1], q[3], P[0] * q[2])));
-    d[3] = fmaf(P[3], q[0], fmaf(-P[2], q[1], fmaf(P[1], q[2], P[0] * q[3])));
-    return d;
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
+
+// How a workgroup works: waves, query rows (columns) of each, tiles in LDS.  With two tiles every wave reconstructs its part of
+// the next one and multiplies the present one between two barriers, half of the waves in the other order; with one the workgroups
+// that share a compute unit fill each other's waits.
+template <int kWaves_, int kCols_, int kBufs_, int kPerSimd_>
+struct Form {
+    static constexpr int kWaves = kWaves_, kCols = kCols_, kBufs = kBufs_, kPerSimd = kPerSimd_;
+};
+using FormSmall = Form<4, 16, 1, 3>;
+using FormMiddle = Form<4, 32, 1, 2>;
+using FormLarge = Form<8, 32, 2, 2>;
 
 }  // namespace
 
-template <int kNc, bool kTable, bool kPow2, int kCols>
-__global__ __launch_bounds__(kThreadsShared, 2) void k_shared(Geometry g, SharedArgs a)
+template <int kNc, bool kTable, bool kPow2, typename F>
+__global__ __launch_bounds__(64 * F::kWaves, F::kPerSimd) void k_shared(Geometry g, SharedArgs a)
 {
-    using L = GroupLds<kNc>;
-    constexpr int kTok = L::kTok, kD = 4 * kNc;
-    constexpr int kLoads = (kTok * (kNc * 24 / 32) + kGroupThreads - 1) / kGroupThreads;  // code words per thread and side, at the largest w
-    constexpr bool kWide = kCols >= 32;           // 32x32x16 products, else 16x16x32
-    constexpr int kCb = kWide ? kCols / 32 : 1;   // blocks of columns (query rows) of a wave
+    using Tile = TileLds<kNc>;
+    using Stage = StageLds<kNc>;
+    constexpr int kTok = tile_tokens<kNc>(), kD = 4 * kNc;
+    constexpr int kWaves = F::kWaves, kCols = F::kCols, kBufs = F::kBufs, kThreads = 64 * kWaves;
+    constexpr int kSides = kWaves == 4 ? 2 : 1;   // that a wave fetches and reconstructs
+    constexpr bool kWide = kCols == 32;           // 32x32x16 products, else 16x16x32
     constexpr int kSteps = kWide ? kD / 16 : kD / 32;
     constexpr int kBlocks = kWide ? kD / 32 : kD / 16;
     constexpr int kRegs = kWide ? 16 : 4;         // of a block's result
     using acc_t = std::conditional_t<kWide, float16_t, float4_t>;
     extern __shared__ __align__(16) float lds[];
-    uint2 *lut = reinterpret_cast<uint2 *>(lds);  // [48] of a primary: byte offset of its rows in a table (number without one), sign bit
-    float *prim = lds + 96;                       // [24][4], without tables
-    float *dir_k = prim + (kTable ? 0 : 96);
-    float *dir_v = dir_k + side_floats<kTable>(g.S);
-    uint32_t *groups = reinterpret_cast<uint32_t *>(dir_v + side_floats<kTable>(g.S));
+    uint4v *lut = reinterpret_cast<uint4v *>(lds);  // [48]: a Primary, with the byte offset of its entries
+    float *dir = lds + 4 * 48;                      // [K, V][3 or 1][S][4]
+    const uint32_t dir_side = (uint32_t)(kTable ? 3 : 1) * g.S * 4;
+    uint32_t *tiles = reinterpret_cast<uint32_t *>(dir + 2 * dir_side);
+    uint32_t *stages = tiles + kBufs * Tile::total;  // [kBufs][K, V]
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int group = wave >> 2, gt = tid & (kGroupThreads - 1), gw = wave & 3;
+    const int st = tid & (kSideThreads - 1), sw = wave & 3;  // within the threads of a side
+    const int side0 = kSides == 2 ? 0 : wave >> 2;           // the first side of this wave
     const int seg = blockIdx.y, b = seg / g.H, h = seg % g.H;
     const uint32_t row_words = kNc == 32 ? (uint32_t)g.w : (uint32_t)g.row_words;
     const uint32_t w = g.w, w_idx = g.w_idx;
 
-    uint32_t *mine = groups + group * L::total((int)row_words);
-    _Float16 *keys = reinterpret_cast<_Float16 *>(mine);
-    _Float16 *values = reinterpret_cast<_Float16 *>(mine + L::keys);
-    uint32_t *words[2], *row_part[2];
-    uint2 *pays[2];
-    {
-        uint32_t *p = mine + L::keys + L::values;
-        const int nw = L::words((int)row_words);
-        words[0] = p;
-        words[1] = p + nw;
-        row_part[0] = p + 2 * nw;
-        row_part[1] = row_part[0] + L::rows;
-        pays[0] = reinterpret_cast<uint2 *>(row_part[1] + L::rows);
-        pays[1] = pays[0] + L::pay / 2;
-    }
-
     // ---- columns of this wave: query rows r of the kv head ---------------------------------------------------------
     const int n_rows = a.n_share * a.G;
-    const int col0 = (int)blockIdx.z * 4 * kCols + gw * kCols;
-    const int col = kWide ? (lane & 31) : (lane & 15);
-    const int kgrp = kWide ? (lane >> 5) : (lane >> 4);  // which 8 of a product's terms the lane supplies, which rows of a result it holds
-    const bool has_cols = col0 < n_rows;                 // uniform
+    const int col0 = ((int)blockIdx.z * kWaves + wave) * kCols;
+    const int col = lane & (kCols - 1);
+    const int kgrp = lane / kCols;         // which 8 of a product's terms the lane supplies, which rows of a result it holds
+    const bool has_cols = col0 < n_rows;   // uniform
     const uint32_t flip = a.qscale < 0.f ? 0x80008000u : 0u;
-    const float qscale = fabsf(a.qscale);                // a negative scale goes into the queries' signs
-    half8_t qf[kCb][kSteps];
-    int vis[kCb];
-    int least = g.T, most = 0;
-#pragma unroll
-    for (int cb = 0; cb < kCb; ++cb) {
-        const int r = col0 + 32 * cb + col;
-        const bool there = r < n_rows;
+    const float qscale = fabsf(a.qscale);  // a negative scale goes into the queries' signs
+    const int r = col0 + col;
+    const bool there = r < n_rows;
+    size_t head;
+    {
         const int rr = there ? r : 0, m = rr / a.G;
-        const size_t head = ((size_t)(b * a.n_share + m) * g.H + h) * a.G + (rr - m * a.G);
+        head = ((size_t)(b * a.n_share + m) * g.H + h) * a.G + (rr - m * a.G);
+    }
+    half8_t qf[kSteps];
+    {
         const _Float16 *q = a.q + head * kD + 8 * kgrp;
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) {
@@ -131,250 +167,275 @@ __global__ __launch_bounds__(kThreadsShared, 2) void k_shared(Geometry g, Shared
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 v[i] = there ? v[i] ^ flip : 0u;
-            qf[cb][s] = __builtin_bit_cast(half8_t, v);
+            qf[s] = __builtin_bit_cast(half8_t, v);
         }
-        vis[cb] = g.T;
-        if (a.visible) {
-            if (there)
-                vis[cb] = min(max(a.visible[head], 0), g.T);
-            least = min(least, vis[cb]);
-        }
-        most = max(most, there ? vis[cb] : 0);
     }
+    int vis = g.T;
+    if (a.visible && there)
+        vis = min(max(a.visible[head], 0), g.T);
 
-    // ---- the tables --------------------------------------------------------------------------------------------------
+    // ---- the tables: directions divided by the radius codes' range L, so that a chunk is (radius code * scale, exact in fp32)
+    //      times an entry, rounded once.  Entries are taken in fp64 and rounded once too. ------------------------------------------
     {
         const double over_L = 1.0 / (double)((1 << g.b_r) - 1);
         const float *sk = a.k.sec + (size_t)h * g.S * 4, *sv = a.v.sec + (size_t)h * g.S * 4;
-        for (int i = tid; i < 2 * g.S; i += kThreadsShared) {
+        for (int i = tid; i < 2 * g.S; i += kThreads) {
             const bool is_v = i >= g.S;
             const int s = is_v ? i - g.S : i;
             const float4_t q = *reinterpret_cast<const float4_t *>((is_v ? sv : sk) + 4 * s);
-            float4_t *dst = reinterpret_cast<float4_t *>(is_v ? dir_v : dir_k) + s;
-            double x[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                x[e] = (double)q[e] * over_L;
-            if (!kTable) {
-                *dst = float4_t{(float)x[0], (float)x[1], (float)x[2], (float)x[3]};
-            } else {
-#pragma unroll
-                for (int c = 0; c < 13; ++c) {
-                    double P[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        P[e] = c < 4 ? (c == e ? 1.0 : 0.0) : (c == 12 ? 0.0 : (e == 0 ? 0.5 : ((((c - 4) >> (3 - e)) & 1) ? -0.5 : 0.5)));
-                    float4_t d;
-                    d[0] = (float)fma(-P[3], x[3], fma(-P[2], x[2], fma(-P[1], x[1], P[0] * x[0])));
-                    d[1] = (float)fma(-P[3], x[2], fma(P[2], x[3], fma(P[1], x[0], P[0] * x[1])));
-                    d[2] = (float)fma(P[3], x[1], fma(P[2], x[0], fma(-P[1], x[3], P[0] * x[2])));
-                    d[3] = (float)fma(P[3], x[0], fma(-P[2], x[1], fma(P[1], x[2], P[0] * x[3])));
-                    dst[(size_t)c * g.S] = d;
-                }
+            float4_t *dst = reinterpret_cast<float4_t *>(dir + (is_v ? dir_side : 0u)) + s;
+            const double x0 = q[0] * over_L, x1 = q[1] * over_L, x2 = q[2] * over_L, x3 = q[3] * over_L;
+            dst[0] = float4_t{(float)x0, (float)x1, (float)x2, (float)x3};
+            if (kTable) {  // w (x) x = ((1, 1, 1, 1) (x) x) / 2, and w^2 = w - 1
+                const double y0 = 0.5 * (x0 - x1 - x2 - x3), y1 = 0.5 * (x0 + x1 - x2 + x3);
+                const double y2 = 0.5 * (x0 + x1 + x2 - x3), y3 = 0.5 * (x0 - x1 + x2 + x3);
+                dst[g.S] = float4_t{(float)y0, (float)y1, (float)y2, (float)y3};
+                dst[2 * g.S] = float4_t{(float)(y0 - x0), (float)(y1 - x1), (float)(y2 - x2), (float)(y3 - x3)};
             }
         }
         if (tid < 48) {
-            const uint32_t p = tid;
-            uint32_t c = 12u, neg = 0u;
-            if (p < 8) {
-                c = p >> 1;
-                neg = p & 1u;
-            } else if (p < 24) {
-                const uint32_t bits = p - 8u;
-                neg = bits >> 3;
-                c = 4u + ((neg ? ~bits : bits) & 7u);
-            }
-            lut[p] = make_uint2(kTable ? c * (uint32_t)g.S * 16u : c * 16u, neg << 31);
-        }
-        if (!kTable && tid < 96) {
-            const int c = tid >> 2, e = tid & 3;
-            prim[tid] = c < 4 ? (c == e ? 1.f : 0.f) : (c >= 12 ? 0.f : (e == 0 ? 0.5f : ((((c - 4) >> (3 - e)) & 1) ? -0.5f : 0.5f)));
+            const Primary p = kPrimaries.p[min(tid, 31)];
+            lut[tid] = uint4v{kTable ? p.m * (uint32_t)g.S * 16u : p.m, p.select, p.flip_lo, p.flip_hi};
         }
     }
 
     // ---- the tiles of this workgroup -----------------------------------------------------------------------------------
     const int begin = (int)blockIdx.x * a.rows_per_split;
     int end = min(g.T, begin + a.rows_per_split);
-    if (a.visible) {  // nothing that no row of the workgroup sees is read; every wave needs the same end
-        int *both = reinterpret_cast<int *>(mine);
-        for (int d = 32; d > 0; d /= 2)
+    int least = g.T;      // every query row of the wave sees the tokens below
+    if (a.visible) {      // what no row of the workgroup sees is not read
+        int *most_of = reinterpret_cast<int *>(tiles);
+        int most = there ? vis : 0;
+        least = vis;
+        for (int d = 32; d > 0; d /= 2) {
             most = max(most, __shfl_xor(most, d));
-        for (int d = 32; d > 0; d /= 2)
             least = min(least, __shfl_xor(least, d));
+        }
         if (lane == 0)
-            both[gw] = most;
+            most_of[wave] = most;
         __syncthreads();
-        end = min(end, max(max(both[0], both[1]), max(both[2], both[3])));
+        most = 0;
+        for (int i = 0; i < kWaves; ++i)
+            most = max(most, most_of[i]);
+        end = __builtin_amdgcn_readfirstlane(min(end, most));
         least = __builtin_amdgcn_readfirstlane(least);
-        end = __builtin_amdgcn_readfirstlane(end);
         __syncthreads();
     }
     const int n_tiles = end > begin ? (end - begin + kTok - 1) / kTok : 0;
-    const int n_mine = (n_tiles + 1 - group) >> 1;  // tiles group, group + 2, ...
 
-    float m_ref[kCb], l_run[kCb];
-    acc_t acc[kCb][kBlocks];
+    float m_ref = kNoToken, l_run = 0.f;
+    acc_t acc[kBlocks];
 #pragma unroll
-    for (int cb = 0; cb < kCb; ++cb) {
-        m_ref[cb] = kNoToken;
-        l_run[cb] = 0.f;
+    for (int k = 0; k < kBlocks; ++k)
 #pragma unroll
-        for (int k = 0; k < kBlocks; ++k)
-#pragma unroll
-            for (int i = 0; i < kRegs; ++i)
-                acc[cb][k][i] = 0.f;
-    }
+        for (int i = 0; i < kRegs; ++i)
+            acc[k][i] = 0.f;
 
     // ---- a tile's packed rows on their way to LDS ------------------------------------------------------------------------
-    uint32_t cw[2][kLoads], fw = 0u, sg = 0u, ro = 0u;
-    uint32_t list0[2], listn[2];  // window of the outlier list: first entry and length
+    // Every load is issued a tile's time or more before its value is needed, and without a condition, past the last tile for that
+    // one again.  The outlier list's bounds come a tile before rows and payloads.
+    uint32_t cw[kSides][kLoads], fw = 0u, ro = 0u, bounds = 0u;
+    uint16_t sg = 0u;  // as loaded: widening it before it is staged would wait for it
     uint2 pay = make_uint2(0u, 0u);
-    uint32_t pay_base[2] = {0u, 0u}, pay_n[2] = {0u, 0u};  // of the tile in LDS
-    const AttendSide *const sides[2] = {&a.k, &a.v};
-    auto tile_start = [&](int j) { return begin + (2 * j + group) * kTok; };
+    uint32_t next_base[kSides], next_n[kSides];  // window of the outlier list, of the tile on its way
+    int next_rows = 0;
+    uint32_t next_in_list = 0u;  // of the side that this wave fetches payloads of
+    const int row_side = kSides == 2 ? (st / kTok) & 1 : side0, pay_side = kSides == 2 ? sw >> 1 : side0;
+    auto tile_start = [&](int j) { return begin + max(min(j, n_tiles - 1), 0) * kTok; };
+    auto request_bounds = [&](int j) {  // lanes 0 .. 3: first and end of K's window, of V's
+        const int t0 = tile_start(j);
+        const uint32_t *off = (lane & 2) ? a.v.row_off : a.k.row_off;
+        bounds = off[(int64_t)seg * g.T + ((lane & 1) ? min(t0 + kTok, end) : t0)];
+    };
     auto request = [&](int j) {
         const int t0 = tile_start(j);
         const int nr = min(kTok, end - t0);
         const int64_t R0 = (int64_t)seg * g.T + t0;
         const uint32_t last = (uint32_t)nr * row_words - 1u;
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            const uint32_t *src = sides[s]->codes + R0 * row_words;
+        for (int s = 0; s < kSides; ++s) {
+            const uint32_t *src = (side0 + s ? a.v.codes : a.k.codes) + R0 * row_words;
 #pragma unroll
             for (int i = 0; i < kLoads; ++i)
-                cw[s][i] = src[min((uint32_t)gt + kGroupThreads * i, last)];
-            list0[s] = sides[s]->row_off[R0];
-            listn[s] = sides[s]->row_off[R0 + nr];
+                cw[s][i] = src[min((uint32_t)st + kSideThreads * i, last)];
         }
-        if (gt < 2 * kTok) {
-            const int s = gt / kTok, row = gt % kTok, r = min(row, nr - 1);
-            const bool there = row < nr;
-            fw = (s ? a.v.flags : a.k.flags)[R0 + r];
-            sg = (s ? a.v.sigma : a.k.sigma)[R0 + r];
-            ro = (s ? a.v.row_off : a.k.row_off)[R0 + r];
-            fw = there ? fw : 0u;
-            sg = there ? sg : 0u;
-        }
-    };
-    auto request_payloads = [&]() {
-        const int s = gt >> 7;  // uniform
-        const AttendSide &sd = s ? a.v : a.k;
-        const uint32_t base = s ? list0[1] : list0[0], n = (s ? listn[1] : listn[0]) - base;
-        const uint32_t in_list = (uint64_t)base < sd.outlier_capacity ? (uint32_t)min((uint64_t)n, sd.outlier_capacity - base) : 0u;
-        const uint32_t slot = (uint32_t)gt & (kPay - 1);
-        pay = make_uint2(0u, 0u);
-        if (slot < in_list)
-            pay = reinterpret_cast<const uint2 *>(sd.outliers)[base + (uint64_t)slot];
-    };
-    auto stage = [&]() {
+        next_rows = nr;
+        const int64_t at = R0 + min(st % kTok, nr - 1);
+        fw = (row_side ? a.v.flags : a.k.flags)[at];
+        sg = (row_side ? a.v.sigma : a.k.sigma)[at];
+        ro = (row_side ? a.v.row_off : a.k.row_off)[at];
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            const int nw = L::words((int)row_words);
+        for (int s = 0; s < kSides; ++s) {
+            next_base[s] = (uint32_t)__builtin_amdgcn_readlane((int)bounds, 2 * (side0 + s));
+            next_n[s] = (uint32_t)__builtin_amdgcn_readlane((int)bounds, 2 * (side0 + s) + 1) - next_base[s];
+        }
+        const AttendSide &sd = pay_side ? a.v : a.k;
+        const uint32_t base = kSides == 2 && pay_side ? next_base[kSides - 1] : next_base[0];
+        const uint32_t n = kSides == 2 && pay_side ? next_n[kSides - 1] : next_n[0];
+        next_in_list = (uint64_t)base < sd.outlier_capacity ? (uint32_t)min((uint64_t)n, sd.outlier_capacity - base) : 0u;
+        const uint2 *list = next_in_list ? reinterpret_cast<const uint2 *>(sd.outliers) + base : reinterpret_cast<const uint2 *>(sd.codes);
+        // an empty window: the first code words (a row has three or more), which nothing uses
+        pay = list[next_in_list ? min((uint32_t)st & (kPay - 1), next_in_list - 1u) : 0u];
+    };
+    auto stage = [&](int buf) {
+#pragma unroll
+        for (int s = 0; s < kSides; ++s) {
+            uint32_t *dst = stages + (2 * buf + side0 + s) * Stage::total;
 #pragma unroll
             for (int i = 0; i < kLoads; ++i)
-                if (gt + kGroupThreads * i < nw)
-                    words[s][gt + kGroupThreads * i] = cw[s][i];
-            pay_base[s] = list0[s];
-            pay_n[s] = listn[s] - list0[s];
+                dst[st + kSideThreads * i] = cw[s][i];
+            if (sw == 0 && lane == 0)
+                dst[Stage::about + 2] = next_base[s];
         }
-        if (gt < 2 * kTok) {
-            uint32_t *dst = row_part[gt / kTok] + gt % kTok;
-            dst[0] = fw;
-            dst[kTok] = sg;
+        if (st < kSides * kTok) {  // uniform for 64 tokens or both sides; rows that are not there: a scale of zero and no flags
+            uint32_t *dst = stages + (2 * buf + row_side) * Stage::total + Stage::words + st % kTok;
+            const bool in = st % kTok < next_rows;
+            dst[0] = in ? fw : 0u;
+            dst[kTok] = in ? (uint32_t)sg : 0u;
             dst[2 * kTok] = ro;
         }
-        pays[gt >> 7][gt & (kPay - 1)] = pay;
+        {
+            // what can leave the fp16 range, or payloads past the staged ones, send the tile down a careful form
+            const bool mine = st < kSides * kTok && st % kTok < next_rows && (uint32_t)sg >= kBigScale;
+            bool care = __any(mine);
+#pragma unroll
+            for (int s = 0; s < kSides; ++s)
+                care = care || next_n[s] > (uint32_t)kPay;
+            if (sw < 2 && lane == 0)  // the waves that stage rows; 64 tokens of both sides are two waves'
+                stages[(2 * buf + side0) * Stage::total + Stage::about + sw] = care ? 1u : 0u;
+        }
+        const uint32_t slot = (uint32_t)st & (kPay - 1);
+        if (kSides == 2 || sw < 2)
+            reinterpret_cast<uint2 *>(stages + (2 * buf + pay_side) * Stage::total + Stage::pays)[slot] =
+                slot < next_in_list ? pay : make_uint2(0u, 0u);
     };
 
     // ---- reconstruction ----------------------------------------------------------------------------------------------------
+    // One chunk in three steps, so that the LDS round trips of a thread's four overlap: its primary and payload, the codeword's
+    // direction, the arithmetic.  slot: place in the window of the payload that the chunk takes if it is flagged.
     const uint32_t idx_mask = (1u << w_idx) - 1u;
-    const uint32_t div_shift = 32u - (uint32_t)__clz((int)(48u * (uint32_t)g.S * (uint32_t)g.S));
-    const uint32_t div_mul = ((1u << div_shift) + (uint32_t)g.S - 1u) / (uint32_t)g.S;  // k / S = k * div_mul >> div_shift for k < 48 S, in 32 bits while
-                                                                                                   // the tables fit (S < 300)
-    auto read_code = [&](int s, int row, uint32_t c) {
+    struct Pre {
+        uint32_t code, s_idx, slot;
+        uint4v l;
+        uint2 pay;
+    };
+    auto read_code = [&](const uint32_t *sp, int row, uint32_t c) {
         const uint32_t bit = c * w;
-        const uint32_t *rw = words[s] + row * row_words + (bit >> 5);
+        const uint32_t *rw = sp + row * row_words + (bit >> 5);
         return __builtin_amdgcn_alignbit(rw[1], rw[0], bit & 31u);
     };
-    auto chunk = [&](auto fast_tag, int s, uint32_t code, float scale, uint32_t slot, bool flagged) {
-        constexpr bool kFast = decltype(fast_tag)::value;
-        uint32_t p, s_idx;
+    auto pre = [&](auto fast_tag, const uint32_t *sp, uint32_t code, uint32_t slot) {
+        Pre f;
+        uint32_t p;
         if (kPow2) {
             p = (code >> g.log2_S) & 31u;
-            s_idx = code & ((uint32_t)g.S - 1u);
+            f.s_idx = code & ((uint32_t)g.S - 1u);
         } else {
             const uint32_t kk = code & idx_mask;
-            p = kTable ? __umul24(kk, div_mul) >> div_shift : (uint32_t)((float)kk * g.inv_S);
-            s_idx = kk - __umul24(p, (uint32_t)g.S);
+            p = (uint32_t)((float)kk * g.inv_S);
+            f.s_idx = kk - __umul24(p, (uint32_t)g.S);
         }
-        const uint2 l = lut[p];
-        const char *dir = reinterpret_cast<const char *>(s ? dir_v : dir_k) + (s_idx << 4);
-        float4_t d;
-        if (kTable) {
-            d = *reinterpret_cast<const float4_t *>(dir + l.x);
-        } else {
-            const float4_t P = *reinterpret_cast<const float4_t *>(reinterpret_cast<const char *>(prim) + l.x);
-            const float Pa[4] = {P[0], P[1], P[2], P[3]};
-            d = product(Pa, *reinterpret_cast<const float4_t *>(dir));
-        }
-        const float r = __uint_as_float(__float_as_uint((float)__builtin_amdgcn_ubfe(code, w_idx, w - w_idx) * scale) | l.y);
-        float y[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            y[e] = r * d[e];
-            if (!kFast)
-                y[e] = __builtin_amdgcn_fmed3f(y[e], -65504.f, 65504.f);  // the decode saturates
-        }
+        f.code = code;
+        f.slot = slot;
+        f.l = lut[p];
+        f.pay = reinterpret_cast<const uint2 *>(sp + Stage::pays)[decltype(fast_tag)::value ? slot : min(slot, (uint32_t)kPay)];
+        return f;
+    };
+    auto direction = [&](int s, const Pre &f) {
+        const char *at = reinterpret_cast<const char *>(dir + (s ? dir_side : 0u)) + (f.s_idx << 4);
+        if (kTable)
+            return *reinterpret_cast<const float4_t *>(at + f.l[0]);
+        const float4_t x = *reinterpret_cast<const float4_t *>(at);
+        const float4_t y = {0.5f * (x[0] - x[1] - x[2] - x[3]), 0.5f * (x[0] + x[1] - x[2] + x[3]), 0.5f * (x[0] + x[1] + x[2] - x[3]),
+                            0.5f * (x[0] - x[1] + x[2] + x[3])};
+        return f.l[0] == 0u ? x : f.l[0] == 1u ? y : y - x;
+    };
+    auto finish = [&](auto fast_tag, int s, uint32_t base, const Pre &f, float4_t d, uint32_t scale, bool flagged) {
+        constexpr bool kFast = decltype(fast_tag)::value;
+        const float r = (float)__builtin_amdgcn_ubfe(f.code, w_idx, w - w_idx) * (float)__builtin_bit_cast(_Float16, (uint16_t)scale);
         half4_t out;
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            out[e] = (_Float16)y[e];
-        uint2 o = __builtin_bit_cast(uint2, out);
-        uint2 v = pays[s][min(slot, (uint32_t)kPay)];
-        if (!kFast && slot >= (uint32_t)kPay && flagged) {  // past the staged ones: straight from the list
+        for (int e = 0; e < 4; ++e) {
+            float y = r * d[e];
+            if (!kFast)
+                y = __builtin_amdgcn_fmed3f(y, -65504.f, 65504.f);  // the decode saturates
+            out[e] = (_Float16)y;
+        }
+        const uint2 o = __builtin_bit_cast(uint2, out);
+        uint2 v = f.pay;
+        if (!kFast && f.slot >= (uint32_t)kPay && flagged) {  // past the staged ones: straight from the list
             const AttendSide &sd = s ? a.v : a.k;
-            const uint64_t at = (uint64_t)pay_base[s] + slot;
+            const uint64_t at = (uint64_t)base + f.slot;
             v = at < sd.outlier_capacity ? reinterpret_cast<const uint2 *>(sd.outliers)[at] : make_uint2(0u, 0u);
         }
-        o.x = flagged ? v.x : o.x;
-        o.y = flagged ? v.y : o.y;
-        return o;
+        const uint32_t x = __builtin_amdgcn_perm(o.y, o.x, f.l[1]) ^ f.l[2], y = __builtin_amdgcn_perm(o.y, o.x, f.l[1] ^ 0x04040404u) ^ f.l[3];
+        return make_uint2(flagged ? v.x : x, flagged ? v.y : y);
     };
-    auto scale_of = [&](int s, int row) { return (float)__builtin_bit_cast(_Float16, (uint16_t)row_part[s][kTok + row]); };
-    auto decode_keys = [&](auto fast_tag) {
+    // A thread's part of a tile: two pairs of neighbouring chunks of K, one chunk of V in four neighbouring tokens.  Threads beyond a
+    // tile's last unit (24 chunks per row) do that one again.
+    constexpr int kKeyUnits = kTok * kNc / 2, kValueUnits = kTok * kNc / 4;
+    static_assert(kKeyUnits <= 2 * kSideThreads && kValueUnits <= kSideThreads, "a thread's four chunks of a side");
+    auto decode_keys = [&](auto fast_tag, const uint32_t *sp, uint32_t *tile, uint32_t base) {
+        int row[2], c[2];
+        uint32_t code[4], word[2], scale[2], off[2];
 #pragma unroll
-        for (int u0 = 0; u0 < kTok * kNc / 2; u0 += kGroupThreads) {
-            const int u = u0 + gt;
-            if (kTok * kNc / 2 % kGroupThreads != 0 && u >= kTok * kNc / 2)
-                break;
-            const int row = u / (kNc / 2), c = 2 * (u % (kNc / 2));
-            const uint32_t word = row_part[0][row];
-            const uint32_t slot = row_part[0][2 * kTok + row] - pay_base[0] + __popc(word & ((1u << c) - 1u));
-            const float scale = scale_of(0, row);
-            const bool f0 = (word >> c) & 1u, f1 = (word >> c) & 2u;
-            const uint2 x = chunk(fast_tag, 0, read_code(0, row, c), scale, slot, f0);
-            const uint2 y = chunk(fast_tag, 0, read_code(0, row, c + 1), scale, slot + (f0 ? 1u : 0u), f1);
-            *reinterpret_cast<uint4v *>(keys + row * key_pitch<kNc>() + 4 * c) = uint4v{x.x, x.y, y.x, y.y};
+        for (int i = 0; i < 2; ++i) {
+            const int u = min(st + kSideThreads * i, kKeyUnits - 1);
+            row[i] = u / (kNc / 2);
+            c[i] = 2 * (u % (kNc / 2));
+            code[2 * i] = read_code(sp, row[i], c[i]);
+            code[2 * i + 1] = read_code(sp, row[i], c[i] + 1);
+            const uint32_t *rp = sp + Stage::words + row[i];
+            word[i] = rp[0];
+            scale[i] = rp[kTok];
+            off[i] = rp[2 * kTok];
+        }
+        bool flag[4];
+        Pre f[4];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            flag[2 * i] = (word[i] >> c[i]) & 1u;
+            flag[2 * i + 1] = (word[i] >> c[i]) & 2u;
+            const uint32_t slot = off[i] - base + __popc(word[i] & ((1u << c[i]) - 1u));
+            f[2 * i] = pre(fast_tag, sp, code[2 * i], slot);
+            f[2 * i + 1] = pre(fast_tag, sp, code[2 * i + 1], slot + (flag[2 * i] ? 1u : 0u));
+        }
+        float4_t d[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            d[i] = direction(0, f[i]);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const uint2 x = finish(fast_tag, 0, base, f[2 * i], d[2 * i], scale[i], flag[2 * i]);
+            const uint2 y = finish(fast_tag, 0, base, f[2 * i + 1], d[2 * i + 1], scale[i], flag[2 * i + 1]);
+            *reinterpret_cast<uint4v *>(reinterpret_cast<_Float16 *>(tile) + row[i] * key_pitch<kNc>() + 4 * c[i]) = uint4v{x.x, x.y, y.x, y.y};
         }
     };
-    auto decode_values = [&](auto fast_tag) {
-        const int u = gt;
-        if (kNc * kTok / 4 < kGroupThreads && u >= kNc * kTok / 4)
-            return;
-        static_assert(kNc * kTok / 4 <= kGroupThreads, "one chunk of four tokens per thread");
-        const int c = u % kNc, quad = u / kNc;
-        const uint4v word = *reinterpret_cast<const uint4v *>(row_part[1] + 4 * quad);
-        const uint4v off = *reinterpret_cast<const uint4v *>(row_part[1] + 2 * kTok + 4 * quad);
+    auto decode_values = [&](auto fast_tag, const uint32_t *sp, uint32_t *tile, uint32_t base) {
+        const int u = min(st, kValueUnits - 1), c = u % kNc, quad = u / kNc;
+        uint32_t code[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            code[i] = read_code(sp, 4 * quad + i, c);
+        const uint32_t *rp = sp + Stage::words + 4 * quad;
+        const uint4v word = *reinterpret_cast<const uint4v *>(rp), scale = *reinterpret_cast<const uint4v *>(rp + kTok);
+        const uint4v off = *reinterpret_cast<const uint4v *>(rp + 2 * kTok);
+        Pre f[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            f[i] = pre(fast_tag, sp, code[i], off[i] - base + __popc(word[i] & ((1u << c) - 1u)));
+        float4_t d[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            d[i] = direction(1, f[i]);
         uint2 v[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t slot = off[i] - pay_base[1] + __popc(word[i] & ((1u << c) - 1u));
-            v[i] = chunk(fast_tag, 1, read_code(1, 4 * quad + i, c), scale_of(1, 4 * quad + i), slot, (word[i] >> c) & 1u);
-        }
+        for (int i = 0; i < 4; ++i)
+            v[i] = finish(fast_tag, 1, base, f[i], d[i], scale[i], (word[i] >> c) & 1u);
         // where the four tokens stand in the order in which a product takes a block of scores as its operand
-        const int at = kWide ? 4 * ((quad & ~3) | ((quad & 1) << 1) | ((quad >> 1) & 1)) : 4 * ((quad & ~7) | ((quad & 3) << 1) | ((quad >> 2) & 1));
+        const int at = 4 * (kWide ? (quad & ~3) | ((quad & 1) << 1) | ((quad >> 1) & 1) : (quad & ~7) | ((quad & 3) << 1) | ((quad >> 2) & 1));
         const uint32_t lo = 0x05040100u, hi = 0x07060302u;
-        _Float16 *dst = values + value_row(c, 0) * value_pitch<kNc>() + at;
+        _Float16 *dst = reinterpret_cast<_Float16 *>(tile + Tile::keys) + value_row(c, 0) * value_pitch<kNc>() + at;
         const auto put = [&](int e, uint32_t x, uint32_t y) {
             *reinterpret_cast<uint2 *>(dst + 8 * e * value_pitch<kNc>()) = make_uint2(x, y);
         };
@@ -383,20 +444,27 @@ __global__ __launch_bounds__(kThreadsShared, 2) void k_shared(Geometry g, Shared
         put(2, __builtin_amdgcn_perm(v[1].y, v[0].y, lo), __builtin_amdgcn_perm(v[3].y, v[2].y, lo));
         put(3, __builtin_amdgcn_perm(v[1].y, v[0].y, hi), __builtin_amdgcn_perm(v[3].y, v[2].y, hi));
     };
-    auto decode = [&]() {
-        // uniform per wave: what can leave the fp16 range or lies past the staged payloads is taken with care
-        bool big = false;
-        for (int row = lane; row < kTok; row += 64)
-            big |= row_part[0][kTok + row] >= kBigScale || row_part[1][kTok + row] >= kBigScale;
-        const bool care = __any(big);
-        if (!care && pay_n[0] <= (uint32_t)kPay)
-            decode_keys(std::true_type{});
+    auto reconstruct = [&](auto side_tag, int buf) {
+        constexpr int s = decltype(side_tag)::value;
+        const uint32_t *sp = stages + (2 * buf + s) * Stage::total;
+        uint32_t *tile = tiles + buf * Tile::total;
+        const uint4v about = *reinterpret_cast<const uint4v *>(sp + Stage::about);
+        const uint32_t base = (uint32_t)__builtin_amdgcn_readfirstlane((int)about[2]);
+        uint32_t care = about[0] | about[1];
+        if (kSides == 2 && s == 1) {
+            const uint32_t *k = stages + 2 * buf * Stage::total + Stage::about;
+            care = k[0] | k[1];
+        }
+        const auto form = [&](auto fast_tag) {
+            if constexpr (s == 0)
+                decode_keys(fast_tag, sp, tile, base);
+            else
+                decode_values(fast_tag, sp, tile, base);
+        };
+        if (__builtin_amdgcn_readfirstlane((int)care) == 0)
+            form(std::true_type{});
         else
-            decode_keys(std::false_type{});
-        if (!care && pay_n[1] <= (uint32_t)kPay)
-            decode_values(std::true_type{});
-        else
-            decode_values(std::false_type{});
+            form(std::false_type{});
     };
 
     // ---- the two products of a tile and the softmax between them --------------------------------------------------------------
@@ -408,254 +476,235 @@ __global__ __launch_bounds__(kThreadsShared, 2) void k_shared(Geometry g, Shared
         const auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
         return f(__uint_as_float(y[0]), __uint_as_float(y[1]));
     };
-    auto attend = [&](int j, auto between) {
+    auto attend = [&](int j, int buf) {
+        const _Float16 *keys = reinterpret_cast<const _Float16 *>(tiles + buf * Tile::total);
+        const _Float16 *values = reinterpret_cast<const _Float16 *>(tiles + buf * Tile::total + Tile::keys);
 #pragma unroll
         for (int sub = 0; sub < kTok; sub += 32) {
             const int t0 = tile_start(j) + sub;
-            float s[kCb][16];  // wide: token 8 (i / 4) + 4 kgrp + i % 4; else (8 of them) 16 (i / 4) + 4 kgrp + i % 4
             constexpr int kS = kWide ? 16 : 8;
+            float s[kS];  // wide: token 8 (i / 4) + 4 kgrp + i % 4; else 16 (i / 4) + 4 kgrp + i % 4
             if constexpr (kWide) {
-                float16_t sc[kCb];
-#pragma unroll
-                for (int cb = 0; cb < kCb; ++cb)
-                    sc[cb] = float16_t{0.f};
+                float16_t sc = float16_t{0.f};
                 const _Float16 *kp = keys + (sub + (lane & 31)) * key_pitch<kNc>() + 8 * kgrp;
 #pragma unroll
-                for (int st = 0; st < kSteps; ++st) {
-                    const half8_t kf = *reinterpret_cast<const half8_t *>(kp + 16 * st);
+                for (int x = 0; x < kSteps; ++x)
+                    sc = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const half8_t *>(kp + 16 * x), qf[x], sc, 0, 0, 0);
 #pragma unroll
-                    for (int cb = 0; cb < kCb; ++cb)
-                        sc[cb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, qf[cb][st], sc[cb], 0, 0, 0);
-                }
-#pragma unroll
-                for (int cb = 0; cb < kCb; ++cb)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        s[cb][i] = sc[cb][i];
+                for (int i = 0; i < 16; ++i)
+                    s[i] = sc[i];
             } else {
                 float4_t sc[2] = {float4_t{0.f, 0.f, 0.f, 0.f}, float4_t{0.f, 0.f, 0.f, 0.f}};
                 const _Float16 *kp = keys + (sub + (lane & 15)) * key_pitch<kNc>() + 8 * kgrp;
 #pragma unroll
-                for (int st = 0; st < kSteps; ++st)
+                for (int x = 0; x < kSteps; ++x)
 #pragma unroll
                     for (int u = 0; u < 2; ++u)
-                        sc[u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(*reinterpret_cast<const half8_t *>(kp + 16 * u * key_pitch<kNc>() + 32 * st),
-                                                                       qf[0][st], sc[u], 0, 0, 0);
+                        sc[u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(*reinterpret_cast<const half8_t *>(kp + 16 * u * key_pitch<kNc>() + 32 * x),
+                                                                       qf[x], sc[u], 0, 0, 0);
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
-                    s[0][i] = sc[i >> 2][i & 3];
+                    s[i] = sc[i >> 2][i & 3];
             }
-            const bool whole = t0 + 32 <= end && t0 + 32 <= least;  // uniform: every row sees every token
-            half8_t ph[kCb][2], pl[kCb][2];
+            float mul = qscale;
+            if (t0 + 32 > end || t0 + 32 > least) {  // uniform: some query row does not see every token
+                const int seen = min(end, vis) - t0 - 4 * kgrp;
 #pragma unroll
-            for (int cb = 0; cb < kCb; ++cb) {
-                float mul = qscale;
-                if (!whole) {
-                    const int seen = min(end, vis[cb]) - t0 - 4 * kgrp;
-#pragma unroll
-                    for (int i = 0; i < kS; ++i)
-                        s[cb][i] = (kWide ? 8 : 16) * (i >> 2) + (i & 3) < seen ? s[cb][i] * qscale : 3.f * kNoToken;
-                    mul = 1.f;
-                }
-                float top = s[cb][0];
-#pragma unroll
-                for (int i = 1; i < kS; ++i)
-                    top = fmaxf(top, s[cb][i]);
-                top = over_lanes(top * mul, [](float x, float y) { return fmaxf(x, y); });
-                // Weights are 2^(s - m_ref): with m_ref 10 below the largest score seen they reach 2^10, their fp16 parts hold weights
-                // down to 2^-24 of the largest as normal numbers, and m_ref is raised (and what was summed scaled) only when a score
-                // would pass 2^15, so hardly ever after the first tiles.
-                const bool raise = top - m_ref[cb] > kRise;
-                if (__any(raise)) {
-                    const float m_new = raise ? top - kTop : m_ref[cb];
-                    const float corr = __builtin_amdgcn_exp2f(m_ref[cb] - m_new);
-                    m_ref[cb] = m_new;
-                    l_run[cb] *= corr;
-#pragma unroll
-                    for (int k = 0; k < kBlocks; ++k)
-#pragma unroll
-                        for (int i = 0; i < kRegs; ++i)
-                            acc[cb][k][i] *= corr;
-                }
-                float sum = 0.f;
-#pragma unroll
-                for (int i = 0; i < kS; ++i) {
-                    const float p = __builtin_amdgcn_exp2f(fmaf(s[cb][i], mul, -m_ref[cb]));
-                    sum += p;
-                    const _Float16 hi = (_Float16)p;
-                    ph[cb][i >> 3][i & 7] = hi;
-                    pl[cb][i >> 3][i & 7] = (_Float16)(p - (float)hi);  // the weight in 22 bits
-                }
-                l_run[cb] += sum;
+                for (int i = 0; i < kS; ++i)
+                    s[i] = (kWide ? 8 : 16) * (i >> 2) + (i & 3) < seen ? s[i] * qscale : 3.f * kNoToken;
+                mul = 1.f;
             }
-            if (sub == 0)
-                between();
+            float top = s[0];
+#pragma unroll
+            for (int i = 1; i < kS; ++i)
+                top = fmaxf(top, s[i]);
+            top = over_lanes(top * mul, [](float x, float y) { return fmaxf(x, y); });
+            // Weights are 2^(s - m_ref): with m_ref 10 below the largest score seen they reach 2^10, their fp16 parts hold weights
+            // down to 2^-24 of the largest as normal numbers, and m_ref is raised (and what was summed scaled) only when a score
+            // would pass 2^15, so hardly ever after the first tiles.
+            const bool raise = top - m_ref > kRise;
+            if (__any(raise)) {
+                const float m_new = raise ? top - kTop : m_ref;
+                const float corr = __builtin_amdgcn_exp2f(m_ref - m_new);
+                m_ref = m_new;
+                l_run *= corr;
+#pragma unroll
+                for (int k = 0; k < kBlocks; ++k)
+#pragma unroll
+                    for (int i = 0; i < kRegs; ++i)
+                        acc[k][i] *= corr;
+            }
+            half8_t ph[2], pl[2];
+            float sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < kS; ++i) {
+                const float p = __builtin_amdgcn_exp2f(fmaf(s[i], mul, -m_ref));
+                sum += p;
+                const _Float16 hi = (_Float16)p;
+                ph[i >> 3][i & 7] = hi;
+                pl[i >> 3][i & 7] = (_Float16)(p - (float)hi);  // the weight in 22 bits
+            }
+            l_run += sum;
             const _Float16 *vp = values + (kWide ? (lane & 31) : (lane & 15)) * value_pitch<kNc>() + sub + 8 * kgrp;
 #pragma unroll
-            for (int k = 0; k < kBlocks; ++k) {
-                if constexpr (kWide) {
+            for (int u = 0; u < (kWide ? 2 : 1); ++u) {
+                half8_t vf[kBlocks];
 #pragma unroll
-                    for (int u = 0; u < 2; ++u) {
-                        const half8_t vf = *reinterpret_cast<const half8_t *>(vp + 32 * k * value_pitch<kNc>() + 16 * u);
+                for (int k = 0; k < kBlocks; ++k)
+                    vf[k] = *reinterpret_cast<const half8_t *>(vp + (kWide ? 32 : 16) * k * value_pitch<kNc>() + 16 * u);
 #pragma unroll
-                        for (int cb = 0; cb < kCb; ++cb) {
-                            acc[cb][k] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, ph[cb][u], acc[cb][k], 0, 0, 0);
-                            acc[cb][k] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, pl[cb][u], acc[cb][k], 0, 0, 0);
-                        }
+                for (int part = 0; part < 2; ++part)
+#pragma unroll
+                    for (int k = 0; k < kBlocks; ++k) {
+                        const half8_t p = part ? pl[u] : ph[u];
+                        if constexpr (kWide)
+                            acc[k] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[k], p, acc[k], 0, 0, 0);
+                        else
+                            acc[k] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf[k], p, acc[k], 0, 0, 0);
                     }
-                } else {
-                    const half8_t vf = *reinterpret_cast<const half8_t *>(vp + 16 * k * value_pitch<kNc>());
-                    acc[0][k] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, ph[0][0], acc[0][k], 0, 0, 0);
-                    acc[0][k] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pl[0][0], acc[0][k], 0, 0, 0);
-                }
             }
         }
     };
 
-    // ---- phases: while one group multiplies a tile, the other reconstructs its next -----------------------------------------------
-    if (group == 0 && n_mine > 0) {
+    // ---- the loop -------------------------------------------------------------------------------------------------------------
+    using Keys = std::integral_constant<int, 0>;
+    using Values = std::integral_constant<int, 1>;
+    if (n_tiles > 0) {
+        request_bounds(0);
         request(0);
-        request_payloads();
-        stage();
+        request_bounds(1);
+        stage(0);
+        request(1);
+        request_bounds(2);
     }
-    __syncthreads();
-    const int n0 = (n_tiles + 1) >> 1, n1 = n_tiles >> 1;
-    const int last = max(2 * n0, n1 > 0 ? 2 * n1 + 1 : 0);
-    for (int ph = 1; ph <= last; ++ph) {
-        if ((ph + group) & 1) {
-            if ((ph - 1 - group) / 2 < n_mine)
-                decode();
-        } else {
-            const int j = (ph - 2 - group) / 2;  // -1 in the second group's first phase
-            const bool more = j + 1 < n_mine;
-            if (more)
-                request(j + 1);
-            const auto payloads = [&]() {
-                if (more)
-                    request_payloads();
-            };
-            if (has_cols && j >= 0 && j < n_mine)
-                attend(j, payloads);
-            else
-                payloads();
-            if (more)
-                stage();
+    lds_barrier();
+    if constexpr (kBufs == 1) {
+        for (int j = 0; j < n_tiles; ++j) {
+            reconstruct(Keys{}, 0);
+            reconstruct(Values{}, 0);
+            lds_barrier();
+            if (has_cols)
+                attend(j, 0);
+            stage(0);
+            request(j + 2);
+            request_bounds(j + 3);
+            lds_barrier();
         }
-        __syncthreads();
+    } else {
+        if (n_tiles > 0) {
+            if (side0 == 0)
+                reconstruct(Keys{}, 0);
+            else
+                reconstruct(Values{}, 0);
+            stage(1);
+            request(2);
+            request_bounds(3);
+        }
+        lds_barrier();
+        for (int j = 0; j < n_tiles; ++j) {
+            if (side0 == 0)
+                reconstruct(Keys{}, (j + 1) & 1);
+            if (has_cols)
+                attend(j, j & 1);
+            if (side0 == 1)
+                reconstruct(Values{}, (j + 1) & 1);
+            stage(j & 1);
+            request(j + 3);
+            request_bounds(j + 4);
+            lds_barrier();
+        }
     }
 
-    // ---- the second group's state joins the first's, which writes the workgroup's ------------------------------------------------
-    float *xch = lds + (size_t)gw * 64 * (kCb * (kBlocks * kRegs + 2)) + lane;  // over everything: no wave reads tiles or tables any more
-#pragma unroll
-    for (int cb = 0; cb < kCb; ++cb)
-        l_run[cb] = over_lanes(l_run[cb], [](float x, float y) { return x + y; });
-    if (group == 1 && has_cols) {
-        int at = 0;
-#pragma unroll
-        for (int cb = 0; cb < kCb; ++cb) {
-            xch[64 * at++] = m_ref[cb];
-            xch[64 * at++] = l_run[cb];
-#pragma unroll
-            for (int k = 0; k < kBlocks; ++k)
-#pragma unroll
-                for (int i = 0; i < kRegs; ++i)
-                    xch[64 * at++] = acc[cb][k][i];
-        }
-    }
-    __syncthreads();
-    if (group == 1 || !has_cols)
+    // ---- the wave's columns of this share -----------------------------------------------------------------------------------------
+    l_run = over_lanes(l_run, [](float x, float y) { return x + y; });
+    if (!there)
         return;
-    int at = 0;
+    const size_t part = head * a.part_pitch + blockIdx.x;
+    if (kgrp == 0) {
+        a.part_ml[2 * part] = m_ref;
+        a.part_ml[2 * part + 1] = l_run;
+    }
+    float *dst = a.part_acc + part * 128;
 #pragma unroll
-    for (int cb = 0; cb < kCb; ++cb) {
-        const float m2 = xch[64 * at++], l2 = xch[64 * at++];
-        const float m = fmaxf(m_ref[cb], m2);
-        const float c1 = __builtin_amdgcn_exp2f(m_ref[cb] - m), c2 = __builtin_amdgcn_exp2f(m2 - m);
-        const int r = col0 + 32 * cb + col;
-        const bool there = r < n_rows;
-        const int rr = there ? r : 0, q = rr / a.G;
-        const size_t head = ((size_t)(b * a.n_share + q) * g.H + h) * a.G + (rr - q * a.G);
-        const size_t part = head * a.part_pitch + blockIdx.x;
-        if (there && kgrp == 0) {
-            a.part_ml[2 * part] = m;
-            a.part_ml[2 * part + 1] = fmaf(l_run[cb], c1, l2 * c2);
-        }
-        float *dst = a.part_acc + part * 128;
+    for (int k = 0; k < kBlocks; ++k) {
+        if constexpr (kWide) {  // row 8 e + c % 8 of block c / 8: the lane has chunks 8 k + 4 kgrp + 0 .. 3
 #pragma unroll
-        for (int k = 0; k < kBlocks; ++k) {
-            float o[kRegs];
+            for (int i = 0; i < 4; ++i)
+                *reinterpret_cast<float4_t *>(dst + 4 * (8 * k + 4 * kgrp + i)) = float4_t{acc[k][i], acc[k][4 + i], acc[k][8 + i], acc[k][12 + i]};
+        } else {
 #pragma unroll
-            for (int i = 0; i < kRegs; ++i)
-                o[i] = fmaf(acc[cb][k][i], c1, xch[64 * at++] * c2);
-            if (!there)
-                continue;
-            if constexpr (kWide) {  // row 8 e + c % 8 of block c / 8: the lane has chunks 8 k + 4 kgrp + 0 .. 3
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    *reinterpret_cast<float4_t *>(dst + 4 * (8 * k + 4 * kgrp + i)) = float4_t{o[i], o[4 + i], o[8 + i], o[12 + i]};
-            } else {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int row = 16 * k + 4 * kgrp + i;
-                    dst[4 * (8 * (row >> 5) + (row & 7)) + ((row >> 3) & 3)] = o[i];
-                }
+            for (int i = 0; i < 4; ++i) {
+                const int row = 16 * k + 4 * kgrp + i;
+                dst[4 * (8 * (row >> 5) + (row & 7)) + ((row >> 3) & 3)] = acc[k][i];
             }
         }
     }
 }
 
-// Columns of a wave: 16, 32 or 64, the fewest with which four waves hold all query rows of a kv head.
-static int shared_cols(const Geometry &g, int n_rows)
+namespace {
+
+enum SharedForm { kSmall, kMiddle, kLarge };
+struct SharedChoice {
+    SharedForm form;
+    bool table;
+    int rows, resident;  // query rows of a workgroup, workgroups of a compute unit
+    size_t lds;
+};
+SharedChoice choose_shared(const Geometry &g, int n_rows)
 {
-    return n_rows <= 64 ? 16 : n_rows <= 128 ? 32 : 64;
+    SharedChoice c;
+    c.form = n_rows <= 64 ? kSmall : n_rows <= 128 ? kMiddle : kLarge;
+    c.rows = c.form == kSmall ? 64 : c.form == kMiddle ? 128 : 256;
+    const int bufs = c.form == kLarge ? FormLarge::kBufs : 1;
+    const int tile = g.n_c == 32 ? TileLds<32>::total : g.n_c == 24 ? TileLds<24>::total : TileLds<16>::total;
+    const int stage = g.n_c == 32 ? StageLds<32>::total : g.n_c == 24 ? StageLds<24>::total : StageLds<16>::total;
+    const auto lds = [&](bool table) { return ((size_t)4 * 48 + (table ? 6 : 2) * (size_t)g.S * 4 + bufs * ((size_t)tile + 2 * stage)) * sizeof(float); };
+    c.table = lds(true) <= kLdsPerCu / 2 || c.form == kLarge && lds(true) <= kLdsPerCu;
+    c.lds = lds(c.table);
+    const int most = c.form == kSmall ? FormSmall::kPerSimd : c.form == kMiddle ? FormMiddle::kPerSimd : 1;
+    c.resident = (int)(kLdsPerCu / c.lds);
+    c.resident = c.resident < most ? c.resident : most;
+    return c;
 }
 
-static size_t shared_lds_bytes(const Geometry &g, int cols, bool table)
+template <int kNc, typename F>
+const void *shared_kernel(bool table, bool pow2)
 {
-    const int group = g.n_c == 32 ? GroupLds<32>::total(g.row_words) : g.n_c == 24 ? GroupLds<24>::total(g.row_words) : GroupLds<16>::total(g.row_words);
-    const size_t loop = 96 + (table ? 2 * side_floats<true>(g.S) : 96 + 2 * side_floats<false>(g.S)) + 2 * (size_t)group;
-    const size_t merge = (size_t)4 * (cols * g.D + 2 * 64 * (cols > 32 ? 2 : 1));
-    return (loop > merge ? loop : merge) * sizeof(float);
+    if (!table)
+        return reinterpret_cast<const void *>(&k_shared<kNc, false, false, F>);
+    return pow2 ? reinterpret_cast<const void *>(&k_shared<kNc, true, true, F>) : reinterpret_cast<const void *>(&k_shared<kNc, true, false, F>);
 }
+template <int kNc>
+const void *shared_kernel(SharedForm form, bool table, bool pow2)
+{
+    return form == kSmall ? shared_kernel<kNc, FormSmall>(table, pow2) : form == kMiddle ? shared_kernel<kNc, FormMiddle>(table, pow2)
+                                                                                          : shared_kernel<kNc, FormLarge>(table, pow2);
+}
+const void *shared_kernel(int n_c, SharedForm form, bool table, bool pow2)
+{
+    return n_c == 32 ? shared_kernel<32>(form, table, pow2) : n_c == 24 ? shared_kernel<24>(form, table, pow2) : shared_kernel<16>(form, table, pow2);
+}
+
+}  // namespace
 
 SharedPlan plan_shared(const Geometry &g, int G, int n_share)
 {
-    const int tok = g.n_c == 16 ? 64 : 32;
-    const int n_rows = G * n_share, per_wg = 4 * shared_cols(g, n_rows);
-    const int64_t per = (int64_t)g.B * g.H * ((n_rows + per_wg - 1) / per_wg), pairs = (g.T + 2 * tok - 1) / (2 * tok);
-    int64_t want = 256 / per;  // one workgroup per compute unit
-    want = want < 1 ? 1 : want < pairs ? want : pairs;
-    const int64_t pairs_per = (pairs + want - 1) / want;
-    return {(int32_t)((pairs + pairs_per - 1) / pairs_per), (int32_t)(pairs_per * 2 * tok)};
+    const SharedChoice c = choose_shared(g, G * n_share);
+    const int tok = g.n_c == 16 ? tile_tokens<16>() : tile_tokens<32>();
+    const int64_t per = (int64_t)g.B * g.H * ((G * n_share + c.rows - 1) / c.rows), tiles = (g.T + tok - 1) / tok;
+    int64_t want = (int64_t)256 * c.resident / per;  // what the chip holds at once
+    want = want > kMostSharedSplits ? kMostSharedSplits : want;
+    want = want < 1 ? 1 : want < tiles ? want : tiles;
+    const int64_t tiles_per = (tiles + want - 1) / want;
+    return {(int32_t)((tiles + tiles_per - 1) / tiles_per), (int32_t)(tiles_per * tok)};
 }
-
-namespace {
-template <int kNc, bool kTable, bool kPow2>
-const void *shared_kernel(int cols)
-{
-    return cols == 16 ? reinterpret_cast<const void *>(&k_shared<kNc, kTable, kPow2, 16>)
-         : cols == 32 ? reinterpret_cast<const void *>(&k_shared<kNc, kTable, kPow2, 32>)
-                      : reinterpret_cast<const void *>(&k_shared<kNc, kTable, kPow2, 64>);
-}
-template <int kNc>
-const void *shared_kernel(bool table, bool pow2, int cols)
-{
-    if (!table)
-        return shared_kernel<kNc, false, false>(cols);
-    return pow2 ? shared_kernel<kNc, true, true>(cols) : shared_kernel<kNc, true, false>(cols);
-}
-const void *shared_kernel(int n_c, bool table, bool pow2, int cols)
-{
-    return n_c == 32 ? shared_kernel<32>(table, pow2, cols) : n_c == 24 ? shared_kernel<24>(table, pow2, cols) : shared_kernel<16>(table, pow2, cols);
-}
-}  // namespace
 
 hipError_t prepare_shared_kernels()
 {
     for (int n_c : {32, 24, 16})
-        for (int cols : {16, 32, 64})
-            for (int form = 0; form < 3; ++form) {
-                const hipError_t err = hipFuncSetAttribute(shared_kernel(n_c, form > 0, form > 1, cols), hipFuncAttributeMaxDynamicSharedMemorySize, (int)kLdsPerCu);
+        for (SharedForm form : {kSmall, kMiddle, kLarge})
+            for (int t = 0; t < 3; ++t) {
+                const hipError_t err = hipFuncSetAttribute(shared_kernel(n_c, form, t > 0, t > 1), hipFuncAttributeMaxDynamicSharedMemorySize, (int)kLdsPerCu);
                 if (err != hipSuccess)
                     return err;
             }
@@ -666,13 +715,14 @@ hipError_t launch_shared(const Geometry &g, const SharedArgs &a, hipStream_t str
 {
     if (g.D != 128 && g.D != 96 && g.D != 64)
         return hipErrorInvalidValue;
-    const int n_rows = a.G * a.n_share, cols = shared_cols(g, n_rows);
-    const bool table = shared_lds_bytes(g, cols, true) <= kLdsPerCu, pow2 = (g.S & (g.S - 1)) == 0;
-    const dim3 grid((unsigned)a.n_splits, (unsigned)(g.B * g.H), (unsigned)((n_rows + 4 * cols - 1) / (4 * cols)));
+    const int n_rows = a.G * a.n_share;
+    const SharedChoice c = choose_shared(g, n_rows);
+    const dim3 grid((unsigned)a.n_splits, (unsigned)(g.B * g.H), (unsigned)((n_rows + c.rows - 1) / c.rows));
+    const unsigned threads = c.form == kLarge ? 64 * FormLarge::kWaves : 64 * FormSmall::kWaves;
     Geometry gc = g;
     SharedArgs ac = a;
     void *args[] = {&gc, &ac};
-    return hipLaunchKernel(shared_kernel(g.n_c, table, pow2, cols), grid, dim3(kThreadsShared), args, shared_lds_bytes(g, cols, table), stream);
+    return hipLaunchKernel(shared_kernel(g.n_c, c.form, c.table, (g.S & (g.S - 1)) == 0), grid, dim3(threads), args, c.lds, stream);
 }
 
 }  // namespace hqmq
