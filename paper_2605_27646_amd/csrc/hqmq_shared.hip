@@ -8,7 +8,7 @@ namespace hqmq {
 
 namespace {
 
-constexpr int kSideThreads = 256;   // that fetch and reconstruct a side (K or V) of a tile; workgroups of four waves do both sides
+constexpr int kMakers = 256;        // threads that fetch and reconstruct tiles: four waves
 constexpr int kLoads = 3;           // code words of a tile and side per thread
 constexpr int kPay = 128;           // outlier payloads of a tile and side kept in LDS
 constexpr float kNoToken = -1.0e30f;
@@ -35,17 +35,17 @@ struct TileLds {
     static constexpr int total = keys + 4 * kNc * value_pitch<kNc>() / 2;
     static_assert(keys % 4 == 0 && total % 4 == 0, "16-byte accesses");
 };
-// A tile's packed rows of one side: code words (room for the largest w) | flags, scales, offsets | payloads, with a slot past the last
-// that is read and not used | two words that say whether the tile wants care, the window's first entry
+// A tile's packed rows of one side: code words (room for the largest w) | flags, scales, places in the outlier list's window | payloads,
+// with a slot past the last that is read and not used | whether the tile wants care, the window's first entry
 template <int kNc>
 struct StageLds {
     static constexpr int kTok = tile_tokens<kNc>();
-    static constexpr int words = kLoads * kSideThreads;
+    static constexpr int words = kLoads * kMakers;
     static_assert(kTok * (kNc * 24 / 32) <= words, "w <= 24");
     static constexpr int pays = words + 3 * kTok;
-    static constexpr int about = pays + 2 * kPay + 4;
-    static constexpr int total = about + 4;
-    static_assert(words % 4 == 0 && kTok % 4 == 0 && about % 4 == 0, "16-byte reads");
+    static constexpr int about = pays + 2 * kPay + 2;
+    static constexpr int total = about + 2;
+    static_assert(words % 4 == 0 && kTok % 4 == 0 && total % 4 == 0, "16-byte reads");
 };
 
 // The 24 primaries are +-u w^m with u one of 1, i, j, k, w = (1 + i + j + k) / 2 and m = 0, 1, 2.  A product with u reorders the
@@ -102,27 +102,32 @@ __device__ __forceinline__ void lds_barrier()
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
-// How a workgroup works: waves, query rows (columns) of each, tiles in LDS.  With two tiles every wave reconstructs its part of
-// the next one and multiplies the present one between two barriers, half of the waves in the other order; with one the workgroups
-// that share a compute unit fill each other's waits.
-template <int kWaves_, int kCols_, int kBufs_, int kPerSimd_>
+// How a workgroup works: waves that multiply, query rows (columns) of each, tiles in LDS, waves per SIMD.  With one tile in LDS four
+// waves reconstruct a tile and then multiply it, and the workgroups that share a compute unit fill each other's waits; with two, four
+// waves more reconstruct the next tile while these multiply.
+template <int kTakers_, int kCols_, int kBufs_, int kPerSimd_>
 struct Form {
-    static constexpr int kWaves = kWaves_, kCols = kCols_, kBufs = kBufs_, kPerSimd = kPerSimd_;
+    static constexpr int kTakers = kTakers_, kCols = kCols_, kBufs = kBufs_, kPerSimd = kPerSimd_;
+    static constexpr int kThreads = 64 * kTakers + (kBufs == 2 ? kMakers : 0);
 };
 using FormSmall = Form<4, 16, 1, 3>;
 using FormMiddle = Form<4, 32, 1, 2>;
-using FormLarge = Form<8, 32, 2, 2>;
+using FormLarge = Form<8, 32, 2, 3>;
+
+typedef __amdgpu_buffer_rsrc_t rsrc_t;
+// n elements from p on, as a buffer: what lies past them reads as zero
+template <typename T>
+__device__ __forceinline__ rsrc_t buffer_of(const T *p, uint32_t n) { return __builtin_amdgcn_make_buffer_rsrc((void *)p, 0, (int)(n * (uint32_t)sizeof(T)), 0x00020000); }
 
 }  // namespace
 
 template <int kNc, bool kTable, bool kPow2, typename F>
-__global__ __launch_bounds__(64 * F::kWaves, F::kPerSimd) void k_shared(Geometry g, SharedArgs a)
+__global__ __launch_bounds__(F::kThreads, F::kPerSimd) void k_shared(Geometry g, SharedArgs a)
 {
     using Tile = TileLds<kNc>;
     using Stage = StageLds<kNc>;
     constexpr int kTok = tile_tokens<kNc>(), kD = 4 * kNc;
-    constexpr int kWaves = F::kWaves, kCols = F::kCols, kBufs = F::kBufs, kThreads = 64 * kWaves;
-    constexpr int kSides = kWaves == 4 ? 2 : 1;   // that a wave fetches and reconstructs
+    constexpr int kCols = F::kCols, kBufs = F::kBufs, kThreads = F::kThreads, kWaves = kThreads / 64;
     constexpr bool kWide = kCols == 32;           // 32x32x16 products, else 16x16x32
     constexpr int kSteps = kWide ? kD / 16 : kD / 32;
     constexpr int kBlocks = kWide ? kD / 32 : kD / 16;
@@ -137,22 +142,22 @@ __global__ __launch_bounds__(64 * F::kWaves, F::kPerSimd) void k_shared(Geometry
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int st = tid & (kSideThreads - 1), sw = wave & 3;  // within the threads of a side
-    const int side0 = kSides == 2 ? 0 : wave >> 2;           // the first side of this wave
+    const bool maker = kBufs == 1 || wave < 4, taker = kBufs == 1 || wave >= 4;  // uniform
+    const int st = tid & (kMakers - 1);
     const int seg = blockIdx.y, b = seg / g.H, h = seg % g.H;
     const uint32_t row_words = kNc == 32 ? (uint32_t)g.w : (uint32_t)g.row_words;
     const uint32_t w = g.w, w_idx = g.w_idx;
 
     // ---- columns of this wave: query rows r of the kv head ---------------------------------------------------------
     const int n_rows = a.n_share * a.G;
-    const int col0 = ((int)blockIdx.z * kWaves + wave) * kCols;
+    const int col0 = ((int)blockIdx.z * F::kTakers + (kBufs == 1 ? wave : wave - 4)) * kCols;
     const int col = lane & (kCols - 1);
     const int kgrp = lane / kCols;         // which 8 of a product's terms the lane supplies, which rows of a result it holds
-    const bool has_cols = col0 < n_rows;   // uniform
+    const bool has_cols = taker && col0 < n_rows;  // uniform
     const uint32_t flip = a.qscale < 0.f ? 0x80008000u : 0u;
     const float qscale = fabsf(a.qscale);  // a negative scale goes into the queries' signs
     const int r = col0 + col;
-    const bool there = r < n_rows;
+    const bool there = taker && r < n_rows;
     size_t head;
     {
         const int rr = there ? r : 0, m = rr / a.G;
@@ -232,82 +237,65 @@ __global__ __launch_bounds__(64 * F::kWaves, F::kPerSimd) void k_shared(Geometry
             acc[k][i] = 0.f;
 
     // ---- a tile's packed rows on their way to LDS ------------------------------------------------------------------------
-    // Every load is issued a tile's time or more before its value is needed, and without a condition, past the last tile for that
-    // one again.  The outlier list's bounds come a tile before rows and payloads.
-    uint32_t cw[kSides][kLoads], fw = 0u, ro = 0u, bounds = 0u;
+    // Every load is issued a tile's time or more before its value is needed, and without a condition: tokens past the last read as
+    // zeros (no flags, a scale of zero).  The outlier list's bounds come a tile before rows and payloads.
+    // Waves 0 and 1 look after K's rows and payloads, 2 and 3 after V's; all of them fetch code words of both.
+    const bool of_v = (wave & 2) != 0, row_wave = (wave & 1) == 0;
+    const uint32_t n_tok = (uint32_t)max(end - begin, 0);
+    const int64_t first_row = (int64_t)seg * g.T + begin;
+    const rsrc_t code_k = buffer_of(a.k.codes + first_row * row_words, n_tok * row_words);
+    const rsrc_t code_v = buffer_of(a.v.codes + first_row * row_words, n_tok * row_words);
+    const rsrc_t flag_b = buffer_of((of_v ? a.v.flags : a.k.flags) + first_row, n_tok);
+    const rsrc_t scale_b = buffer_of((of_v ? a.v.sigma : a.k.sigma) + first_row, n_tok);
+    const rsrc_t place_b = buffer_of((of_v ? a.v.row_off : a.k.row_off) + first_row, n_tok + 1u);
+    const uint2 *const list = reinterpret_cast<const uint2 *>(of_v ? a.v.outliers : a.k.outliers);
+    const uint2 *const no_list = reinterpret_cast<const uint2 *>(of_v ? a.v.codes : a.k.codes);  // any two words: a row has three or more
+    const uint32_t capacity = (uint32_t)min(of_v ? a.v.outlier_capacity : a.k.outlier_capacity, (uint64_t)0xffffffffu);
+    uint32_t code_at = 4u * st, row_at = 4u * (lane & (kTok - 1)), bound_at = (lane & 1) * kTok;
+    uint32_t cw[2][kLoads], fw = 0u, ro = 0u, bounds = 0u;
     uint16_t sg = 0u;  // as loaded: widening it before it is staged would wait for it
     uint2 pay = make_uint2(0u, 0u);
-    uint32_t next_base[kSides], next_n[kSides];  // window of the outlier list, of the tile on its way
-    int next_rows = 0;
-    uint32_t next_in_list = 0u;  // of the side that this wave fetches payloads of
-    const int row_side = kSides == 2 ? (st / kTok) & 1 : side0, pay_side = kSides == 2 ? sw >> 1 : side0;
-    auto tile_start = [&](int j) { return begin + max(min(j, n_tiles - 1), 0) * kTok; };
-    auto request_bounds = [&](int j) {  // lanes 0 .. 3: first and end of K's window, of V's
-        const int t0 = tile_start(j);
-        const uint32_t *off = (lane & 2) ? a.v.row_off : a.k.row_off;
-        bounds = off[(int64_t)seg * g.T + ((lane & 1) ? min(t0 + kTok, end) : t0)];
+    uint32_t next_base = 0u, next_n = 0u, next_in_list = 0u;  // window of the outlier list, of the tile on its way
+    auto request_bounds = [&]() {  // even lanes: first entry of the next tile's window, odd ones: the entry behind it
+        bounds = __builtin_amdgcn_raw_buffer_load_b32(place_b, 4u * min(bound_at, n_tok), 0, 0);
+        bound_at += kTok;
     };
-    auto request = [&](int j) {
-        const int t0 = tile_start(j);
-        const int nr = min(kTok, end - t0);
-        const int64_t R0 = (int64_t)seg * g.T + t0;
-        const uint32_t last = (uint32_t)nr * row_words - 1u;
+    auto request = [&]() {
 #pragma unroll
-        for (int s = 0; s < kSides; ++s) {
-            const uint32_t *src = (side0 + s ? a.v.codes : a.k.codes) + R0 * row_words;
-#pragma unroll
-            for (int i = 0; i < kLoads; ++i)
-                cw[s][i] = src[min((uint32_t)st + kSideThreads * i, last)];
+        for (int i = 0; i < kLoads; ++i) {
+            cw[0][i] = __builtin_amdgcn_raw_buffer_load_b32(code_k, code_at + 4u * kMakers * i, 0, 0);
+            cw[1][i] = __builtin_amdgcn_raw_buffer_load_b32(code_v, code_at + 4u * kMakers * i, 0, 0);
         }
-        next_rows = nr;
-        const int64_t at = R0 + min(st % kTok, nr - 1);
-        fw = (row_side ? a.v.flags : a.k.flags)[at];
-        sg = (row_side ? a.v.sigma : a.k.sigma)[at];
-        ro = (row_side ? a.v.row_off : a.k.row_off)[at];
-#pragma unroll
-        for (int s = 0; s < kSides; ++s) {
-            next_base[s] = (uint32_t)__builtin_amdgcn_readlane((int)bounds, 2 * (side0 + s));
-            next_n[s] = (uint32_t)__builtin_amdgcn_readlane((int)bounds, 2 * (side0 + s) + 1) - next_base[s];
-        }
-        const AttendSide &sd = pay_side ? a.v : a.k;
-        const uint32_t base = kSides == 2 && pay_side ? next_base[kSides - 1] : next_base[0];
-        const uint32_t n = kSides == 2 && pay_side ? next_n[kSides - 1] : next_n[0];
-        next_in_list = (uint64_t)base < sd.outlier_capacity ? (uint32_t)min((uint64_t)n, sd.outlier_capacity - base) : 0u;
-        const uint2 *list = next_in_list ? reinterpret_cast<const uint2 *>(sd.outliers) + base : reinterpret_cast<const uint2 *>(sd.codes);
-        // an empty window: the first code words (a row has three or more), which nothing uses
-        pay = list[next_in_list ? min((uint32_t)st & (kPay - 1), next_in_list - 1u) : 0u];
+        fw = __builtin_amdgcn_raw_buffer_load_b32(flag_b, row_at, 0, 0);
+        sg = __builtin_amdgcn_raw_buffer_load_b16(scale_b, row_at >> 1, 0, 0);
+        ro = __builtin_amdgcn_raw_buffer_load_b32(place_b, row_at, 0, 0);
+        code_at += 4u * kTok * row_words;
+        row_at += 4u * kTok;
+        next_base = (uint32_t)__builtin_amdgcn_readlane((int)bounds, 0);
+        next_n = (uint32_t)__builtin_amdgcn_readlane((int)bounds, 1) - next_base;
+        next_in_list = min(next_n, capacity - min(next_base, capacity));
+        const uint2 *src = next_in_list ? list + next_base : no_list;
+        pay = src[min((uint32_t)st & (kPay - 1), max(next_in_list, 1u) - 1u)];
     };
     auto stage = [&](int buf) {
+        uint32_t *dst = stages + 2 * buf * Stage::total;
 #pragma unroll
-        for (int s = 0; s < kSides; ++s) {
-            uint32_t *dst = stages + (2 * buf + side0 + s) * Stage::total;
-#pragma unroll
-            for (int i = 0; i < kLoads; ++i)
-                dst[st + kSideThreads * i] = cw[s][i];
-            if (sw == 0 && lane == 0)
-                dst[Stage::about + 2] = next_base[s];
+        for (int i = 0; i < kLoads; ++i) {
+            dst[st + kMakers * i] = cw[0][i];
+            dst[Stage::total + st + kMakers * i] = cw[1][i];
         }
-        if (st < kSides * kTok) {  // uniform for 64 tokens or both sides; rows that are not there: a scale of zero and no flags
-            uint32_t *dst = stages + (2 * buf + row_side) * Stage::total + Stage::words + st % kTok;
-            const bool in = st % kTok < next_rows;
-            dst[0] = in ? fw : 0u;
-            dst[kTok] = in ? (uint32_t)sg : 0u;
-            dst[2 * kTok] = ro;
-        }
-        {
+        uint32_t *mine = dst + (of_v ? Stage::total : 0);
+        if (row_wave) {
+            uint32_t *rp = mine + Stage::words + (lane & (kTok - 1));
+            rp[0] = fw;
+            rp[kTok] = (uint32_t)sg;
+            rp[2 * kTok] = ro - next_base;
             // what can leave the fp16 range, or payloads past the staged ones, send the tile down a careful form
-            const bool mine = st < kSides * kTok && st % kTok < next_rows && (uint32_t)sg >= kBigScale;
-            bool care = __any(mine);
-#pragma unroll
-            for (int s = 0; s < kSides; ++s)
-                care = care || next_n[s] > (uint32_t)kPay;
-            if (sw < 2 && lane == 0)  // the waves that stage rows; 64 tokens of both sides are two waves'
-                stages[(2 * buf + side0) * Stage::total + Stage::about + sw] = care ? 1u : 0u;
+            const bool care = __any((uint32_t)sg >= kBigScale) || next_n > (uint32_t)kPay;
+            *reinterpret_cast<uint2 *>(mine + Stage::about) = make_uint2(care ? 1u : 0u, next_base);
         }
         const uint32_t slot = (uint32_t)st & (kPay - 1);
-        if (kSides == 2 || sw < 2)
-            reinterpret_cast<uint2 *>(stages + (2 * buf + pay_side) * Stage::total + Stage::pays)[slot] =
-                slot < next_in_list ? pay : make_uint2(0u, 0u);
+        reinterpret_cast<uint2 *>(mine + Stage::pays)[slot] = slot < next_in_list ? pay : make_uint2(0u, 0u);
     };
 
     // ---- reconstruction ----------------------------------------------------------------------------------------------------
@@ -374,13 +362,16 @@ __global__ __launch_bounds__(64 * F::kWaves, F::kPerSimd) void k_shared(Geometry
     // A thread's part of a tile: two pairs of neighbouring chunks of K, one chunk of V in four neighbouring tokens.  Threads beyond a
     // tile's last unit (24 chunks per row) do that one again.
     constexpr int kKeyUnits = kTok * kNc / 2, kValueUnits = kTok * kNc / 4;
-    static_assert(kKeyUnits <= 2 * kSideThreads && kValueUnits <= kSideThreads, "a thread's four chunks of a side");
-    auto decode_keys = [&](auto fast_tag, const uint32_t *sp, uint32_t *tile, uint32_t base) {
+    static_assert(kKeyUnits <= 2 * kMakers && kValueUnits <= kMakers, "a thread's four chunks of a side");
+    auto decode_keys = [&](int buf) {
+        const uint32_t *sp = stages + 2 * buf * Stage::total;
+        _Float16 *keys = reinterpret_cast<_Float16 *>(tiles + buf * Tile::total);
+        const uint2 about = *reinterpret_cast<const uint2 *>(sp + Stage::about);
         int row[2], c[2];
         uint32_t code[4], word[2], scale[2], off[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            const int u = min(st + kSideThreads * i, kKeyUnits - 1);
+            const int u = min(st + kMakers * i, kKeyUnits - 1);
             row[i] = u / (kNc / 2);
             c[i] = 2 * (u % (kNc / 2));
             code[2 * i] = read_code(sp, row[i], c[i]);
@@ -390,28 +381,36 @@ __global__ __launch_bounds__(64 * F::kWaves, F::kPerSimd) void k_shared(Geometry
             scale[i] = rp[kTok];
             off[i] = rp[2 * kTok];
         }
-        bool flag[4];
-        Pre f[4];
+        const auto form = [&](auto fast_tag) {
+            bool flag[4];
+            Pre f[4];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            flag[2 * i] = (word[i] >> c[i]) & 1u;
-            flag[2 * i + 1] = (word[i] >> c[i]) & 2u;
-            const uint32_t slot = off[i] - base + __popc(word[i] & ((1u << c[i]) - 1u));
-            f[2 * i] = pre(fast_tag, sp, code[2 * i], slot);
-            f[2 * i + 1] = pre(fast_tag, sp, code[2 * i + 1], slot + (flag[2 * i] ? 1u : 0u));
-        }
-        float4_t d[4];
+            for (int i = 0; i < 2; ++i) {
+                flag[2 * i] = (word[i] >> c[i]) & 1u;
+                flag[2 * i + 1] = (word[i] >> c[i]) & 2u;
+                const uint32_t slot = off[i] + __popc(word[i] & ((1u << c[i]) - 1u));
+                f[2 * i] = pre(fast_tag, sp, code[2 * i], slot);
+                f[2 * i + 1] = pre(fast_tag, sp, code[2 * i + 1], slot + (flag[2 * i] ? 1u : 0u));
+            }
+            float4_t d[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            d[i] = direction(0, f[i]);
+            for (int i = 0; i < 4; ++i)
+                d[i] = direction(0, f[i]);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const uint2 x = finish(fast_tag, 0, base, f[2 * i], d[2 * i], scale[i], flag[2 * i]);
-            const uint2 y = finish(fast_tag, 0, base, f[2 * i + 1], d[2 * i + 1], scale[i], flag[2 * i + 1]);
-            *reinterpret_cast<uint4v *>(reinterpret_cast<_Float16 *>(tile) + row[i] * key_pitch<kNc>() + 4 * c[i]) = uint4v{x.x, x.y, y.x, y.y};
-        }
+            for (int i = 0; i < 2; ++i) {
+                const uint2 x = finish(fast_tag, 0, about.y, f[2 * i], d[2 * i], scale[i], flag[2 * i]);
+                const uint2 y = finish(fast_tag, 0, about.y, f[2 * i + 1], d[2 * i + 1], scale[i], flag[2 * i + 1]);
+                *reinterpret_cast<uint4v *>(keys + row[i] * key_pitch<kNc>() + 4 * c[i]) = uint4v{x.x, x.y, y.x, y.y};
+            }
+        };
+        if (__builtin_amdgcn_readfirstlane((int)about.x) == 0)
+            form(std::true_type{});
+        else
+            form(std::false_type{});
     };
-    auto decode_values = [&](auto fast_tag, const uint32_t *sp, uint32_t *tile, uint32_t base) {
+    auto decode_values = [&](int buf) {
+        const uint32_t *sp = stages + (2 * buf + 1) * Stage::total;
+        const uint2 about = *reinterpret_cast<const uint2 *>(sp + Stage::about);
         const int u = min(st, kValueUnits - 1), c = u % kNc, quad = u / kNc;
         uint32_t code[4];
 #pragma unroll
@@ -420,48 +419,32 @@ __global__ __launch_bounds__(64 * F::kWaves, F::kPerSimd) void k_shared(Geometry
         const uint32_t *rp = sp + Stage::words + 4 * quad;
         const uint4v word = *reinterpret_cast<const uint4v *>(rp), scale = *reinterpret_cast<const uint4v *>(rp + kTok);
         const uint4v off = *reinterpret_cast<const uint4v *>(rp + 2 * kTok);
-        Pre f[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            f[i] = pre(fast_tag, sp, code[i], off[i] - base + __popc(word[i] & ((1u << c) - 1u)));
-        float4_t d[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            d[i] = direction(1, f[i]);
-        uint2 v[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            v[i] = finish(fast_tag, 1, base, f[i], d[i], scale[i], (word[i] >> c) & 1u);
         // where the four tokens stand in the order in which a product takes a block of scores as its operand
         const int at = 4 * (kWide ? (quad & ~3) | ((quad & 1) << 1) | ((quad >> 1) & 1) : (quad & ~7) | ((quad & 3) << 1) | ((quad >> 2) & 1));
-        const uint32_t lo = 0x05040100u, hi = 0x07060302u;
-        _Float16 *dst = reinterpret_cast<_Float16 *>(tile + Tile::keys) + value_row(c, 0) * value_pitch<kNc>() + at;
-        const auto put = [&](int e, uint32_t x, uint32_t y) {
-            *reinterpret_cast<uint2 *>(dst + 8 * e * value_pitch<kNc>()) = make_uint2(x, y);
-        };
-        put(0, __builtin_amdgcn_perm(v[1].x, v[0].x, lo), __builtin_amdgcn_perm(v[3].x, v[2].x, lo));
-        put(1, __builtin_amdgcn_perm(v[1].x, v[0].x, hi), __builtin_amdgcn_perm(v[3].x, v[2].x, hi));
-        put(2, __builtin_amdgcn_perm(v[1].y, v[0].y, lo), __builtin_amdgcn_perm(v[3].y, v[2].y, lo));
-        put(3, __builtin_amdgcn_perm(v[1].y, v[0].y, hi), __builtin_amdgcn_perm(v[3].y, v[2].y, hi));
-    };
-    auto reconstruct = [&](auto side_tag, int buf) {
-        constexpr int s = decltype(side_tag)::value;
-        const uint32_t *sp = stages + (2 * buf + s) * Stage::total;
-        uint32_t *tile = tiles + buf * Tile::total;
-        const uint4v about = *reinterpret_cast<const uint4v *>(sp + Stage::about);
-        const uint32_t base = (uint32_t)__builtin_amdgcn_readfirstlane((int)about[2]);
-        uint32_t care = about[0] | about[1];
-        if (kSides == 2 && s == 1) {
-            const uint32_t *k = stages + 2 * buf * Stage::total + Stage::about;
-            care = k[0] | k[1];
-        }
+        _Float16 *dst = reinterpret_cast<_Float16 *>(tiles + buf * Tile::total + Tile::keys) + value_row(c, 0) * value_pitch<kNc>() + at;
         const auto form = [&](auto fast_tag) {
-            if constexpr (s == 0)
-                decode_keys(fast_tag, sp, tile, base);
-            else
-                decode_values(fast_tag, sp, tile, base);
+            Pre f[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                f[i] = pre(fast_tag, sp, code[i], off[i] + __popc(word[i] & ((1u << c) - 1u)));
+            float4_t d[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                d[i] = direction(1, f[i]);
+            uint2 v[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                v[i] = finish(fast_tag, 1, about.y, f[i], d[i], scale[i], (word[i] >> c) & 1u);
+            const uint32_t lo = 0x05040100u, hi = 0x07060302u;
+            const auto put = [&](int e, uint32_t x, uint32_t y) {
+                *reinterpret_cast<uint2 *>(dst + 8 * e * value_pitch<kNc>()) = make_uint2(x, y);
+            };
+            put(0, __builtin_amdgcn_perm(v[1].x, v[0].x, lo), __builtin_amdgcn_perm(v[3].x, v[2].x, lo));
+            put(1, __builtin_amdgcn_perm(v[1].x, v[0].x, hi), __builtin_amdgcn_perm(v[3].x, v[2].x, hi));
+            put(2, __builtin_amdgcn_perm(v[1].y, v[0].y, lo), __builtin_amdgcn_perm(v[3].y, v[2].y, lo));
+            put(3, __builtin_amdgcn_perm(v[1].y, v[0].y, hi), __builtin_amdgcn_perm(v[3].y, v[2].y, hi));
         };
-        if (__builtin_amdgcn_readfirstlane((int)care) == 0)
+        if (__builtin_amdgcn_readfirstlane((int)about.x) == 0)
             form(std::true_type{});
         else
             form(std::false_type{});
@@ -481,7 +464,7 @@ __global__ __launch_bounds__(64 * F::kWaves, F::kPerSimd) void k_shared(Geometry
         const _Float16 *values = reinterpret_cast<const _Float16 *>(tiles + buf * Tile::total + Tile::keys);
 #pragma unroll
         for (int sub = 0; sub < kTok; sub += 32) {
-            const int t0 = tile_start(j) + sub;
+            const int t0 = begin + j * kTok + sub;
             constexpr int kS = kWide ? 16 : 8;
             float s[kS];  // wide: token 8 (i / 4) + 4 kgrp + i % 4; else 16 (i / 4) + 4 kgrp + i % 4
             if constexpr (kWide) {
@@ -567,50 +550,49 @@ __global__ __launch_bounds__(64 * F::kWaves, F::kPerSimd) void k_shared(Geometry
     };
 
     // ---- the loop -------------------------------------------------------------------------------------------------------------
-    using Keys = std::integral_constant<int, 0>;
-    using Values = std::integral_constant<int, 1>;
-    if (n_tiles > 0) {
-        request_bounds(0);
-        request(0);
-        request_bounds(1);
+    if (maker && n_tiles > 0) {
+        request_bounds();
+        request();
+        request_bounds();
         stage(0);
-        request(1);
-        request_bounds(2);
+        request();
+        request_bounds();
     }
     lds_barrier();
     if constexpr (kBufs == 1) {
         for (int j = 0; j < n_tiles; ++j) {
-            reconstruct(Keys{}, 0);
-            reconstruct(Values{}, 0);
+            decode_keys(0);
+            decode_values(0);
             lds_barrier();
             if (has_cols)
                 attend(j, 0);
             stage(0);
-            request(j + 2);
-            request_bounds(j + 3);
+            request();
+            request_bounds();
+            lds_barrier();
+        }
+    } else if (maker) {
+        if (n_tiles > 0) {
+            decode_keys(0);
+            decode_values(0);
+            stage(1);
+            request();
+            request_bounds();
+        }
+        lds_barrier();
+        for (int j = 1; j <= n_tiles; ++j) {  // past the last tile: zeros, which nothing reads
+            decode_keys(j & 1);
+            decode_values(j & 1);
+            stage((j + 1) & 1);
+            request();
+            request_bounds();
             lds_barrier();
         }
     } else {
-        if (n_tiles > 0) {
-            if (side0 == 0)
-                reconstruct(Keys{}, 0);
-            else
-                reconstruct(Values{}, 0);
-            stage(1);
-            request(2);
-            request_bounds(3);
-        }
         lds_barrier();
         for (int j = 0; j < n_tiles; ++j) {
-            if (side0 == 0)
-                reconstruct(Keys{}, (j + 1) & 1);
             if (has_cols)
                 attend(j, j & 1);
-            if (side0 == 1)
-                reconstruct(Values{}, (j + 1) & 1);
-            stage(j & 1);
-            request(j + 3);
-            request_bounds(j + 4);
             lds_barrier();
         }
     }
@@ -659,7 +641,7 @@ SharedChoice choose_shared(const Geometry &g, int n_rows)
     const int tile = g.n_c == 32 ? TileLds<32>::total : g.n_c == 24 ? TileLds<24>::total : TileLds<16>::total;
     const int stage = g.n_c == 32 ? StageLds<32>::total : g.n_c == 24 ? StageLds<24>::total : StageLds<16>::total;
     const auto lds = [&](bool table) { return ((size_t)4 * 48 + (table ? 6 : 2) * (size_t)g.S * 4 + bufs * ((size_t)tile + 2 * stage)) * sizeof(float); };
-    c.table = lds(true) <= kLdsPerCu / 2 || c.form == kLarge && lds(true) <= kLdsPerCu;
+    c.table = lds(true) <= (c.form == kLarge ? kLdsPerCu : kLdsPerCu / 2);
     c.lds = lds(c.table);
     const int most = c.form == kSmall ? FormSmall::kPerSimd : c.form == kMiddle ? FormMiddle::kPerSimd : 1;
     c.resident = (int)(kLdsPerCu / c.lds);
@@ -718,7 +700,7 @@ hipError_t launch_shared(const Geometry &g, const SharedArgs &a, hipStream_t str
     const int n_rows = a.G * a.n_share;
     const SharedChoice c = choose_shared(g, n_rows);
     const dim3 grid((unsigned)a.n_splits, (unsigned)(g.B * g.H), (unsigned)((n_rows + c.rows - 1) / c.rows));
-    const unsigned threads = c.form == kLarge ? 64 * FormLarge::kWaves : 64 * FormSmall::kWaves;
+    const unsigned threads = c.form == kLarge ? FormLarge::kThreads : c.form == kMiddle ? FormMiddle::kThreads : FormSmall::kThreads;
     Geometry gc = g;
     SharedArgs ac = a;
     void *args[] = {&gc, &ac};
