@@ -861,7 +861,7 @@ static int32_t attend_impl(const hqmq_params *params, int32_t n_q_heads, const v
     a.joint = plan.joint;
     hipError_t err = launch_attend_partials(g, a, static_cast<hipStream_t>(stream));
     if (err == hipSuccess)
-        err = launch_attend_merge((int64_t)g.B * g.H * G, a, static_cast<hipStream_t>(stream));
+        err = launch_attend_merge((int64_t)g.B * g.H * G, a, false, static_cast<hipStream_t>(stream));
     if (err != hipSuccess)
         return hip_failed(err);
     return HQMQ_OK;
@@ -1033,7 +1033,8 @@ extern "C" int32_t hqmq_attend_shared(const hqmq_params *params, int32_t n_share
         if (err != hipSuccess)
             return hip_failed(err);
     }
-    err = launch_attend_merge((int64_t)g.B * n_share * g.H * G, o, static_cast<hipStream_t>(stream));
+    const int64_t heads = (int64_t)g.B * n_share * g.H * G;
+    err = launch_attend_merge(heads, o, heads >= 512, static_cast<hipStream_t>(stream));
     return err == hipSuccess ? HQMQ_OK : hip_failed(err);
 }
 

@@ -159,6 +159,14 @@ __device__ __forceinline__ float max_over_rows(float v)
     return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
+// The largest of 16 neighbouring lanes' values, of the wave's first 16.
+__device__ __forceinline__ int max_of_row(int v)
+{
+    for (int d = 1; d < 16; d *= 2)
+        v = max(v, __shfl_xor(v, d));
+    return __builtin_amdgcn_readfirstlane(v);
+}
+
 __device__ __forceinline__ uint32_t pack_half2(float lo, float hi)
 {
     typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
@@ -204,12 +212,14 @@ __global__ __launch_bounds__(kAttThreads, 2) void k_attend_partial(Geometry g, A
     // tokens this lane's query head (n16) may see: all of them unless the caller limits it (a query
     // token of a multi-token step sees the cache only up to its own position)
     int vis = 0x7fffffff;
-    if (a.visible)
+    int row_end = min(g.T, (split + 1) * a.rows_per_split);
+    if (a.visible) {
         vis = (n16 < G) ? a.visible[((size_t)b * g.H + h) * G + n16] : 0;
+        row_end = min(row_end, max_of_row(vis));  // rows that no query head sees are not read
+    }
     const uint32_t w = g.w, w_idx = g.w_idx;
     const uint32_t row_words = kNc == 32 ? w : (uint32_t)g.row_words;
     const int row_begin = split * a.rows_per_split;
-    const int row_end = min(g.T, row_begin + a.rows_per_split);
 
     uint32_t *stage_k = stage_all + (wv * 2 + 0) * kSideWords;
     uint32_t *stage_v = stage_all + (wv * 2 + 1) * kSideWords;
@@ -643,12 +653,14 @@ __global__ __launch_bounds__(kJointThreads, 1) void k_attend_joint(Geometry g, A
     // tokens this lane's query head (n16) may see: all of them unless the caller limits it (a query
     // token of a multi-token step sees the cache only up to its own position)
     int vis = 0x7fffffff;
-    if (a.visible)
+    int row_end = min(g.T, (split + 1) * a.rows_per_split);
+    if (a.visible) {
         vis = (n16 < G) ? a.visible[((size_t)b * g.H + h) * G + n16] : 0;
+        row_end = min(row_end, max_of_row(vis));  // rows that no query head sees are not read
+    }
     const uint32_t w = g.w, w_idx = g.w_idx;
     const uint32_t row_words = kNc == 32 ? w : (uint32_t)g.row_words;
     const int row_begin = split * a.rows_per_split;
-    const int row_end = min(g.T, row_begin + a.rows_per_split);
 
     uint32_t *stage_k = stage_all + (wv * 2 + 0) * kSideWords;
     uint32_t *stage_v = stage_all + (wv * 2 + 1) * kSideWords;
@@ -1253,13 +1265,13 @@ hipError_t launch_attend_partials(const Geometry &g, const AttendArgs &a, hipStr
     return hipGetLastError();
 }
 
-hipError_t launch_attend_merge(int64_t heads, const AttendArgs &a, hipStream_t stream)
+hipError_t launch_attend_merge(int64_t heads, const AttendArgs &a, bool many, hipStream_t stream)
 {
     const dim3 outputs((unsigned)heads, (unsigned)((a.D + kMergeDims - 1) / kMergeDims));
     static_assert(kMostParts <= 64 * 16, "a lane per split of a wave's share");
     if (a.part_pitch > kMostParts)
         return hipErrorInvalidValue;
-    if (a.part_pitch <= kMergeFew)
+    if (a.part_pitch <= kMergeFew || (many && a.part_pitch <= 64 * 4))
         hipLaunchKernelGGL(k_attend_merge<4>, outputs, dim3(64 * 4), 0, stream, a);
     else
         hipLaunchKernelGGL(k_attend_merge<16>, outputs, dim3(64 * 16), 0, stream, a);

@@ -400,7 +400,8 @@ hipError_t launch_outlier_list(const Geometry &g, const WorkspaceOffsets &wo, co
 hipError_t launch_decode(const Geometry &g, const DecodeBatch &batch, int n_tensors, hipStream_t stream);
 hipError_t prepare_attend_kernels();  // once per device, before the first launch_attend on it
 hipError_t launch_attend_partials(const Geometry &g, const AttendArgs &args, hipStream_t stream);
-hipError_t launch_attend_merge(int64_t heads, const AttendArgs &args, hipStream_t stream);  // uses what describes the partial sums and the results
+// Merges what the partial sums' arrays of `args` hold.  many: of so many heads that workgroups of four waves fill the chip.
+hipError_t launch_attend_merge(int64_t heads, const AttendArgs &args, bool many, hipStream_t stream);
 constexpr int kMostParts = 1024;  // that launch_attend_merge merges
 
 }  // namespace hqmq

@@ -28,12 +28,15 @@ constexpr int key_pitch() { return 4 * kNc + 8; }  // halves; an odd number of 1
 template <int kNc>
 constexpr int value_pitch() { return tile_tokens<kNc>() + 8; }
 
-// A tile in LDS, in 32-bit words: keys [tokens][key_pitch] halves | values [D rows][value_pitch] halves
+// A tile in LDS, in 32-bit words: keys [tokens][key_pitch] halves; values [D rows][value_pitch] halves
 template <int kNc>
 struct TileLds {
     static constexpr int keys = tile_tokens<kNc>() * key_pitch<kNc>() / 2;
-    static constexpr int total = keys + 4 * kNc * value_pitch<kNc>() / 2;
-    static_assert(keys % 4 == 0 && total % 4 == 0, "16-byte accesses");
+    static constexpr int values = 4 * kNc * value_pitch<kNc>() / 2;
+    static_assert(keys % 4 == 0 && values % 4 == 0, "16-byte accesses");
+    // of a form with so many tiles in flight: of two, the values one longer
+    __host__ __device__ static constexpr int value_bufs(int bufs) { return bufs == 2 ? 3 : 1; }
+    __host__ __device__ static constexpr int total(int bufs) { return bufs * keys + value_bufs(bufs) * values; }
 };
 // A tile's packed rows of one side: code words (room for the largest w) | flags, scales, places in the outlier list's window | payloads,
 // with a slot past the last that is read and not used | whether the tile wants care, the window's first entry
@@ -129,6 +132,7 @@ __global__ __launch_bounds__(F::kThreads, F::kPerSimd) void k_shared(Geometry g,
     constexpr int kTok = tile_tokens<kNc>(), kD = 4 * kNc;
     constexpr int kCols = F::kCols, kBufs = F::kBufs, kThreads = F::kThreads, kWaves = kThreads / 64;
     constexpr bool kWide = kCols == 32;           // 32x32x16 products, else 16x16x32
+    constexpr bool kPairs = !kWide;               // weights as pairs of fp16 values, 22 bits
     constexpr int kSteps = kWide ? kD / 16 : kD / 32;
     constexpr int kBlocks = kWide ? kD / 32 : kD / 16;
     constexpr int kRegs = kWide ? 16 : 4;         // of a block's result
@@ -137,8 +141,9 @@ __global__ __launch_bounds__(F::kThreads, F::kPerSimd) void k_shared(Geometry g,
     uint4v *lut = reinterpret_cast<uint4v *>(lds);  // [48]: a Primary, with the byte offset of its entries
     float *dir = lds + 4 * 48;                      // [K, V][3 or 1][S][4]
     const uint32_t dir_side = (uint32_t)(kTable ? 3 : 1) * g.S * 4;
-    uint32_t *tiles = reinterpret_cast<uint32_t *>(dir + 2 * dir_side);
-    uint32_t *stages = tiles + kBufs * Tile::total;  // [kBufs][K, V]
+    uint32_t *key_tiles = reinterpret_cast<uint32_t *>(dir + 2 * dir_side);
+    uint32_t *value_tiles = key_tiles + kBufs * Tile::keys;
+    uint32_t *stages = key_tiles + Tile::total(kBufs);  // [kBufs][K, V]
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -209,7 +214,7 @@ __global__ __launch_bounds__(F::kThreads, F::kPerSimd) void k_shared(Geometry g,
     int end = min(g.T, begin + a.rows_per_split);
     int least = g.T;      // every query row of the wave sees the tokens below
     if (a.visible) {      // what no row of the workgroup sees is not read
-        int *most_of = reinterpret_cast<int *>(tiles);
+        int *most_of = reinterpret_cast<int *>(key_tiles);
         int most = there ? vis : 0;
         least = vis;
         for (int d = 32; d > 0; d /= 2) {
@@ -363,88 +368,92 @@ __global__ __launch_bounds__(F::kThreads, F::kPerSimd) void k_shared(Geometry g,
     // tile's last unit (24 chunks per row) do that one again.
     constexpr int kKeyUnits = kTok * kNc / 2, kValueUnits = kTok * kNc / 4;
     static_assert(kKeyUnits <= 2 * kMakers && kValueUnits <= kMakers, "a thread's four chunks of a side");
-    auto decode_keys = [&](int buf) {
-        const uint32_t *sp = stages + 2 * buf * Stage::total;
-        _Float16 *keys = reinterpret_cast<_Float16 *>(tiles + buf * Tile::total);
-        const uint2 about = *reinterpret_cast<const uint2 *>(sp + Stage::about);
+    // side: 0 keys, 1 values, 2 both at once, for which only waves that do not multiply have the registers
+    auto decode = [&](auto side_tag, int buf, int value_buf) {
+        constexpr bool kKeys = decltype(side_tag)::value != 1, kValues = decltype(side_tag)::value != 0;
+        const uint32_t *sk = stages + 2 * buf * Stage::total, *sv = sk + Stage::total;
+        const uint2 about_k = *reinterpret_cast<const uint2 *>(sk + Stage::about), about_v = *reinterpret_cast<const uint2 *>(sv + Stage::about);
         int row[2], c[2];
-        uint32_t code[4], word[2], scale[2], off[2];
+        uint32_t code[8], word[2], scale[2], off[2];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; kKeys && i < 2; ++i) {
             const int u = min(st + kMakers * i, kKeyUnits - 1);
             row[i] = u / (kNc / 2);
             c[i] = 2 * (u % (kNc / 2));
-            code[2 * i] = read_code(sp, row[i], c[i]);
-            code[2 * i + 1] = read_code(sp, row[i], c[i] + 1);
-            const uint32_t *rp = sp + Stage::words + row[i];
+            code[2 * i] = read_code(sk, row[i], c[i]);
+            code[2 * i + 1] = read_code(sk, row[i], c[i] + 1);
+            const uint32_t *rp = sk + Stage::words + row[i];
             word[i] = rp[0];
             scale[i] = rp[kTok];
             off[i] = rp[2 * kTok];
         }
+        const int vu = min(st, kValueUnits - 1), vc = vu % kNc, quad = vu / kNc;
+        uint4v vword = {}, vscale = {}, voff = {};
+        if (kValues) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                code[4 + i] = read_code(sv, 4 * quad + i, vc);
+            const uint32_t *vp = sv + Stage::words + 4 * quad;
+            vword = *reinterpret_cast<const uint4v *>(vp);
+            vscale = *reinterpret_cast<const uint4v *>(vp + kTok);
+            voff = *reinterpret_cast<const uint4v *>(vp + 2 * kTok);
+        }
+        // where the four tokens stand in the order in which a product takes a block of scores as its operand
+        const int at = 4 * (kWide ? (quad & ~3) | ((quad & 1) << 1) | ((quad >> 1) & 1) : (quad & ~7) | ((quad & 3) << 1) | ((quad >> 2) & 1));
+        _Float16 *keys = reinterpret_cast<_Float16 *>(key_tiles + buf * Tile::keys);
+        _Float16 *values = reinterpret_cast<_Float16 *>(value_tiles + value_buf * Tile::values) + value_row(vc, 0) * value_pitch<kNc>() + at;
         const auto form = [&](auto fast_tag) {
             bool flag[4];
-            Pre f[4];
+            Pre f[8];
+            float4_t d[8];
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
+            for (int i = 0; kKeys && i < 2; ++i) {
                 flag[2 * i] = (word[i] >> c[i]) & 1u;
                 flag[2 * i + 1] = (word[i] >> c[i]) & 2u;
                 const uint32_t slot = off[i] + __popc(word[i] & ((1u << c[i]) - 1u));
-                f[2 * i] = pre(fast_tag, sp, code[2 * i], slot);
-                f[2 * i + 1] = pre(fast_tag, sp, code[2 * i + 1], slot + (flag[2 * i] ? 1u : 0u));
+                f[2 * i] = pre(fast_tag, sk, code[2 * i], slot);
+                f[2 * i + 1] = pre(fast_tag, sk, code[2 * i + 1], slot + (flag[2 * i] ? 1u : 0u));
             }
-            float4_t d[4];
+            if (kKeys && kValues)
+                __builtin_amdgcn_sched_barrier(0);  // the order of the steps: it is what overlaps their LDS round trips
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int i = 0; kKeys && i < 4; ++i)
                 d[i] = direction(0, f[i]);
 #pragma unroll
+            for (int i = 0; kValues && i < 4; ++i)
+                f[4 + i] = pre(fast_tag, sv, code[4 + i], voff[i] + __popc(vword[i] & ((1u << vc) - 1u)));
+            if (kKeys && kValues)
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const uint2 x = finish(fast_tag, 0, about.y, f[2 * i], d[2 * i], scale[i], flag[2 * i]);
-                const uint2 y = finish(fast_tag, 0, about.y, f[2 * i + 1], d[2 * i + 1], scale[i], flag[2 * i + 1]);
-                *reinterpret_cast<uint4v *>(keys + row[i] * key_pitch<kNc>() + 4 * c[i]) = uint4v{x.x, x.y, y.x, y.y};
+                if (kKeys) {
+                    const uint2 x = finish(fast_tag, 0, about_k.y, f[2 * i], d[2 * i], scale[i], flag[2 * i]);
+                    const uint2 y = finish(fast_tag, 0, about_k.y, f[2 * i + 1], d[2 * i + 1], scale[i], flag[2 * i + 1]);
+                    *reinterpret_cast<uint4v *>(keys + row[i] * key_pitch<kNc>() + 4 * c[i]) = uint4v{x.x, x.y, y.x, y.y};
+                }
+                if (kValues) {
+                    d[4 + 2 * i] = direction(1, f[4 + 2 * i]);
+                    d[5 + 2 * i] = direction(1, f[5 + 2 * i]);
+                }
+                if (kKeys && kValues)
+                    __builtin_amdgcn_sched_barrier(0);
             }
-        };
-        if (__builtin_amdgcn_readfirstlane((int)about.x) == 0)
-            form(std::true_type{});
-        else
-            form(std::false_type{});
-    };
-    auto decode_values = [&](int buf) {
-        const uint32_t *sp = stages + (2 * buf + 1) * Stage::total;
-        const uint2 about = *reinterpret_cast<const uint2 *>(sp + Stage::about);
-        const int u = min(st, kValueUnits - 1), c = u % kNc, quad = u / kNc;
-        uint32_t code[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            code[i] = read_code(sp, 4 * quad + i, c);
-        const uint32_t *rp = sp + Stage::words + 4 * quad;
-        const uint4v word = *reinterpret_cast<const uint4v *>(rp), scale = *reinterpret_cast<const uint4v *>(rp + kTok);
-        const uint4v off = *reinterpret_cast<const uint4v *>(rp + 2 * kTok);
-        // where the four tokens stand in the order in which a product takes a block of scores as its operand
-        const int at = 4 * (kWide ? (quad & ~3) | ((quad & 1) << 1) | ((quad >> 1) & 1) : (quad & ~7) | ((quad & 3) << 1) | ((quad >> 2) & 1));
-        _Float16 *dst = reinterpret_cast<_Float16 *>(tiles + buf * Tile::total + Tile::keys) + value_row(c, 0) * value_pitch<kNc>() + at;
-        const auto form = [&](auto fast_tag) {
-            Pre f[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                f[i] = pre(fast_tag, sp, code[i], off[i] + __popc(word[i] & ((1u << c) - 1u)));
-            float4_t d[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                d[i] = direction(1, f[i]);
+            if (!kValues)
+                return;
             uint2 v[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                v[i] = finish(fast_tag, 1, about.y, f[i], d[i], scale[i], (word[i] >> c) & 1u);
+                v[i] = finish(fast_tag, 1, about_v.y, f[4 + i], d[4 + i], vscale[i], (vword[i] >> vc) & 1u);
             const uint32_t lo = 0x05040100u, hi = 0x07060302u;
             const auto put = [&](int e, uint32_t x, uint32_t y) {
-                *reinterpret_cast<uint2 *>(dst + 8 * e * value_pitch<kNc>()) = make_uint2(x, y);
+                *reinterpret_cast<uint2 *>(values + 8 * e * value_pitch<kNc>()) = make_uint2(x, y);
             };
             put(0, __builtin_amdgcn_perm(v[1].x, v[0].x, lo), __builtin_amdgcn_perm(v[3].x, v[2].x, lo));
             put(1, __builtin_amdgcn_perm(v[1].x, v[0].x, hi), __builtin_amdgcn_perm(v[3].x, v[2].x, hi));
             put(2, __builtin_amdgcn_perm(v[1].y, v[0].y, lo), __builtin_amdgcn_perm(v[3].y, v[2].y, lo));
             put(3, __builtin_amdgcn_perm(v[1].y, v[0].y, hi), __builtin_amdgcn_perm(v[3].y, v[2].y, hi));
         };
-        if (__builtin_amdgcn_readfirstlane((int)about.x) == 0)
+        if (__builtin_amdgcn_readfirstlane((int)((kKeys ? about_k.x : 0u) | (kValues ? about_v.x : 0u))) == 0)
             form(std::true_type{});
         else
             form(std::false_type{});
@@ -459,94 +468,137 @@ __global__ __launch_bounds__(F::kThreads, F::kPerSimd) void k_shared(Geometry g,
         const auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
         return f(__uint_as_float(y[0]), __uint_as_float(y[1]));
     };
-    auto attend = [&](int j, int buf) {
-        const _Float16 *keys = reinterpret_cast<const _Float16 *>(tiles + buf * Tile::total);
-        const _Float16 *values = reinterpret_cast<const _Float16 *>(tiles + buf * Tile::total + Tile::keys);
+    constexpr int kS = kWide ? 16 : 8;  // scores of a lane and 32 tokens; wide: token 8 (i / 4) + 4 kgrp + i % 4; else 16 (i / 4) + 4 kgrp + i % 4
+    constexpr int kU = kWide ? 2 : 1;   // products of 32 tokens' values per block
+    half8_t held[kU];                   // two tiles in LDS: the last tile's weights, whose values are still to come
+    // Scores of 32 tokens from t0 on, the factor that is still missing from them, and m_ref raised if need be.
+    // Weights are 2^(s - m_ref): with m_ref some 10 below the largest score seen they reach 2^10, their fp16 values are normal numbers
+    // down to 2^-24 of the largest, and m_ref is raised (and what was summed scaled) only when a score would pass 2^15, so hardly
+    // ever after the first tiles.  It is a whole number: scaling by a power of two rounds nothing.
+    auto scores = [&](const _Float16 *keys, int t0, float *s) {
+        if constexpr (kWide) {
+            float16_t sc = float16_t{0.f};
+            const _Float16 *kp = keys + (lane & 31) * key_pitch<kNc>() + 8 * kgrp;
+#pragma unroll
+            for (int x = 0; x < kSteps; ++x)
+                sc = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const half8_t *>(kp + 16 * x), qf[x], sc, 0, 0, 0);
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                s[i] = sc[i];
+        } else {
+            float4_t sc[2] = {float4_t{0.f, 0.f, 0.f, 0.f}, float4_t{0.f, 0.f, 0.f, 0.f}};
+            const _Float16 *kp = keys + (lane & 15) * key_pitch<kNc>() + 8 * kgrp;
+#pragma unroll
+            for (int x = 0; x < kSteps; ++x)
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+                    sc[u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(*reinterpret_cast<const half8_t *>(kp + 16 * u * key_pitch<kNc>() + 32 * x),
+                                                                   qf[x], sc[u], 0, 0, 0);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                s[i] = sc[i >> 2][i & 3];
+        }
+        float mul = qscale;
+        if (t0 + 32 > end || t0 + 32 > least) {  // uniform: some query row does not see every token
+            const int seen = min(end, vis) - t0 - 4 * kgrp;
+#pragma unroll
+            for (int i = 0; i < kS; ++i)
+                s[i] = (kWide ? 8 : 16) * (i >> 2) + (i & 3) < seen ? s[i] * qscale : 3.f * kNoToken;
+            mul = 1.f;
+        }
+        float top = s[0];
+#pragma unroll
+        for (int i = 1; i < kS; ++i)
+            top = fmaxf(top, s[i]);
+        top = over_lanes(top * mul, [](float x, float y) { return fmaxf(x, y); });
+        const bool raise = top - m_ref > kRise;
+        if (__any(raise)) {
+            const float m_new = raise ? ceilf(top) - kTop : m_ref;
+            const float corr = __builtin_amdgcn_exp2f(m_ref - m_new);
+            m_ref = m_new;
+            l_run *= corr;
+#pragma unroll
+            for (int k = 0; k < kBlocks; ++k)
+#pragma unroll
+                for (int i = 0; i < kRegs; ++i)
+                    acc[k][i] *= corr;
+            if constexpr (kBufs == 2)
+#pragma unroll
+                for (int u = 0; u < kU; ++u)
+                    held[u] *= (_Float16)corr;
+        }
+        return mul;
+    };
+    auto value_operand = [&](const _Float16 *values, int k, int u) {
+        return *reinterpret_cast<const half8_t *>(values + ((kWide ? 32 : 16) * k + (lane & (kWide ? 31 : 15))) * value_pitch<kNc>() + 8 * kgrp + 16 * u);
+    };
+    auto multiply = [&](half8_t v, half8_t p, int k) {
+        if constexpr (kWide)
+            acc[k] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, p, acc[k], 0, 0, 0);
+        else
+            acc[k] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, p, acc[k], 0, 0, 0);
+    };
+    auto weight = [&](const float *s, float mul, int i) {
+        const float p = __builtin_amdgcn_exp2f(fmaf(s[i], mul, -m_ref));
+        l_run += p;
+        return p;
+    };
+    // One tile in LDS: scores, weights, products with the values.
+    auto attend = [&](int j) {
 #pragma unroll
         for (int sub = 0; sub < kTok; sub += 32) {
-            const int t0 = begin + j * kTok + sub;
-            constexpr int kS = kWide ? 16 : 8;
-            float s[kS];  // wide: token 8 (i / 4) + 4 kgrp + i % 4; else 16 (i / 4) + 4 kgrp + i % 4
-            if constexpr (kWide) {
-                float16_t sc = float16_t{0.f};
-                const _Float16 *kp = keys + (sub + (lane & 31)) * key_pitch<kNc>() + 8 * kgrp;
-#pragma unroll
-                for (int x = 0; x < kSteps; ++x)
-                    sc = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const half8_t *>(kp + 16 * x), qf[x], sc, 0, 0, 0);
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    s[i] = sc[i];
-            } else {
-                float4_t sc[2] = {float4_t{0.f, 0.f, 0.f, 0.f}, float4_t{0.f, 0.f, 0.f, 0.f}};
-                const _Float16 *kp = keys + (sub + (lane & 15)) * key_pitch<kNc>() + 8 * kgrp;
-#pragma unroll
-                for (int x = 0; x < kSteps; ++x)
-#pragma unroll
-                    for (int u = 0; u < 2; ++u)
-                        sc[u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(*reinterpret_cast<const half8_t *>(kp + 16 * u * key_pitch<kNc>() + 32 * x),
-                                                                       qf[x], sc[u], 0, 0, 0);
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    s[i] = sc[i >> 2][i & 3];
-            }
-            float mul = qscale;
-            if (t0 + 32 > end || t0 + 32 > least) {  // uniform: some query row does not see every token
-                const int seen = min(end, vis) - t0 - 4 * kgrp;
-#pragma unroll
-                for (int i = 0; i < kS; ++i)
-                    s[i] = (kWide ? 8 : 16) * (i >> 2) + (i & 3) < seen ? s[i] * qscale : 3.f * kNoToken;
-                mul = 1.f;
-            }
-            float top = s[0];
-#pragma unroll
-            for (int i = 1; i < kS; ++i)
-                top = fmaxf(top, s[i]);
-            top = over_lanes(top * mul, [](float x, float y) { return fmaxf(x, y); });
-            // Weights are 2^(s - m_ref): with m_ref 10 below the largest score seen they reach 2^10, their fp16 parts hold weights
-            // down to 2^-24 of the largest as normal numbers, and m_ref is raised (and what was summed scaled) only when a score
-            // would pass 2^15, so hardly ever after the first tiles.
-            const bool raise = top - m_ref > kRise;
-            if (__any(raise)) {
-                const float m_new = raise ? top - kTop : m_ref;
-                const float corr = __builtin_amdgcn_exp2f(m_ref - m_new);
-                m_ref = m_new;
-                l_run *= corr;
-#pragma unroll
-                for (int k = 0; k < kBlocks; ++k)
-#pragma unroll
-                    for (int i = 0; i < kRegs; ++i)
-                        acc[k][i] *= corr;
-            }
-            half8_t ph[2], pl[2];
-            float sum = 0.f;
+            float s[kS];
+            const float mul = scores(reinterpret_cast<const _Float16 *>(key_tiles) + sub * key_pitch<kNc>(), begin + j * kTok + sub, s);
+            half8_t hi[kU], lo[kU];
 #pragma unroll
             for (int i = 0; i < kS; ++i) {
-                const float p = __builtin_amdgcn_exp2f(fmaf(s[i], mul, -m_ref));
-                sum += p;
-                const _Float16 hi = (_Float16)p;
-                ph[i >> 3][i & 7] = hi;
-                pl[i >> 3][i & 7] = (_Float16)(p - (float)hi);  // the weight in 22 bits
+                const float p = weight(s, mul, i);
+                hi[i >> 3][i & 7] = (_Float16)p;
+                if (kPairs)
+                    lo[i >> 3][i & 7] = (_Float16)(p - (float)hi[i >> 3][i & 7]);
             }
-            l_run += sum;
-            const _Float16 *vp = values + (kWide ? (lane & 31) : (lane & 15)) * value_pitch<kNc>() + sub + 8 * kgrp;
+            const _Float16 *values = reinterpret_cast<const _Float16 *>(value_tiles) + sub;
 #pragma unroll
-            for (int u = 0; u < (kWide ? 2 : 1); ++u) {
-                half8_t vf[kBlocks];
+            for (int u = 0; u < kU; ++u) {
+                half8_t v[kBlocks];
 #pragma unroll
                 for (int k = 0; k < kBlocks; ++k)
-                    vf[k] = *reinterpret_cast<const half8_t *>(vp + (kWide ? 32 : 16) * k * value_pitch<kNc>() + 16 * u);
+                    v[k] = value_operand(values, k, u);
 #pragma unroll
-                for (int part = 0; part < 2; ++part)
+                for (int k = 0; k < kBlocks; ++k)
+                    multiply(v[k], hi[u], k);
+                if (kPairs)
 #pragma unroll
-                    for (int k = 0; k < kBlocks; ++k) {
-                        const half8_t p = part ? pl[u] : ph[u];
-                        if constexpr (kWide)
-                            acc[k] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[k], p, acc[k], 0, 0, 0);
-                        else
-                            acc[k] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf[k], p, acc[k], 0, 0, 0);
-                    }
+                    for (int k = 0; k < kBlocks; ++k)
+                        multiply(v[k], lo[u], k);
             }
         }
+    };
+    // Two tiles: the weights of these 32 tokens between the products of the last ones' with their values, so that vector and matrix
+    // instructions issue side by side.
+    auto attend_held = [&](const _Float16 *keys, const _Float16 *last_values, int t0, bool first) {
+        float s[kS];
+        const float mul = scores(keys, t0, s);
+        half8_t next[kU];
+        if (first) {
+#pragma unroll
+            for (int i = 0; i < kS; ++i)
+                next[i >> 3][i & 7] = (_Float16)weight(s, mul, i);
+        } else {
+#pragma unroll
+            for (int n = 0; n < kU * kBlocks; ++n) {
+                const int u = n / kBlocks, k = n % kBlocks;
+                multiply(value_operand(last_values, k, u), held[u], k);
+                const int i0 = n * kS / (kU * kBlocks), i1 = (n + 1) * kS / (kU * kBlocks);
+#pragma unroll
+                for (int i = i0; i < i1; ++i)
+                    next[i >> 3][i & 7] = (_Float16)weight(s, mul, i);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kU; ++u)
+            held[u] = next[u];
     };
 
     // ---- the loop -------------------------------------------------------------------------------------------------------------
@@ -561,11 +613,11 @@ __global__ __launch_bounds__(F::kThreads, F::kPerSimd) void k_shared(Geometry g,
     lds_barrier();
     if constexpr (kBufs == 1) {
         for (int j = 0; j < n_tiles; ++j) {
-            decode_keys(0);
-            decode_values(0);
+            decode(std::integral_constant<int, 0>{}, 0, 0);
+            decode(std::integral_constant<int, 1>{}, 0, 0);
             lds_barrier();
             if (has_cols)
-                attend(j, 0);
+                attend(j);
             stage(0);
             request();
             request_bounds();
@@ -573,53 +625,76 @@ __global__ __launch_bounds__(F::kThreads, F::kPerSimd) void k_shared(Geometry g,
         }
     } else if (maker) {
         if (n_tiles > 0) {
-            decode_keys(0);
-            decode_values(0);
+            decode(std::integral_constant<int, 2>{}, 0, 0);
             stage(1);
             request();
             request_bounds();
         }
         lds_barrier();
+        int v = 0;
         for (int j = 1; j <= n_tiles; ++j) {  // past the last tile: zeros, which nothing reads
-            decode_keys(j & 1);
-            decode_values(j & 1);
+            v = v == 2 ? 0 : v + 1;
+            decode(std::integral_constant<int, 2>{}, j & 1, v);
             stage((j + 1) & 1);
             request();
             request_bounds();
             lds_barrier();
         }
     } else {
+        const _Float16 *keys = reinterpret_cast<const _Float16 *>(key_tiles), *values = reinterpret_cast<const _Float16 *>(value_tiles);
+        const _Float16 *last = values;
         lds_barrier();
+        int v = 0;
         for (int j = 0; j < n_tiles; ++j) {
-            if (has_cols)
-                attend(j, j & 1);
+            const _Float16 *kt = keys + 2 * (j & 1) * Tile::keys, *vt = values + 2 * v * Tile::values;
+            if (has_cols) {
+#pragma unroll
+                for (int sub = 0; sub < kTok; sub += 32)
+                    attend_held(kt + sub * key_pitch<kNc>(), sub ? vt + sub - 32 : last, begin + j * kTok + sub, j == 0 && sub == 0);
+            }
+            last = vt + kTok - 32;
+            v = v == 2 ? 0 : v + 1;
             lds_barrier();
         }
+        if (has_cols && n_tiles > 0)
+#pragma unroll
+            for (int n = 0; n < kU * kBlocks; ++n)
+                multiply(value_operand(last, n % kBlocks, n / kBlocks), held[n / kBlocks], n % kBlocks);
     }
 
-    // ---- the wave's columns of this share -----------------------------------------------------------------------------------------
+    // ---- the wave's columns of this share: through LDS, so that a row's sums leave in whole lines -------------------------------------
     l_run = over_lanes(l_run, [](float x, float y) { return x + y; });
-    if (!there)
+    if (!has_cols)
         return;
-    const size_t part = head * a.part_pitch + blockIdx.x;
-    if (kgrp == 0) {
-        a.part_ml[2 * part] = m_ref;
-        a.part_ml[2 * part + 1] = l_run;
+    if (there && kgrp == 0) {
+        float *ml = a.part_ml + 2 * (head * a.part_pitch + blockIdx.x);
+        ml[0] = m_ref;
+        ml[1] = l_run;
     }
-    float *dst = a.part_acc + part * 128;
+    constexpr int kPitch = 32 + 4;  // 32 dimensions, a line of 128 bytes, at a time
+    float *out = reinterpret_cast<float *>(key_tiles) + (kBufs == 1 ? wave : wave - 4) * kCols * kPitch;  // tiles and packed rows are done with
 #pragma unroll
-    for (int k = 0; k < kBlocks; ++k) {
-        if constexpr (kWide) {  // row 8 e + c % 8 of block c / 8: the lane has chunks 8 k + 4 kgrp + 0 .. 3
+    for (int part = 0; part < kD / 32; ++part) {
+        constexpr int kOf = kWide ? 1 : 2;  // blocks of a part
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                *reinterpret_cast<float4_t *>(dst + 4 * (8 * k + 4 * kgrp + i)) = float4_t{acc[k][i], acc[k][4 + i], acc[k][8 + i], acc[k][12 + i]};
-        } else {
+        for (int k = 0; k < kOf; ++k)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int row = 16 * k + 4 * kgrp + i;
-                dst[4 * (8 * (row >> 5) + (row & 7)) + ((row >> 3) & 3)] = acc[k][i];
+            for (int i = 0; i < kRegs; ++i) {
+                const int row = kWide ? 8 * (i >> 2) + 4 * kgrp + (i & 3) : 16 * k + 4 * kgrp + i;  // 8 e + c % 8
+                out[col * kPitch + 4 * (row & 7) + (row >> 3)] = acc[kOf * part + k][i];
+            }
+        wave_lds_sync();
+#pragma unroll
+        for (int i = lane; i < kCols * 8; i += 64) {
+            const int c = i >> 3, d = 4 * (i & 7), rr = col0 + c;
+            if (rr < n_rows) {
+                const int m = rr / a.G;
+                const size_t hd = ((size_t)(b * a.n_share + m) * g.H + h) * a.G + (rr - m * a.G);
+                *reinterpret_cast<float4_t *>(a.part_acc + (hd * a.part_pitch + blockIdx.x) * 128 + 32 * part + d) =
+                    *reinterpret_cast<const float4_t *>(out + c * kPitch + d);
             }
         }
+        wave_lds_sync();
     }
 }
 
@@ -638,9 +713,9 @@ SharedChoice choose_shared(const Geometry &g, int n_rows)
     c.form = n_rows <= 64 ? kSmall : n_rows <= 128 ? kMiddle : kLarge;
     c.rows = c.form == kSmall ? 64 : c.form == kMiddle ? 128 : 256;
     const int bufs = c.form == kLarge ? FormLarge::kBufs : 1;
-    const int tile = g.n_c == 32 ? TileLds<32>::total : g.n_c == 24 ? TileLds<24>::total : TileLds<16>::total;
+    const int tile = g.n_c == 32 ? TileLds<32>::total(bufs) : g.n_c == 24 ? TileLds<24>::total(bufs) : TileLds<16>::total(bufs);
     const int stage = g.n_c == 32 ? StageLds<32>::total : g.n_c == 24 ? StageLds<24>::total : StageLds<16>::total;
-    const auto lds = [&](bool table) { return ((size_t)4 * 48 + (table ? 6 : 2) * (size_t)g.S * 4 + bufs * ((size_t)tile + 2 * stage)) * sizeof(float); };
+    const auto lds = [&](bool table) { return ((size_t)4 * 48 + (table ? 6 : 2) * (size_t)g.S * 4 + tile + (size_t)bufs * 2 * stage) * sizeof(float); };
     c.table = lds(true) <= (c.form == kLarge ? kLdsPerCu : kLdsPerCu / 2);
     c.lds = lds(c.table);
     const int most = c.form == kSmall ? FormSmall::kPerSimd : c.form == kMiddle ? FormMiddle::kPerSimd : 1;
