@@ -929,16 +929,31 @@ static int32_t check_own(const hqmq_params *params, int32_t n_share, const hqmq_
 struct SharedLayout {
     SharedPlan prefix;
     AttendPlan own;
+    bool own_short;  // the own tokens take the prefix's kernel too, every sequence a prefix of its own
     uint64_t ml_bytes, total;
     int32_t parts;
 };
-static SharedLayout shared_layout(const Geometry &g, int G, int n_share, const hqmq_params *own)
+static SharedLayout shared_layout(const hqmq_params *params, int G, int n_share, const hqmq_params *own)
 {
+    const Geometry g = make_geometry(params);
     SharedLayout l;
     l.prefix = plan_shared(g, G, n_share);
     l.own.n_splits = 0;
-    if (own)
-        l.own = plan_attend(make_geometry(own), G, false);
+    l.own_short = false;
+    if (own) {
+        const Geometry go = make_geometry(own);
+        // Short segments are bound by what a workgroup does before and after its tokens, of which the prefix's kernel has less (tables a
+        // quarter of the size, three workgroups per compute unit).  The kernel of hqmq_attend / this one: 768 segments of 64 tokens x 96
+        // 18.9 / 11.6 us; 512 of up to 512 x 128 35.5 / 40; 48 of up to 97 x 64 6.3 / 7.0.
+        l.own_short = go.T <= 128 && go.B * go.H >= 256;
+        if (l.own_short) {
+            const SharedPlan p = plan_shared(go, G, 1);
+            l.own.n_splits = p.n_splits;
+            l.own.rows_per_split = p.rows_per_split;
+        } else {
+            l.own = plan_attend(go, G, (params->flags & HQMQ_FLAG_ATTEND_TABLES) != 0);
+        }
+    }
     l.parts = l.prefix.n_splits + l.own.n_splits;
     const uint64_t parts = (uint64_t)g.B * n_share * g.H * G * l.parts;
     l.ml_bytes = align_up(parts * 2 * sizeof(float), 256);
@@ -951,7 +966,7 @@ extern "C" uint64_t hqmq_attend_shared_workspace_bytes(const hqmq_params *params
 {
     if (check_share(params, n_share, n_q_heads) != HQMQ_OK || (own_params && check_own(params, n_share, own_params) != HQMQ_OK))
         return 0;
-    return shared_layout(make_geometry(params), n_q_heads / params->H, n_share, own_params).total;
+    return shared_layout(params, n_q_heads / params->H, n_share, own_params).total;
 }
 
 extern "C" int32_t hqmq_attend_shared(const hqmq_params *params, int32_t n_share, int32_t n_q_heads, const void *q_dev, float scale,
@@ -984,7 +999,7 @@ extern "C" int32_t hqmq_attend_shared(const hqmq_params *params, int32_t n_share
         return rc;
     const Geometry g = make_geometry(params);
     const int G = n_q_heads / params->H;
-    const SharedLayout l = shared_layout(g, G, n_share, own ? own->params : nullptr);
+    const SharedLayout l = shared_layout(params, G, n_share, own ? own->params : nullptr);
     if (workspace_bytes < l.total)
         return HQMQ_ERR_BUFFER_TOO_SMALL;
     const hipError_t ready = ensure_device_setup();
@@ -1005,6 +1020,7 @@ extern "C" int32_t hqmq_attend_shared(const hqmq_params *params, int32_t n_share
     a.n_share = n_share;
     a.n_splits = l.prefix.n_splits;
     a.rows_per_split = l.prefix.rows_per_split;
+    a.split0 = 0;
     a.part_pitch = l.parts;
     hipError_t err = launch_shared(g, a, static_cast<hipStream_t>(stream));
     if (err != hipSuccess)
@@ -1021,7 +1037,18 @@ extern "C" int32_t hqmq_attend_shared(const hqmq_params *params, int32_t n_share
     o.G = G;
     o.D = params->D;
     o.part_pitch = l.parts;
-    if (own) {
+    if (own && l.own_short) {
+        a.k = attend_side(own->enc_k, sec_k_dev, own->cap_k);
+        a.v = attend_side(own->enc_v, sec_v_dev, own->cap_v);
+        a.visible = own->visible_dev;
+        a.n_share = 1;
+        a.n_splits = l.own.n_splits;
+        a.rows_per_split = l.own.rows_per_split;
+        a.split0 = l.prefix.n_splits;
+        err = launch_shared(make_geometry(own->params), a, static_cast<hipStream_t>(stream));
+        if (err != hipSuccess)
+            return hip_failed(err);
+    } else if (own) {
         o.k = attend_side(own->enc_k, sec_k_dev, own->cap_k);
         o.v = attend_side(own->enc_v, sec_v_dev, own->cap_v);
         o.visible = own->visible_dev;

@@ -17,7 +17,7 @@ struct SharedArgs {
     float qscale;            // softmax scale * log2(e)
     int32_t G, n_share;
     int32_t n_splits, rows_per_split;  // workgroups along the prefix and its tokens per workgroup
-    int32_t part_pitch;      // splits of the partial arrays, the own tokens' included
+    int32_t split0, part_pitch;        // the first one's place in the partial arrays, and how many places there are, the own tokens' included
 };
 constexpr int kMostSharedSplits = 512;  // and as many of the own tokens: kMostParts in all
 struct SharedPlan {

@@ -1,8 +1,6 @@
 // Attention of many sequences over one packed prefix (include/hqmq_serve.h, hqmq_attend_shared): O = softmax(Q K^T scale) V
 // with the n_share * G query rows of a kv head against one reconstruction of its K and V.
-#include <type_traits>
-
-#include "hqmq_serve_device.h"
+#include "hqmq_packed.h"
 
 namespace hqmq {
 
@@ -11,14 +9,6 @@ namespace {
 constexpr int kMakers = 256;        // threads that fetch and reconstruct tiles: four waves
 constexpr int kLoads = 3;           // code words of a tile and side per thread
 constexpr int kPay = 128;           // outlier payloads of a tile and side kept in LDS
-constexpr float kNoToken = -1.0e30f;
-constexpr float kTop = 10.f;        // weights are taken relative to 2^-kTop of the largest score,
-constexpr float kRise = 15.f;       // and relative to a newer one once they would pass 2^kRise
-constexpr uint32_t kBigScale = 0x77ffu;  // 32752 as fp16 bits: below it no product of a unit codeword leaves the fp16 range
-
-typedef _Float16 half8_t __attribute__((ext_vector_type(8)));
-typedef float float16_t __attribute__((ext_vector_type(16)));
-typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
 
 // Tokens of a tile: 1024 chunks of K and of V (24 chunks per row: 768), four for each of a side's threads.
 template <int kNc>
@@ -51,59 +41,9 @@ struct StageLds {
     static_assert(words % 4 == 0 && kTok % 4 == 0 && total % 4 == 0, "16-byte reads");
 };
 
-// The 24 primaries are +-u w^m with u one of 1, i, j, k, w = (1 + i + j + k) / 2 and m = 0, 1, 2.  A product with u reorders the
-// components (e takes that of e ^ u) and flips signs, which costs nothing on the packed fp16 result, rounding being symmetric: two
-// byte permutes and two exclusive ors.  So a table of three entries per secondary, w^m (x) q_s, serves all 24.
-struct Primary {
-    uint32_t m, select, flip_lo, flip_hi;  // select: of the result's first dword; the second's is select ^ 0x04040404
-};
-struct Primaries {
-    Primary p[32];
-};
-constexpr Primaries make_primaries()
-{
-    Primaries out{};
-    const int w[3][4] = {{2, 0, 0, 0}, {1, 1, 1, 1}, {-1, 1, 1, 1}};                               // twice w^m
-    const int sign[4][4] = {{1, 1, 1, 1}, {-1, 1, -1, 1}, {-1, 1, 1, -1}, {-1, -1, 1, 1}};  // of component e ^ u in u (x) x
-    for (int p = 0; p < 32; ++p) {
-        int P[4] = {0, 0, 0, 0};  // twice the primary
-        if (p < 8)
-            P[p >> 1] = (p & 1) ? -2 : 2;
-        else if (p < 24)
-            for (int e = 0; e < 4; ++e)
-                P[e] = ((p - 8) >> (3 - e)) & 1 ? -1 : 1;
-        out.p[p] = Primary{0u, 0x03020100u, 0u, 0u};  // past the 24: any that stays in the table
-        for (int u = 0; p < 24 && u < 4; ++u)
-            for (int m = 0; m < 3; ++m)
-                for (int s = -1; s < 2; s += 2) {
-                    bool same = true;
-                    for (int e = 0; e < 4; ++e)
-                        same = same && P[e] == s * sign[u][e] * w[m][e ^ u];
-                    if (!same)
-                        continue;
-                    const uint32_t lo = 2u * (0u ^ u), hi = 2u * (1u ^ u);
-                    uint32_t flip[2] = {0u, 0u};
-                    for (int e = 0; e < 4; ++e)
-                        if (s * sign[u][e] < 0)
-                            flip[e >> 1] |= 0x8000u << (16 * (e & 1));
-                    out.p[p] = Primary{(uint32_t)m, lo | (lo + 1u) << 8 | hi << 16 | (hi + 1u) << 24, flip[0], flip[1]};
-                }
-    }
-    return out;
-}
-__constant__ const Primaries kPrimaries = make_primaries();
-
 // Row of V^T in LDS for component e of chunk c: blocks of 32 rows are the operands of one product; in a product's result a lane
 // then holds all four components of a chunk.
 __device__ __forceinline__ int value_row(int c, int e) { return 32 * (c >> 3) + 8 * e + (c & 7); }
-
-// A barrier for what goes through LDS: loads from memory stay in flight across it.
-__device__ __forceinline__ void lds_barrier()
-{
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
-    __builtin_amdgcn_s_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
-}
 
 // How a workgroup works: waves that multiply, query rows (columns) of each, tiles in LDS, waves per SIMD.  With one tile in LDS four
 // waves reconstruct a tile and then multiply it, and the workgroups that share a compute unit fill each other's waits; with two, four
@@ -116,11 +56,6 @@ struct Form {
 using FormSmall = Form<4, 16, 1, 3>;
 using FormMiddle = Form<4, 32, 1, 2>;
 using FormLarge = Form<8, 32, 2, 3>;
-
-typedef __amdgpu_buffer_rsrc_t rsrc_t;
-// n elements from p on, as a buffer: what lies past them reads as zero
-template <typename T>
-__device__ __forceinline__ rsrc_t buffer_of(const T *p, uint32_t n) { return __builtin_amdgcn_make_buffer_rsrc((void *)p, 0, (int)(n * (uint32_t)sizeof(T)), 0x00020000); }
 
 }  // namespace
 
@@ -138,10 +73,7 @@ __global__ __launch_bounds__(F::kThreads, F::kPerSimd) void k_shared(Geometry g,
     constexpr int kRegs = kWide ? 16 : 4;         // of a block's result
     using acc_t = std::conditional_t<kWide, float16_t, float4_t>;
     extern __shared__ __align__(16) float lds[];
-    uint4v *lut = reinterpret_cast<uint4v *>(lds);  // [48]: a Primary, with the byte offset of its entries
-    float *dir = lds + 4 * 48;                      // [K, V][3 or 1][S][4]
-    const uint32_t dir_side = (uint32_t)(kTable ? 3 : 1) * g.S * 4;
-    uint32_t *key_tiles = reinterpret_cast<uint32_t *>(dir + 2 * dir_side);
+    uint32_t *key_tiles = reinterpret_cast<uint32_t *>(lds + kLutFloats + 2 * direction_floats<kTable>(g.S));
     uint32_t *value_tiles = key_tiles + kBufs * Tile::keys;
     uint32_t *stages = key_tiles + Tile::total(kBufs);  // [kBufs][K, V]
 
@@ -151,7 +83,7 @@ __global__ __launch_bounds__(F::kThreads, F::kPerSimd) void k_shared(Geometry g,
     const int st = tid & (kMakers - 1);
     const int seg = blockIdx.y, b = seg / g.H, h = seg % g.H;
     const uint32_t row_words = kNc == 32 ? (uint32_t)g.w : (uint32_t)g.row_words;
-    const uint32_t w = g.w, w_idx = g.w_idx;
+    const uint32_t w = g.w;
 
     // ---- columns of this wave: query rows r of the kv head ---------------------------------------------------------
     const int n_rows = a.n_share * a.G;
@@ -184,30 +116,8 @@ __global__ __launch_bounds__(F::kThreads, F::kPerSimd) void k_shared(Geometry g,
     if (a.visible && there)
         vis = min(max(a.visible[head], 0), g.T);
 
-    // ---- the tables: directions divided by the radius codes' range L, so that a chunk is (radius code * scale, exact in fp32)
-    //      times an entry, rounded once.  Entries are taken in fp64 and rounded once too. ------------------------------------------
-    {
-        const double over_L = 1.0 / (double)((1 << g.b_r) - 1);
-        const float *sk = a.k.sec + (size_t)h * g.S * 4, *sv = a.v.sec + (size_t)h * g.S * 4;
-        for (int i = tid; i < 2 * g.S; i += kThreads) {
-            const bool is_v = i >= g.S;
-            const int s = is_v ? i - g.S : i;
-            const float4_t q = *reinterpret_cast<const float4_t *>((is_v ? sv : sk) + 4 * s);
-            float4_t *dst = reinterpret_cast<float4_t *>(dir + (is_v ? dir_side : 0u)) + s;
-            const double x0 = q[0] * over_L, x1 = q[1] * over_L, x2 = q[2] * over_L, x3 = q[3] * over_L;
-            dst[0] = float4_t{(float)x0, (float)x1, (float)x2, (float)x3};
-            if (kTable) {  // w (x) x = ((1, 1, 1, 1) (x) x) / 2, and w^2 = w - 1
-                const double y0 = 0.5 * (x0 - x1 - x2 - x3), y1 = 0.5 * (x0 + x1 - x2 + x3);
-                const double y2 = 0.5 * (x0 + x1 + x2 - x3), y3 = 0.5 * (x0 - x1 + x2 + x3);
-                dst[g.S] = float4_t{(float)y0, (float)y1, (float)y2, (float)y3};
-                dst[2 * g.S] = float4_t{(float)(y0 - x0), (float)(y1 - x1), (float)(y2 - x2), (float)(y3 - x3)};
-            }
-        }
-        if (tid < 48) {
-            const Primary p = kPrimaries.p[min(tid, 31)];
-            lut[tid] = uint4v{kTable ? p.m * (uint32_t)g.S * 16u : p.m, p.select, p.flip_lo, p.flip_hi};
-        }
-    }
+    build_tables<kTable>(lds, g, a.k.sec + (size_t)h * g.S * 4, a.v.sec + (size_t)h * g.S * 4, 2, tid, kThreads);
+    const Decoder<kTable, kPow2> decoder(lds, g);
 
     // ---- the tiles of this workgroup -----------------------------------------------------------------------------------
     const int begin = (int)blockIdx.x * a.rows_per_split;
@@ -304,65 +214,17 @@ __global__ __launch_bounds__(F::kThreads, F::kPerSimd) void k_shared(Geometry g,
     };
 
     // ---- reconstruction ----------------------------------------------------------------------------------------------------
-    // One chunk in three steps, so that the LDS round trips of a thread's four overlap: its primary and payload, the codeword's
-    // direction, the arithmetic.  slot: place in the window of the payload that the chunk takes if it is flagged.
-    const uint32_t idx_mask = (1u << w_idx) - 1u;
-    struct Pre {
-        uint32_t code, s_idx, slot;
-        uint4v l;
-        uint2 pay;
-    };
     auto read_code = [&](const uint32_t *sp, int row, uint32_t c) {
         const uint32_t bit = c * w;
         const uint32_t *rw = sp + row * row_words + (bit >> 5);
         return __builtin_amdgcn_alignbit(rw[1], rw[0], bit & 31u);
     };
     auto pre = [&](auto fast_tag, const uint32_t *sp, uint32_t code, uint32_t slot) {
-        Pre f;
-        uint32_t p;
-        if (kPow2) {
-            p = (code >> g.log2_S) & 31u;
-            f.s_idx = code & ((uint32_t)g.S - 1u);
-        } else {
-            const uint32_t kk = code & idx_mask;
-            p = (uint32_t)((float)kk * g.inv_S);
-            f.s_idx = kk - __umul24(p, (uint32_t)g.S);
-        }
-        f.code = code;
-        f.slot = slot;
-        f.l = lut[p];
-        f.pay = reinterpret_cast<const uint2 *>(sp + Stage::pays)[decltype(fast_tag)::value ? slot : min(slot, (uint32_t)kPay)];
-        return f;
+        return decoder.template pre<decltype(fast_tag)::value, kPay>(reinterpret_cast<const uint2 *>(sp + Stage::pays), code, slot);
     };
-    auto direction = [&](int s, const Pre &f) {
-        const char *at = reinterpret_cast<const char *>(dir + (s ? dir_side : 0u)) + (f.s_idx << 4);
-        if (kTable)
-            return *reinterpret_cast<const float4_t *>(at + f.l[0]);
-        const float4_t x = *reinterpret_cast<const float4_t *>(at);
-        const float4_t y = {0.5f * (x[0] - x[1] - x[2] - x[3]), 0.5f * (x[0] + x[1] - x[2] + x[3]), 0.5f * (x[0] + x[1] + x[2] - x[3]),
-                            0.5f * (x[0] - x[1] + x[2] + x[3])};
-        return f.l[0] == 0u ? x : f.l[0] == 1u ? y : y - x;
-    };
-    auto finish = [&](auto fast_tag, int s, uint32_t base, const Pre &f, float4_t d, uint32_t scale, bool flagged) {
-        constexpr bool kFast = decltype(fast_tag)::value;
-        const float r = (float)__builtin_amdgcn_ubfe(f.code, w_idx, w - w_idx) * (float)__builtin_bit_cast(_Float16, (uint16_t)scale);
-        half4_t out;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            float y = r * d[e];
-            if (!kFast)
-                y = __builtin_amdgcn_fmed3f(y, -65504.f, 65504.f);  // the decode saturates
-            out[e] = (_Float16)y;
-        }
-        const uint2 o = __builtin_bit_cast(uint2, out);
-        uint2 v = f.pay;
-        if (!kFast && f.slot >= (uint32_t)kPay && flagged) {  // past the staged ones: straight from the list
-            const AttendSide &sd = s ? a.v : a.k;
-            const uint64_t at = (uint64_t)base + f.slot;
-            v = at < sd.outlier_capacity ? reinterpret_cast<const uint2 *>(sd.outliers)[at] : make_uint2(0u, 0u);
-        }
-        const uint32_t x = __builtin_amdgcn_perm(o.y, o.x, f.l[1]) ^ f.l[2], y = __builtin_amdgcn_perm(o.y, o.x, f.l[1] ^ 0x04040404u) ^ f.l[3];
-        return make_uint2(flagged ? v.x : x, flagged ? v.y : y);
+    auto direction = [&](int s, const Chunk &f) { return decoder.direction(s, f); };
+    auto finish = [&](auto fast_tag, int s, uint32_t base, const Chunk &f, float4_t d, uint32_t scale, bool flagged) {
+        return decoder.template finish<decltype(fast_tag)::value, kPay>(s ? a.v : a.k, base, f, d, scale_value(scale), flagged);
     };
     // A thread's part of a tile: two pairs of neighbouring chunks of K, one chunk of V in four neighbouring tokens.  Threads beyond a
     // tile's last unit (24 chunks per row) do that one again.
@@ -404,7 +266,7 @@ __global__ __launch_bounds__(F::kThreads, F::kPerSimd) void k_shared(Geometry g,
         _Float16 *values = reinterpret_cast<_Float16 *>(value_tiles + value_buf * Tile::values) + value_row(vc, 0) * value_pitch<kNc>() + at;
         const auto form = [&](auto fast_tag) {
             bool flag[4];
-            Pre f[8];
+            Chunk f[8];
             float4_t d[8];
 #pragma unroll
             for (int i = 0; kKeys && i < 2; ++i) {
@@ -667,7 +529,7 @@ __global__ __launch_bounds__(F::kThreads, F::kPerSimd) void k_shared(Geometry g,
     if (!has_cols)
         return;
     if (there && kgrp == 0) {
-        float *ml = a.part_ml + 2 * (head * a.part_pitch + blockIdx.x);
+        float *ml = a.part_ml + 2 * (head * a.part_pitch + a.split0 + blockIdx.x);
         ml[0] = m_ref;
         ml[1] = l_run;
     }
@@ -690,7 +552,7 @@ __global__ __launch_bounds__(F::kThreads, F::kPerSimd) void k_shared(Geometry g,
             if (rr < n_rows) {
                 const int m = rr / a.G;
                 const size_t hd = ((size_t)(b * a.n_share + m) * g.H + h) * a.G + (rr - m * a.G);
-                *reinterpret_cast<float4_t *>(a.part_acc + (hd * a.part_pitch + blockIdx.x) * 128 + 32 * part + d) =
+                *reinterpret_cast<float4_t *>(a.part_acc + (hd * a.part_pitch + a.split0 + blockIdx.x) * 128 + 32 * part + d) =
                     *reinterpret_cast<const float4_t *>(out + c * kPitch + d);
             }
         }
@@ -700,27 +562,33 @@ __global__ __launch_bounds__(F::kThreads, F::kPerSimd) void k_shared(Geometry g,
 
 namespace {
 
-enum SharedForm { kSmall, kMiddle, kLarge };
+enum SharedForm { kSmall, kMiddle, kLarge };  // up to 64, 128 and 256 query rows per workgroup
 struct SharedChoice {
     SharedForm form;
     bool table;
-    int rows, resident;  // query rows of a workgroup, workgroups of a compute unit
+    int rows, threads, resident;  // query rows and threads of a workgroup, workgroups of a compute unit
     size_t lds;
 };
 SharedChoice choose_shared(const Geometry &g, int n_rows)
 {
     SharedChoice c;
     c.form = n_rows <= 64 ? kSmall : n_rows <= 128 ? kMiddle : kLarge;
+    int most = 0;
+    const auto fit = [&](auto lds, size_t table_room) {
+        c.table = lds(true) <= table_room;
+        c.lds = lds(c.table);
+        c.resident = (int)(kLdsPerCu / c.lds);
+        c.resident = c.resident < most ? c.resident : most;
+    };
     c.rows = c.form == kSmall ? 64 : c.form == kMiddle ? 128 : 256;
+    c.threads = c.form == kLarge ? FormLarge::kThreads : c.form == kMiddle ? FormMiddle::kThreads : FormSmall::kThreads;
+    most = c.form == kSmall ? FormSmall::kPerSimd : c.form == kMiddle ? FormMiddle::kPerSimd : 1;
     const int bufs = c.form == kLarge ? FormLarge::kBufs : 1;
     const int tile = g.n_c == 32 ? TileLds<32>::total(bufs) : g.n_c == 24 ? TileLds<24>::total(bufs) : TileLds<16>::total(bufs);
     const int stage = g.n_c == 32 ? StageLds<32>::total : g.n_c == 24 ? StageLds<24>::total : StageLds<16>::total;
-    const auto lds = [&](bool table) { return ((size_t)4 * 48 + (table ? 6 : 2) * (size_t)g.S * 4 + tile + (size_t)bufs * 2 * stage) * sizeof(float); };
-    c.table = lds(true) <= (c.form == kLarge ? kLdsPerCu : kLdsPerCu / 2);
-    c.lds = lds(c.table);
-    const int most = c.form == kSmall ? FormSmall::kPerSimd : c.form == kMiddle ? FormMiddle::kPerSimd : 1;
-    c.resident = (int)(kLdsPerCu / c.lds);
-    c.resident = c.resident < most ? c.resident : most;
+    fit([&](bool table) {
+        return (kLutFloats + 2 * (table ? direction_floats<true>(g.S) : direction_floats<false>(g.S)) + tile + (size_t)bufs * 2 * stage) * sizeof(float);
+    }, c.form == kLarge ? kLdsPerCu : kLdsPerCu / 2);
     return c;
 }
 
@@ -775,11 +643,10 @@ hipError_t launch_shared(const Geometry &g, const SharedArgs &a, hipStream_t str
     const int n_rows = a.G * a.n_share;
     const SharedChoice c = choose_shared(g, n_rows);
     const dim3 grid((unsigned)a.n_splits, (unsigned)(g.B * g.H), (unsigned)((n_rows + c.rows - 1) / c.rows));
-    const unsigned threads = c.form == kLarge ? FormLarge::kThreads : c.form == kMiddle ? FormMiddle::kThreads : FormSmall::kThreads;
     Geometry gc = g;
     SharedArgs ac = a;
     void *args[] = {&gc, &ac};
-    return hipLaunchKernel(shared_kernel(g.n_c, c.form, c.table, (g.S & (g.S - 1)) == 0), grid, dim3(threads), args, c.lds, stream);
+    return hipLaunchKernel(shared_kernel(g.n_c, c.form, c.table, (g.S & (g.S - 1)) == 0), grid, dim3(c.threads), args, c.lds, stream);
 }
 
 }  // namespace hqmq
