@@ -46,6 +46,8 @@ static hipError_t ensure_device_setup(void **scratch_out = nullptr)
                 err = prepare_attend_kernels();
             if (err == hipSuccess)
                 err = prepare_shared_kernels();
+            if (err == hipSuccess)
+                err = prepare_mass_kernels();
             if (err != hipSuccess)
                 return err;
             void *ptr = nullptr;

@@ -152,27 +152,44 @@ struct Decoder {
                             0.5f * (x[0] - x[1] + x[2] + x[3])};
         return f.l[0] == 0u ? x : f.l[0] == 1u ? y : y - x;
     }
-    // sigma: the row's scale; base: the window's first entry
-    template <bool kFast, int kSlots>
-    __device__ __forceinline__ uint2 finish(const AttendSide &sd, uint32_t base, const Chunk &f, float4_t d, float sigma, bool flagged) const
+    // The four values in fp32, of a row with this scale.
+    __device__ __forceinline__ float4_t scaled(const Chunk &f, float4_t d, float sigma) const
     {
         const float r = (float)__builtin_amdgcn_ubfe(f.code, w_idx, r_bits) * sigma;
+        return float4_t{r * d[0], r * d[1], r * d[2], r * d[3]};
+    }
+    static __device__ __forceinline__ float4_t saturated(float4_t y)  // as the decode does
+    {
+        return float4_t{__builtin_amdgcn_fmed3f(y[0], -65504.f, 65504.f), __builtin_amdgcn_fmed3f(y[1], -65504.f, 65504.f),
+                        __builtin_amdgcn_fmed3f(y[2], -65504.f, 65504.f), __builtin_amdgcn_fmed3f(y[3], -65504.f, 65504.f)};
+    }
+    // The payload of a flagged chunk past the staged ones: straight from the list.  base: the window's first entry.
+    static __device__ __forceinline__ uint2 far_payload(const AttendSide &sd, uint32_t base, const Chunk &f)
+    {
+        const uint64_t at = (uint64_t)base + f.slot;
+        return at < sd.outlier_capacity ? reinterpret_cast<const uint2 *>(sd.outliers)[at] : make_uint2(0u, 0u);
+    }
+    // The chunk: its values rounded to fp16, in their places and with their signs, or its payload.
+    static __device__ __forceinline__ uint2 packed(const Chunk &f, float4_t y, bool flagged)
+    {
         half4_t out;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            float y = r * d[e];
-            if (!kFast)
-                y = __builtin_amdgcn_fmed3f(y, -65504.f, 65504.f);  // the decode saturates
-            out[e] = (_Float16)y;
-        }
+        for (int e = 0; e < 4; ++e)
+            out[e] = (_Float16)y[e];
         const uint2 o = __builtin_bit_cast(uint2, out);
-        uint2 v = f.pay;
-        if (!kFast && f.slot >= (uint32_t)kSlots && flagged) {  // past the staged ones: straight from the list
-            const uint64_t at = (uint64_t)base + f.slot;
-            v = at < sd.outlier_capacity ? reinterpret_cast<const uint2 *>(sd.outliers)[at] : make_uint2(0u, 0u);
+        const uint32_t lo = __builtin_amdgcn_perm(o.y, o.x, f.l[1]) ^ f.l[2], hi = __builtin_amdgcn_perm(o.y, o.x, f.l[1] ^ 0x04040404u) ^ f.l[3];
+        return make_uint2(flagged ? f.pay.x : lo, flagged ? f.pay.y : hi);
+    }
+    template <bool kFast, int kSlots>
+    __device__ __forceinline__ uint2 finish(const AttendSide &sd, uint32_t base, Chunk f, float4_t d, float sigma, bool flagged) const
+    {
+        float4_t y = scaled(f, d, sigma);
+        if (!kFast) {
+            y = saturated(y);
+            if (f.slot >= (uint32_t)kSlots && flagged)
+                f.pay = far_payload(sd, base, f);
         }
-        const uint32_t x = __builtin_amdgcn_perm(o.y, o.x, f.l[1]) ^ f.l[2], y = __builtin_amdgcn_perm(o.y, o.x, f.l[1] ^ 0x04040404u) ^ f.l[3];
-        return make_uint2(flagged ? v.x : x, flagged ? v.y : y);
+        return packed(f, y, flagged);
     }
 };
 

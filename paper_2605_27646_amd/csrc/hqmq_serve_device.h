@@ -37,6 +37,7 @@ struct MassArgs {
     float qscale, decay;
     int32_t G, n_share;
 };
+hipError_t prepare_mass_kernels();  // once per device, before the first launch_mass on it
 hipError_t launch_mass(const Geometry &g, const MassArgs &a, hipStream_t stream);
 
 struct SelectArgs {
