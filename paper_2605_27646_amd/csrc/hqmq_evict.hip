@@ -1,45 +1,52 @@
 // The tokens that a cache keeps, and their packed rows moved into a cache of their own (include/hqmq_serve.h,
 // hqmq_evict_select and hqmq_evict_compact).
+#include <type_traits>
+
 #include "hqmq_serve_device.h"
 
 namespace hqmq {
 
 namespace {
 
-// The rank order of masses as unsigned numbers: larger mass, larger key; -0 and +0 equal; every NaN below -infinity.
+// The rank order of masses as unsigned numbers: larger mass, larger key; -0 and +0 equal; every NaN (1) below -infinity.  0 is left
+// for what is not there, the largest number for tokens that are kept anyway.
 // On the bit patterns: the build tells the compiler that no arithmetic sees a NaN.
 __device__ __forceinline__ uint32_t mass_key(uint32_t bits)
 {
     const uint32_t magnitude = bits & 0x7fffffffu;
     if (magnitude > 0x7f800000u)
-        return 0u;
-    return magnitude == 0u ? 0x80000000u : (bits >> 31 ? ~bits : bits | 0x80000000u);
+        return 1u;
+    return (magnitude == 0u ? 0x80000000u : (bits >> 31 ? ~bits : bits | 0x80000000u)) + 1u;
 }
+constexpr uint32_t kKeptKey = 0xffffffffu;
 
-constexpr int kSelThreads = 1024;
+constexpr int kDigit0 = 12, kDigit1 = 10, kDigit2 = 10;  // of a key, from the top
+static_assert(kDigit0 + kDigit1 + kDigit2 == 32, "a key");
 
-__device__ __forceinline__ uint32_t block_sum(uint32_t v, uint32_t *red)
+__device__ __forceinline__ uint32_t wave_scan(uint32_t v, int lane)  // inclusive
 {
-    for (int d = 32; d > 0; d /= 2)
-        v += __shfl_xor(v, d);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0)
-        red[threadIdx.x >> 6] = v;
-    __syncthreads();
-    uint32_t s = 0;
-    for (int i = 0; i < kSelThreads / 64; ++i)
-        s += red[i];
-    return s;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const uint32_t o = __shfl_up(v, d);
+        v += lane >= d ? o : 0u;
+    }
+    return v;
 }
 
 }  // namespace
 
-// A workgroup per (b, h).  The key of the last token kept is found bit by bit from the top (a count of the keys at or
-// above a candidate decides a bit); then the tokens in order: all above it, and of those that equal it the first ones.
-__global__ __launch_bounds__(kSelThreads) void k_evict_select(SelectArgs a)
+// A workgroup per (b, h); a wave has kPer * 64 tokens in a row (of every kThreads * kPer), lane by lane, so that it reads whole lines and
+// finds the places of what it keeps with ballots.  The key of the last token kept is found digit by digit from the top: a histogram in LDS of
+// the keys that share the digits found so far, and a scan of it.  Keys stay in registers; cache lines beyond kThreads * kPer tokens
+// (kLoop) are read again for each digit, from the L2.
+// Bound by latency: one workgroup's loads, three histograms and scans, and the ballots.
+template <int kThreads, int kPer, bool kLoop>
+__global__ __launch_bounds__(kThreads) void k_evict_select(SelectArgs a)
 {
-    __shared__ uint32_t red[kSelThreads / 64];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    constexpr int kWaves = kThreads / 64, kSpan = kThreads * kPer;
+    __shared__ uint32_t hist[1 << kDigit0];
+    __shared__ uint32_t wave_sum[2][kWaves], found[3];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int64_t seg = blockIdx.x;
     const int b = (int)(seg / a.H);
     const int len = a.length ? min(max(a.length[b], 0), a.T) : a.T;
@@ -47,75 +54,170 @@ __global__ __launch_bounds__(kSelThreads) void k_evict_select(SelectArgs a)
     int32_t *keep = a.keep + seg * a.n_keep;
     uint32_t *kept = reinterpret_cast<uint32_t *>(a.kept_mass) + seg * a.n_keep;
     const int n = min(len, a.n_keep);
+    const int lo = a.n_sink, hi = len - a.n_recent;
+    const int mine = wave * kPer * 64 + lane;
+
+    uint32_t key[kPer];
+    const auto load = [&](int span) {
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) {
+            const int t = span + mine + 64 * j;
+            key[j] = mass[min(t, a.T - 1)];
+        }
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) {
+            const int t = span + mine + 64 * j;
+            const uint32_t k = t < lo || t >= hi ? kKeptKey : mass_key(key[j]);
+            key[j] = t < len ? k : 0u;
+        }
+    };
+    load(0);
     if (tid == 0)
         a.n_kept[seg] = n;
-    for (int j = n + tid; j < a.n_keep; j += kSelThreads) {
+    for (int j = n + tid; j < a.n_keep; j += kThreads) {
         keep[j] = -1;
         if (a.kept_mass)
             kept[j] = 0u;
     }
-    const bool all = len <= a.n_keep;
-    const int lo = all ? len : a.n_sink, hi = all ? len : len - a.n_recent;
-    const uint32_t want = all ? 0u : (uint32_t)(a.n_keep - a.n_sink - a.n_recent);  // of the tokens lo .. hi - 1, which are more
-    uint32_t last = 0u;
-    for (int bit = 31; bit >= 0 && want > 0; --bit) {
-        const uint32_t candidate = last | (1u << bit);
-        uint32_t c = 0;
-        for (int t = lo + tid; t < hi; t += kSelThreads)
-            c += mass_key(mass[t]) >= candidate;
-        if (block_sum(c, red) >= want)
-            last = candidate;
+
+    // ---- keys above `last` are kept, and of those equal to it the first `ties` -------------------------------------------------
+    uint32_t last = 0u, ties = 0u;
+    if (len > a.n_keep) {
+        uint32_t rank = (uint32_t)n, prefix = 0u;
+        const auto digit = [&](auto shift_tag, auto bits_tag) {
+            constexpr int kShift = decltype(shift_tag)::value, kBits = decltype(bits_tag)::value, kBins = 1 << kBits;
+            constexpr int kEach = kBins / kThreads > 0 ? kBins / kThreads : 1;  // bins of a thread, the highest of them with the first
+            for (int i = tid; i < kBins; i += kThreads)
+                hist[i] = 0u;
+            __syncthreads();
+            for (int span = 0; span < a.T; span += kSpan) {
+                if (kLoop)
+                    load(span);
+#pragma unroll
+                for (int j = 0; j < kPer; ++j) {
+                    const bool in = kShift + kBits == 32 ? key[j] != 0u : (kShift + kBits < 32 && key[j] >> ((kShift + kBits) & 31) == prefix && key[j] != 0u);
+                    if (in)
+                        atomicAdd(&hist[(key[j] >> kShift) & (kBins - 1)], 1u);
+                }
+                if (!kLoop)
+                    break;
+            }
+            __syncthreads();
+            uint32_t c[kEach], sum = 0u;
+            const int top = kBins - 1 - tid * kEach;
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+                c[i] = top - i >= 0 ? hist[top - i] : 0u;
+                sum += c[i];
+            }
+            const uint32_t scan = wave_scan(sum, lane);
+            if (lane == 63)
+                wave_sum[0][wave] = scan;
+            __syncthreads();
+            uint32_t above = scan - sum;
+            for (int i = 0; i < wave; ++i)
+                above += wave_sum[0][i];
+            if (above < rank && rank <= above + sum) {  // one thread
+#pragma unroll
+                for (int i = 0; i < kEach; ++i) {
+                    if (above < rank && rank <= above + c[i]) {
+                        found[0] = (uint32_t)(top - i);
+                        found[1] = rank - above;
+                        found[2] = c[i];
+                    }
+                    above += c[i];
+                }
+            }
+            __syncthreads();
+            prefix = prefix << kBits | found[0];
+            rank = found[1];
+            return found[2] == rank;  // every key with these digits is kept
+        };
+        bool whole = digit(std::integral_constant<int, 32 - kDigit0>{}, std::integral_constant<int, kDigit0>{});
+        int shift = 32 - kDigit0;
+        if (!whole) {
+            whole = digit(std::integral_constant<int, kDigit2>{}, std::integral_constant<int, kDigit1>{});
+            shift = kDigit2;
+        }
+        if (!whole) {
+            whole = digit(std::integral_constant<int, 0>{}, std::integral_constant<int, kDigit2>{});
+            shift = 0;
+        }
+        last = prefix << shift;
+        if (whole)
+            last = max(last, 1u) - 1u;
+        else
+            ties = rank;
     }
-    uint32_t above = 0;
-    for (int t = lo + tid; t < hi; t += kSelThreads)
-        above += mass_key(mass[t]) > last;
-    const uint32_t equal_wanted = want - (want > 0 ? block_sum(above, red) : 0u);
-    uint32_t done = 0, equal_done = 0;
-    for (int t0 = 0; t0 < len; t0 += kSelThreads) {
-        const int t = t0 + tid;
-        uint32_t key = 0;
-        bool mid = t >= lo && t < hi, eq = false, in = t < len && !mid;
-        if (mid && want > 0) {
-            key = mass_key(mass[t]);
-            in = key > last;
-            eq = key == last;
+
+    // ---- places, in token order --------------------------------------------------------------------------------------------------
+    uint32_t kept_before = 0u, ties_before = 0u;
+    for (int span = 0; span < a.T; span += kSpan) {
+        if (kLoop)
+            load(span);
+        uint32_t n_above = 0u, n_equal = 0u;  // of the wave
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) {
+            n_above += (uint32_t)__popcll(ballot(key[j] > last));
+            n_equal += (uint32_t)__popcll(ballot(key[j] == last));
         }
-        const unsigned long long me = ballot(eq);
-        __syncthreads();
-        if (lane == 0)
-            red[wave] = (uint32_t)__popcll(me);
-        __syncthreads();
-        uint32_t before = equal_done, total = 0;
-        for (int i = 0; i < kSelThreads / 64; ++i) {
-            before += i < wave ? red[i] : 0u;
-            total += red[i];
+        if (ties == 0u)
+            n_equal = 0u;
+        __syncthreads();  // the last reads of these words
+        if (lane == 0) {
+            wave_sum[0][wave] = n_above;
+            wave_sum[1][wave] = n_equal;
         }
-        equal_done += total;
-        in |= eq && before + (uint32_t)__popcll(me & ((1ull << lane) - 1ull)) < equal_wanted;
-        const unsigned long long mi = ballot(in);
         __syncthreads();
-        if (lane == 0)
-            red[wave] = (uint32_t)__popcll(mi);
-        __syncthreads();
-        before = done;
-        total = 0;
-        for (int i = 0; i < kSelThreads / 64; ++i) {
-            before += i < wave ? red[i] : 0u;
-            total += red[i];
+        uint32_t at = kept_before, equal = ties_before;
+#pragma unroll
+        for (int i = 0; i < kWaves; ++i) {
+            const uint32_t e = wave_sum[1][i], k = wave_sum[0][i] + (min(ties_before + e, ties) - min(ties_before, ties));
+            if (i < wave) {
+                at += k;
+                equal += e;
+            }
+            kept_before += k;
+            ties_before += e;
         }
-        done += total;
-        if (in) {
-            const uint32_t at = before + (uint32_t)__popcll(mi & ((1ull << lane) - 1ull));
-            keep[at] = t;
-            if (a.kept_mass)
-                kept[at] = mass[t];
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) {
+            const int t = span + mine + 64 * j;
+            const unsigned long long same = ties == 0u ? 0ull : ballot(key[j] == last);
+            const unsigned long long below = (1ull << lane) - 1ull;
+            const bool in = key[j] > last || (of_mask(same) && equal + (uint32_t)__popcll(same & below) < ties);
+            const unsigned long long kept_mask = ballot(in);
+            if (in) {
+                const uint32_t place = at + (uint32_t)__popcll(kept_mask & below);
+                keep[place] = t;
+                if (a.kept_mass)
+                    kept[place] = mass[t];
+            }
+            at += (uint32_t)__popcll(kept_mask);
+            equal += (uint32_t)__popcll(same);
         }
+        if (!kLoop)
+            break;
     }
 }
 
+// Threads and tokens of a thread by the tokens of a head: as many waves as can share them, up to 16, and the keys in registers up to
+// 32768 tokens.
 hipError_t launch_evict_select(const SelectArgs &a, hipStream_t stream)
 {
-    hipLaunchKernelGGL(k_evict_select, dim3((unsigned)(a.B * a.H)), dim3(kSelThreads), 0, stream, a);
+    const dim3 grid((unsigned)(a.B * a.H));
+    if (a.T <= 256 * 4)
+        hipLaunchKernelGGL((k_evict_select<256, 4, false>), grid, dim3(256), 0, stream, a);
+    else if (a.T <= 1024 * 4)
+        hipLaunchKernelGGL((k_evict_select<1024, 4, false>), grid, dim3(1024), 0, stream, a);
+    else if (a.T <= 1024 * 8)
+        hipLaunchKernelGGL((k_evict_select<1024, 8, false>), grid, dim3(1024), 0, stream, a);
+    else if (a.T <= 1024 * 16)
+        hipLaunchKernelGGL((k_evict_select<1024, 16, false>), grid, dim3(1024), 0, stream, a);
+    else if (a.T <= 1024 * 32)
+        hipLaunchKernelGGL((k_evict_select<1024, 32, false>), grid, dim3(1024), 0, stream, a);
+    else
+        hipLaunchKernelGGL((k_evict_select<1024, 32, true>), grid, dim3(1024), 0, stream, a);
     return hipGetLastError();
 }
 
