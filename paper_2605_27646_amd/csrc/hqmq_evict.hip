@@ -57,17 +57,17 @@ __global__ __launch_bounds__(kThreads) void k_evict_select(SelectArgs a)
     const int lo = a.n_sink, hi = len - a.n_recent;
     const int mine = wave * kPer * 64 + lane;
 
-    uint32_t key[kPer];
+    uint32_t key[kPer], raw[kPer];
     const auto load = [&](int span) {
 #pragma unroll
         for (int j = 0; j < kPer; ++j) {
             const int t = span + mine + 64 * j;
-            key[j] = mass[min(t, a.T - 1)];
+            raw[j] = mass[min(t, a.T - 1)];
         }
 #pragma unroll
         for (int j = 0; j < kPer; ++j) {
             const int t = span + mine + 64 * j;
-            const uint32_t k = t < lo || t >= hi ? kKeptKey : mass_key(key[j]);
+            const uint32_t k = t < lo || t >= hi ? kKeptKey : mass_key(raw[j]);
             key[j] = t < len ? k : 0u;
         }
     };
@@ -159,10 +159,9 @@ __global__ __launch_bounds__(kThreads) void k_evict_select(SelectArgs a)
 #pragma unroll
         for (int j = 0; j < kPer; ++j) {
             n_above += (uint32_t)__popcll(ballot(key[j] > last));
-            n_equal += (uint32_t)__popcll(ballot(key[j] == last));
+            if (ties != 0u)
+                n_equal += (uint32_t)__popcll(ballot(key[j] == last));
         }
-        if (ties == 0u)
-            n_equal = 0u;
         __syncthreads();  // the last reads of these words
         if (lane == 0) {
             wave_sum[0][wave] = n_above;
@@ -180,22 +179,30 @@ __global__ __launch_bounds__(kThreads) void k_evict_select(SelectArgs a)
             kept_before += k;
             ties_before += e;
         }
+        const auto place = [&](bool with_ties) {
 #pragma unroll
-        for (int j = 0; j < kPer; ++j) {
-            const int t = span + mine + 64 * j;
-            const unsigned long long same = ties == 0u ? 0ull : ballot(key[j] == last);
-            const unsigned long long below = (1ull << lane) - 1ull;
-            const bool in = key[j] > last || (of_mask(same) && equal + (uint32_t)__popcll(same & below) < ties);
-            const unsigned long long kept_mask = ballot(in);
-            if (in) {
-                const uint32_t place = at + (uint32_t)__popcll(kept_mask & below);
-                keep[place] = t;
-                if (a.kept_mass)
-                    kept[place] = mass[t];
+            for (int j = 0; j < kPer; ++j) {
+                const unsigned long long below = (1ull << lane) - 1ull;
+                bool in = key[j] > last;
+                if (with_ties) {
+                    const unsigned long long same = ballot(key[j] == last);
+                    in = in || (of_mask(same) && equal + (uint32_t)__popcll(same & below) < ties);
+                    equal += (uint32_t)__popcll(same);
+                }
+                const unsigned long long kept_mask = ballot(in);
+                if (in) {
+                    const uint32_t to = at + (uint32_t)__popcll(kept_mask & below);
+                    keep[to] = span + mine + 64 * j;
+                    if (a.kept_mass)
+                        kept[to] = raw[j];
+                }
+                at += (uint32_t)__popcll(kept_mask);
             }
-            at += (uint32_t)__popcll(kept_mask);
-            equal += (uint32_t)__popcll(same);
-        }
+        };
+        if (ties == 0u)
+            place(false);
+        else
+            place(true);
         if (!kLoop)
             break;
     }
