@@ -1115,7 +1115,7 @@ extern "C" uint64_t hqmq_evict_select_workspace_bytes(int32_t B, int32_t H, int3
 {
     if (check_select(B, H, T, n_keep) != HQMQ_OK)
         return 0;
-    return 0;
+    return evict_select_workspace_bytes(B, H, T);
 }
 
 extern "C" int32_t hqmq_evict_select(int32_t B, int32_t H, int32_t T, const float *mass_dev, const int32_t *length_dev,
@@ -1147,7 +1147,7 @@ extern "C" int32_t hqmq_evict_select(int32_t B, int32_t H, int32_t T, const floa
     a.n_sink = n_sink;
     a.n_recent = n_recent;
     a.n_keep = n_keep;
-    const hipError_t err = launch_evict_select(a, static_cast<hipStream_t>(stream));
+    const hipError_t err = launch_evict_select(a, static_cast<uint32_t *>(workspace_dev), static_cast<hipStream_t>(stream));
     return err == hipSuccess ? HQMQ_OK : hip_failed(err);
 }
 
@@ -1174,7 +1174,7 @@ static CompactShape compact_shape(const hqmq_params *params, int32_t n_keep)
     s.row_words = g.row_words;
     s.blocks_per_seg = (n_keep + kCompactRows - 1) / kCompactRows;
     s.totals = nullptr;
-    s.totals_stride = align_up((uint64_t)g.B * g.H * s.blocks_per_seg, 64);
+    s.totals_stride = align_up(5ull * g.B * g.H * s.blocks_per_seg, 64);
     return s;
 }
 

@@ -18,7 +18,7 @@ __device__ __forceinline__ uint32_t mass_key(uint32_t bits)
         return 1u;
     return (magnitude == 0u ? 0x80000000u : (bits >> 31 ? ~bits : bits | 0x80000000u)) + 1u;
 }
-constexpr uint32_t kKeptKey = 0xffffffffu;
+constexpr uint32_t kKeptKey = 0xffffffffu, kZeroKey = 0x80000001u;
 
 constexpr int kDigit0 = 12, kDigit1 = 10, kDigit2 = 10;  // of a key, from the top
 static_assert(kDigit0 + kDigit1 + kDigit2 == 32, "a key");
@@ -33,102 +33,202 @@ __device__ __forceinline__ uint32_t wave_scan(uint32_t v, int lane)  // inclusiv
     return v;
 }
 
+// The tokens of a head, and the keys of kThreads * kPer of them from `first` on: a wave has kPer * 64 in a row, lane by lane, so that it
+// reads whole lines and finds the places of what it keeps with ballots.
+struct Head {
+    const uint32_t *mass;
+    int T, len, lo, hi, n_keep;  // lo .. hi - 1: the tokens that are not kept anyway
+    __device__ __forceinline__ Head(const SelectArgs &a, int64_t seg)
+    {
+        T = a.T;
+        len = a.length ? min(max(a.length[seg / a.H], 0), a.T) : a.T;
+        mass = reinterpret_cast<const uint32_t *>(a.mass) + seg * a.T;
+        lo = a.n_sink;
+        hi = len - a.n_recent;
+        n_keep = a.n_keep;
+    }
+    __device__ __forceinline__ uint32_t key(int t, uint32_t raw) const
+    {
+        const uint32_t k = t < lo || t >= hi ? kKeptKey : mass_key(raw);
+        return t < len ? k : 0u;
+    }
+};
+template <int kPer>
+struct Keys {
+    uint32_t key[kPer];
+    int mine;  // the token of key[0]; key[j]'s is 64 j further
+    __device__ __forceinline__ void load(const Head &h, int first, int wave, int lane)
+    {
+        mine = first + wave * kPer * 64 + lane;
+#pragma unroll
+        for (int j = 0; j < kPer; ++j)
+            key[j] = h.mass[min(mine + 64 * j, h.T - 1)];
+#pragma unroll
+        for (int j = 0; j < kPer; ++j)
+            key[j] = h.key(mine + 64 * j, key[j]);
+    }
+};
+
+// The keys' digit of kBits bits above kShift, of those that share the digits above it with prefix, added to hist in LDS.  Where a quarter of
+// a wave's first keys have one digit (a value that many tokens have would be added one by one: 32768 equal masses 100 us instead of 36), a
+// wave adds the keys that have its first lane's digit at once.
+template <int kShift, int kBits, int kPer>
+__device__ __forceinline__ void count_digit(const Keys<kPer> &k, uint32_t prefix, uint32_t *hist, int lane)
+{
+    const auto bin_of = [&](uint32_t x) { return (x >> kShift) & ((1u << kBits) - 1u); };
+    const auto counts = [&](uint32_t x) { return x != 0u && (kShift + kBits >= 32 || x >> ((kShift + kBits) & 31) == prefix); };
+    const auto common = [&](int l) {
+        const uint32_t its = (uint32_t)__builtin_amdgcn_readlane((int)bin_of(k.key[0]), l);
+        return __popcll(ballot(counts(k.key[0]) && bin_of(k.key[0]) == its)) >= 16;
+    };
+    if (kPer == 1 || common(0) || common(21) || common(42)) {
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) {
+            const uint32_t bin = bin_of(k.key[j]);
+            const bool in = counts(k.key[j]);
+            const unsigned long long all = ballot(in);
+            if (all == 0ull)
+                continue;
+            const int first = (int)__ffsll((unsigned long long)all) - 1;
+            const uint32_t its = (uint32_t)__builtin_amdgcn_readlane((int)bin, first);
+            const unsigned long long same = ballot(in && bin == its);
+            if (lane == first)
+                atomicAdd(&hist[its], (uint32_t)__popcll(same));
+            else if (in && bin != its)
+                atomicAdd(&hist[bin], 1u);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < kPer; ++j)
+            if (counts(k.key[j]))
+                atomicAdd(&hist[bin_of(k.key[j])], 1u);
+    }
+}
+
+// From a histogram, kEach bins of it in this thread (bin kBins - 1 - kEach * tid - i in c[i]), the bin that holds the key of the given rank
+// from the top: found[0], found[1] its rank there, found[2] the bin's keys.
+template <int kThreads, int kEach>
+__device__ __forceinline__ void find_bin(const uint32_t *c, int top, uint32_t rank, uint32_t *wave_sum, uint32_t *found, int wave, int lane)
+{
+    uint32_t sum = 0u;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i)
+        sum += c[i];
+    const uint32_t scan = wave_scan(sum, lane);
+    if (lane == 63)
+        wave_sum[wave] = scan;
+    __syncthreads();
+    uint32_t above = scan - sum;
+    for (int i = 0; i < wave; ++i)
+        above += wave_sum[i];
+    if (above < rank && rank <= above + sum) {  // one thread
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            if (above < rank && rank <= above + c[i]) {
+                found[0] = (uint32_t)(top - i);
+                found[1] = rank - above;
+                found[2] = c[i];
+            }
+            above += c[i];
+        }
+    }
+    __syncthreads();
+}
+
+// The tokens above `last`, and the first `ties` of those equal to it, to their places.  at, equal: how many of either this wave's tokens
+// come behind.
+template <int kPer>
+__device__ __forceinline__ void place_keys(const Keys<kPer> &k, uint32_t last, uint32_t ties, uint32_t at, uint32_t equal, const Head &head, int32_t *keep, uint32_t *kept, int lane)
+{
+    const unsigned long long below = (1ull << lane) - 1ull;
+    const uint32_t *mass = head.mass;
+    const int lo = head.lo, hi = head.hi;
+    const auto place = [&](auto plain_tag) {
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) {
+            bool in = k.key[j] > last;
+            if (!decltype(plain_tag)::value && ties != 0u) {
+                const unsigned long long same = ballot(k.key[j] == last);
+                in = in || (of_mask(same) && equal + (uint32_t)__popcll(same & below) < ties);
+                equal += (uint32_t)__popcll(same);
+            }
+            const unsigned long long kept_mask = ballot(in);
+            if (in) {
+                const uint32_t to = at + (uint32_t)__popcll(kept_mask & below);
+                keep[to] = k.mine + 64 * j;
+                if (kept)
+                    kept[to] = decltype(plain_tag)::value ? k.key[j] - kZeroKey : mass[k.mine + 64 * j];
+            }
+            at += (uint32_t)__popcll(kept_mask);
+        }
+    };
+    // most waves: no ties, and of the keys only those of positive masses, which tell the masses
+    const int first = k.mine - lane;
+    if (ties == 0u && last >= kZeroKey && first >= lo && first + 64 * kPer <= hi)
+        place(std::true_type{});
+    else
+        place(std::false_type{});
+}
+template <int kPer>
+__device__ __forceinline__ void count_kept(const Keys<kPer> &k, uint32_t last, uint32_t ties, uint32_t &above, uint32_t &equal)
+{
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+        above += (uint32_t)__popcll(ballot(k.key[j] > last));
+        if (ties != 0u)
+            equal += (uint32_t)__popcll(ballot(k.key[j] == last));
+    }
+}
+
+// Counts, and -1 and zeros behind the kept tokens of a head that has fewer than n_keep.
+__device__ __forceinline__ void fill_rest(const SelectArgs &a, int64_t seg, int n, int tid, int threads)
+{
+    if (tid == 0)
+        a.n_kept[seg] = n;
+    for (int j = n + tid; j < a.n_keep; j += threads) {
+        a.keep[seg * a.n_keep + j] = -1;
+        if (a.kept_mass)
+            a.kept_mass[seg * a.n_keep + j] = 0.f;
+    }
+}
+
 }  // namespace
 
-// A workgroup per (b, h); a wave has kPer * 64 tokens in a row (of every kThreads * kPer), lane by lane, so that it reads whole lines and
-// finds the places of what it keeps with ballots.  The key of the last token kept is found digit by digit from the top: a histogram in LDS of
-// the keys that share the digits found so far, and a scan of it.  Keys stay in registers; cache lines beyond kThreads * kPer tokens
-// (kLoop) are read again for each digit, from the L2.
-// Bound by latency: one workgroup's loads, three histograms and scans, and the ballots.
-template <int kThreads, int kPer, bool kLoop>
+// A workgroup per (b, h), its keys in registers.  The key of the last token kept is found digit by digit from the top: a histogram in LDS of
+// the keys that share the digits found so far, and a scan of it.
+// Bound by latency: one workgroup's loads, three histograms and scans, and 0.5 us for every 1024 tokens.
+template <int kThreads, int kPer>
 __global__ __launch_bounds__(kThreads) void k_evict_select(SelectArgs a)
 {
-    constexpr int kWaves = kThreads / 64, kSpan = kThreads * kPer;
+    constexpr int kWaves = kThreads / 64;
     __shared__ uint32_t hist[1 << kDigit0];
     __shared__ uint32_t wave_sum[2][kWaves], found[3];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int64_t seg = blockIdx.x;
-    const int b = (int)(seg / a.H);
-    const int len = a.length ? min(max(a.length[b], 0), a.T) : a.T;
-    const uint32_t *mass = reinterpret_cast<const uint32_t *>(a.mass) + seg * a.T;
-    int32_t *keep = a.keep + seg * a.n_keep;
-    uint32_t *kept = reinterpret_cast<uint32_t *>(a.kept_mass) + seg * a.n_keep;
-    const int n = min(len, a.n_keep);
-    const int lo = a.n_sink, hi = len - a.n_recent;
-    const int mine = wave * kPer * 64 + lane;
-
-    uint32_t key[kPer], raw[kPer];
-    const auto load = [&](int span) {
-#pragma unroll
-        for (int j = 0; j < kPer; ++j) {
-            const int t = span + mine + 64 * j;
-            raw[j] = mass[min(t, a.T - 1)];
-        }
-#pragma unroll
-        for (int j = 0; j < kPer; ++j) {
-            const int t = span + mine + 64 * j;
-            const uint32_t k = t < lo || t >= hi ? kKeptKey : mass_key(raw[j]);
-            key[j] = t < len ? k : 0u;
-        }
-    };
-    load(0);
-    if (tid == 0)
-        a.n_kept[seg] = n;
-    for (int j = n + tid; j < a.n_keep; j += kThreads) {
-        keep[j] = -1;
-        if (a.kept_mass)
-            kept[j] = 0u;
-    }
+    const Head head(a, seg);
+    const int n = min(head.len, a.n_keep);
+    Keys<kPer> k;
+    k.load(head, 0, wave, lane);
+    fill_rest(a, seg, n, tid, kThreads);
 
     // ---- keys above `last` are kept, and of those equal to it the first `ties` -------------------------------------------------
     uint32_t last = 0u, ties = 0u;
-    if (len > a.n_keep) {
+    if (head.len > a.n_keep) {
         uint32_t rank = (uint32_t)n, prefix = 0u;
         const auto digit = [&](auto shift_tag, auto bits_tag) {
             constexpr int kShift = decltype(shift_tag)::value, kBits = decltype(bits_tag)::value, kBins = 1 << kBits;
-            constexpr int kEach = kBins / kThreads > 0 ? kBins / kThreads : 1;  // bins of a thread, the highest of them with the first
+            constexpr int kEach = kBins / kThreads;
             for (int i = tid; i < kBins; i += kThreads)
                 hist[i] = 0u;
             __syncthreads();
-            for (int span = 0; span < a.T; span += kSpan) {
-                if (kLoop)
-                    load(span);
-#pragma unroll
-                for (int j = 0; j < kPer; ++j) {
-                    const bool in = kShift + kBits == 32 ? key[j] != 0u : (kShift + kBits < 32 && key[j] >> ((kShift + kBits) & 31) == prefix && key[j] != 0u);
-                    if (in)
-                        atomicAdd(&hist[(key[j] >> kShift) & (kBins - 1)], 1u);
-                }
-                if (!kLoop)
-                    break;
-            }
+            count_digit<kShift, kBits>(k, prefix, hist, lane);
             __syncthreads();
-            uint32_t c[kEach], sum = 0u;
+            uint32_t c[kEach];
             const int top = kBins - 1 - tid * kEach;
 #pragma unroll
-            for (int i = 0; i < kEach; ++i) {
-                c[i] = top - i >= 0 ? hist[top - i] : 0u;
-                sum += c[i];
-            }
-            const uint32_t scan = wave_scan(sum, lane);
-            if (lane == 63)
-                wave_sum[0][wave] = scan;
-            __syncthreads();
-            uint32_t above = scan - sum;
-            for (int i = 0; i < wave; ++i)
-                above += wave_sum[0][i];
-            if (above < rank && rank <= above + sum) {  // one thread
-#pragma unroll
-                for (int i = 0; i < kEach; ++i) {
-                    if (above < rank && rank <= above + c[i]) {
-                        found[0] = (uint32_t)(top - i);
-                        found[1] = rank - above;
-                        found[2] = c[i];
-                    }
-                    above += c[i];
-                }
-            }
-            __syncthreads();
+            for (int i = 0; i < kEach; ++i)
+                c[i] = hist[top - i];
+            find_bin<kThreads, kEach>(c, top, rank, wave_sum[0], found, wave, lane);
             prefix = prefix << kBits | found[0];
             rank = found[1];
             return found[2] == rank;  // every key with these digits is kept
@@ -151,185 +251,346 @@ __global__ __launch_bounds__(kThreads) void k_evict_select(SelectArgs a)
     }
 
     // ---- places, in token order --------------------------------------------------------------------------------------------------
-    uint32_t kept_before = 0u, ties_before = 0u;
-    for (int span = 0; span < a.T; span += kSpan) {
-        if (kLoop)
-            load(span);
-        uint32_t n_above = 0u, n_equal = 0u;  // of the wave
-#pragma unroll
-        for (int j = 0; j < kPer; ++j) {
-            n_above += (uint32_t)__popcll(ballot(key[j] > last));
-            if (ties != 0u)
-                n_equal += (uint32_t)__popcll(ballot(key[j] == last));
+    uint32_t above = 0u, equal = 0u;  // of the wave
+    count_kept(k, last, ties, above, equal);
+    __syncthreads();
+    if (lane == 0) {
+        wave_sum[0][wave] = above;
+        wave_sum[1][wave] = equal;
+    }
+    __syncthreads();
+    above = equal = 0u;  // of the waves before it
+    for (int i = 0; i < wave; ++i) {
+        above += wave_sum[0][i];
+        equal += wave_sum[1][i];
+    }
+    place_keys(k, last, ties, above + min(equal, ties), equal, head, a.keep + seg * a.n_keep,
+               a.kept_mass ? reinterpret_cast<uint32_t *>(a.kept_mass) + seg * a.n_keep : nullptr, lane);
+}
+
+// Longer heads are shared by workgroups of kPart tokens, in four launches: the histogram of each digit, left in the workspace for the next
+// launch to sum, and the places.  Every workgroup finds the last digit for itself, which saves a launch per digit.
+constexpr int kPartThreads = 1024, kPartPer = 8, kPart = kPartThreads * kPartPer;
+constexpr int kDigitBits[3] = {kDigit0, kDigit1, kDigit2}, kDigitShift[3] = {32 - kDigit0, kDigit2, 0};
+// A workspace, in 32-bit words: histograms of the three digits [segs][parts][bins], and what the first two left [2][segs][4]:
+// prefix, rank in its last bin, whether the search ended there.
+struct PartLayout {
+    uint64_t hist[3], state[2], total;
+    int parts;
+    __host__ __device__ PartLayout(int64_t segs, int T)
+    {
+        parts = (T + kPart - 1) / kPart;
+        uint64_t at = 0;
+        const int bits[3] = {kDigit0, kDigit1, kDigit2};
+        for (int d = 0; d < 3; ++d) {
+            hist[d] = at;
+            at += (uint64_t)segs * parts << bits[d];
         }
-        __syncthreads();  // the last reads of these words
-        if (lane == 0) {
-            wave_sum[0][wave] = n_above;
-            wave_sum[1][wave] = n_equal;
+        for (int d = 0; d < 2; ++d) {
+            state[d] = at;
+            at += (uint64_t)segs * 4;
+        }
+        total = at;
+    }
+};
+
+template <int kStep>  // 0, 1, 2: that digit's histogram; 3: the places
+__global__ __launch_bounds__(kPartThreads) void k_evict_select_part(SelectArgs a, uint32_t *ws)
+{
+    constexpr int kWaves = kPartThreads / 64;
+    __shared__ uint32_t hist[1 << kDigit0];
+    __shared__ uint32_t wave_sum[2][kWaves], found[3];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int64_t seg = blockIdx.y;
+    const int part = blockIdx.x;
+    const Head head(a, seg);
+    const PartLayout l((int64_t)a.B * a.H, a.T);
+    const int n = min(head.len, a.n_keep);
+    const bool all = head.len <= a.n_keep;  // kept whole: nothing to find
+    if (kStep < 3 && all)
+        return;
+    Keys<kPartPer> k;
+    k.load(head, part * kPart, wave, lane);
+
+    uint32_t prefix = 0u, rank = (uint32_t)n;
+    bool done = false;
+    int digits = 0;  // found so far, their bins in prefix
+    if (kStep > 0 && !all) {
+        constexpr int kD = kStep - 1, kBins = 1 << kDigitBits[kD < 0 ? 0 : kD], kEach = kBins / kPartThreads;
+        if (kD > 0) {
+            const uint32_t *before = ws + l.state[kD > 0 ? kD - 1 : 0] + seg * 4;
+            prefix = before[0];
+            rank = before[1];
+            digits = (int)before[2];
+            done = before[3] != 0u;
+        }
+        if (!done) {
+            const uint32_t *h = ws + l.hist[kD < 0 ? 0 : kD] + seg * l.parts * kBins;
+            const int top = kBins - 1 - tid * kEach;
+            uint32_t c[kEach];
+#pragma unroll
+            for (int i = 0; i < kEach; ++i)
+                c[i] = 0u;
+            for (int p = 0; p < l.parts; ++p)
+#pragma unroll
+                for (int i = 0; i < kEach; ++i)
+                    c[i] += h[(int64_t)p * kBins + top - i];
+            find_bin<kPartThreads, kEach>(c, top, rank, wave_sum[0], found, wave, lane);
+            prefix = prefix << kDigitBits[kD < 0 ? 0 : kD] | found[0];
+            rank = found[1];
+            done = found[2] == rank || kD == 2;
+            digits = kD + 1;
+        }
+        if (kD < 2 && part == 0 && tid == 0) {
+            uint32_t *after = ws + l.state[kD < 0 || kD > 1 ? 0 : kD] + seg * 4;
+            after[0] = prefix;
+            after[1] = rank;
+            after[2] = (uint32_t)digits;
+            after[3] = done ? 1u : 0u;
+        }
+    }
+    if constexpr (kStep < 3) {
+        if (done)
+            return;
+        constexpr int kBins = 1 << kDigitBits[kStep];
+        for (int i = tid; i < kBins; i += kPartThreads)
+            hist[i] = 0u;
+        __syncthreads();
+        count_digit<kDigitShift[kStep], kDigitBits[kStep]>(k, prefix, hist, lane);
+        __syncthreads();
+        uint32_t *h = ws + l.hist[kStep] + (seg * l.parts + part) * kBins;
+        for (int i = tid; i < kBins; i += kPartThreads)
+            h[i] = hist[i];
+    } else {
+        if (part == 0)
+            fill_rest(a, seg, n, tid, kPartThreads);
+        // keys above `last` are kept, and of those equal to it the first `ties`; below the first digits' bins everything is one key
+        const int shift = digits == 1 ? kDigitShift[0] : digits == 2 ? kDigitShift[1] : kDigitShift[2];
+        // the last bin whole (or, of one key, as many as are kept: the search by rank ends there too)
+        uint32_t last = all ? 0u : prefix << shift, ties = 0u;
+        bool whole = false;
+        if (!all) {
+            // `done` with fewer than three digits, or with all of the third's keys kept: told apart by the rank
+            const int d = digits - 1, bins = 1 << (d == 0 ? kDigit0 : d == 1 ? kDigit1 : kDigit2);
+            const uint32_t *h = ws + l.hist[d] + seg * l.parts * bins + (prefix & (uint32_t)(bins - 1));
+            uint32_t its = 0u;
+            for (int p = 0; p < l.parts; ++p)
+                its += h[(int64_t)p * bins];
+            whole = its == rank;
+            if (whole)
+                last = max(last, 1u) - 1u;
+            else
+                ties = rank;
+        }
+        // what the parts before this one keep, from their histograms
+        uint32_t above = 0u, equal = 0u;
+        if (all) {
+            if (tid == 0)
+                above = (uint32_t)min(part * kPart, head.len);
+        } else {
+            uint32_t path = prefix;
+            for (int d = digits - 1; d >= 0; --d) {
+                const int bits = d == 0 ? kDigit0 : d == 1 ? kDigit1 : kDigit2, bins = 1 << bits;
+                const uint32_t its = path & (uint32_t)(bins - 1);
+                path >>= bits;
+                const bool with_its = whole && d == digits - 1;
+                const uint32_t *h = ws + l.hist[d] + seg * l.parts * bins;
+                for (int p = 0; p < part; ++p)
+                    for (int i = tid; i < bins; i += kPartThreads) {
+                        const uint32_t c = h[(int64_t)p * bins + i];
+                        above += (uint32_t)i > its || (with_its && (uint32_t)i == its) ? c : 0u;
+                        equal += ties != 0u && d == digits - 1 && (uint32_t)i == its ? c : 0u;
+                    }
+            }
+        }
+        above = wave_scan(above, lane);
+        equal = wave_scan(equal, lane);
+        __syncthreads();
+        if (lane == 63) {
+            wave_sum[0][wave] = above;
+            wave_sum[1][wave] = equal;
         }
         __syncthreads();
-        uint32_t at = kept_before, equal = ties_before;
-#pragma unroll
+        uint32_t above_before = 0u, equal_before = 0u;
         for (int i = 0; i < kWaves; ++i) {
-            const uint32_t e = wave_sum[1][i], k = wave_sum[0][i] + (min(ties_before + e, ties) - min(ties_before, ties));
-            if (i < wave) {
-                at += k;
-                equal += e;
-            }
-            kept_before += k;
-            ties_before += e;
+            above_before += wave_sum[0][i];
+            equal_before += wave_sum[1][i];
         }
-        const auto place = [&](bool with_ties) {
-#pragma unroll
-            for (int j = 0; j < kPer; ++j) {
-                const unsigned long long below = (1ull << lane) - 1ull;
-                bool in = key[j] > last;
-                if (with_ties) {
-                    const unsigned long long same = ballot(key[j] == last);
-                    in = in || (of_mask(same) && equal + (uint32_t)__popcll(same & below) < ties);
-                    equal += (uint32_t)__popcll(same);
-                }
-                const unsigned long long kept_mask = ballot(in);
-                if (in) {
-                    const uint32_t to = at + (uint32_t)__popcll(kept_mask & below);
-                    keep[to] = span + mine + 64 * j;
-                    if (a.kept_mass)
-                        kept[to] = raw[j];
-                }
-                at += (uint32_t)__popcll(kept_mask);
-            }
-        };
-        if (ties == 0u)
-            place(false);
-        else
-            place(true);
-        if (!kLoop)
-            break;
+        above = equal = 0u;  // of the wave
+        count_kept(k, last, ties, above, equal);
+        __syncthreads();
+        if (lane == 0) {
+            wave_sum[0][wave] = above;
+            wave_sum[1][wave] = equal;
+        }
+        __syncthreads();
+        for (int i = 0; i < wave; ++i) {
+            above_before += wave_sum[0][i];
+            equal_before += wave_sum[1][i];
+        }
+        place_keys(k, last, ties, above_before + min(equal_before, ties), equal_before, head, a.keep + seg * a.n_keep,
+                   a.kept_mass ? reinterpret_cast<uint32_t *>(a.kept_mass) + seg * a.n_keep : nullptr, lane);
     }
 }
 
-// Threads and tokens of a thread by the tokens of a head: as many waves as can share them, up to 16, and the keys in registers up to
-// 32768 tokens.
-hipError_t launch_evict_select(const SelectArgs &a, hipStream_t stream)
+// One workgroup takes a head of up to 32768 tokens, with as many waves as can share them, up to 16.
+static bool select_in_parts(int T) { return T > 1024 * 32; }
+
+uint64_t evict_select_workspace_bytes(int B, int H, int T)
+{
+    return select_in_parts(T) ? PartLayout((int64_t)B * H, T).total * sizeof(uint32_t) : 0;
+}
+
+hipError_t launch_evict_select(const SelectArgs &a, uint32_t *workspace, hipStream_t stream)
 {
     const dim3 grid((unsigned)(a.B * a.H));
-    if (a.T <= 256 * 4)
-        hipLaunchKernelGGL((k_evict_select<256, 4, false>), grid, dim3(256), 0, stream, a);
+    if (select_in_parts(a.T)) {
+        const dim3 parts((unsigned)((a.T + kPart - 1) / kPart), (unsigned)(a.B * a.H));
+        hipLaunchKernelGGL(k_evict_select_part<0>, parts, dim3(kPartThreads), 0, stream, a, workspace);
+        hipLaunchKernelGGL(k_evict_select_part<1>, parts, dim3(kPartThreads), 0, stream, a, workspace);
+        hipLaunchKernelGGL(k_evict_select_part<2>, parts, dim3(kPartThreads), 0, stream, a, workspace);
+        hipLaunchKernelGGL(k_evict_select_part<3>, parts, dim3(kPartThreads), 0, stream, a, workspace);
+    } else if (a.T <= 256 * 4)
+        hipLaunchKernelGGL((k_evict_select<256, 4>), grid, dim3(256), 0, stream, a);
     else if (a.T <= 1024 * 4)
-        hipLaunchKernelGGL((k_evict_select<1024, 4, false>), grid, dim3(1024), 0, stream, a);
+        hipLaunchKernelGGL((k_evict_select<1024, 4>), grid, dim3(1024), 0, stream, a);
     else if (a.T <= 1024 * 8)
-        hipLaunchKernelGGL((k_evict_select<1024, 8, false>), grid, dim3(1024), 0, stream, a);
+        hipLaunchKernelGGL((k_evict_select<1024, 8>), grid, dim3(1024), 0, stream, a);
     else if (a.T <= 1024 * 16)
-        hipLaunchKernelGGL((k_evict_select<1024, 16, false>), grid, dim3(1024), 0, stream, a);
-    else if (a.T <= 1024 * 32)
-        hipLaunchKernelGGL((k_evict_select<1024, 32, false>), grid, dim3(1024), 0, stream, a);
+        hipLaunchKernelGGL((k_evict_select<1024, 16>), grid, dim3(1024), 0, stream, a);
     else
-        hipLaunchKernelGGL((k_evict_select<1024, 32, true>), grid, dim3(1024), 0, stream, a);
+        hipLaunchKernelGGL((k_evict_select<1024, 32>), grid, dim3(1024), 0, stream, a);
     return hipGetLastError();
 }
 
-// ---- compaction: outliers per workgroup of 256 rows, then every workgroup finds its place and moves its rows ----------
+// ---- compaction ------------------------------------------------------------------------------------------------------------------
+// A launch counts the outliers of every 64 and every 256 kept rows; in the next a workgroup takes 64 rows, sums what comes before them,
+// and moves code words and payloads lane by lane along the new tensor, so that they are written in whole lines.
+// Bound by latency: the chain of loads from a kept index over its flags to its payloads, in each of the two launches.
+
+namespace {
+constexpr int kMoveThreads = 256, kMoveRows = 64;
+constexpr int kMoveList = 512;  // payloads of 64 rows that are moved line by line; more than a quarter of the chunks: row by row
+static_assert(kCompactRows == 4 * kMoveRows, "a count for every wave");
 
 __device__ __forceinline__ int64_t source_row(const CompactShape &s, const CompactTensor &t, int seg, int j)
 {
+    if (j >= s.n_keep)
+        return -1;
     const int k = t.keep[(int64_t)seg * s.n_keep + j];
     return k >= 0 && k < s.T ? (int64_t)seg * s.T + k : -1;
 }
+__device__ __forceinline__ uint32_t wave_total(uint32_t v)
+{
+#pragma unroll
+    for (int d = 32; d > 0; d /= 2)
+        v += __shfl_xor(v, d);
+    return v;
+}
+}  // namespace
 
 __global__ __launch_bounds__(kCompactRows) void k_compact_count(CompactShape s, CompactBatch batch)
 {
-    __shared__ uint32_t red[kCompactRows / 64];
+    __shared__ uint32_t sub[4];
     const CompactTensor &t = batch.t[blockIdx.z];
-    const int seg = blockIdx.y, j = blockIdx.x * kCompactRows + threadIdx.x;
-    uint32_t c = 0;
-    if (j < s.n_keep) {
-        const int64_t from = source_row(s, t, seg, j);
-        c = from >= 0 ? __popc(t.in.flags[from]) : 0;
-    }
-    for (int d = 32; d > 0; d /= 2)
-        c += __shfl_xor(c, d);
+    const int seg = blockIdx.y;
+    const int64_t from = source_row(s, t, seg, blockIdx.x * kCompactRows + threadIdx.x);
+    const uint32_t c = wave_total(from >= 0 ? __popc(t.in.flags[from]) : 0u);
     if ((threadIdx.x & 63) == 0)
-        red[threadIdx.x >> 6] = c;
+        sub[threadIdx.x >> 6] = c;
     __syncthreads();
+    uint32_t *totals = s.totals + blockIdx.z * s.totals_stride;
+    const int64_t block = (int64_t)seg * s.blocks_per_seg + blockIdx.x, blocks = (int64_t)s.B * s.H * s.blocks_per_seg;
     if (threadIdx.x == 0)
-        s.totals[blockIdx.z * s.totals_stride + (uint64_t)seg * s.blocks_per_seg + blockIdx.x] = red[0] + red[1] + red[2] + red[3];
+        totals[block] = sub[0] + sub[1] + sub[2] + sub[3];
+    if (threadIdx.x < 4)
+        totals[blocks + 4 * block + threadIdx.x] = sub[threadIdx.x];
 }
 
-__global__ __launch_bounds__(kCompactRows) void k_compact_move(CompactShape s, CompactBatch batch)
+__global__ __launch_bounds__(kMoveThreads) void k_compact_move(CompactShape s, CompactBatch batch)
 {
-    __shared__ uint32_t red[2][kCompactRows / 64], base_s;
+    __shared__ int64_t row_of[kMoveRows];
+    __shared__ uint32_t red[2][kMoveThreads / 64], list[kMoveList];
     const CompactTensor &t = batch.t[blockIdx.z];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int seg = blockIdx.y, j = blockIdx.x * kCompactRows + tid, segs = s.B * s.H;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int seg = blockIdx.y, j0 = blockIdx.x * kMoveRows, n = min(s.n_keep - j0, kMoveRows);
     const uint32_t *totals = s.totals + blockIdx.z * s.totals_stride;
-    const int64_t me = (int64_t)seg * s.blocks_per_seg + blockIdx.x;
-    uint32_t before = 0;
-    for (int64_t i = tid; i < me; i += kCompactRows)
-        before += totals[i];
-    for (int d = 32; d > 0; d /= 2)
-        before += __shfl_xor(before, d);
-    const int64_t from = j < s.n_keep ? source_row(s, t, seg, j) : -1;
+    const int64_t blocks = (int64_t)s.B * s.H * s.blocks_per_seg;
+    const int64_t block = (int64_t)seg * s.blocks_per_seg + blockIdx.x / 4;
+    const int64_t to0 = (int64_t)seg * s.n_keep + j0;
+
+    // every wave looks at the rows, so that none waits for another's loads
+    const int64_t from = source_row(s, t, seg, j0 + lane);
     const uint32_t word = from >= 0 ? t.in.flags[from] : 0u;
-    uint32_t scan = __popc(word);
-    for (int d = 1; d < 64; d *= 2) {
-        const uint32_t o = __shfl_up(scan, d);
-        scan += lane >= d ? o : 0u;
-    }
-    if (lane == 63)
-        red[1][wave] = scan;
+    const uint32_t src = from >= 0 ? t.in.row_off[from] : 0u;
+    if (wave == 0)
+        row_of[lane] = from;
+    uint32_t before = tid < (int)(blockIdx.x & 3) ? totals[blocks + 4 * block + tid] : 0u;
+    for (int64_t i = tid; i < block; i += kMoveThreads)
+        before += totals[i];
+    before = wave_total(before);
     if (lane == 0)
         red[0][wave] = before;
+    if (blockIdx.x == 0 && seg < s.H) {  // the head's count: its batch entries' rows
+        uint32_t c = 0;
+        for (int64_t i = tid; i < (int64_t)s.B * s.blocks_per_seg; i += kMoveThreads)
+            c += totals[(i / s.blocks_per_seg * s.H + seg) * s.blocks_per_seg + i % s.blocks_per_seg];
+        c = wave_total(c);
+        if (lane == 0)
+            red[1][wave] = c;
+    }
+    const uint32_t mine = __popc(word), scan = wave_scan(mine, lane), sum = (uint32_t)__builtin_amdgcn_readlane((int)scan, 63);
+    const bool listed = sum <= (uint32_t)kMoveList;
+    if (wave == 0 && listed)
+        for (uint32_t i = 0; i < mine; ++i)
+            list[scan - mine + i] = src + i;
     __syncthreads();
-    uint32_t at = scan - __popc(word);
-    for (int i = 0; i < kCompactRows / 64; ++i)
-        at += red[0][i] + (i < wave ? red[1][i] : 0u);
-    const int64_t to = (int64_t)seg * s.n_keep + j;
-    if (j < s.n_keep) {
-        t.out.flags[to] = word;
-        t.out.sigma[to] = from >= 0 ? t.in.sigma[from] : (uint16_t)0;
-        t.out.row_off[to] = at;
-        for (int i = 0; i < s.row_words; ++i)
-            t.out.codes[to * s.row_words + i] = from >= 0 ? t.in.codes[from * s.row_words + i] : 0u;
-        const uint32_t src = from >= 0 ? t.in.row_off[from] : 0u;
-        for (int i = 0; i < __popc(word); ++i) {
+    const uint32_t base = red[0][0] + red[0][1] + red[0][2] + red[0][3], at = base + scan - mine;
+    if (tid == 0 && blockIdx.x == 0 && seg < s.H)
+        t.out.n_outliers[seg] = red[1][0] + red[1][1] + red[1][2] + red[1][3];
+
+    for (int i = tid; i < n * s.row_words; i += kMoveThreads) {
+        const int r = i / s.row_words;
+        const int64_t row = row_of[r];
+        t.out.codes[to0 * s.row_words + i] = row >= 0 ? t.in.codes[row * s.row_words + (i - r * s.row_words)] : 0u;
+    }
+    const uint2 *pay = reinterpret_cast<const uint2 *>(t.in.outliers);
+    uint2 *out = reinterpret_cast<uint2 *>(t.out.outliers);
+    if (listed) {
+        for (uint32_t i = tid; i < sum; i += kMoveThreads) {
+            const uint64_t f = list[i], o = (uint64_t)base + i;
+            if (o < t.out_capacity)
+                out[o] = f < t.in_capacity ? pay[f] : make_uint2(0u, 0u);
+        }
+    } else {
+        for (uint32_t i = wave; i < mine; i += kMoveThreads / 64) {
             const uint64_t f = (uint64_t)src + i, o = (uint64_t)at + i;
             if (o < t.out_capacity)
-                reinterpret_cast<uint2 *>(t.out.outliers)[o] =
-                    f < t.in_capacity ? reinterpret_cast<const uint2 *>(t.in.outliers)[f] : make_uint2(0u, 0u);
+                out[o] = f < t.in_capacity ? pay[f] : make_uint2(0u, 0u);
         }
-        if (to == (int64_t)segs * s.n_keep - 1) {
-            const uint32_t total = at + __popc(word);
+    }
+    if (wave == 1 && lane < n) {
+        const int64_t to = to0 + lane;
+        t.out.flags[to] = word;
+        t.out.row_off[to] = at;
+        t.out.sigma[to] = from >= 0 ? t.in.sigma[from] : (uint16_t)0;
+        if (to == (int64_t)s.B * s.H * s.n_keep - 1) {
+            const uint32_t total = at + mine;
             t.out.row_off[to + 1] = total;
             t.out.n_outliers[s.H] = total;
             *t.out.status = *t.in.status | (total > t.out_capacity ? HQMQ_STATUS_OUTLIER_OVERFLOW : 0u);
         }
     }
-    if (blockIdx.x == 0 && seg < s.H) {  // the head's count: its batch entries' workgroups
-        uint32_t c = 0;
-        for (int b = 0; b < s.B; ++b)
-            for (int i = tid; i < s.blocks_per_seg; i += kCompactRows)
-                c += totals[((int64_t)b * s.H + seg) * s.blocks_per_seg + i];
-        for (int d = 32; d > 0; d /= 2)
-            c += __shfl_xor(c, d);
-        if (tid == 0)
-            base_s = 0;
-        __syncthreads();
-        if (lane == 0)
-            atomicAdd(&base_s, c);
-        __syncthreads();
-        if (tid == 0)
-            t.out.n_outliers[seg] = base_s;
-    }
 }
 
 hipError_t launch_evict_compact(const CompactShape &s, const CompactBatch &batch, int n_tensors, hipStream_t stream)
 {
-    const dim3 grid((unsigned)s.blocks_per_seg, (unsigned)(s.B * s.H), (unsigned)n_tensors);
-    hipLaunchKernelGGL(k_compact_count, grid, dim3(kCompactRows), 0, stream, s, batch);
+    hipLaunchKernelGGL(k_compact_count, dim3((unsigned)s.blocks_per_seg, (unsigned)(s.B * s.H), (unsigned)n_tensors), dim3(kCompactRows), 0, stream, s, batch);
     hipError_t err = hipGetLastError();
     if (err != hipSuccess)
         return err;
-    hipLaunchKernelGGL(k_compact_move, grid, dim3(kCompactRows), 0, stream, s, batch);
+    const dim3 grid((unsigned)((s.n_keep + kMoveRows - 1) / kMoveRows), (unsigned)(s.B * s.H), (unsigned)n_tensors);
+    hipLaunchKernelGGL(k_compact_move, grid, dim3(kMoveThreads), 0, stream, s, batch);
     return hipGetLastError();
 }
 

@@ -47,7 +47,8 @@ struct SelectArgs {
     float *kept_mass;
     int32_t B, H, T, n_sink, n_recent, n_keep;
 };
-hipError_t launch_evict_select(const SelectArgs &a, hipStream_t stream);
+uint64_t evict_select_workspace_bytes(int B, int H, int T);
+hipError_t launch_evict_select(const SelectArgs &a, uint32_t *workspace, hipStream_t stream);
 
 struct CompactTensor {
     EncodedPtrs in, out;
@@ -60,8 +61,8 @@ struct CompactBatch {
 };
 struct CompactShape {
     int32_t B, H, T, n_keep, row_words;
-    int32_t blocks_per_seg;  // workgroups per (b, h), of kCompactRows rows each
-    uint32_t *totals;        // [tensor][B * H * blocks_per_seg] outliers per workgroup
+    int32_t blocks_per_seg;  // per (b, h), of kCompactRows rows each
+    uint32_t *totals;        // [tensor]: outliers of each block [B * H * blocks_per_seg], of each quarter of one [4 * B * H * blocks_per_seg]
     uint64_t totals_stride;  // of a tensor, in entries
 };
 constexpr int kCompactRows = 256;

@@ -396,6 +396,14 @@ def test_select_ragged(kind):
     _select(_values(kind, (3, 2, 20000), 4), 3000, 4, 100, [20000, 2999, 9000])
 
 
+@pytest.mark.parametrize("kind", ["spread", "ties", "odd", "zeros", "equal"])
+@pytest.mark.parametrize("n_keep,n_sink,n_recent", [(3000, 4, 100), (36000, 0, 1), (1, 0, 0)])
+def test_select_ragged_long(kind, n_keep, n_sink, n_recent):
+    """Heads that several workgroups share: lengths that end in the first of them, between two, and that keep everything."""
+    lengths = [40000, 33000, 8192, 8193, 100, 0, 3000]
+    _select(_values(kind, (len(lengths), 2, 40000), 5), n_keep, n_sink, n_recent, lengths)
+
+
 def test_select_many_heads():
     _select(_values("spread", (40, 32, 257), 9), 64, 4, 16)
 
