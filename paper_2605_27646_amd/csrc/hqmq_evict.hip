@@ -519,15 +519,28 @@ __global__ __launch_bounds__(kMoveThreads) void k_compact_move(CompactShape s, C
     const int64_t block = (int64_t)seg * s.blocks_per_seg + blockIdx.x / 4;
     const int64_t to0 = (int64_t)seg * s.n_keep + j0;
 
-    // every wave looks at the rows, so that none waits for another's loads
+    // every wave looks at the rows, so that none waits for another's loads; the code words are on their way before flags and counts are
+    // looked at
     const int64_t from = source_row(s, t, seg, j0 + lane);
-    const uint32_t word = from >= 0 ? t.in.flags[from] : 0u;
-    const uint32_t src = from >= 0 ? t.in.row_off[from] : 0u;
     if (wave == 0)
         row_of[lane] = from;
+    const uint32_t word = from >= 0 ? t.in.flags[from] : 0u;
+    const uint32_t src = from >= 0 ? t.in.row_off[from] : 0u;
+    const uint16_t sigma = from >= 0 ? t.in.sigma[from] : (uint16_t)0;
     uint32_t before = tid < (int)(blockIdx.x & 3) ? totals[blocks + 4 * block + tid] : 0u;
     for (int64_t i = tid; i < block; i += kMoveThreads)
         before += totals[i];
+    __syncthreads();
+    constexpr int kWords = (kMoveRows * 24 + kMoveThreads - 1) / kMoveThreads;  // of a thread: a row has 24 at most
+    const int n_words = n * s.row_words;
+    uint32_t code[kWords];
+#pragma unroll
+    for (int u = 0; u < kWords; ++u) {
+        const int i = min(tid + kMoveThreads * u, n_words - 1), r = i / s.row_words;
+        const int64_t row = row_of[r];
+        code[u] = t.in.codes[max(row, (int64_t)0) * s.row_words + (i - r * s.row_words)];
+        code[u] = row >= 0 ? code[u] : 0u;
+    }
     before = wave_total(before);
     if (lane == 0)
         red[0][wave] = before;
@@ -549,11 +562,10 @@ __global__ __launch_bounds__(kMoveThreads) void k_compact_move(CompactShape s, C
     if (tid == 0 && blockIdx.x == 0 && seg < s.H)
         t.out.n_outliers[seg] = red[1][0] + red[1][1] + red[1][2] + red[1][3];
 
-    for (int i = tid; i < n * s.row_words; i += kMoveThreads) {
-        const int r = i / s.row_words;
-        const int64_t row = row_of[r];
-        t.out.codes[to0 * s.row_words + i] = row >= 0 ? t.in.codes[row * s.row_words + (i - r * s.row_words)] : 0u;
-    }
+#pragma unroll
+    for (int u = 0; u < kWords; ++u)
+        if (tid + kMoveThreads * u < n_words)
+            t.out.codes[to0 * s.row_words + tid + kMoveThreads * u] = code[u];
     const uint2 *pay = reinterpret_cast<const uint2 *>(t.in.outliers);
     uint2 *out = reinterpret_cast<uint2 *>(t.out.outliers);
     if (listed) {
@@ -573,7 +585,7 @@ __global__ __launch_bounds__(kMoveThreads) void k_compact_move(CompactShape s, C
         const int64_t to = to0 + lane;
         t.out.flags[to] = word;
         t.out.row_off[to] = at;
-        t.out.sigma[to] = from >= 0 ? t.in.sigma[from] : (uint16_t)0;
+        t.out.sigma[to] = sigma;
         if (to == (int64_t)s.B * s.H * s.n_keep - 1) {
             const uint32_t total = at + mine;
             t.out.row_off[to + 1] = total;
