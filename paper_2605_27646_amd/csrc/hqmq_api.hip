@@ -1094,7 +1094,7 @@ extern "C" int32_t hqmq_attend_mass(const hqmq_params *params, int32_t n_share, 
     a.visible = visible_dev;
     a.mass_in = decay != 0.f ? mass_in_dev : nullptr;
     a.mass_out = mass_out_dev;
-    a.qscale = scale * 1.44269504088896340736f;
+    a.scale = scale;
     a.decay = decay;
     a.G = n_q_heads / params->H;
     a.n_share = n_share;

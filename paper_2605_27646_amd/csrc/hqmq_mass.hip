@@ -5,6 +5,9 @@
 // kM half + kM - 1), which is the operand of v_mfma_f32_32x32x16_f16 as it stands and stays in registers while the query rows go past
 // in blocks of 32 from LDS.  With the rows as the other operand a lane receives the scores of one token, so that their weights are
 // summed in it, in one fixed order.
+//
+// The exponent is fma(score, scale, -lse), small wherever the weight is not, and only then taken to base 2: with log2 e inside the scale
+// and inside lse, each rounded once, the weights of a row whose scores are near 50 were off by 1e-6, the same way in all of them.
 #include "hqmq_packed.h"
 
 namespace hqmq {
@@ -14,6 +17,7 @@ namespace {
 constexpr int kMassWaves = 16, kMassThreads = 64 * kMassWaves;
 constexpr int kMassRows = 128;   // query rows in LDS at a time
 constexpr int kMassPay = 64;     // outlier payloads of a wave's 32 tokens kept in LDS
+constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kNoRow = 1.0e30f;  // the lse of a row that is not there or saw nothing: its weights are zeros
 
 // A wave's packed rows in LDS, in words: code words (room for the largest w) | flags, scales, places in the outlier list's window |
@@ -33,7 +37,7 @@ __global__ __launch_bounds__(kMassThreads, 4) void k_mass(Geometry g, MassArgs a
     constexpr int kD = 4 * kNc, kM = kNc / 2, kQPitch = kD + 8;
     extern __shared__ __align__(16) float lds[];
     _Float16 *queries = reinterpret_cast<_Float16 *>(lds + kLutFloats + direction_floats<kTable>(g.S));  // [kMassRows][kQPitch]
-    float *row_lse = reinterpret_cast<float *>(queries + kMassRows * kQPitch);                           // [kMassRows], log2 domain
+    float *row_lse = reinterpret_cast<float *>(queries + kMassRows * kQPitch);                           // [kMassRows]
     int *row_vis = reinterpret_cast<int *>(row_lse + kMassRows);                                         // [kMassRows]
     uint32_t *stages = reinterpret_cast<uint32_t *>(row_vis + kMassRows);
 
@@ -44,10 +48,10 @@ __global__ __launch_bounds__(kMassThreads, 4) void k_mass(Geometry g, MassArgs a
     uint32_t *mine = stages + wave * Stage::total;
     const uint2 *pays = reinterpret_cast<const uint2 *>(mine + Stage::pays);
     const int n_rows = a.n_share * a.G, n_groups = (n_rows + kMassRows - 1) / kMassRows;
-    const float qscale = fabsf(a.qscale);  // a negative scale goes into the queries' signs
+    const float scale = fabsf(a.scale);  // a negative scale goes into the queries' signs
 
     const auto load_rows = [&](int group) {
-        const uint32_t flip = a.qscale < 0.f ? 0x80008000u : 0u;
+        const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
         const int first = group * kMassRows, n = min(n_rows - first, kMassRows);
         const auto head_of = [&](int r) {
             const int m = (first + r) / a.G;
@@ -68,7 +72,7 @@ __global__ __launch_bounds__(kMassThreads, 4) void k_mass(Geometry g, MassArgs a
             float lse = kNoRow;
             int vis = g.T;
             if (tid < n) {
-                lse = a.lse[head_of(tid)] * 1.44269504088896340736f;
+                lse = a.lse[head_of(tid)];
                 lse = lse < -kNoRow ? kNoRow : lse;  // minus infinity: the row saw nothing
                 if (a.visible)
                     vis = a.visible[head_of(tid)];
@@ -200,13 +204,13 @@ __global__ __launch_bounds__(kMassThreads, 4) void k_mass(Geometry g, MassArgs a
                 if (!a.visible) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        sum += __builtin_amdgcn_exp2f(fmaf(sc[4 * i + e], qscale, -lse[e]));
+                        sum += __builtin_amdgcn_exp2f(kLog2e * fmaf(sc[4 * i + e], scale, -lse[e]));
                 } else {
                     const int4 vis = *reinterpret_cast<const int4 *>(row_vis + r0 + 8 * i + 4 * half);
                     const int v[4] = {vis.x, vis.y, vis.z, vis.w};
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const float p = __builtin_amdgcn_exp2f(fmaf(sc[4 * i + e], qscale, -lse[e]));
+                        const float p = __builtin_amdgcn_exp2f(kLog2e * fmaf(sc[4 * i + e], scale, -lse[e]));
                         sum += t < v[e] ? p : 0.f;
                     }
                 }

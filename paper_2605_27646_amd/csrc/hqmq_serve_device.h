@@ -34,7 +34,7 @@ struct MassArgs {
     const int32_t *visible;
     const float *mass_in;    // null: decay is 0
     float *mass_out;
-    float qscale, decay;
+    float scale, decay;
     int32_t G, n_share;
 };
 hipError_t prepare_mass_kernels();  // once per device, before the first launch_mass on it
@@ -67,40 +67,5 @@ struct CompactShape {
 };
 constexpr int kCompactRows = 256;
 hipError_t launch_evict_compact(const CompactShape &s, const CompactBatch &batch, int n_tensors, hipStream_t stream);
-
-// Chunk c of a packed row as the decode returns it, straight from memory.  sec: the head's secondaries [S][4].
-__device__ __forceinline__ uint2 chunk_from_memory(const Geometry &g, const AttendSide &s, const float *sec, int64_t row, int c)
-{
-    const uint32_t word = s.flags[row];
-    if ((word >> c) & 1u) {
-        const uint64_t at = (uint64_t)s.row_off[row] + __popc(word & ((1u << c) - 1u));
-        return at < s.outlier_capacity ? reinterpret_cast<const uint2 *>(s.outliers)[at] : make_uint2(0u, 0u);
-    }
-    const uint32_t bit = (uint32_t)(c * g.w);
-    const uint32_t *rw = s.codes + row * g.row_words;
-    const uint32_t d0 = rw[bit >> 5], d1 = rw[min((int)(bit >> 5) + 1, g.row_words - 1)];
-    const uint32_t code = __builtin_amdgcn_alignbit(d1, d0, bit & 31u) & ((1u << g.w) - 1u);
-    const uint32_t k = code & ((1u << g.w_idx) - 1u), p = k / (uint32_t)g.S, si = k - p * (uint32_t)g.S;
-    float P[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        P[i] = p < 8u ? ((p >> 1) == (uint32_t)i ? ((p & 1u) ? -1.f : 1.f) : 0.f)
-                      : (p < 24u ? ((((p - 8u) >> (3 - i)) & 1u) ? -0.5f : 0.5f) : 0.f);
-    const float4_t q = *reinterpret_cast<const float4_t *>(sec + 4 * si);
-    const float r = (float)(code >> g.w_idx) * ((float)__builtin_bit_cast(_Float16, s.sigma[row]) * g.inv_L);
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        P[i] *= r;
-    float y[4];
-    y[0] = fmaf(-P[3], q[3], fmaf(-P[2], q[2], fmaf(-P[1], q[1], P[0] * q[0])));
-    y[1] = fmaf(-P[3], q[2], fmaf(P[2], q[3], fmaf(P[1], q[0], P[0] * q[1])));
-    y[2] = fmaf(P[3], q[1], fmaf(P[2], q[0], fmaf(-P[1], q[3], P[0] * q[2])));
-    y[3] = fmaf(P[3], q[0], fmaf(-P[2], q[1], fmaf(P[1], q[2], P[0] * q[3])));
-    half4_t out;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        out[i] = (_Float16)fminf(fmaxf(y[i], -65504.f), 65504.f);
-    return __builtin_bit_cast(uint2, out);
-}
 
 }  // namespace hqmq

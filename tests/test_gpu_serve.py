@@ -296,6 +296,29 @@ def test_mass_states(kw, M):
     _mass(7900 + M, 2, M, 2, 4, 333, 128, 64, **kw)
 
 
+@pytest.mark.parametrize("scale", [0.088, -0.125])
+def test_mass_of_high_scores(scale):
+    """Scores near 1000 and an lse beside them: a weight is off by the roundings of z = score - lse, not of the two.  With one
+    element per query row the scores are exact, fma(score, scale, -lse) is off by 2^-24 |z|, its product with log2 e by 2^-24 |z|
+    twice over (the constant, the product), and exp2 by 2^-22 of the weight."""
+    H, T, D, d, c = 2, 700, 64, 5, 8192.0
+    sk, _ = _secs(11, H, 64)
+    k = Cache(71, 1, H, T, D, sk)
+    K = k.decoded()
+    scale = float(np.float32(scale))
+    q = torch.zeros(1, H, D, dtype=torch.float16)
+    q[..., d] = c
+    s = scale * c * K.hat[0, :, :, d].astype(np.float64)
+    lse = s.max(-1).astype(np.float32)
+    assert (lse > 500).all()
+    out = torch.empty(1, H, T, device=DEV)
+    hq.hqmq_attend_mass(k.params, q.to(DEV), scale, k.bufs, k.sec, torch.from_numpy(lse)[None].to(DEV), None, decay=0.0, out=out)
+    z = s - lse.astype(np.float64)[:, None]
+    want, sure = np.exp(z), K.slack[0, :, :, d] == 0
+    err, bound = np.abs(out.cpu().numpy()[0] - want), (3 * 2.0 ** -24 * np.abs(z) + 2.0 ** -22) * want * 1.01 + 2.0 ** -126
+    assert sure.any() and (err <= bound)[sure].all(), (err[sure].max(), np.argwhere(sure & (err > bound))[:5])
+
+
 def test_mass_sums_to_the_rows():
     """With the lse that the attention returned, every query row's weights sum to one."""
     B, M, H, G, T, S = 1, 6, 2, 4, 900, 64
