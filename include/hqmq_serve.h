@@ -103,7 +103,7 @@ int32_t hqmq_attend_mass(const hqmq_params *params, int32_t n_share, int32_t n_q
  *   n_kept_dev  DEVICE, out, int32 [B][H]: min(length, n_keep).
  *   kept_mass_dev  DEVICE, out, fp32 [B][H][n_keep]: their mass, 0 behind the last; or NULL.
  *   workspace_dev  DEVICE, 256-byte aligned, hqmq_evict_select_workspace_bytes() bytes; may be NULL if that is 0.
- * Errors: INVALID_ARG, UNSUPPORTED (B * H above 65535, B * H * T at 2^32 or above), BUFFER_TOO_SMALL, HIP. */
+ * Errors: INVALID_ARG, UNSUPPORTED (B * H above 65535, T above 2^30, B * H * T at 2^32 or above), BUFFER_TOO_SMALL, HIP. */
 int32_t hqmq_evict_select(int32_t B, int32_t H, int32_t T, const float *mass_dev, const int32_t *length_dev,
                           int32_t n_sink, int32_t n_recent, int32_t n_keep, int32_t *keep_dev, int32_t *n_kept_dev,
                           float *kept_mass_dev, void *workspace_dev, uint64_t workspace_bytes, void *stream);

@@ -1106,7 +1106,7 @@ static int32_t check_select(int32_t B, int32_t H, int32_t T, int32_t n_keep)
 {
     if (B <= 0 || H <= 0 || T <= 0 || n_keep <= 0 || n_keep > T)
         return HQMQ_ERR_INVALID_ARG;
-    if ((int64_t)B * H > 65535 || (uint64_t)B * H * T >= (1ull << 32))
+    if ((int64_t)B * H > 65535 || T > (1 << 30) || (uint64_t)B * H * T >= (1ull << 32))
         return HQMQ_ERR_UNSUPPORTED;
     return HQMQ_OK;
 }
@@ -1174,7 +1174,8 @@ static CompactShape compact_shape(const hqmq_params *params, int32_t n_keep)
     s.row_words = g.row_words;
     s.blocks_per_seg = (n_keep + kCompactRows - 1) / kCompactRows;
     s.totals = nullptr;
-    s.totals_stride = align_up(5ull * g.B * g.H * s.blocks_per_seg, 64);
+    const uint64_t blocks = (uint64_t)g.B * g.H * s.blocks_per_seg;
+    s.totals_stride = align_up(5ull * blocks + (blocks + kCompactGroup - 1) / kCompactGroup, 64);
     return s;
 }
 

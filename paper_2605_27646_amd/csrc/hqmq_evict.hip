@@ -81,7 +81,7 @@ __device__ __forceinline__ void count_digit(const Keys<kPer> &k, uint32_t prefix
         const uint32_t its = (uint32_t)__builtin_amdgcn_readlane((int)bin_of(k.key[0]), l);
         return __popcll(ballot(counts(k.key[0]) && bin_of(k.key[0]) == its)) >= 16;
     };
-    if (kPer == 1 || common(0) || common(21) || common(42)) {
+    if (common(0) || common(21) || common(42)) {
 #pragma unroll
         for (int j = 0; j < kPer; ++j) {
             const uint32_t bin = bin_of(k.key[j]);
@@ -268,18 +268,21 @@ __global__ __launch_bounds__(kThreads) void k_evict_select(SelectArgs a)
                a.kept_mass ? reinterpret_cast<uint32_t *>(a.kept_mass) + seg * a.n_keep : nullptr, lane);
 }
 
-// Longer heads are shared by workgroups of kPart tokens, in four launches: the histogram of each digit, left in the workspace for the next
-// launch to sum, and the places.  Every workgroup finds the last digit for itself, which saves a launch per digit.
-constexpr int kPartThreads = 1024, kPartPer = 8, kPart = kPartThreads * kPartPer;
+// Longer heads are shared by workgroups in four launches: the histogram of each digit, left in the workspace for the next launch to sum,
+// and the places.  Every workgroup finds the last digit for itself, which saves a launch per digit.  A workgroup takes 8192 tokens, or
+// several times as many where more than kMostSelectParts would share a head: each reads the histograms of all of them.
+constexpr int kPartThreads = 1024, kPartPer = 8, kPart = kPartThreads * kPartPer, kMostSelectParts = 64;
 constexpr int kDigitBits[3] = {kDigit0, kDigit1, kDigit2}, kDigitShift[3] = {32 - kDigit0, kDigit2, 0};
 // A workspace, in 32-bit words: histograms of the three digits [segs][parts][bins], and what the first two left [2][segs][4]:
 // prefix, rank in its last bin, whether the search ended there.
 struct PartLayout {
     uint64_t hist[3], state[2], total;
-    int parts;
+    int parts, loads;  // workgroups of a head, kPart tokens that each takes in turn
     __host__ __device__ PartLayout(int64_t segs, int T)
     {
-        parts = (T + kPart - 1) / kPart;
+        const int all = (T + kPart - 1) / kPart;
+        loads = (all + kMostSelectParts - 1) / kMostSelectParts;
+        parts = (all + loads - 1) / loads;
         uint64_t at = 0;
         const int bits[3] = {kDigit0, kDigit1, kDigit2};
         for (int d = 0; d < 3; ++d) {
@@ -309,8 +312,9 @@ __global__ __launch_bounds__(kPartThreads) void k_evict_select_part(SelectArgs a
     const bool all = head.len <= a.n_keep;  // kept whole: nothing to find
     if (kStep < 3 && all)
         return;
+    const int first = part * l.loads * kPart;
     Keys<kPartPer> k;
-    k.load(head, part * kPart, wave, lane);
+    k.load(head, first, wave, lane);
 
     uint32_t prefix = 0u, rank = (uint32_t)n;
     bool done = false;
@@ -357,6 +361,10 @@ __global__ __launch_bounds__(kPartThreads) void k_evict_select_part(SelectArgs a
             hist[i] = 0u;
         __syncthreads();
         count_digit<kDigitShift[kStep], kDigitBits[kStep]>(k, prefix, hist, lane);
+        for (int i = 1; i < l.loads; ++i) {
+            k.load(head, first + i * kPart, wave, lane);
+            count_digit<kDigitShift[kStep], kDigitBits[kStep]>(k, prefix, hist, lane);
+        }
         __syncthreads();
         uint32_t *h = ws + l.hist[kStep] + (seg * l.parts + part) * kBins;
         for (int i = tid; i < kBins; i += kPartThreads)
@@ -386,7 +394,7 @@ __global__ __launch_bounds__(kPartThreads) void k_evict_select_part(SelectArgs a
         uint32_t above = 0u, equal = 0u;
         if (all) {
             if (tid == 0)
-                above = (uint32_t)min(part * kPart, head.len);
+                above = (uint32_t)min(first, head.len);
         } else {
             uint32_t path = prefix;
             for (int d = digits - 1; d >= 0; --d) {
@@ -416,20 +424,28 @@ __global__ __launch_bounds__(kPartThreads) void k_evict_select_part(SelectArgs a
             above_before += wave_sum[0][i];
             equal_before += wave_sum[1][i];
         }
-        above = equal = 0u;  // of the wave
-        count_kept(k, last, ties, above, equal);
-        __syncthreads();
-        if (lane == 0) {
-            wave_sum[0][wave] = above;
-            wave_sum[1][wave] = equal;
+        for (int x = 0; x < l.loads; ++x) {
+            if (x > 0)
+                k.load(head, first + x * kPart, wave, lane);
+            above = equal = 0u;  // of the wave
+            count_kept(k, last, ties, above, equal);
+            __syncthreads();
+            if (lane == 0) {
+                wave_sum[0][wave] = above;
+                wave_sum[1][wave] = equal;
+            }
+            __syncthreads();
+            uint32_t above_here = above_before, equal_here = equal_before;  // of what comes before the wave's tokens
+            for (int i = 0; i < kWaves; ++i) {
+                const uint32_t more = wave_sum[0][i], same = wave_sum[1][i];
+                above_here += i < wave ? more : 0u;
+                equal_here += i < wave ? same : 0u;
+                above_before += more;
+                equal_before += same;
+            }
+            place_keys(k, last, ties, above_here + min(equal_here, ties), equal_here, head, a.keep + seg * a.n_keep,
+                       a.kept_mass ? reinterpret_cast<uint32_t *>(a.kept_mass) + seg * a.n_keep : nullptr, lane);
         }
-        __syncthreads();
-        for (int i = 0; i < wave; ++i) {
-            above_before += wave_sum[0][i];
-            equal_before += wave_sum[1][i];
-        }
-        place_keys(k, last, ties, above_before + min(equal_before, ties), equal_before, head, a.keep + seg * a.n_keep,
-                   a.kept_mass ? reinterpret_cast<uint32_t *>(a.kept_mass) + seg * a.n_keep : nullptr, lane);
     }
 }
 
@@ -445,7 +461,7 @@ hipError_t launch_evict_select(const SelectArgs &a, uint32_t *workspace, hipStre
 {
     const dim3 grid((unsigned)(a.B * a.H));
     if (select_in_parts(a.T)) {
-        const dim3 parts((unsigned)((a.T + kPart - 1) / kPart), (unsigned)(a.B * a.H));
+        const dim3 parts((unsigned)PartLayout((int64_t)a.B * a.H, a.T).parts, (unsigned)(a.B * a.H));
         hipLaunchKernelGGL(k_evict_select_part<0>, parts, dim3(kPartThreads), 0, stream, a, workspace);
         hipLaunchKernelGGL(k_evict_select_part<1>, parts, dim3(kPartThreads), 0, stream, a, workspace);
         hipLaunchKernelGGL(k_evict_select_part<2>, parts, dim3(kPartThreads), 0, stream, a, workspace);
@@ -464,8 +480,9 @@ hipError_t launch_evict_select(const SelectArgs &a, uint32_t *workspace, hipStre
 }
 
 // ---- compaction ------------------------------------------------------------------------------------------------------------------
-// A launch counts the outliers of every 64 and every 256 kept rows; in the next a workgroup takes 64 rows, sums what comes before them,
-// and moves code words and payloads lane by lane along the new tensor, so that they are written in whole lines.
+// A launch counts the outliers of every 64 and every 256 kept rows; in the last a workgroup takes 64 rows, sums what comes before them
+// (where there are more than kCompactDirect counts, from a third launch's sums of kCompactGroup of them each), and moves code words and
+// payloads lane by lane along the new tensor, so that they are written in whole lines.
 // Bound by latency: the chain of loads from a kept index over its flags to its payloads, in each of the two launches.
 
 namespace {
@@ -507,6 +524,24 @@ __global__ __launch_bounds__(kCompactRows) void k_compact_count(CompactShape s, 
         totals[blocks + 4 * block + threadIdx.x] = sub[threadIdx.x];
 }
 
+// groups[i]: the outliers of kCompactGroup blocks.
+__global__ __launch_bounds__(kMoveThreads) void k_compact_groups(CompactShape s)
+{
+    __shared__ uint32_t red[kMoveThreads / 64];
+    const int tid = threadIdx.x;
+    const int64_t blocks = (int64_t)s.B * s.H * s.blocks_per_seg, first = (int64_t)blockIdx.x * kCompactGroup;
+    uint32_t *totals = s.totals + blockIdx.y * s.totals_stride;
+    uint32_t c = 0u;
+    for (int64_t i = first + tid; i < min(first + kCompactGroup, blocks); i += kMoveThreads)
+        c += totals[i];
+    c = wave_total(c);
+    if ((tid & 63) == 0)
+        red[tid >> 6] = c;
+    __syncthreads();
+    if (tid == 0)
+        totals[5 * blocks + blockIdx.x] = red[0] + red[1] + red[2] + red[3];
+}
+
 __global__ __launch_bounds__(kMoveThreads) void k_compact_move(CompactShape s, CompactBatch batch)
 {
     __shared__ int64_t row_of[kMoveRows];
@@ -528,7 +563,10 @@ __global__ __launch_bounds__(kMoveThreads) void k_compact_move(CompactShape s, C
     const uint32_t src = from >= 0 ? t.in.row_off[from] : 0u;
     const uint16_t sigma = from >= 0 ? t.in.sigma[from] : (uint16_t)0;
     uint32_t before = tid < (int)(blockIdx.x & 3) ? totals[blocks + 4 * block + tid] : 0u;
-    for (int64_t i = tid; i < block; i += kMoveThreads)
+    const int64_t n_groups = blocks > kCompactDirect ? block / kCompactGroup : 0;
+    for (int64_t i = tid; i < n_groups; i += kMoveThreads)
+        before += totals[5 * blocks + i];
+    for (int64_t i = n_groups * kCompactGroup + tid; i < block; i += kMoveThreads)
         before += totals[i];
     __syncthreads();
     constexpr int kWords = (kMoveRows * 24 + kMoveThreads - 1) / kMoveThreads;  // of a thread: a row has 24 at most
@@ -601,6 +639,13 @@ hipError_t launch_evict_compact(const CompactShape &s, const CompactBatch &batch
     hipError_t err = hipGetLastError();
     if (err != hipSuccess)
         return err;
+    const int64_t blocks = (int64_t)s.B * s.H * s.blocks_per_seg;
+    if (blocks > kCompactDirect) {
+        hipLaunchKernelGGL(k_compact_groups, dim3((unsigned)((blocks + kCompactGroup - 1) / kCompactGroup), (unsigned)n_tensors), dim3(kMoveThreads), 0, stream, s);
+        err = hipGetLastError();
+        if (err != hipSuccess)
+            return err;
+    }
     const dim3 grid((unsigned)((s.n_keep + kMoveRows - 1) / kMoveRows), (unsigned)(s.B * s.H), (unsigned)n_tensors);
     hipLaunchKernelGGL(k_compact_move, grid, dim3(kMoveThreads), 0, stream, s, batch);
     return hipGetLastError();

@@ -87,7 +87,7 @@ __global__ __launch_bounds__(kMassThreads, 4) void k_mass(Geometry g, MassArgs a
     const int n_tiles = min((g.T + 31) / 32 - first_tile, tiles_per_split);
     const int64_t first_row = (int64_t)seg * g.T + 32 * (int64_t)first_tile;
     const uint32_t n_tok = (uint32_t)min(g.T - 32 * first_tile, 32 * tiles_per_split);
-    // Tokens past the last read as zeros (no flags, a scale of zero); every load is issued a tile's time before its value is needed.
+    // Tokens past the last read as zeros (no flags, a scale of zero) behind the last payload; every load is issued a tile's time before its value is needed.
     const rsrc_t codes = buffer_of(a.k.codes + first_row * row_words, n_tok * row_words);
     const rsrc_t flags_b = buffer_of(a.k.flags + first_row, n_tok);
     const rsrc_t scales = buffer_of(a.k.sigma + first_row, n_tok);
@@ -109,7 +109,7 @@ __global__ __launch_bounds__(kMassThreads, 4) void k_mass(Geometry g, MassArgs a
             cw[i] = __builtin_amdgcn_raw_buffer_load_b32(codes, code_at + 256u * i, 0, 0);
         fw = __builtin_amdgcn_raw_buffer_load_b32(flags_b, row_at, 0, 0);
         sg = __builtin_amdgcn_raw_buffer_load_b16(scales, row_at >> 1, 0, 0);
-        ro = __builtin_amdgcn_raw_buffer_load_b32(places, row_at, 0, 0);
+        ro = __builtin_amdgcn_raw_buffer_load_b32(places, min(row_at, 4u * n_tok), 0, 0);
         code_at += 4u * 32u * kMassWaves * row_words;
         row_at += 4u * 32u * kMassWaves;
         next_base = (uint32_t)__builtin_amdgcn_readlane((int)bounds, 0);

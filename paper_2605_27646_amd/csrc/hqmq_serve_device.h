@@ -62,10 +62,12 @@ struct CompactBatch {
 struct CompactShape {
     int32_t B, H, T, n_keep, row_words;
     int32_t blocks_per_seg;  // per (b, h), of kCompactRows rows each
-    uint32_t *totals;        // [tensor]: outliers of each block [B * H * blocks_per_seg], of each quarter of one [4 * B * H * blocks_per_seg]
+    uint32_t *totals;        // [tensor]: outliers of each block [B * H * blocks_per_seg], of each quarter of one [4 * B * H * blocks_per_seg],
+                             // and of kCompactGroup blocks each, if there are more than kCompactDirect
     uint64_t totals_stride;  // of a tensor, in entries
 };
 constexpr int kCompactRows = 256;
+constexpr int kCompactGroup = 1024, kCompactDirect = 4096;
 hipError_t launch_evict_compact(const CompactShape &s, const CompactBatch &batch, int n_tensors, hipStream_t stream);
 
 }  // namespace hqmq

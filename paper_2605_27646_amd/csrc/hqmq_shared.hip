@@ -153,7 +153,7 @@ __global__ __launch_bounds__(F::kThreads, F::kPerSimd) void k_shared(Geometry g,
 
     // ---- a tile's packed rows on their way to LDS ------------------------------------------------------------------------
     // Every load is issued a tile's time or more before its value is needed, and without a condition: tokens past the last read as
-    // zeros (no flags, a scale of zero).  The outlier list's bounds come a tile before rows and payloads.
+    // zeros (no flags, a scale of zero) behind the last payload.  The outlier list's bounds come a tile before rows and payloads.
     // Waves 0 and 1 look after K's rows and payloads, 2 and 3 after V's; all of them fetch code words of both.
     const bool of_v = (wave & 2) != 0, row_wave = (wave & 1) == 0;
     const uint32_t n_tok = (uint32_t)max(end - begin, 0);
@@ -183,7 +183,7 @@ __global__ __launch_bounds__(F::kThreads, F::kPerSimd) void k_shared(Geometry g,
         }
         fw = __builtin_amdgcn_raw_buffer_load_b32(flag_b, row_at, 0, 0);
         sg = __builtin_amdgcn_raw_buffer_load_b16(scale_b, row_at >> 1, 0, 0);
-        ro = __builtin_amdgcn_raw_buffer_load_b32(place_b, row_at, 0, 0);
+        ro = __builtin_amdgcn_raw_buffer_load_b32(place_b, min(row_at, 4u * n_tok), 0, 0);
         code_at += 4u * kTok * row_words;
         row_at += 4u * kTok;
         next_base = (uint32_t)__builtin_amdgcn_readlane((int)bounds, 0);

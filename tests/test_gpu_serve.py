@@ -210,6 +210,50 @@ def test_shared_outliers_and_ranges(M, Cmul, capacity, kgain, gain):
     _shared(5000 + M, 1, M, 2, 4, 321, 128, 64, 6, own=30, Cmul=Cmul, capacity=capacity, kgain=kgain, gain=gain)
 
 
+@pytest.mark.parametrize("M,own_T", [(2, 90), (2, 200), (140, 90), (40, 60)])
+def test_shared_ignores_what_nobody_sees(M, own_T):
+    """Payloads with NaN and infinities in tokens that no query head of a sequence sees, a sequence with NaN queries that sees
+    nothing: the result is the one of clean caches, to the bit."""
+    B, H, G, T, D, S = 1, 2, 4, 333, 128, 64
+    N = B * M
+    sk, sv = _secs(13, H, S)
+    k, v = (Cache(1400 + i, B, H, T, D, s, Cmul=1.2) for i, s in enumerate((sk, sv)))
+    ok, ov = (Cache(1410 + i, N, H, own_T, D, s, Cmul=1.2) for i, s in enumerate((sk, sv)))
+    q = torch.randn(N, H * G, D, generator=_gen(1420)).to(torch.float16).to(DEV)
+    most = 217  # of the prefix, by every query head of every sequence but the first, which sees nothing at all
+    visible = torch.full((N, H * G), most, dtype=torch.int32, device=DEV)
+    lengths = torch.randint(1, own_T - 3, (N, 1), generator=_gen(1430), dtype=torch.int32)
+    lengths[0] = 0
+    visible[0] = 0
+    own_visible = lengths.expand(N, H * G).contiguous().to(DEV)
+    ws = torch.empty(hq.hqmq_attend_shared_workspace_bytes(k.params, M, H * G, ok.params), dtype=torch.uint8, device=DEV)
+
+    def run():
+        out, lse = torch.full_like(q, float("nan")), torch.full((N, H * G), float("nan"), device=DEV)
+        hq.hqmq_attend_shared(k.params, q, D ** -0.5, k.bufs, k.sec, v.bufs, v.sec, out, ws,
+                              own=hq.OwnTokens(ok.params, ok.bufs, ov.bufs, own_visible), visible=visible, lse=lse)
+        mass = torch.zeros(B, H, T, device=DEV)
+        hq.hqmq_attend_mass(k.params, q, D ** -0.5, k.bufs, k.sec, lse, mass, visible=visible)
+        torch.cuda.synchronize()
+        return out.view(torch.int16).cpu(), lse.cpu(), mass.cpu()
+
+    clean = run()
+    assert torch.isfinite(clean[0].view(torch.float16)).all() and not clean[0][0].any()
+    for c, limit in ((k, np.full(B, most)), (v, np.full(B, most)), (ok, lengths.numpy()[:, 0]), (ov, lengths.numpy()[:, 0])):
+        off = c.bufs.row_off.cpu().numpy().view(np.uint32)
+        pay = c.bufs.outliers.cpu().numpy().copy()
+        flat = pay.reshape(-1, 4)
+        for b in range(c.B):
+            for h in range(H):
+                r0 = (b * H + h) * c.T
+                flat[off[r0 + limit[b]]:off[r0 + c.T]] = [np.nan, np.inf, -np.inf, 1.0]
+        assert np.isnan(flat).any()
+        c.bufs.outliers.copy_(torch.from_numpy(pay))
+    q[0] = float("nan")
+    for got, want in zip(run(), clean):
+        assert torch.equal(got, want)
+
+
 def test_shared_long_prefix():
     _shared(6000, 1, 9, 1, 4, 20011, 128, 256)
     _shared(6100, 1, 70, 1, 4, 9001, 64, 192, 4, own=17, limits="ragged")
@@ -427,6 +471,12 @@ def test_select_ragged_long(kind, n_keep, n_sink, n_recent):
     _select(_values(kind, (len(lengths), 2, 40000), 5), n_keep, n_sink, n_recent, lengths)
 
 
+@pytest.mark.parametrize("kind", ["spread", "ties", "equal"])
+def test_select_many_tokens(kind):
+    """More tokens than 64 workgroups take in one piece each: three pieces, the last ones short or empty."""
+    _select(_values(kind, (3, 1, 1100003), 6), 5000, 4, 64, [1100003, 600000, 4999])
+
+
 def test_select_many_heads():
     _select(_values("spread", (40, 32, 257), 9), 64, 4, 16)
 
@@ -516,6 +566,12 @@ def test_compact(B, H, T, D, n_keep):
 ])
 def test_compact_states(kw):
     _compact(8500, 1, **{**dict(B=2, H=3, T=290, D=128, n_keep=120), **kw})
+
+
+def test_compact_many_heads():
+    """More counts than are summed directly: 4200 and 8400 blocks of 256 rows."""
+    _compact(8600, 2, 600, 7, 4, 64, 3, order="any")
+    _compact(8650, 1, 300, 14, 4, 64, 257, order="any")
 
 
 @pytest.mark.parametrize("n", [24, 25, 60])
