@@ -33,6 +33,14 @@ __device__ __forceinline__ uint32_t wave_scan(uint32_t v, int lane)  // inclusiv
     return v;
 }
 
+__device__ __forceinline__ uint32_t wave_total(uint32_t v)
+{
+#pragma unroll
+    for (int d = 32; d > 0; d /= 2)
+        v += __shfl_xor(v, d);
+    return v;
+}
+
 // The tokens of a head, and the keys of kThreads * kPer of them from `first` on: a wave has kPer * 64 in a row, lane by lane, so that it
 // reads whole lines and finds the places of what it keeps with ballots.
 struct Head {
@@ -57,26 +65,40 @@ template <int kPer>
 struct Keys {
     uint32_t key[kPer];
     int mine;  // the token of key[0]; key[j]'s is 64 j further
+    __device__ __forceinline__ bool any(const Head &h) const { return __builtin_amdgcn_readfirstlane(mine) < h.len; }  // in the wave
     __device__ __forceinline__ void load(const Head &h, int first, int wave, int lane)
     {
         mine = first + wave * kPer * 64 + lane;
 #pragma unroll
         for (int j = 0; j < kPer; ++j)
             key[j] = h.mass[min(mine + 64 * j, h.T - 1)];
+        // most waves: weights' sums, which are not negative, of tokens that are neither kept anyway nor missing
+        uint32_t most = key[0];
 #pragma unroll
-        for (int j = 0; j < kPer; ++j)
-            key[j] = h.key(mine + 64 * j, key[j]);
+        for (int j = 1; j < kPer; ++j)
+            most = max(most, key[j]);
+        const int from = first + wave * kPer * 64;
+        if (from >= h.lo && from + 64 * kPer <= h.hi && ballot(most > 0x7f800000u) == 0ull) {
+#pragma unroll
+            for (int j = 0; j < kPer; ++j)
+                key[j] += kZeroKey;
+        } else {
+#pragma unroll
+            for (int j = 0; j < kPer; ++j)
+                key[j] = h.key(mine + 64 * j, key[j]);
+        }
     }
 };
 
-// The keys' digit of kBits bits above kShift, of those that share the digits above it with prefix, added to hist in LDS.  Where a quarter of
-// a wave's first keys have one digit (a value that many tokens have would be added one by one: 32768 equal masses 100 us instead of 36), a
+// The keys' digit of kBits bits above kShift, of those that share the digits above it with prefix, added to hist in LDS.  (Keys of 0 too:
+// they are below every key that a rank can ask for.)  Where a quarter of
+// a wave's first keys have one digit (a value that many tokens have would be added one by one: 32768 equal masses 100 us instead of 34), a
 // wave adds the keys that have its first lane's digit at once.
 template <int kShift, int kBits, int kPer>
 __device__ __forceinline__ void count_digit(const Keys<kPer> &k, uint32_t prefix, uint32_t *hist, int lane)
 {
     const auto bin_of = [&](uint32_t x) { return (x >> kShift) & ((1u << kBits) - 1u); };
-    const auto counts = [&](uint32_t x) { return x != 0u && (kShift + kBits >= 32 || x >> ((kShift + kBits) & 31) == prefix); };
+    const auto counts = [&](uint32_t x) { return kShift + kBits >= 32 || x >> ((kShift + kBits) & 31) == prefix; };
     const auto common = [&](int l) {
         const uint32_t its = (uint32_t)__builtin_amdgcn_readlane((int)bin_of(k.key[0]), l);
         return __popcll(ballot(counts(k.key[0]) && bin_of(k.key[0]) == its)) >= 16;
@@ -196,7 +218,8 @@ __device__ __forceinline__ void fill_rest(const SelectArgs &a, int64_t seg, int 
 
 // A workgroup per (b, h), its keys in registers.  The key of the last token kept is found digit by digit from the top: a histogram in LDS of
 // the keys that share the digits found so far, and a scan of it.
-// Bound by latency: one workgroup's loads, three histograms and scans, and 0.5 us for every 1024 tokens.
+// Bound by latency and by what one compute unit loads and issues: 8 heads of 600 tokens 6.4 us, of 8192 10, of 32768 22 (0.5 us for every
+// 1024 tokens).
 template <int kThreads, int kPer>
 __global__ __launch_bounds__(kThreads) void k_evict_select(SelectArgs a)
 {
@@ -221,7 +244,8 @@ __global__ __launch_bounds__(kThreads) void k_evict_select(SelectArgs a)
             for (int i = tid; i < kBins; i += kThreads)
                 hist[i] = 0u;
             __syncthreads();
-            count_digit<kShift, kBits>(k, prefix, hist, lane);
+            if (k.any(head))
+                count_digit<kShift, kBits>(k, prefix, hist, lane);
             __syncthreads();
             uint32_t c[kEach];
             const int top = kBins - 1 - tid * kEach;
@@ -269,12 +293,21 @@ __global__ __launch_bounds__(kThreads) void k_evict_select(SelectArgs a)
 }
 
 // Longer heads are shared by workgroups in four launches: the histogram of each digit, left in the workspace for the next launch to sum,
-// and the places.  Every workgroup finds the last digit for itself, which saves a launch per digit.  A workgroup takes 8192 tokens, or
-// several times as many where more than kMostSelectParts would share a head: each reads the histograms of all of them.
+// and the places.  Every workgroup finds the last digit for itself, and, from the same counts, how many tokens the workgroups before it
+// keep: no launch of its own for either.  A workgroup takes 8192 tokens, or several times as many where more than kMostSelectParts would
+// share a head: each reads the histograms of all of them.
+// Bound by latency: four launches with a chain of loads each, of keys and of counts that another XCD wrote.  8 heads of 40000 tokens
+// 23.6 us, of 131072 28.5; 32 of 131072 45.7.
 constexpr int kPartThreads = 1024, kPartPer = 8, kPart = kPartThreads * kPartPer, kMostSelectParts = 64;
 constexpr int kDigitBits[3] = {kDigit0, kDigit1, kDigit2}, kDigitShift[3] = {32 - kDigit0, kDigit2, 0};
-// A workspace, in 32-bit words: histograms of the three digits [segs][parts][bins], and what the first two left [2][segs][4]:
-// prefix, rank in its last bin, whether the search ended there.
+// What the digits so far say.
+struct PartState {
+    uint32_t prefix, rank;   // the digits of the last key kept, its rank among the keys that have them
+    uint32_t digits, whole;  // how many; whether all keys with them are kept: no further digit then
+    uint32_t above;          // tokens with larger keys (whole: or these digits) in the workgroups before this one
+};
+// A workspace, in 32-bit words: histograms of the three digits [segs][parts][bins], and the PartState after the first two
+// [2][segs][parts][8].
 struct PartLayout {
     uint64_t hist[3], state[2], total;
     int parts, loads;  // workgroups of a head, kPart tokens that each takes in turn
@@ -291,7 +324,7 @@ struct PartLayout {
         }
         for (int d = 0; d < 2; ++d) {
             state[d] = at;
-            at += (uint64_t)segs * 4;
+            at += (uint64_t)segs * parts * 8;
         }
         total = at;
     }
@@ -316,54 +349,69 @@ __global__ __launch_bounds__(kPartThreads) void k_evict_select_part(SelectArgs a
     Keys<kPartPer> k;
     k.load(head, first, wave, lane);
 
-    uint32_t prefix = 0u, rank = (uint32_t)n;
-    bool done = false;
-    int digits = 0;  // found so far, their bins in prefix
-    if (kStep > 0 && !all) {
-        constexpr int kD = kStep - 1, kBins = 1 << kDigitBits[kD < 0 ? 0 : kD], kEach = kBins / kPartThreads;
-        if (kD > 0) {
-            const uint32_t *before = ws + l.state[kD > 0 ? kD - 1 : 0] + seg * 4;
-            prefix = before[0];
-            rank = before[1];
-            digits = (int)before[2];
-            done = before[3] != 0u;
-        }
-        if (!done) {
-            const uint32_t *h = ws + l.hist[kD < 0 ? 0 : kD] + seg * l.parts * kBins;
-            const int top = kBins - 1 - tid * kEach;
-            uint32_t c[kEach];
+    PartState st{0u, (uint32_t)n, 0u, 0u, 0u};
+    uint32_t equal_before = 0u;  // tokens with the last key itself in the workgroups before this one
+    if constexpr (kStep > 0) {
+        constexpr int kD = kStep - 1, kBins = 1 << kDigitBits[kD], kEach = kBins / kPartThreads;
+        typedef uint32_t bins_t __attribute__((ext_vector_type(kEach)));
+        if (kD > 0 && !all)
+            st = *reinterpret_cast<const PartState *>(ws + l.state[kD > 0 ? kD - 1 : 0] + (seg * l.parts + part) * 8);
+        if (!all && st.whole == 0u) {
+            const int low = kBins - kEach * (tid + 1);  // this thread's bins, the lowest of them
+            const uint32_t *h = ws + l.hist[kD] + seg * l.parts * kBins + low;
+            uint32_t c[kEach] = {}, before[kEach] = {};  // from the highest bin down: of all parts, of those before this one
+            for (int p = 0; p < l.parts; p += 8) {       // eight loads on their way at a time
+                bins_t x[8];
 #pragma unroll
-            for (int i = 0; i < kEach; ++i)
-                c[i] = 0u;
-            for (int p = 0; p < l.parts; ++p)
+                for (int u = 0; u < 8; ++u)
+                    x[u] = *reinterpret_cast<const bins_t *>(h + (int64_t)min(p + u, l.parts - 1) * kBins);
 #pragma unroll
-                for (int i = 0; i < kEach; ++i)
-                    c[i] += h[(int64_t)p * kBins + top - i];
-            find_bin<kPartThreads, kEach>(c, top, rank, wave_sum[0], found, wave, lane);
-            prefix = prefix << kDigitBits[kD < 0 ? 0 : kD] | found[0];
-            rank = found[1];
-            done = found[2] == rank || kD == 2;
-            digits = kD + 1;
+                for (int u = 0; u < 8; ++u)
+#pragma unroll
+                    for (int i = 0; i < kEach; ++i) {
+                        c[i] += p + u < l.parts ? x[u][kEach - 1 - i] : 0u;
+                        before[i] += p + u < part ? x[u][kEach - 1 - i] : 0u;
+                    }
+            }
+            find_bin<kPartThreads, kEach>(c, low + kEach - 1, st.rank, wave_sum[0], found, wave, lane);
+            st.prefix = st.prefix << kDigitBits[kD] | found[0];
+            st.rank = found[1];
+            st.digits = kD + 1;
+            st.whole = found[2] == found[1] ? 1u : 0u;
+            uint32_t above = 0u, same = 0u;
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+                const uint32_t bin = (uint32_t)(low + kEach - 1 - i);
+                above += bin > found[0] || (bin == found[0] && st.whole != 0u) ? before[i] : 0u;
+                same += bin == found[0] && st.whole == 0u ? before[i] : 0u;
+            }
+            above = wave_total(above);
+            same = wave_total(same);
+            if (lane == 0) {
+                wave_sum[0][wave] = above;
+                wave_sum[1][wave] = same;
+            }
+            __syncthreads();
+            for (int i = 0; i < kWaves; ++i) {
+                st.above += wave_sum[0][i];
+                equal_before += wave_sum[1][i];
+            }
         }
-        if (kD < 2 && part == 0 && tid == 0) {
-            uint32_t *after = ws + l.state[kD < 0 || kD > 1 ? 0 : kD] + seg * 4;
-            after[0] = prefix;
-            after[1] = rank;
-            after[2] = (uint32_t)digits;
-            after[3] = done ? 1u : 0u;
-        }
+        if (kStep < 3 && tid == 0)
+            *reinterpret_cast<PartState *>(ws + l.state[kD < 2 ? kD : 0] + (seg * l.parts + part) * 8) = st;
     }
     if constexpr (kStep < 3) {
-        if (done)
+        if (st.whole != 0u)
             return;
         constexpr int kBins = 1 << kDigitBits[kStep];
         for (int i = tid; i < kBins; i += kPartThreads)
             hist[i] = 0u;
         __syncthreads();
-        count_digit<kDigitShift[kStep], kDigitBits[kStep]>(k, prefix, hist, lane);
-        for (int i = 1; i < l.loads; ++i) {
-            k.load(head, first + i * kPart, wave, lane);
-            count_digit<kDigitShift[kStep], kDigitBits[kStep]>(k, prefix, hist, lane);
+        for (int x = 0; x < l.loads; ++x) {
+            if (x > 0)
+                k.load(head, first + x * kPart, wave, lane);
+            if (k.any(head))
+                count_digit<kDigitShift[kStep], kDigitBits[kStep]>(k, st.prefix, hist, lane);
         }
         __syncthreads();
         uint32_t *h = ws + l.hist[kStep] + (seg * l.parts + part) * kBins;
@@ -372,62 +420,22 @@ __global__ __launch_bounds__(kPartThreads) void k_evict_select_part(SelectArgs a
     } else {
         if (part == 0)
             fill_rest(a, seg, n, tid, kPartThreads);
-        // keys above `last` are kept, and of those equal to it the first `ties`; below the first digits' bins everything is one key
-        const int shift = digits == 1 ? kDigitShift[0] : digits == 2 ? kDigitShift[1] : kDigitShift[2];
-        // the last bin whole (or, of one key, as many as are kept: the search by rank ends there too)
-        uint32_t last = all ? 0u : prefix << shift, ties = 0u;
-        bool whole = false;
-        if (!all) {
-            // `done` with fewer than three digits, or with all of the third's keys kept: told apart by the rank
-            const int d = digits - 1, bins = 1 << (d == 0 ? kDigit0 : d == 1 ? kDigit1 : kDigit2);
-            const uint32_t *h = ws + l.hist[d] + seg * l.parts * bins + (prefix & (uint32_t)(bins - 1));
-            uint32_t its = 0u;
-            for (int p = 0; p < l.parts; ++p)
-                its += h[(int64_t)p * bins];
-            whole = its == rank;
-            if (whole)
+        // keys above `last` are kept, and of those equal to it the first `ties`
+        uint32_t last = 0u, ties = 0u;
+        if (all) {
+            st.above = (uint32_t)min(first, head.len);
+        } else {
+            last = st.prefix << (st.digits == 1u ? kDigitShift[0] : st.digits == 2u ? kDigitShift[1] : kDigitShift[2]);
+            if (st.whole != 0u)
                 last = max(last, 1u) - 1u;
             else
-                ties = rank;
+                ties = st.rank;
         }
-        // what the parts before this one keep, from their histograms
-        uint32_t above = 0u, equal = 0u;
-        if (all) {
-            if (tid == 0)
-                above = (uint32_t)min(first, head.len);
-        } else {
-            uint32_t path = prefix;
-            for (int d = digits - 1; d >= 0; --d) {
-                const int bits = d == 0 ? kDigit0 : d == 1 ? kDigit1 : kDigit2, bins = 1 << bits;
-                const uint32_t its = path & (uint32_t)(bins - 1);
-                path >>= bits;
-                const bool with_its = whole && d == digits - 1;
-                const uint32_t *h = ws + l.hist[d] + seg * l.parts * bins;
-                for (int p = 0; p < part; ++p)
-                    for (int i = tid; i < bins; i += kPartThreads) {
-                        const uint32_t c = h[(int64_t)p * bins + i];
-                        above += (uint32_t)i > its || (with_its && (uint32_t)i == its) ? c : 0u;
-                        equal += ties != 0u && d == digits - 1 && (uint32_t)i == its ? c : 0u;
-                    }
-            }
-        }
-        above = wave_scan(above, lane);
-        equal = wave_scan(equal, lane);
-        __syncthreads();
-        if (lane == 63) {
-            wave_sum[0][wave] = above;
-            wave_sum[1][wave] = equal;
-        }
-        __syncthreads();
-        uint32_t above_before = 0u, equal_before = 0u;
-        for (int i = 0; i < kWaves; ++i) {
-            above_before += wave_sum[0][i];
-            equal_before += wave_sum[1][i];
-        }
+        uint32_t above_before = st.above;
         for (int x = 0; x < l.loads; ++x) {
             if (x > 0)
                 k.load(head, first + x * kPart, wave, lane);
-            above = equal = 0u;  // of the wave
+            uint32_t above = 0u, equal = 0u;  // of the wave
             count_kept(k, last, ties, above, equal);
             __syncthreads();
             if (lane == 0) {
@@ -449,7 +457,7 @@ __global__ __launch_bounds__(kPartThreads) void k_evict_select_part(SelectArgs a
     }
 }
 
-// One workgroup takes a head of up to 32768 tokens, with as many waves as can share them, up to 16.
+// One workgroup takes a head of up to 32768 tokens, with as many waves as can share them, up to 16: there the two ways take the same time.
 static bool select_in_parts(int T) { return T > 1024 * 32; }
 
 uint64_t evict_select_workspace_bytes(int B, int H, int T)
@@ -496,13 +504,6 @@ __device__ __forceinline__ int64_t source_row(const CompactShape &s, const Compa
         return -1;
     const int k = t.keep[(int64_t)seg * s.n_keep + j];
     return k >= 0 && k < s.T ? (int64_t)seg * s.T + k : -1;
-}
-__device__ __forceinline__ uint32_t wave_total(uint32_t v)
-{
-#pragma unroll
-    for (int d = 32; d > 0; d /= 2)
-        v += __shfl_xor(v, d);
-    return v;
 }
 }  // namespace
 
