@@ -67,7 +67,9 @@ struct CompactShape {
     uint64_t totals_stride;  // of a tensor, in entries
 };
 constexpr int kCompactRows = 256;
-constexpr int kCompactGroup = 1024, kCompactDirect = 4096;
+// Summing the blocks before it costs a workgroup 1.7 us per 1000 of them, the launch that makes the groups 4.6 us (4096 blocks 56.9 us
+// without, 4104 with it 52.3).
+constexpr int kCompactGroup = 1024, kCompactDirect = 2560;
 hipError_t launch_evict_compact(const CompactShape &s, const CompactBatch &batch, int n_tensors, hipStream_t stream);
 
 }  // namespace hqmq
