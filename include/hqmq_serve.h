@@ -59,6 +59,9 @@ typedef struct hqmq_own_tokens {
  *               negative ones 0.
  *   own         HOST, or NULL: no tokens besides the prefix.
  *   out_dev     DEVICE, out, fp16 as q_dev.  A head that sees nothing gets zeros.
+ *               Tokens that no query head of their kv head sees (behind every limit) may hold anything, infinities and NaN
+ *               among their payloads included.  A token's V that some of them see is multiplied by the others' weight of zero:
+ *               it has to be finite for these to stay so.
  *   lse_dev     DEVICE, out, fp32 [B * n_share][n_q_heads], or NULL: M + ln(sum of e^{s - M}) over everything the
  *               head saw, -infinity where that is nothing.
  *   workspace_dev  DEVICE, 256-byte aligned, hqmq_attend_shared_workspace_bytes().

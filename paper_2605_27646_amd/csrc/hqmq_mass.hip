@@ -6,6 +6,10 @@
 // in blocks of 32 from LDS.  With the rows as the other operand a lane receives the scores of one token, so that their weights are
 // summed in it, in one fixed order.
 //
+// One pass over the keys; no wave waits for another but for the tables and the query rows.  Bound by latency for short caches (8 heads of
+// 777 tokens 6 us: launch, tables, one tile), by vector instructions for few rows (8 heads x 32768 x 128, 4 rows a head: 15.5 us, 25.6 MB at
+// 1.65 TB/s; most of them reconstruct) and by the exponentials for many (16 heads of 8001 tokens x 64, 128 rows: 11.5 us).
+//
 // The exponent is fma(score, scale, -lse), small wherever the weight is not, and only then taken to base 2: with log2 e inside the scale
 // and inside lse, each rounded once, the weights of a row whose scores are near 50 were off by 1e-6, the same way in all of them.
 #include "hqmq_packed.h"

@@ -1,5 +1,20 @@
 // Attention of many sequences over one packed prefix (include/hqmq_serve.h, hqmq_attend_shared): O = softmax(Q K^T scale) V
 // with the n_share * G query rows of a kv head against one reconstruction of its K and V.
+//
+// Both products are formed with the tokens as rows, S^T = K Q^T and O^T = V^T P^T: a lane then has scores of one query row, so that the
+// softmax's maximum and sum are the lane's own up to two swaps, and a block of weights, rounded, is the second product's operand as it
+// stands.  Reconstructed keys and values (transposed) go through LDS, where the waves of a workgroup share them.  Workgroups split the
+// prefix; sums and maxima of the splits, in fp32, are joined by the merge of hqmq_attend.
+//
+// What bounds it depends on the rows.  Up to 64 of them: the reconstruction, 40 vector instructions and some 60 cycles of LDS per 64 chunks
+// (8 heads x 32771 tokens x 64, 24 rows a head: 27 us, of which the products take 2; 64 heads x 2049 x 96, 12 rows: 24).  256 rows: the
+// products beside the softmax's exponentials and roundings, 8 heads x 32768 x 128 in 65 us or 530 TFLOP/s, where a large product of two
+// matrices would take 30.  Measured at 256 rows: two groups of four waves that reconstruct and multiply in turn 124 us, eight alike 104,
+// four that reconstruct for eight 86, and with a tile's weights computed between the last one's products and rows written in whole lines 64.
+// 64 columns per wave spill (247 us).
+//
+// The weights: fp16 pairs (22 bits) up to 64 rows, where the second product hardly shows; one fp16 (11 bits) for more, where it was
+// 13 us of 78.  Each weight is then off by 2^-11 of itself at most, either way, in a sum that is rounded to fp16.
 #include "hqmq_packed.h"
 
 namespace hqmq {
@@ -48,6 +63,8 @@ __device__ __forceinline__ int value_row(int c, int e) { return 32 * (c >> 3) + 
 // How a workgroup works: waves that multiply, query rows (columns) of each, tiles in LDS, waves per SIMD.  With one tile in LDS four
 // waves reconstruct a tile and then multiply it, and the workgroups that share a compute unit fill each other's waits; with two, four
 // waves more reconstruct the next tile while these multiply.
+// By rows of a kv head: 16 columns per wave and three workgroups per compute unit up to 64 (two per compute unit, which spills nothing:
+// 24 rows x 64 27.5 -> 30 us, 12 x 96 25.2 -> 26.6, 130 tokens 6.8 -> 6.2), 32 columns up to 128, two tiles and eight waves of them above.
 template <int kTakers_, int kCols_, int kBufs_, int kPerSimd_>
 struct Form {
     static constexpr int kTakers = kTakers_, kCols = kCols_, kBufs = kBufs_, kPerSimd = kPerSimd_;

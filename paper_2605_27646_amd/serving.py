@@ -66,12 +66,24 @@ def _share_of(params: HqmqParams, q: torch.Tensor) -> int:
     return q.shape[0] // params.B
 
 
+def _hold(params: HqmqParams, encs) -> None:
+    info = hqmq_sizes(params)
+    need = {"codes": info.code_bytes, "sigma": info.sigma_bytes, "flags": info.flag_bytes, "row_off": info.row_off_bytes,
+            "outliers": 0, "n_outliers": info.n_outliers_bytes, "status": info.status_bytes}
+    for e in encs:
+        for name, nbytes in need.items():
+            t = getattr(e, name)
+            if not t.is_contiguous() or t.numel() * t.element_size() < nbytes:
+                raise ValueError(f"{name} must be contiguous and hold {nbytes} bytes")
+
+
 class OwnTokens:
     """The packed tokens of every sequence's own, for hqmq_attend_shared: params (B = number of sequences), K and V, and how
     many of them each query head sees (int32 [n_seqs, n_q_heads]; None: all).  Built once, reusable while the buffers stay
     in place."""
 
     def __init__(self, params: HqmqParams, enc_k: EncodedBuffers, enc_v: EncodedBuffers, visible: torch.Tensor | None = None):
+        _hold(params, (enc_k, enc_v))
         self.params = params
         self.visible = visible
         self.keep = (enc_k, enc_v, enc_k.as_struct(), enc_v.as_struct())
@@ -103,7 +115,9 @@ def hqmq_attend_shared(params: HqmqParams, q: torch.Tensor, scale: float, enc_k:
                            ("the own tokens' visible", own.visible if own is not None else None, torch.int32)):
         if t is not None:
             _rows_of(name, t, dtype, rows)
-    _on_this_device(q, out, sec_k, sec_v, workspace, visible, lse, own.visible if own is not None else None, enc_k.codes, enc_v.codes)
+    _on_this_device(q, out, sec_k, sec_v, workspace, visible, lse, enc_k.codes, enc_v.codes)
+    if own is not None:
+        _on_this_device(own.visible, own.keep[0].codes, own.keep[1].codes)
     rc = _load().hqmq_attend_shared(C.byref(params), n_share, int(q.shape[1]), q.data_ptr(), float(scale),
                                     C.byref(enc_k.as_struct()), enc_k.outlier_capacity, sec_k.data_ptr(),
                                     C.byref(enc_v.as_struct()), enc_v.outlier_capacity, sec_v.data_ptr(),
@@ -196,16 +210,9 @@ class CompactBatch:
         for k in keeps:
             _rows_of("keep", k, torch.int32, (params.B, params.H, n_keep))
         for p, tensors in ((params, encs), (compacted_params(params, n_keep), outs)):
-            info = hqmq_sizes(p)
+            _hold(p, tensors)
             for e in tensors:
-                need = {"codes": info.code_bytes, "sigma": info.sigma_bytes, "flags": info.flag_bytes,
-                        "row_off": info.row_off_bytes, "outliers": 0, "n_outliers": info.n_outliers_bytes,
-                        "status": info.status_bytes}
-                for name, nbytes in need.items():
-                    t = getattr(e, name)
-                    if not t.is_contiguous() or t.numel() * t.element_size() < nbytes:
-                        raise ValueError(f"{name} must be contiguous and hold {nbytes} bytes")
-                    _on_this_device(t)
+                _on_this_device(e.codes, e.sigma, e.flags, e.row_off, e.outliers, e.n_outliers, e.status)
         _on_this_device(*keeps, workspace)
         if not workspace.is_contiguous():
             raise ValueError("workspace must be contiguous")

@@ -174,3 +174,18 @@ def test_binding_refuses_shapes():
         hq.hqmq_evict_select(m, 0, 0, torch.zeros(2, 3, 5, dtype=torch.int32), torch.zeros(2, 4, dtype=torch.int32))
     with pytest.raises(ValueError):
         hq.CompactBatch(p, [], [], [], torch.zeros(1))
+
+
+def test_select_refuses_too_many_tokens(lib):
+    assert lib.hqmq_evict_select(1, 1, (1 << 30) + 1, P, None, 0, 0, 1, P, P, None, P, 1 << 60, None) == UNSUPPORTED
+    assert hq.hqmq_evict_select_workspace_bytes(1, 1, (1 << 30) + 1, 1) == 0 and hq.hqmq_evict_select_workspace_bytes(1, 1, 1 << 30, 1) > 0
+
+
+def test_own_tokens_refuse_short_buffers():
+    """Buffers of fewer rows than params says are refused where the sequences' tokens are put together."""
+    p, fewer = _params(), _params(T=900, stride_b=4 * 900 * 128, stride_h=900 * 128)
+    full, short = hq.alloc_encoded(p, "cpu", 10), hq.alloc_encoded(fewer, "cpu", 10)
+    assert hq.OwnTokens(p, full, full).struct.cap_k == 10
+    for k, v in ((full, short), (short, full)):
+        with pytest.raises(ValueError):
+            hq.OwnTokens(p, k, v)
