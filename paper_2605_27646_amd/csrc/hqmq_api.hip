@@ -931,7 +931,7 @@ static int32_t check_own(const hqmq_params *params, int32_t n_share, const hqmq_
 struct SharedLayout {
     SharedPlan prefix;
     AttendPlan own;
-    bool own_short;  // the own tokens take the prefix's kernel too, every sequence a prefix of its own
+    bool own_shared, together;  // the own tokens take the prefix's kernel too, every sequence a prefix of its own; in one launch
     uint64_t ml_bytes, total;
     int32_t parts;
 };
@@ -941,14 +941,15 @@ static SharedLayout shared_layout(const hqmq_params *params, int G, int n_share,
     SharedLayout l;
     l.prefix = plan_shared(g, G, n_share);
     l.own.n_splits = 0;
-    l.own_short = false;
+    l.own_shared = l.together = false;
     if (own) {
         const Geometry go = make_geometry(own);
         // Short segments are bound by what a workgroup does before and after its tokens, of which the prefix's kernel has less (tables a
         // quarter of the size, three workgroups per compute unit).  The kernel of hqmq_attend / this one: 768 segments of 64 tokens x 96
         // 18.9 / 11.6 us; 512 of up to 512 x 128 35.5 / 40; 48 of up to 97 x 64 6.3 / 7.0.
-        l.own_short = go.T <= 128 && go.B * go.H >= 256;
-        if (l.own_short) {
+        l.together = shared_is_small(G * n_share) && (int64_t)go.B * go.H * go.T <= (1 << 18);
+        l.own_shared = l.together || (go.T <= 128 && go.B * go.H >= 256);
+        if (l.own_shared) {
             const SharedPlan p = plan_shared(go, G, 1);
             l.own.n_splits = p.n_splits;
             l.own.rows_per_split = p.rows_per_split;
@@ -1018,13 +1019,25 @@ extern "C" int32_t hqmq_attend_shared(const hqmq_params *params, int32_t n_share
     a.part_ml = part_ml;
     a.part_acc = part_acc;
     a.qscale = scale * 1.44269504088896340736f;
+    a.T = params->T;
     a.G = G;
     a.n_share = n_share;
     a.n_splits = l.prefix.n_splits;
     a.rows_per_split = l.prefix.rows_per_split;
     a.split0 = 0;
     a.part_pitch = l.parts;
-    hipError_t err = launch_shared(g, a, static_cast<hipStream_t>(stream));
+    SharedArgs mine = a;
+    if (own && l.own_shared) {
+        mine.k = attend_side(own->enc_k, sec_k_dev, own->cap_k);
+        mine.v = attend_side(own->enc_v, sec_v_dev, own->cap_v);
+        mine.visible = own->visible_dev;
+        mine.T = own->params->T;
+        mine.n_share = 1;
+        mine.n_splits = l.own.n_splits;
+        mine.rows_per_split = l.own.rows_per_split;
+        mine.split0 = l.prefix.n_splits;
+    }
+    hipError_t err = launch_shared(g, a, own && l.together ? &mine : nullptr, static_cast<hipStream_t>(stream));
     if (err != hipSuccess)
         return hip_failed(err);
 
@@ -1039,18 +1052,11 @@ extern "C" int32_t hqmq_attend_shared(const hqmq_params *params, int32_t n_share
     o.G = G;
     o.D = params->D;
     o.part_pitch = l.parts;
-    if (own && l.own_short) {
-        a.k = attend_side(own->enc_k, sec_k_dev, own->cap_k);
-        a.v = attend_side(own->enc_v, sec_v_dev, own->cap_v);
-        a.visible = own->visible_dev;
-        a.n_share = 1;
-        a.n_splits = l.own.n_splits;
-        a.rows_per_split = l.own.rows_per_split;
-        a.split0 = l.prefix.n_splits;
-        err = launch_shared(make_geometry(own->params), a, static_cast<hipStream_t>(stream));
+    if (own && l.own_shared && !l.together) {
+        err = launch_shared(make_geometry(own->params), mine, nullptr, static_cast<hipStream_t>(stream));
         if (err != hipSuccess)
             return hip_failed(err);
-    } else if (own) {
+    } else if (own && !l.own_shared) {
         o.k = attend_side(own->enc_k, sec_k_dev, own->cap_k);
         o.v = attend_side(own->enc_v, sec_v_dev, own->cap_v);
         o.visible = own->visible_dev;

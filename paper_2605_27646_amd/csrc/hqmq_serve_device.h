@@ -15,7 +15,7 @@ struct SharedArgs {
     float *part_ml;          // [B * n_share * H * G][part_pitch][2]: maximum (log2 domain) and weight sum of a split
     float *part_acc;         // [..][part_pitch][128]: weighted value sums
     float qscale;            // softmax scale * log2(e)
-    int32_t G, n_share;
+    int32_t T, G, n_share;
     int32_t n_splits, rows_per_split;  // workgroups along the prefix and its tokens per workgroup
     int32_t split0, part_pitch;        // the first one's place in the partial arrays, and how many places there are, the own tokens' included
 };
@@ -25,7 +25,9 @@ struct SharedPlan {
 };
 SharedPlan plan_shared(const Geometry &g, int G, int n_share);
 hipError_t prepare_shared_kernels();  // once per device, before the first launch_shared on it
-hipError_t launch_shared(const Geometry &g, const SharedArgs &a, hipStream_t stream);
+bool shared_is_small(int n_rows);     // of a kv head: a launch of prefixes can take the sequences' own tokens with it
+// own: of the sequences' own tokens (B * n_share batch entries), or null
+hipError_t launch_shared(const Geometry &g, const SharedArgs &a, const SharedArgs *own, hipStream_t stream);
 
 struct MassArgs {
     AttendSide k;

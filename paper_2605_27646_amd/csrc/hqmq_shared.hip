@@ -69,6 +69,7 @@ template <int kTakers_, int kCols_, int kBufs_, int kPerSimd_>
 struct Form {
     static constexpr int kTakers = kTakers_, kCols = kCols_, kBufs = kBufs_, kPerSimd = kPerSimd_;
     static constexpr int kThreads = 64 * kTakers + (kBufs == 2 ? kMakers : 0);
+    static constexpr bool kTogether = kBufs == 1 && kCols == 16;  // a launch may hold prefixes and own tokens
 };
 using FormSmall = Form<4, 16, 1, 3>;
 using FormMiddle = Form<4, 32, 1, 2>;
@@ -77,8 +78,14 @@ using FormLarge = Form<8, 32, 2, 3>;
 }  // namespace
 
 template <int kNc, bool kTable, bool kPow2, typename F>
-__global__ __launch_bounds__(F::kThreads, F::kPerSimd) void k_shared(Geometry g, SharedArgs a)
+__global__ __launch_bounds__(F::kThreads, F::kPerSimd) void k_shared(Geometry g, SharedArgs a, SharedArgs own, int n_first)
 {
+    int block = (int)blockIdx.x;
+    if (F::kTogether && block >= n_first) {  // uniform
+        block -= n_first;
+        a = own;
+    }
+    const int split = block % a.n_splits, seg = block / a.n_splits;
     using Tile = TileLds<kNc>;
     using Stage = StageLds<kNc>;
     constexpr int kTok = tile_tokens<kNc>(), kD = 4 * kNc;
@@ -98,7 +105,7 @@ __global__ __launch_bounds__(F::kThreads, F::kPerSimd) void k_shared(Geometry g,
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const bool maker = kBufs == 1 || wave < 4, taker = kBufs == 1 || wave >= 4;  // uniform
     const int st = tid & (kMakers - 1);
-    const int seg = blockIdx.y, b = seg / g.H, h = seg % g.H;
+    const int b = seg / g.H, h = seg % g.H;
     const uint32_t row_words = kNc == 32 ? (uint32_t)g.w : (uint32_t)g.row_words;
     const uint32_t w = g.w;
 
@@ -129,17 +136,17 @@ __global__ __launch_bounds__(F::kThreads, F::kPerSimd) void k_shared(Geometry g,
             qf[s] = __builtin_bit_cast(half8_t, v);
         }
     }
-    int vis = g.T;
+    int vis = a.T;
     if (a.visible && there)
-        vis = min(max(a.visible[head], 0), g.T);
+        vis = min(max(a.visible[head], 0), a.T);
 
     build_tables<kTable>(lds, g, a.k.sec + (size_t)h * g.S * 4, a.v.sec + (size_t)h * g.S * 4, 2, tid, kThreads);
     const Decoder<kTable, kPow2> decoder(lds, g);
 
     // ---- the tiles of this workgroup -----------------------------------------------------------------------------------
-    const int begin = (int)blockIdx.x * a.rows_per_split;
-    int end = min(g.T, begin + a.rows_per_split);
-    int least = g.T;      // every query row of the wave sees the tokens below
+    const int begin = split * a.rows_per_split;
+    int end = min(a.T, begin + a.rows_per_split);
+    int least = a.T;      // every query row of the wave sees the tokens below
     if (a.visible) {      // what no row of the workgroup sees is not read
         int *most_of = reinterpret_cast<int *>(key_tiles);
         int most = there ? vis : 0;
@@ -174,7 +181,7 @@ __global__ __launch_bounds__(F::kThreads, F::kPerSimd) void k_shared(Geometry g,
     // Waves 0 and 1 look after K's rows and payloads, 2 and 3 after V's; all of them fetch code words of both.
     const bool of_v = (wave & 2) != 0, row_wave = (wave & 1) == 0;
     const uint32_t n_tok = (uint32_t)max(end - begin, 0);
-    const int64_t first_row = (int64_t)seg * g.T + begin;
+    const int64_t first_row = (int64_t)seg * a.T + begin;
     const rsrc_t code_k = buffer_of(a.k.codes + first_row * row_words, n_tok * row_words);
     const rsrc_t code_v = buffer_of(a.v.codes + first_row * row_words, n_tok * row_words);
     const rsrc_t flag_b = buffer_of((of_v ? a.v.flags : a.k.flags) + first_row, n_tok);
@@ -546,7 +553,7 @@ __global__ __launch_bounds__(F::kThreads, F::kPerSimd) void k_shared(Geometry g,
     if (!has_cols)
         return;
     if (there && kgrp == 0) {
-        float *ml = a.part_ml + 2 * (head * a.part_pitch + a.split0 + blockIdx.x);
+        float *ml = a.part_ml + 2 * (head * a.part_pitch + a.split0 + split);
         ml[0] = m_ref;
         ml[1] = l_run;
     }
@@ -569,13 +576,15 @@ __global__ __launch_bounds__(F::kThreads, F::kPerSimd) void k_shared(Geometry g,
             if (rr < n_rows) {
                 const int m = rr / a.G;
                 const size_t hd = ((size_t)(b * a.n_share + m) * g.H + h) * a.G + (rr - m * a.G);
-                *reinterpret_cast<float4_t *>(a.part_acc + (hd * a.part_pitch + a.split0 + blockIdx.x) * 128 + 32 * part + d) =
+                *reinterpret_cast<float4_t *>(a.part_acc + (hd * a.part_pitch + a.split0 + split) * 128 + 32 * part + d) =
                     *reinterpret_cast<const float4_t *>(out + c * kPitch + d);
             }
         }
         wave_lds_sync();
     }
 }
+
+bool shared_is_small(int n_rows) { return n_rows <= 64; }
 
 namespace {
 
@@ -589,7 +598,7 @@ struct SharedChoice {
 SharedChoice choose_shared(const Geometry &g, int n_rows)
 {
     SharedChoice c;
-    c.form = n_rows <= 64 ? kSmall : n_rows <= 128 ? kMiddle : kLarge;
+    c.form = shared_is_small(n_rows) ? kSmall : n_rows <= 128 ? kMiddle : kLarge;
     int most = 0;
     const auto fit = [&](auto lds, size_t table_room) {
         c.table = lds(true) <= table_room;
@@ -653,16 +662,20 @@ hipError_t prepare_shared_kernels()
     return hipSuccess;
 }
 
-hipError_t launch_shared(const Geometry &g, const SharedArgs &a, hipStream_t stream)
+hipError_t launch_shared(const Geometry &g, const SharedArgs &a, const SharedArgs *own, hipStream_t stream)
 {
     if (g.D != 128 && g.D != 96 && g.D != 64)
         return hipErrorInvalidValue;
     const int n_rows = a.G * a.n_share;
     const SharedChoice c = choose_shared(g, n_rows);
-    const dim3 grid((unsigned)a.n_splits, (unsigned)(g.B * g.H), (unsigned)((n_rows + c.rows - 1) / c.rows));
+    if (own && c.form != kSmall)
+        return hipErrorInvalidValue;
+    int n_first = a.n_splits * g.B * g.H;
+    const int n_own = own ? own->n_splits * g.B * a.n_share * g.H : 0;
+    const dim3 grid((unsigned)(n_first + n_own), 1, (unsigned)((n_rows + c.rows - 1) / c.rows));
     Geometry gc = g;
-    SharedArgs ac = a;
-    void *args[] = {&gc, &ac};
+    SharedArgs ac = a, oc = own ? *own : a;
+    void *args[] = {&gc, &ac, &oc, &n_first};
     return hipLaunchKernel(shared_kernel(g.n_c, c.form, c.table, (g.S & (g.S - 1)) == 0), grid, dim3(c.threads), args, c.lds, stream);
 }
 
