@@ -944,9 +944,12 @@ static SharedLayout shared_layout(const hqmq_params *params, int G, int n_share,
     l.own_shared = l.together = false;
     if (own) {
         const Geometry go = make_geometry(own);
-        // Short segments are bound by what a workgroup does before and after its tokens, of which the prefix's kernel has less (tables a
-        // quarter of the size, three workgroups per compute unit).  The kernel of hqmq_attend / this one: 768 segments of 64 tokens x 96
-        // 18.9 / 11.6 us; 512 of up to 512 x 128 35.5 / 40; 48 of up to 97 x 64 6.3 / 7.0.
+        // Beside a prefix of few query rows the own tokens are more workgroups of its launch, unless they are so many that
+        // hqmq_attend's kernel makes up for its launch.  In one / apart, 16 sequences, 8 heads, prefix 8192 x 128: 64 own tokens 32.6 / 38.8 us,
+        // 512 41.2 / 44.0, 1024 49.4 / 50.4, 2048 (2^18 rows) 64.0 / 63.3, 4096 88.6 / 89.0; 2048 x 64 37.8 / 42.9.
+        // Apart, short segments are bound by what a workgroup does before and after its tokens, of which the prefix's kernel has less
+        // (tables a quarter of the size, three workgroups per compute unit).  The kernel of hqmq_attend / this one: 768 segments of 64
+        // tokens x 96 18.9 / 11.6 us; 512 of up to 512 x 128 35.5 / 40; 48 of up to 97 x 64 6.3 / 7.0.
         l.together = shared_is_small(G * n_share) && (int64_t)go.B * go.H * go.T <= (1 << 18);
         l.own_shared = l.together || (go.T <= 128 && go.B * go.H >= 256);
         if (l.own_shared) {
