@@ -259,6 +259,11 @@ def test_shared_long_prefix():
     _shared(6100, 1, 70, 1, 4, 9001, 64, 192, 4, own=17, limits="ragged")
 
 
+def test_shared_long_own_tokens():
+    """More own tokens than go with the prefix's launch."""
+    _shared(6200, 1, 16, 1, 4, 50, 64, 48, 4, own=16500, own_limits="ragged")
+
+
 def test_shared_with_one_sequence_is_attend():
     """n_share = 1 without own tokens is hqmq_attend_lse: the same value up to the rounding of both."""
     B, H, G, T, S = 2, 2, 4, 600, 64
