@@ -49,21 +49,22 @@ def _on_this_device(*tensors) -> None:
     """The library enqueues on a stream of the current device: a tensor of another one would be read across devices."""
     here = torch.cuda.current_device()
     for t in tensors:
-        if t is not None and (not t.is_cuda or t.get_device() != here):
+        if t is not None and t.get_device() != here:  # -1: of the host
             raise ValueError("every tensor must be on torch's current device")
 
 
 def _rows_of(name, t, dtype, shape) -> None:
-    if t.dtype != dtype or not t.is_contiguous() or tuple(t.shape) != tuple(shape):
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous {str(dtype)[6:]} {list(shape)}")
 
 
 def _share_of(params: HqmqParams, q: torch.Tensor) -> int:
-    if q.dtype != torch.float16 or not q.is_contiguous() or q.dim() != 3 or q.shape[2] != params.D:
+    shape, B = q.shape, params.B
+    if q.dtype is not torch.float16 or len(shape) != 3 or shape[2] != params.D or not q.is_contiguous():
         raise ValueError("q must be contiguous fp16 [n_seqs, n_q_heads, D]")
-    if params.B <= 0 or q.shape[0] % params.B or q.shape[0] == 0:
+    if B <= 0 or shape[0] % B or shape[0] == 0:
         raise ValueError("q must have a multiple of the caches' batch entries")
-    return q.shape[0] // params.B
+    return shape[0] // B
 
 
 def _hold(params: HqmqParams, encs) -> None:
@@ -104,27 +105,29 @@ def hqmq_attend_shared(params: HqmqParams, q: torch.Tensor, scale: float, enc_k:
     sequences each, and over the sequences' own packed tokens.  visible: int32 [B * n_share, n_q_heads], the prefix tokens
     that each query head sees (None: all); lse: optional fp32 output of the same shape."""
     n_share = _share_of(params, q)
-    rows = q.shape[:2]
-    if out.shape != q.shape or out.dtype != torch.float16 or not out.is_contiguous():
-        raise ValueError("out must be contiguous fp16 with the shape of q")
-    for sec in (sec_k, sec_v):
-        _rows_of("sec", sec, torch.float32, (params.H, params.S, 4))
+    shape = q.shape
+    rows, sec_shape = shape[:2], (params.H, params.S, 4)
+    _rows_of("out", out, torch.float16, shape)
+    _rows_of("sec", sec_k, torch.float32, sec_shape)
+    _rows_of("sec", sec_v, torch.float32, sec_shape)
     if not workspace.is_contiguous():
         raise ValueError("workspace must be contiguous")
-    for name, t, dtype in (("visible", visible, torch.int32), ("lse", lse, torch.float32),
-                           ("the own tokens' visible", own.visible if own is not None else None, torch.int32)):
-        if t is not None:
-            _rows_of(name, t, dtype, rows)
+    if visible is not None:
+        _rows_of("visible", visible, torch.int32, rows)
+    if lse is not None:
+        _rows_of("lse", lse, torch.float32, rows)
     _on_this_device(q, out, sec_k, sec_v, workspace, visible, lse, enc_k.codes, enc_v.codes)
     if own is not None:
+        if own.visible is not None:
+            _rows_of("the own tokens' visible", own.visible, torch.int32, rows)
         _on_this_device(own.visible, own.keep[0].codes, own.keep[1].codes)
-    rc = _load().hqmq_attend_shared(C.byref(params), n_share, int(q.shape[1]), q.data_ptr(), float(scale),
+    rc = _load().hqmq_attend_shared(C.byref(params), n_share, shape[1], q.data_ptr(), float(scale),
                                     C.byref(enc_k.as_struct()), enc_k.outlier_capacity, sec_k.data_ptr(),
                                     C.byref(enc_v.as_struct()), enc_v.outlier_capacity, sec_v.data_ptr(),
                                     None if visible is None else visible.data_ptr(),
                                     None if own is None else C.byref(own.struct), out.data_ptr(),
                                     None if lse is None else lse.data_ptr(), workspace.data_ptr(),
-                                    workspace.numel() * workspace.element_size(), _stream_ptr(stream))
+                                    workspace.nbytes, _stream_ptr(stream))
     _check(rc, "hqmq_attend_shared")
 
 
@@ -139,15 +142,15 @@ def hqmq_attend_mass(params: HqmqParams, q: torch.Tensor, scale: float, enc_k: E
     out = mass if out is None else out
     if out is None or (mass is None and decay != 0.0):
         raise ValueError("mass is needed unless decay is 0 and out is given")
-    for name, t in (("mass", mass), ("out", out)):
-        if t is not None:
-            _rows_of(name, t, torch.float32, (params.B, params.H, params.T))
+    _rows_of("out", out, torch.float32, (params.B, params.H, params.T))
+    if mass is not None and mass is not out:
+        _rows_of("mass", mass, torch.float32, out.shape)
     _rows_of("lse", lse, torch.float32, rows)
     _rows_of("sec", sec_k, torch.float32, (params.H, params.S, 4))
     if visible is not None:
         _rows_of("visible", visible, torch.int32, rows)
     _on_this_device(q, sec_k, lse, mass, out, visible, enc_k.codes)
-    rc = _load().hqmq_attend_mass(C.byref(params), n_share, int(q.shape[1]), q.data_ptr(), float(scale),
+    rc = _load().hqmq_attend_mass(C.byref(params), n_share, rows[1], q.data_ptr(), float(scale),
                                   C.byref(enc_k.as_struct()), enc_k.outlier_capacity, sec_k.data_ptr(), lse.data_ptr(),
                                   None if visible is None else visible.data_ptr(), None if mass is None else mass.data_ptr(),
                                   float(decay), out.data_ptr(), _stream_ptr(stream))
@@ -164,24 +167,25 @@ def hqmq_evict_select(mass: torch.Tensor, n_sink: int, n_recent: int, keep: torc
     """Enqueue the choice of the keep.shape[2] tokens that every (b, h) of mass (fp32 [B, H, T]) keeps: the first n_sink and
     last n_recent of lengths[b] (int32 [B]; None: T), and those of largest mass between them.  keep: int32 [B, H, n_keep],
     ascending, -1 behind the last; n_kept: int32 [B, H]; kept_mass: optional fp32 [B, H, n_keep]."""
-    if mass.dim() != 3 or keep.dim() != 3:
+    shape, kept = mass.shape, keep.shape
+    if len(shape) != 3 or len(kept) != 3:
         raise ValueError("mass must be [B, H, T] and keep [B, H, n_keep]")
-    B, H, T = mass.shape
-    _rows_of("mass", mass, torch.float32, (B, H, T))
-    _rows_of("keep", keep, torch.int32, (B, H, keep.shape[2]))
+    B, H, T = shape
+    _rows_of("mass", mass, torch.float32, shape)
+    _rows_of("keep", keep, torch.int32, (B, H, kept[2]))
     _rows_of("n_kept", n_kept, torch.int32, (B, H))
     if kept_mass is not None:
-        _rows_of("kept_mass", kept_mass, torch.float32, keep.shape)
+        _rows_of("kept_mass", kept_mass, torch.float32, kept)
     if lengths is not None:
         _rows_of("lengths", lengths, torch.int32, (B,))
     if workspace is not None and not workspace.is_contiguous():
         raise ValueError("workspace must be contiguous")
     _on_this_device(mass, keep, n_kept, kept_mass, lengths, workspace)
     rc = _load().hqmq_evict_select(B, H, T, mass.data_ptr(), None if lengths is None else lengths.data_ptr(), int(n_sink),
-                                   int(n_recent), keep.shape[2], keep.data_ptr(), n_kept.data_ptr(),
+                                   int(n_recent), kept[2], keep.data_ptr(), n_kept.data_ptr(),
                                    None if kept_mass is None else kept_mass.data_ptr(),
                                    None if workspace is None else workspace.data_ptr(),
-                                   0 if workspace is None else workspace.numel() * workspace.element_size(), _stream_ptr(stream))
+                                   0 if workspace is None else workspace.nbytes, _stream_ptr(stream))
     _check(rc, "hqmq_evict_select")
 
 
@@ -233,5 +237,5 @@ def hqmq_evict_compact(batch: CompactBatch, stream=None) -> None:
     ws = batch.workspace
     _on_this_device(ws)
     rc = _load().hqmq_evict_compact(C.byref(batch.params), batch.n_keep, batch.n, batch.enc, batch.cap, batch.rows, batch.out,
-                                    batch.out_cap, ws.data_ptr(), ws.numel() * ws.element_size(), _stream_ptr(stream))
+                                    batch.out_cap, ws.data_ptr(), ws.nbytes, _stream_ptr(stream))
     _check(rc, "hqmq_evict_compact")
