@@ -332,14 +332,15 @@ __global__ __launch_bounds__(kDecThreads) void k_decode(Geometry g, DecodeBatch 
 // for d_h not divisible by 4").  Bound by the latency of its loads: kGeneralBatch chunks of a lane are requested before the
 // first is used, then their outliers.  Two tensors with 8 heads of 32768 rows, in us, one row per half-wave and pass / now: D = 100
 // 54 / 40, D = 45 68 / 33, D = 126 76 / 50, D = 101 75 / 49 (batches of 2: 42, 32, 50, 51; of 8: 45, 38, 52, 53).
-// grid = (ceil(T / 64), B*H, tensors), block = 256.
+// grid = (ceil(T / 64), B*H, tensors), block = 256, or 64 where a segment has no more chunks: waves without any only fill the tables
+// (the 8 tensors below, T = 1: 15.0 -> 10.7).
 // dynamic LDS: prim [48][4] f32 | secl [S][4] f32
 // kBatch: 4; 1 or 2 where a segment has no more chunks than so many per lane, as the rest of a batch of 4 decodes its last chunk
 // over again.  In us, one row per half-wave and pass / always 4 / so: 8 tensors of 256 x 8 segments of 100 elements, T = 1 15.0 /
 // 26.5 / 15.2, T = 7 23.3 / 29.4 / 20.8, T = 11 30.6 / 32.3 / 26.5; one of 512 x 8, T = 11 9.3 / 10.6 / 9.0.
 constexpr int kGeneralBatch = 4;
-template <bool kPow2, int kBatch>
-__global__ __launch_bounds__(kDecThreads) void k_decode_rows(Geometry g, DecodeBatch batch)
+template <bool kPow2, int kBatch, int kThreads = kDecThreads>
+__global__ __launch_bounds__(kThreads) void k_decode_rows(Geometry g, DecodeBatch batch)
 {
     const DecodeTensor &dt = batch.t[blockIdx.z];
     const uint64_t outlier_capacity = dt.outlier_capacity;
@@ -380,18 +381,18 @@ __global__ __launch_bounds__(kDecThreads) void k_decode_rows(Geometry g, DecodeB
     Fetched f[kBatch];
 #pragma unroll
     for (int u = 0; u < kBatch; ++u)
-        f[u] = fetch(tid + u * kDecThreads);
+        f[u] = fetch(tid + u * kThreads);
     const float *sec_h = dt.sec + (size_t)h * g.S * 4;
-    for (int s = tid; s < g.S; s += kDecThreads)
+    for (int s = tid; s < g.S; s += kThreads)
         *reinterpret_cast<float4_t *>(secl + 4 * s) = *reinterpret_cast<const float4_t *>(sec_h + 4 * s);
-    if (tid < 48 * 4) {
-        const int p = tid >> 2, i = tid & 3;
+    for (int x = tid; x < 48 * 4; x += kThreads) {
+        const int p = x >> 2, i = x & 3;
         float v = 0.f;
         if (p < 8)
             v = ((p >> 1) == i) ? ((p & 1) ? -1.f : 1.f) : 0.f;
         else if (p < 24)
             v = (((p - 8) >> (3 - i)) & 1) ? -0.5f : 0.5f;
-        prim[tid] = v;
+        prim[x] = v;
     }
     __syncthreads();
     if (kBatch == 1 && (tid & ~63) >= n_chunks)  // a wave without chunks
@@ -440,7 +441,7 @@ __global__ __launch_bounds__(kDecThreads) void k_decode_rows(Geometry g, DecodeB
                 hv[i] = (_Float16)y[i];
             if ((f[u].word >> f[u].c) & 1u)
                 hv = __builtin_bit_cast(half4_t, pay[u]);
-            if (q0 + u * kDecThreads < n_chunks) {
+            if (q0 + u * kThreads < n_chunks) {
                 _Float16 *dst = out + (int64_t)f[u].r * g.st + 4 * f[u].c;
                 const int left = g.D - 4 * (int)f[u].c;  // elements of the row from this chunk on
                 if (g.vec_ok) {
@@ -458,12 +459,12 @@ __global__ __launch_bounds__(kDecThreads) void k_decode_rows(Geometry g, DecodeB
                 }
             }
         }
-        q0 += kBatch * kDecThreads;
+        q0 += kBatch * kThreads;
         if (q0 - tid >= n_chunks)  // uniform
             break;
 #pragma unroll
         for (int u = 0; u < kBatch; ++u)
-            f[u] = fetch(q0 + u * kDecThreads);
+            f[u] = fetch(q0 + u * kThreads);
     }
 }
 
@@ -494,19 +495,21 @@ hipError_t launch_decode(const Geometry &g, const DecodeBatch &batch, int n_tens
         dim3 grid((unsigned)((g.T + kGeneralRows - 1) / kGeneralRows), (unsigned)(g.B * g.H), (unsigned)n_tensors);
         const bool pow2 = (g.S & (g.S - 1)) == 0;
         const int64_t chunks = (int64_t)g.T * g.n_c;  // of a segment
-#define HQMQ_LAUNCH_ROWS(N)                                                                                                \
+#define HQMQ_LAUNCH_ROWS(N, THREADS)                                                                                       \
     do {                                                                                                                   \
         if (pow2)                                                                                                          \
-            hipLaunchKernelGGL((k_decode_rows<true, N>), grid, dim3(kDecThreads), lds_rows, stream, g, batch);             \
+            hipLaunchKernelGGL((k_decode_rows<true, N, THREADS>), grid, dim3(THREADS), lds_rows, stream, g, batch);        \
         else                                                                                                               \
-            hipLaunchKernelGGL((k_decode_rows<false, N>), grid, dim3(kDecThreads), lds_rows, stream, g, batch);            \
+            hipLaunchKernelGGL((k_decode_rows<false, N, THREADS>), grid, dim3(THREADS), lds_rows, stream, g, batch);       \
     } while (0)
-        if (chunks <= kDecThreads)
-            HQMQ_LAUNCH_ROWS(1);
+        if (chunks <= 64)
+            HQMQ_LAUNCH_ROWS(1, 64);
+        else if (chunks <= kDecThreads)
+            HQMQ_LAUNCH_ROWS(1, kDecThreads);
         else if (chunks <= 2 * kDecThreads)
-            HQMQ_LAUNCH_ROWS(2);
+            HQMQ_LAUNCH_ROWS(2, kDecThreads);
         else
-            HQMQ_LAUNCH_ROWS(kGeneralBatch);
+            HQMQ_LAUNCH_ROWS(kGeneralBatch, kDecThreads);
 #undef HQMQ_LAUNCH_ROWS
     }
     return hipGetLastError();
