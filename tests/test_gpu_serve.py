@@ -259,6 +259,11 @@ def test_shared_long_prefix():
     _shared(6100, 1, 70, 1, 4, 9001, 64, 192, 4, own=17, limits="ragged")
 
 
+def test_shared_most_parts():
+    """One head: prefix and own tokens in 512 shares each, all of which the merge takes."""
+    _shared(6300, 1, 1, 1, 2, 32768, 128, 32, own=32768)
+
+
 def test_shared_long_own_tokens():
     """More own tokens than go with the prefix's launch."""
     _shared(6200, 1, 16, 1, 4, 50, 64, 48, 4, own=16500, own_limits="ragged")
@@ -681,8 +686,10 @@ def test_serving_step():
     assert abs(total - s.B * s.M * s.H * s.G) < 1e-2
 
 
-def test_serving_graph_replays():
-    s = Serving(9500, M=20, T=500, own=130, D=64, S=24)
+@pytest.mark.parametrize("kw", [dict(M=20, T=500, own=130, D=64, S=24), dict(M=3, T=500, own=33000, D=64, S=24)])
+def test_serving_graph_replays(kw):
+    """A short step, and one whose own tokens are chosen from by several workgroups per head."""
+    s = Serving(9500, **kw)
     hq.hqmq_init()
     s.scrub()
     s.step()
