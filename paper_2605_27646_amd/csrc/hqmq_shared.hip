@@ -547,6 +547,8 @@ __global__ __launch_bounds__(F::kThreads, F::kPerSimd) void k_shared(Geometry g,
             for (int n = 0; n < kU * kBlocks; ++n)
                 multiply(value_operand(last, n % kBlocks, n / kBlocks), held[n / kBlocks], n % kBlocks);
     }
+    if constexpr (kBufs == 2)
+        lds_barrier();  // what follows is written over the last values, which slower waves may still read
 
     // ---- the wave's columns of this share: through LDS, so that a row's sums leave in whole lines -------------------------------------
     l_run = over_lanes(l_run, [](float x, float y) { return x + y; });
