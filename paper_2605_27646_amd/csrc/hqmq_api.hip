@@ -939,7 +939,7 @@ static SharedLayout shared_layout(const hqmq_params *params, int G, int n_share,
 {
     const Geometry g = make_geometry(params);
     SharedLayout l;
-    l.prefix = plan_shared(g, G, n_share);
+    l.prefix = plan_shared(g, G, n_share, own == nullptr);
     l.own.n_splits = 0;
     l.own_shared = l.together = false;
     if (own) {
@@ -953,7 +953,7 @@ static SharedLayout shared_layout(const hqmq_params *params, int G, int n_share,
         l.together = shared_is_small(G * n_share) && (int64_t)go.B * go.H * go.T <= (1 << 18);
         l.own_shared = l.together || (go.T <= 128 && go.B * go.H >= 256);
         if (l.own_shared) {
-            const SharedPlan p = plan_shared(go, G, 1);
+            const SharedPlan p = plan_shared(go, G, 1, false);
             l.own.n_splits = p.n_splits;
             l.own.rows_per_split = p.rows_per_split;
         } else {
@@ -1021,6 +1021,8 @@ extern "C" int32_t hqmq_attend_shared(const hqmq_params *params, int32_t n_share
     a.visible = visible_dev;
     a.part_ml = part_ml;
     a.part_acc = part_acc;
+    a.out = l.parts == 1 ? static_cast<_Float16 *>(out_dev) : nullptr;
+    a.lse = lse_dev;
     a.qscale = scale * 1.44269504088896340736f;
     a.T = params->T;
     a.G = G;
@@ -1043,6 +1045,9 @@ extern "C" int32_t hqmq_attend_shared(const hqmq_params *params, int32_t n_share
     hipError_t err = launch_shared(g, a, own && l.together ? &mine : nullptr, static_cast<hipStream_t>(stream));
     if (err != hipSuccess)
         return hip_failed(err);
+
+    if (l.parts == 1)
+        return HQMQ_OK;
 
     AttendArgs o;
     std::memset(&o, 0, sizeof(o));

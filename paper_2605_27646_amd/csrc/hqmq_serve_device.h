@@ -14,6 +14,8 @@ struct SharedArgs {
     const int32_t *visible;  // [B * n_share][H * G] or null
     float *part_ml;          // [B * n_share * H * G][part_pitch][2]: maximum (log2 domain) and weight sum of a split
     float *part_acc;         // [..][part_pitch][128]: weighted value sums
+    _Float16 *out;           // [B * n_share][H * G][D], and lse [B * n_share][H * G] or null: one share only, no partial sums; else null
+    float *lse;
     float qscale;            // softmax scale * log2(e)
     int32_t T, G, n_share;
     int32_t n_splits, rows_per_split;  // workgroups along the prefix and its tokens per workgroup
@@ -23,7 +25,10 @@ constexpr int kMostSharedSplits = 512;  // and as many of the own tokens: kMostP
 struct SharedPlan {
     int32_t n_splits, rows_per_split;
 };
-SharedPlan plan_shared(const Geometry &g, int G, int n_share);
+// alone: without own tokens, so that a prefix of kTilesAlone tiles is one share and needs no merge.  One share / one per tile and the merge,
+// 2 sequences, 8 heads x 128: one tile 6.0 / 8.3 us, two 7.6 / 8.3, three 8.5 / 8.3, five 12.5 / 9.8.
+constexpr int kTilesAlone = 2;
+SharedPlan plan_shared(const Geometry &g, int G, int n_share, bool alone);
 hipError_t prepare_shared_kernels();  // once per device, before the first launch_shared on it
 bool shared_is_small(int n_rows);     // of a kv head: a launch of prefixes can take the sequences' own tokens with it
 // own: of the sequences' own tokens (B * n_share batch entries), or null

@@ -4,7 +4,7 @@
 // Both products are formed with the tokens as rows, S^T = K Q^T and O^T = V^T P^T: a lane then has scores of one query row, so that the
 // softmax's maximum and sum are the lane's own up to two swaps, and a block of weights, rounded, is the second product's operand as it
 // stands.  Reconstructed keys and values (transposed) go through LDS, where the waves of a workgroup share them.  Workgroups split the
-// prefix; sums and maxima of the splits, in fp32, are joined by the merge of hqmq_attend.
+// prefix; sums and maxima of the splits, in fp32, are joined by the merge of hqmq_attend where there is more than one.
 //
 // What bounds it depends on the rows.  Up to 64 of them: the reconstruction, 40 vector instructions and some 60 cycles of LDS per 64 chunks
 // (8 heads x 32771 tokens x 64, 24 rows a head: 27 us, of which the products take 2; 64 heads x 2049 x 96, 12 rows: 24).  256 rows: the
@@ -554,7 +554,13 @@ __global__ __launch_bounds__(F::kThreads, F::kPerSimd) void k_shared(Geometry g,
     l_run = over_lanes(l_run, [](float x, float y) { return x + y; });
     if (!has_cols)
         return;
-    if (there && kgrp == 0) {
+    // The only share writes the result itself: 256 x 8 heads of 64 tokens x 64, 64 rows, 25 us instead of 101 with partial sums and the merge;
+    // 40 x 8 of 500 x 128, 80 rows, 43 instead of 75.
+    const float factor = !a.out ? 1.f : l_run > 0.f ? 1.f / l_run : 0.f;  // a row that saw no token: zeros
+    if (a.out) {
+        if (there && kgrp == 0 && a.lse)
+            a.lse[head] = l_run > 0.f ? (m_ref + __builtin_amdgcn_logf(l_run)) * 0.693147180559945309417f : -__builtin_inff();
+    } else if (there && kgrp == 0) {
         float *ml = a.part_ml + 2 * (head * a.part_pitch + a.split0 + split);
         ml[0] = m_ref;
         ml[1] = l_run;
@@ -569,7 +575,7 @@ __global__ __launch_bounds__(F::kThreads, F::kPerSimd) void k_shared(Geometry g,
 #pragma unroll
             for (int i = 0; i < kRegs; ++i) {
                 const int row = kWide ? 8 * (i >> 2) + 4 * kgrp + (i & 3) : 16 * k + 4 * kgrp + i;  // 8 e + c % 8
-                out[col * kPitch + 4 * (row & 7) + (row >> 3)] = acc[kOf * part + k][i];
+                out[col * kPitch + 4 * (row & 7) + (row >> 3)] = acc[kOf * part + k][i] * factor;
             }
         wave_lds_sync();
 #pragma unroll
@@ -578,6 +584,15 @@ __global__ __launch_bounds__(F::kThreads, F::kPerSimd) void k_shared(Geometry g,
             if (rr < n_rows) {
                 const int m = rr / a.G;
                 const size_t hd = ((size_t)(b * a.n_share + m) * g.H + h) * a.G + (rr - m * a.G);
+                if (a.out) {
+                    const float4_t x = *reinterpret_cast<const float4_t *>(out + c * kPitch + d);
+                    half4_t y;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        y[e] = (_Float16)x[e];
+                    *reinterpret_cast<half4_t *>(a.out + hd * kD + 32 * part + d) = y;
+                    continue;
+                }
                 *reinterpret_cast<float4_t *>(a.part_acc + (hd * a.part_pitch + a.split0 + split) * 128 + 32 * part + d) =
                     *reinterpret_cast<const float4_t *>(out + c * kPitch + d);
             }
@@ -640,13 +655,15 @@ const void *shared_kernel(int n_c, SharedForm form, bool table, bool pow2)
 
 }  // namespace
 
-SharedPlan plan_shared(const Geometry &g, int G, int n_share)
+SharedPlan plan_shared(const Geometry &g, int G, int n_share, bool alone)
 {
     const SharedChoice c = choose_shared(g, G * n_share);
     const int tok = g.n_c == 16 ? tile_tokens<16>() : tile_tokens<32>();
     const int64_t per = (int64_t)g.B * g.H * ((G * n_share + c.rows - 1) / c.rows), tiles = (g.T + tok - 1) / tok;
     int64_t want = (int64_t)256 * c.resident / per;  // what the chip holds at once
     want = want > kMostSharedSplits ? kMostSharedSplits : want;
+    if (alone && tiles <= kTilesAlone)
+        want = 1;
     want = want < 1 ? 1 : want < tiles ? want : tiles;
     const int64_t tiles_per = (tiles + want - 1) / want;
     return {(int32_t)((tiles + tiles_per - 1) / tiles_per), (int32_t)(tiles_per * tok)};

@@ -259,6 +259,12 @@ def test_shared_long_prefix():
     _shared(6100, 1, 70, 1, 4, 9001, 64, 192, 4, own=17, limits="ragged")
 
 
+@pytest.mark.parametrize("B,M,G,D,limits", [(100, 3, 2, 64, "ragged"), (140, 40, 2, 128, None), (130, 70, 2, 96, "some"), (140, 9, 3, 128, "ragged")])
+def test_shared_one_share(B, M, G, D, limits):
+    """As many heads as the chip holds: every workgroup has its rows' whole prefix and writes the result itself."""
+    _shared(6400 + B + M, B, M, 8 if B == 100 else 2, G, 71, D, 16, 4, limits=limits)
+
+
 def test_shared_most_parts():
     """One head: prefix and own tokens in 512 shares each, all of which the merge takes."""
     _shared(6300, 1, 1, 1, 2, 32768, 128, 32, own=32768)
