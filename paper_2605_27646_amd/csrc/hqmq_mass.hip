@@ -22,7 +22,6 @@ constexpr int kMassWaves = 16, kMassThreads = 64 * kMassWaves;
 constexpr int kMassRows = 128;   // query rows in LDS at a time
 constexpr int kMassPay = 64;     // outlier payloads of a wave's 32 tokens kept in LDS
 constexpr float kLog2e = 1.44269504088896340736f;
-constexpr float kNoRow = 1.0e30f;  // the lse of a row that is not there or saw nothing: its weights are zeros
 
 // A wave's packed rows in LDS, in words: code words (room for the largest w) | flags, scales, places in the outlier list's window |
 // payloads, with a slot past the last that is read and not used
@@ -43,7 +42,8 @@ __global__ __launch_bounds__(kMassThreads, 4) void k_mass(Geometry g, MassArgs a
     _Float16 *queries = reinterpret_cast<_Float16 *>(lds + kLutFloats + direction_floats<kTable>(g.S));  // [kMassRows][kQPitch]
     float *row_lse = reinterpret_cast<float *>(queries + kMassRows * kQPitch);                           // [kMassRows]
     int *row_vis = reinterpret_cast<int *>(row_lse + kMassRows);                                         // [kMassRows]
-    uint32_t *stages = reinterpret_cast<uint32_t *>(row_vis + kMassRows);
+    int *row_limits = row_vis + kMassRows;  // [kMassRows / 64]: whether row_vis counts for any of these rows
+    uint32_t *stages = reinterpret_cast<uint32_t *>(row_limits + kMassRows / 64 + 2);  // aligned to 16 bytes
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -72,17 +72,24 @@ __global__ __launch_bounds__(kMassThreads, 4) void k_mass(Geometry g, MassArgs a
                 q[e] ^= flip;
             *reinterpret_cast<uint4v *>(queries + r * kQPitch + d) = q;
         }
-        if (tid < padded) {
-            float lse = kNoRow;
-            int vis = g.T;
+        if (tid < kMassRows) {  // whole waves
+            // Rows that are not there, and those that saw nothing (an lse of minus infinity), see no token: a weight of zero would
+            // not do, as their score is not a number where the key is not finite.
+            float lse = 0.f;
+            int vis = 0;
             if (tid < n) {
                 lse = a.lse[head_of(tid)];
-                lse = lse < -kNoRow ? kNoRow : lse;  // minus infinity: the row saw nothing
-                if (a.visible)
-                    vis = a.visible[head_of(tid)];
+                vis = a.visible ? a.visible[head_of(tid)] : g.T;
+                if (lse == -__builtin_inff()) {
+                    lse = 0.f;
+                    vis = 0;
+                }
             }
             row_lse[tid] = lse;
             row_vis[tid] = vis;
+            const bool some = ballot(vis < g.T) != 0ull;
+            if (lane == 0)
+                row_limits[wave] = some;
         }
     };
 
@@ -195,6 +202,7 @@ __global__ __launch_bounds__(kMassThreads, 4) void k_mass(Geometry g, MassArgs a
         const int half = lane >> 5;
         float sum = 0.f;
         for (int r0 = 0; r0 < n; r0 += 32) {
+            const bool limits = __builtin_amdgcn_readfirstlane(row_limits[r0 / 64]) != 0;
             float16_t sc = float16_t{0.f};
             const _Float16 *q = queries + (r0 + (lane & 31)) * kQPitch + 4 * kM * half;
 #pragma unroll
@@ -205,7 +213,7 @@ __global__ __launch_bounds__(kMassThreads, 4) void k_mass(Geometry g, MassArgs a
                 if (r0 + 8 * i >= n)  // uniform
                     break;
                 const float4_t lse = *reinterpret_cast<const float4_t *>(row_lse + r0 + 8 * i + 4 * half);
-                if (!a.visible) {
+                if (!limits) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
                         sum += __builtin_amdgcn_exp2f(kLog2e * fmaf(sc[4 * i + e], scale, -lse[e]));
@@ -252,7 +260,7 @@ namespace {
 size_t mass_lds_bytes(const Geometry &g, bool table)
 {
     const int stage = g.n_c == 32 ? MassStage<32>::total : g.n_c == 24 ? MassStage<24>::total : MassStage<16>::total;
-    return (kLutFloats + (table ? direction_floats<true>(g.S) : direction_floats<false>(g.S)) + (size_t)kMassRows * (g.D + 8) / 2 + 2 * kMassRows +
+    return (kLutFloats + (table ? direction_floats<true>(g.S) : direction_floats<false>(g.S)) + (size_t)kMassRows * (g.D + 8) / 2 + 2 * kMassRows + kMassRows / 64 + 2 +
             (size_t)kMassWaves * stage) * sizeof(float);
 }
 template <int kNc>
