@@ -29,6 +29,7 @@
 #include <type_traits>
 
 #include "hqmq_device.h"
+#include "hqmq_limits.h"
 
 namespace hqmq {
 
@@ -214,7 +215,7 @@ __global__ __launch_bounds__(kAttThreads, 2) void k_attend_partial(Geometry g, A
     int vis = 0x7fffffff;
     int row_end = min(g.T, (split + 1) * a.rows_per_split);
     if (a.visible) {
-        vis = (n16 < G) ? a.visible[((size_t)b * g.H + h) * G + n16] : 0;
+        vis = (n16 < G) ? seen_tokens(a.visible[((size_t)b * g.H + h) * G + n16]) : 0;
         row_end = min(row_end, max_of_row(vis));  // rows that no query head sees are not read
     }
     const uint32_t w = g.w, w_idx = g.w_idx;
@@ -226,7 +227,7 @@ __global__ __launch_bounds__(kAttThreads, 2) void k_attend_partial(Geometry g, A
 
     // ---- first tile on its way while the tables are set up ----------------------------------------------
     TileRegs<kNc> tk = {}, tv = {};
-    int nrows = min(kStageRows, row_end - (row_begin + wv * kStageRows));
+    int nrows = tile_rows(row_end, row_begin + wv * kStageRows, kStageRows);
     {
         const int64_t R0 = (int64_t)seg * g.T + row_begin + wv * kStageRows;
         load_tile(tk, a.k, R0, nrows, row_words, lane);
@@ -372,7 +373,7 @@ __global__ __launch_bounds__(kAttThreads, 2) void k_attend_partial(Geometry g, A
         const bool fast_k = !big_k && wk.n <= (uint32_t)kPaySlots, fast_v = !big_v && wvw.n <= (uint32_t)kPaySlots;
         const bool more = t0 + kAttendTile < row_end;
         const int tgn = t0 + kAttendTile + wv * kStageRows;
-        const int nn = more ? min(kStageRows, row_end - tgn) : 0;
+        const int nn = more ? tile_rows(row_end, tgn, kStageRows) : 0;
         if (more) {
             const int64_t R0n = (int64_t)seg * g.T + tgn;
             load_tile(tk, a.k, R0n, nn, row_words, lane);
@@ -655,7 +656,7 @@ __global__ __launch_bounds__(kJointThreads, 1) void k_attend_joint(Geometry g, A
     int vis = 0x7fffffff;
     int row_end = min(g.T, (split + 1) * a.rows_per_split);
     if (a.visible) {
-        vis = (n16 < G) ? a.visible[((size_t)b * g.H + h) * G + n16] : 0;
+        vis = (n16 < G) ? seen_tokens(a.visible[((size_t)b * g.H + h) * G + n16]) : 0;
         row_end = min(row_end, max_of_row(vis));  // rows that no query head sees are not read
     }
     const uint32_t w = g.w, w_idx = g.w_idx;
@@ -674,7 +675,7 @@ __global__ __launch_bounds__(kJointThreads, 1) void k_attend_joint(Geometry g, A
     };
     float4_t sec = secondary(min((uint32_t)tid, 2u * (uint32_t)g.S - 1u));
     TileRegs<kNc> tk = {}, tv = {};
-    int nrows = min(kStageRows, row_end - (row_begin + wv * kStageRows));
+    int nrows = tile_rows(row_end, row_begin + wv * kStageRows, kStageRows);
     {
         const int64_t R0 = (int64_t)seg * g.T + row_begin + wv * kStageRows;
         load_tile(tk, a.k, R0, nrows, row_words, lane);
@@ -829,7 +830,7 @@ __global__ __launch_bounds__(kJointThreads, 1) void k_attend_joint(Geometry g, A
         const bool fast_k = !big_k && wk.n <= (uint32_t)kPaySlots, fast_v = !big_v && wvw.n <= (uint32_t)kPaySlots;
         const bool more = t0 + kJointTile < row_end;
         const int tgn = t0 + kJointTile + wv * kStageRows;
-        const int nn = more ? min(kStageRows, row_end - tgn) : 0;
+        const int nn = more ? tile_rows(row_end, tgn, kStageRows) : 0;
         if (more) {
             const int64_t R0n = (int64_t)seg * g.T + tgn;
             load_tile(tk, a.k, R0n, nn, row_words, lane);
@@ -892,7 +893,7 @@ __global__ __launch_bounds__(kJointThreads, 1) void k_attend_joint(Geometry g, A
             // ---- softmax update: lane (head n16, j4) holds the scores of rows 4 j4 + i --------------------
             float s4[4];
             float mx = kNegBig;
-            const int seen = min(nrows, vis - (t0 + wv * kStageRows)) - 4 * j4;  // of the lane's four rows
+            const int seen = tile_rows(vis, t0 + wv * kStageRows, nrows) - 4 * j4;  // of the lane's four rows
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 s4[i] = i < seen ? sc[i] * a.qscale : 3.f * kNegBig;  // its weight is 0 whatever the maximum

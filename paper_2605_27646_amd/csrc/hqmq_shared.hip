@@ -15,6 +15,7 @@
 //
 // The weights: fp16 pairs (22 bits) up to 64 rows, where the second product hardly shows; one fp16 (11 bits) for more, where it was
 // 13 us of 78.  Each weight is then off by 2^-11 of itself at most, either way, in a sum that is rounded to fp16.
+#include "hqmq_limits.h"
 #include "hqmq_packed.h"
 
 namespace hqmq {
@@ -138,7 +139,7 @@ __global__ __launch_bounds__(F::kThreads, F::kPerSimd) void k_shared(Geometry g,
     }
     int vis = a.T;
     if (a.visible && there)
-        vis = min(max(a.visible[head], 0), a.T);
+        vis = min(seen_tokens(a.visible[head]), a.T);
 
     build_tables<kTable>(lds, g, a.k.sec + (size_t)h * g.S * 4, a.v.sec + (size_t)h * g.S * 4, 2, tid, kThreads);
     const Decoder<kTable, kPow2> decoder(lds, g);

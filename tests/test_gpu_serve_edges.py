@@ -75,3 +75,59 @@ def test_mass_of_infinite_keys(M, G):
     assert torch.isfinite(out).all()
     assert torch.equal(out[has], mass[has])
     assert (out[~has] > mass[~has]).any()
+
+
+# ---- limits --------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("T,S,flags", [(1, 16, 0), (5, 16, 0), (130, 300, 0), (3000, 16, 0), (3000, 300, 0), (3000, 64, hq.HQMQ_FLAG_ATTEND_TABLES)])
+@pytest.mark.parametrize("G", [16, 3])
+def test_attention_with_limits_far_below_zero(T, S, flags, G):
+    """The lowest limits there are mean that nothing is seen: by every query head, and by some beside others that see all."""
+    B, H, D, low = 2, 2, 128, -(2 ** 31)
+    sk, sv = _secs(17, H, S)
+    k, v = Cache(1700, B, H, T, D, sk), Cache(1701, B, H, T, D, sv)
+    p = hq.HqmqParams(B, H, T, D, H * T * D, T * D, D, S, k.b_r, 3.0, flags)
+    q = torch.randn(B, H * G, D, generator=_gen(1702)).to(torch.float16).to(DEV)
+    ws = torch.empty(hq.hqmq_attend_workspace_bytes(p, H * G), dtype=torch.uint8, device=DEV)
+
+    def run(visible):
+        out, lse = torch.full_like(q, float("nan")), torch.full((B, H * G), float("nan"), device=DEV)
+        hq.hqmq_attend_masked(p, q, 0.09, k.bufs, k.sec, v.bufs, v.sec, visible.to(DEV), out, ws, lse)
+        torch.cuda.synchronize()
+        return out.cpu(), lse.cpu()
+
+    none = torch.full((B, H * G), low, dtype=torch.int32)
+    out, lse = run(none)
+    assert not out.any() and torch.isneginf(lse).all()
+    some = torch.full((B, H * G), T, dtype=torch.int32)
+    whole = run(some)
+    some[:, ::2] = low
+    some[0, 0] = -T
+    out, lse = run(some)
+    blind = some < 0
+    assert not out[blind].any() and torch.isneginf(lse[blind]).all()
+    assert torch.equal(out[~blind], whole[0][~blind]) and torch.equal(lse[~blind], whole[1][~blind])
+
+
+@pytest.mark.parametrize("M,G,T,own", [(2, 16, 40, 200), (9, 16, 40, 300), (40, 2, 40, 70), (20, 16, 70, 1)])
+def test_shared_with_limits_far_below_zero(M, G, T, own):
+    """The same for prefix and own tokens, own tokens in the prefix's launch and in one of their own."""
+    H, D, S, low = 2, 64, 24, -(2 ** 31)
+    sk, sv = _secs(19, H, S)
+    k, v = Cache(1900, 1, H, T, D, sk), Cache(1901, 1, H, T, D, sv)
+    ok, ov = Cache(1902, M, H, own, D, sk), Cache(1903, M, H, own, D, sv)
+    q = torch.randn(M, H * G, D, generator=_gen(1904)).to(torch.float16).to(DEV)
+    ws = torch.empty(hq.hqmq_attend_shared_workspace_bytes(k.params, M, H * G, ok.params), dtype=torch.uint8, device=DEV)
+
+    def run(limit, own_limit):
+        out, lse = torch.full_like(q, float("nan")), torch.full((M, H * G), float("nan"), device=DEV)
+        visible, own_visible = (torch.full((M, H * G), x, dtype=torch.int32, device=DEV) for x in (limit, own_limit))
+        hq.hqmq_attend_shared(k.params, q, 0.1, k.bufs, k.sec, v.bufs, v.sec, out, ws, lse=lse, visible=visible,
+                              own=hq.OwnTokens(ok.params, ok.bufs, ov.bufs, own_visible))
+        torch.cuda.synchronize()
+        return out.cpu(), lse.cpu()
+
+    out, lse = run(low, low)
+    assert not out.any() and torch.isneginf(lse).all()
+    for got, want in ((run(T, low), run(T, 0)), (run(low, own), run(0, own))):
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])

@@ -3,6 +3,7 @@ arguments before anything is enqueued (pointers here are addresses that are neve
 import ctypes as C
 import os
 import re
+import subprocess
 
 import pytest
 import torch
@@ -189,3 +190,30 @@ def test_own_tokens_refuse_short_buffers():
     for k, v in ((full, short), (short, full)):
         with pytest.raises(ValueError):
             hq.OwnTokens(p, k, v)
+
+
+LIMITS = """
+#include <climits>
+#include "hqmq_limits.h"
+using namespace hqmq;
+constexpr int smaller(int a, int b) { return a < b ? a : b; }
+// rows of the tile that wave `wave` of a split begins with, of tokens of which the heads' largest limit is `most`
+constexpr int first_rows(int T, int begin, int wave, int most) { return tile_rows(smaller(T, seen_tokens(most)), begin + 16 * wave, 16); }
+static_assert(seen_tokens(INT_MIN) == 0 && seen_tokens(-1) == 0 && seen_tokens(0) == 0 && seen_tokens(7) == 7 && seen_tokens(INT_MAX) == INT_MAX, "");
+static_assert(first_rows(1, 0, 3, INT_MIN) <= 0 && first_rows(1 << 27, (1 << 27) - 64, 7, INT_MIN) <= 0 && first_rows(1, 0, 0, INT_MIN) <= 0, "");
+static_assert(first_rows(100, 64, 0, INT_MAX) == 16 && first_rows(100, 64, 2, 1000) == 4 && first_rows(100, 64, 3, 1000) <= 0, "");
+static_assert(first_rows(100, 64, 0, 70) == 6 && first_rows(100, 64, 1, 70) <= 0, "");
+// of the rows that a tile has, those that a head with this limit sees
+static_assert(tile_rows(seen_tokens(INT_MIN), 48, 16) <= 0 && tile_rows(seen_tokens(50), 48, 16) == 2 && tile_rows(INT_MAX, 48, 5) == 5, "");
+"""
+
+
+def test_limits_far_below_zero(tmp_path):
+    """The attention kernels' arithmetic on limits, as constant expressions: one that overflows does not compile."""
+    src = tmp_path / "limits.cpp"
+    src.write_text(LIMITS)
+    include = os.path.join(ROOT, "paper_2605_27646_amd", "csrc")
+    res = subprocess.run(["g++", "-std=c++17", "-fsyntax-only", "-I", include, str(src)], capture_output=True, text=True)
+    assert res.returncode == 0, res.stderr
+    source = open(os.path.join(include, "hqmq_attend.hip")).read()
+    assert source.count("a.visible[") == source.count("seen_tokens(a.visible[") == 2
