@@ -357,11 +357,12 @@ __global__ __launch_bounds__(F::kThreads, F::kPerSimd) void k_shared(Geometry g,
     };
     constexpr int kS = kWide ? 16 : 8;  // scores of a lane and 32 tokens; wide: token 8 (i / 4) + 4 kgrp + i % 4; else 16 (i / 4) + 4 kgrp + i % 4
     constexpr int kU = kWide ? 2 : 1;   // products of 32 tokens' values per block
-    half8_t held[kU];                   // two tiles in LDS: the last tile's weights, whose values are still to come
+    half8_t held[kU] = {};              // two tiles in LDS: the last tile's weights, whose values are still to come
     // Scores of 32 tokens from t0 on, the factor that is still missing from them, and m_ref raised if need be.
     // Weights are 2^(s - m_ref): with m_ref some 10 below the largest score seen they reach 2^10, their fp16 values are normal numbers
     // down to 2^-24 of the largest, and m_ref is raised (and what was summed scaled) only when a score would pass 2^15, so hardly
-    // ever after the first tiles.  It is a whole number: scaling by a power of two rounds nothing.
+    // ever after the first tiles.  It is a whole number: scaling by a power of two rounds nothing, but for held weights that become
+    // subnormal fp16 numbers: these are off by 2^-25 at most, 2^-34 of the largest weight.
     auto scores = [&](const _Float16 *keys, int t0, float *s) {
         if constexpr (kWide) {
             float16_t sc = float16_t{0.f};
@@ -409,10 +410,12 @@ __global__ __launch_bounds__(F::kThreads, F::kPerSimd) void k_shared(Geometry g,
 #pragma unroll
                 for (int i = 0; i < kRegs; ++i)
                     acc[k][i] *= corr;
-            if constexpr (kBufs == 2)
+            if constexpr (kBufs == 2)  // in fp32: the factor alone may be less than any fp16 number, or a coarse one
 #pragma unroll
                 for (int u = 0; u < kU; ++u)
-                    held[u] *= (_Float16)corr;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        held[u][i] = (_Float16)((float)held[u][i] * corr);
         }
         return mul;
     };

@@ -2,11 +2,14 @@
 finite, limits far outside, weights' bits, and the forms of each kernel."""
 from __future__ import annotations
 
+import math
+
 import numpy as np
 import pytest
 import torch
 
 import paper_2605_27646_amd as hq
+from gpu_util import gpu_encode
 from test_gpu_serve import DEV, Cache, _gen, _secs
 
 pytestmark = pytest.mark.gpu
@@ -131,3 +134,49 @@ def test_shared_with_limits_far_below_zero(M, G, T, own):
     assert not out.any() and torch.isneginf(lse).all()
     for got, want in ((run(T, low), run(T, 0)), (run(low, own), run(0, own))):
         assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+# ---- weights' bits -------------------------------------------------------------------------------------------------
+
+def _verbatim(x, sec):
+    """Packed rows whose chunks are zeros or kept as they are: at most every fourth chunk of x is not zero, so that the median
+    norm is zero and every other chunk lies above it."""
+    g = gpu_encode(x.to(torch.float16).to(DEV), sec, 6, 3.0)
+    back = torch.empty(x.shape, dtype=torch.float16, device=DEV)
+    hq.hqmq_decode(g.params, g.bufs, sec, back)
+    assert torch.equal(back.cpu(), x.to(torch.float16))
+    return g
+
+
+@pytest.mark.parametrize("M", [10, 20, 33])
+@pytest.mark.parametrize("D", [128, 96, 64])
+@pytest.mark.parametrize("rise", [16.5, 20.5, 24.5, 25.5, 26.5, 30.5])
+def test_shared_weights_far_below_a_later_one(M, D, rise):
+    """Scores 0 of 32 tokens, 4.9 of the next 32, then one of `rise` and some far below, in the log2 domain: the middle ones' weights are down to
+    2^-26 of the last one's, and their values as much larger.  One value per token and query row counts, so that the result is the
+    weighted sum of the middle tokens' values.  A weight is off by 2^-22 of itself or 2^-34 of the largest one (fp16 pairs), 11 bits where it
+    is one fp16; arithmetic and exponents 1e-4, the result 2^-11."""
+    B, H, G, T, S = 1, 256, 4, 96, 16
+    sec = torch.stack([_secs(23, 1, S)[0][0]] * H).to(DEV)
+    s2 = torch.full((T,), -90.0)
+    s2[:32], s2[32:64], s2[64] = 0.0, 4.9, rise
+    k, v = torch.zeros(B, H, T, D), torch.zeros(B, H, T, D)
+    k[..., 0] = s2.to(torch.float16)
+    v[:, :, 32:64, :8] = 6e4 * (0.5 + 0.5 * torch.rand(B, H, 32, 8, generator=_gen(2300)))
+    gk, gv = _verbatim(k, sec), _verbatim(v, sec)
+    q = torch.zeros(M, H * G, D, dtype=torch.float16)
+    q[..., 0] = 1.0
+    scale = math.log(2.0)
+    out, lse = torch.full((M, H * G, D), float("nan"), dtype=torch.float16, device=DEV), torch.empty(M, H * G, device=DEV)
+    ws = torch.empty(hq.hqmq_attend_shared_workspace_bytes(gk.params, M, H * G), dtype=torch.uint8, device=DEV)
+    hq.hqmq_attend_shared(gk.params, q.to(DEV), scale, gk.bufs, sec, gv.bufs, sec, out, ws, lse=lse)
+    torch.cuda.synchronize()
+    w = torch.exp2(k[0, 0, :, 0].to(torch.float16).double() - rise)
+    v64 = v[0].to(torch.float16).double()
+    want = (w[:, None] * v64).sum(1) / w.sum()  # [H, D]
+    one = 2.0 ** -11 if M * G > 64 else 0.0
+    bound = (2.0 ** -11 + 1e-4 + one) * want + 2.0 ** -34 * v64.sum(1) + 2.0 ** -24
+    got = out.cpu().double().view(M, H, G, D)
+    err = (got - want[None, :, None]).abs()
+    assert (want[:, :8] > 0.02).all()
+    assert (err <= bound[None, :, None]).all(), (err.max().item(), want.max().item(), got.max().item())
