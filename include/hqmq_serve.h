@@ -46,8 +46,7 @@ typedef struct hqmq_own_tokens {
  *     o = (sum_t e^{s_t - M} V_hat_t + sum_u e^{s'_u - M} V_hat'_u) / (the same sums without V),  s = scale <q, K_hat>
  * K_hat and V_hat are the fp16 tensors hqmq_decode returns (up to the last fp32 bit before that rounding).  Products
  * are accumulated in fp32, the softmax subtracts a running maximum, the result is rounded once to fp16.  The softmax weights
- * enter the products with V with 22 significant bits, those of a prefix that more than 64 query rows of a kv head share with
- * 11 (fp16): each is then off by at most 2^-11 of itself, about as much as the result's own rounding.
+ * enter the products with V with 22 significant bits.
  *   params      HOST; the prefix tensors': B prefixes, H, T, D (64, 96 or 128), S, b_r (strides are ignored).
  *   n_share     1 .. HQMQ_MAX_SHARE sequences per prefix; several query positions of one sequence are sequences here.
  *   n_q_heads   a multiple of H, at most 16 * H; query head hq reads kv head hq / (n_q_heads / H).

@@ -8,13 +8,14 @@
 //
 // What bounds it depends on the rows.  Up to 64 of them: the reconstruction, 40 vector instructions and some 60 cycles of LDS per 64 chunks
 // (8 heads x 32771 tokens x 64, 24 rows a head: 27 us, of which the products take 2; 64 heads x 2049 x 96, 12 rows: 24).  256 rows: the
-// products beside the softmax's exponentials and roundings, 8 heads x 32768 x 128 in 65 us or 530 TFLOP/s, where a large product of two
-// matrices would take 30.  Measured at 256 rows: two groups of four waves that reconstruct and multiply in turn 124 us, eight alike 104,
-// four that reconstruct for eight 86, and with a tile's weights computed between the last one's products and rows written in whole lines 64.
-// 64 columns per wave spill (247 us).
+// products beside the softmax's exponentials and roundings, 8 heads x 32768 x 128 in 74 us or 460 TFLOP/s, where a large product of two
+// matrices would take 30.  Measured at 256 rows, with one fp16 number per weight: two groups of four waves that reconstruct and multiply in
+// turn 124 us, eight alike 104, four that reconstruct for eight 86, and with a tile's weights computed between the last one's products and
+// rows written in whole lines 64.  64 columns per wave spill (247 us).
 //
-// The weights: fp16 pairs (22 bits) up to 64 rows, where the second product hardly shows; one fp16 (11 bits) for more, where it was
-// 13 us of 78.  Each weight is then off by 2^-11 of itself at most, either way, in a sum that is rounded to fp16.
+// The weights enter the second product as fp16 pairs, 22 bits, whatever the number of rows.  One fp16 number each, 11 bits, would take
+// 63 us instead of 74 at 256 rows x 128, 42 instead of 47 x 64, 51 instead of 54 at 96 rows x 128, and a row in which one token has nearly all
+// of the weight would be off by up to 2^-11 of it besides the result's own rounding.
 #include "hqmq_limits.h"
 #include "hqmq_packed.h"
 
@@ -92,7 +93,6 @@ __global__ __launch_bounds__(F::kThreads, F::kPerSimd) void k_shared(Geometry g,
     constexpr int kTok = tile_tokens<kNc>(), kD = 4 * kNc;
     constexpr int kCols = F::kCols, kBufs = F::kBufs, kThreads = F::kThreads, kWaves = kThreads / 64;
     constexpr bool kWide = kCols == 32;           // 32x32x16 products, else 16x16x32
-    constexpr bool kPairs = !kWide;               // weights as pairs of fp16 values, 22 bits
     constexpr int kSteps = kWide ? kD / 16 : kD / 32;
     constexpr int kBlocks = kWide ? kD / 32 : kD / 16;
     constexpr int kRegs = kWide ? 16 : 4;         // of a block's result
@@ -357,7 +357,22 @@ __global__ __launch_bounds__(F::kThreads, F::kPerSimd) void k_shared(Geometry g,
     };
     constexpr int kS = kWide ? 16 : 8;  // scores of a lane and 32 tokens; wide: token 8 (i / 4) + 4 kgrp + i % 4; else 16 (i / 4) + 4 kgrp + i % 4
     constexpr int kU = kWide ? 2 : 1;   // products of 32 tokens' values per block
-    half8_t held[kU] = {};              // two tiles in LDS: the last tile's weights, whose values are still to come
+    half8_t held[2][kU] = {};           // two tiles in LDS: the last tile's weights, whose values are still to come
+    // Weights enter the products as pairs of fp16 values: 22 bits.
+    const auto set_pairs = [](half8_t (*to)[kU], int i, float p0, float p1) {  // of weights i and i + 1
+        typedef float float2_t __attribute__((ext_vector_type(2)));
+        typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
+        const half2_t hi = __builtin_convertvector(float2_t{p0, p1}, half2_t);
+        const uint32_t both = __builtin_bit_cast(uint32_t, hi);
+        float r0, r1;  // p - hi in one instruction each; the compiler converts first
+        asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel_hi:[1,0,0]" : "=v"(r0) : "v"(both), "v"(p0));
+        asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "=v"(r1) : "v"(both), "v"(p1));
+        const half2_t lo = __builtin_convertvector(float2_t{r0, r1}, half2_t);
+        to[0][i >> 3][i & 7] = hi[0];
+        to[0][i >> 3][(i & 7) + 1] = hi[1];
+        to[1][i >> 3][i & 7] = lo[0];
+        to[1][i >> 3][(i & 7) + 1] = lo[1];
+    };
     // Scores of 32 tokens from t0 on, the factor that is still missing from them, and m_ref raised if need be.
     // Weights are 2^(s - m_ref): with m_ref some 10 below the largest score seen they reach 2^10, their fp16 values are normal numbers
     // down to 2^-24 of the largest, and m_ref is raised (and what was summed scaled) only when a score would pass 2^15, so hardly
@@ -412,10 +427,10 @@ __global__ __launch_bounds__(F::kThreads, F::kPerSimd) void k_shared(Geometry g,
                     acc[k][i] *= corr;
             if constexpr (kBufs == 2)  // in fp32: the factor alone may be less than any fp16 number, or a coarse one
 #pragma unroll
-                for (int u = 0; u < kU; ++u)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        held[u][i] = (_Float16)((float)held[u][i] * corr);
+                for (int i = 0; i < kS; i += 2) {
+                    const half8_t hi = held[0][i >> 3], lo = held[1][i >> 3];
+                    set_pairs(held, i, ((float)hi[i & 7] + (float)lo[i & 7]) * corr, ((float)hi[(i & 7) + 1] + (float)lo[(i & 7) + 1]) * corr);
+                }
         }
         return mul;
     };
@@ -428,10 +443,11 @@ __global__ __launch_bounds__(F::kThreads, F::kPerSimd) void k_shared(Geometry g,
         else
             acc[k] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, p, acc[k], 0, 0, 0);
     };
-    auto weight = [&](const float *s, float mul, int i) {
-        const float p = __builtin_amdgcn_exp2f(fmaf(s[i], mul, -m_ref));
-        l_run += p;
-        return p;
+    auto weights = [&](const float *s, float mul, int i, half8_t (*to)[kU]) {
+        const float p0 = __builtin_amdgcn_exp2f(fmaf(s[i], mul, -m_ref)), p1 = __builtin_amdgcn_exp2f(fmaf(s[i + 1], mul, -m_ref));
+        l_run += p0;
+        l_run += p1;
+        set_pairs(to, i, p0, p1);
     };
     // One tile in LDS: scores, weights, products with the values.
     auto attend = [&](int j) {
@@ -439,14 +455,10 @@ __global__ __launch_bounds__(F::kThreads, F::kPerSimd) void k_shared(Geometry g,
         for (int sub = 0; sub < kTok; sub += 32) {
             float s[kS];
             const float mul = scores(reinterpret_cast<const _Float16 *>(key_tiles) + sub * key_pitch<kNc>(), begin + j * kTok + sub, s);
-            half8_t hi[kU], lo[kU];
+            half8_t p[2][kU];
 #pragma unroll
-            for (int i = 0; i < kS; ++i) {
-                const float p = weight(s, mul, i);
-                hi[i >> 3][i & 7] = (_Float16)p;
-                if (kPairs)
-                    lo[i >> 3][i & 7] = (_Float16)(p - (float)hi[i >> 3][i & 7]);
-            }
+            for (int i = 0; i < kS; i += 2)
+                weights(s, mul, i, p);
             const _Float16 *values = reinterpret_cast<const _Float16 *>(value_tiles) + sub;
 #pragma unroll
             for (int u = 0; u < kU; ++u) {
@@ -455,12 +467,10 @@ __global__ __launch_bounds__(F::kThreads, F::kPerSimd) void k_shared(Geometry g,
                 for (int k = 0; k < kBlocks; ++k)
                     v[k] = value_operand(values, k, u);
 #pragma unroll
-                for (int k = 0; k < kBlocks; ++k)
-                    multiply(v[k], hi[u], k);
-                if (kPairs)
+                for (int half = 0; half < 2; ++half)
 #pragma unroll
                     for (int k = 0; k < kBlocks; ++k)
-                        multiply(v[k], lo[u], k);
+                        multiply(v[k], p[half][u], k);
             }
         }
     };
@@ -469,26 +479,30 @@ __global__ __launch_bounds__(F::kThreads, F::kPerSimd) void k_shared(Geometry g,
     auto attend_held = [&](const _Float16 *keys, const _Float16 *last_values, int t0, bool first) {
         float s[kS];
         const float mul = scores(keys, t0, s);
-        half8_t next[kU];
+        half8_t next[2][kU];
         if (first) {
 #pragma unroll
-            for (int i = 0; i < kS; ++i)
-                next[i >> 3][i & 7] = (_Float16)weight(s, mul, i);
+            for (int i = 0; i < kS; i += 2)
+                weights(s, mul, i, next);
         } else {
 #pragma unroll
             for (int n = 0; n < kU * kBlocks; ++n) {
                 const int u = n / kBlocks, k = n % kBlocks;
-                multiply(value_operand(last_values, k, u), held[u], k);
-                const int i0 = n * kS / (kU * kBlocks), i1 = (n + 1) * kS / (kU * kBlocks);
+                const half8_t v = value_operand(last_values, k, u);
+                multiply(v, held[0][u], k);
+                const int i0 = 2 * (n * kS / 2 / (kU * kBlocks)), i1 = 2 * ((n + 1) * kS / 2 / (kU * kBlocks));
 #pragma unroll
-                for (int i = i0; i < i1; ++i)
-                    next[i >> 3][i & 7] = (_Float16)weight(s, mul, i);
+                for (int i = i0; i < i1; i += 2)
+                    weights(s, mul, i, next);
+                multiply(v, held[1][u], k);
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
 #pragma unroll
-        for (int u = 0; u < kU; ++u)
-            held[u] = next[u];
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int u = 0; u < kU; ++u)
+                held[half][u] = next[half][u];
     };
 
     // ---- the loop -------------------------------------------------------------------------------------------------------------
@@ -549,7 +563,9 @@ __global__ __launch_bounds__(F::kThreads, F::kPerSimd) void k_shared(Geometry g,
         if (has_cols && n_tiles > 0)
 #pragma unroll
             for (int n = 0; n < kU * kBlocks; ++n)
-                multiply(value_operand(last, n % kBlocks, n / kBlocks), held[n / kBlocks], n % kBlocks);
+#pragma unroll
+                for (int half = 0; half < 2; ++half)
+                    multiply(value_operand(last, n % kBlocks, n / kBlocks), held[half][n / kBlocks], n % kBlocks);
     }
     if constexpr (kBufs == 2)
         lds_barrier();  // what follows is written over the last values, which slower waves may still read

@@ -10,6 +10,7 @@ import torch
 
 import paper_2605_27646_amd as hq
 from gpu_util import gpu_encode
+import test_gpu_serve as serve
 from test_gpu_serve import DEV, Cache, _gen, _secs
 
 pytestmark = pytest.mark.gpu
@@ -154,8 +155,8 @@ def _verbatim(x, sec):
 def test_shared_weights_far_below_a_later_one(M, D, rise):
     """Scores 0 of 32 tokens, 4.9 of the next 32, then one of `rise` and some far below, in the log2 domain: the middle ones' weights are down to
     2^-26 of the last one's, and their values as much larger.  One value per token and query row counts, so that the result is the
-    weighted sum of the middle tokens' values.  A weight is off by 2^-22 of itself or 2^-34 of the largest one (fp16 pairs), 11 bits where it
-    is one fp16; arithmetic and exponents 1e-4, the result 2^-11."""
+    weighted sum of the middle tokens' values.  A weight is off by 2^-22 of itself or 2^-34 of the largest one (fp16 pairs); arithmetic
+    and exponents 1e-4, the result 2^-11."""
     B, H, G, T, S = 1, 256, 4, 96, 16
     sec = torch.stack([_secs(23, 1, S)[0][0]] * H).to(DEV)
     s2 = torch.full((T,), -90.0)
@@ -174,9 +175,43 @@ def test_shared_weights_far_below_a_later_one(M, D, rise):
     w = torch.exp2(k[0, 0, :, 0].to(torch.float16).double() - rise)
     v64 = v[0].to(torch.float16).double()
     want = (w[:, None] * v64).sum(1) / w.sum()  # [H, D]
-    one = 2.0 ** -11 if M * G > 64 else 0.0
-    bound = (2.0 ** -11 + 1e-4 + one) * want + 2.0 ** -34 * v64.sum(1) + 2.0 ** -24
+    bound = (2.0 ** -11 + 1e-4) * want + 2.0 ** -34 * v64.sum(1) + 2.0 ** -24
     got = out.cpu().double().view(M, H, G, D)
     err = (got - want[None, :, None]).abs()
     assert (want[:, :8] > 0.02).all()
     assert (err <= bound[None, :, None]).all(), (err.max().item(), want.max().item(), got.max().item())
+
+
+def _check_by_sixty_four(got, lse, q, scale, K, V, visible, own_kv, own_visible, B, M, H, G):
+    """test_gpu_serve._check_shared with its bound for up to 64 query rows of a kv head, whatever their number: 1e-4 of the weighted sum of
+    |V|, of which weights of 22 bits take 2^-22."""
+    class Some:
+        def __init__(self, c, first, end):
+            self.hat, self.slack = c.hat[first:end], c.slack[first:end]
+
+    step = 64 // G
+    for b in range(B):
+        for first in range(b * M, (b + 1) * M, step):
+            seq = slice(first, min(first + step, (b + 1) * M))
+            cut = lambda x: None if x is None else x[seq]  # noqa: E731
+            of_seq = None if own_kv is None else tuple(Some(c, seq.start, seq.stop) for c in own_kv)
+            serve_check(got[seq], lse[seq], q[seq], scale, Some(K, b, b + 1), Some(V, b, b + 1), cut(visible), of_seq, cut(own_visible), 1,
+                        seq.stop - seq.start, H, G)
+
+
+serve_check = serve._check_shared
+
+
+@pytest.fixture
+def tight(monkeypatch):
+    """serve._shared, its outputs held to 22-bit weights at every number of query rows."""
+    monkeypatch.setattr(serve, "_check_shared", _check_by_sixty_four)
+    return serve._shared
+
+
+@pytest.mark.parametrize("M,G,own", [(17, 4, 0), (32, 4, 30), (9, 11, 0), (33, 4, 0), (64, 4, 30), (65, 4, 0), (20, 16, 7)])
+@pytest.mark.parametrize("D", [128, 96, 64])
+@pytest.mark.parametrize("gain", [30.0, 2.0])
+def test_shared_weights_of_many_rows(tight, M, G, own, D, gain):
+    """One token with nearly all of the weight, and many: no query row's weights have fewer bits for there being more rows."""
+    tight(2500 + M + D, 1, M, 2, G, 333, D, 24, own=own, gain=gain)
