@@ -4,6 +4,7 @@ only, as in binding.py; the same conventions on buffers and streams."""
 from __future__ import annotations
 
 import ctypes as C
+import functools
 
 import torch
 
@@ -53,6 +54,25 @@ def _on_this_device(*tensors) -> None:
             raise ValueError("every tensor must be on torch's current device")
 
 
+@functools.lru_cache(maxsize=1024)
+def _row_bytes(params: bytes) -> tuple:
+    info = hqmq_sizes(HqmqParams.from_buffer_copy(params))
+    return info.code_bytes, info.sigma_bytes, info.flag_bytes, info.row_off_bytes
+
+
+def _hold_rows(params: HqmqParams, enc: EncodedBuffers) -> torch.Tensor:
+    """What a call reads of a packed tensor is long enough for the rows that params describes, which the library cannot know, and on
+    one device: that of the code words, which are returned."""
+    c, s, f, r, o = enc.codes, enc.sigma, enc.flags, enc.row_off, enc.outliers
+    n_c, n_s, n_f, n_r = _row_bytes(bytes(params))
+    if (c.nbytes < n_c or s.nbytes < n_s or f.nbytes < n_f or r.nbytes < n_r or o.nbytes < 8 * o.shape[0]
+            or not (c.is_contiguous() and s.is_contiguous() and f.is_contiguous() and r.is_contiguous() and o.is_contiguous())
+            or not (c.get_device() == s.get_device() == f.get_device() == r.get_device() == o.get_device())):
+        raise ValueError(f"codes, sigma, flags, row_off and outliers must be contiguous, on one device, and hold {n_c}, {n_s}, {n_f}, {n_r} "
+                         "bytes and 8 per payload")
+    return c
+
+
 def _rows_of(name, t, dtype, shape) -> None:
     if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous {str(dtype)[6:]} {list(shape)}")
@@ -72,6 +92,7 @@ def _hold(params: HqmqParams, encs) -> None:
     need = {"codes": info.code_bytes, "sigma": info.sigma_bytes, "flags": info.flag_bytes, "row_off": info.row_off_bytes,
             "outliers": 0, "n_outliers": info.n_outliers_bytes, "status": info.status_bytes}
     for e in encs:
+        _hold_rows(params, e)
         for name, nbytes in need.items():
             t = getattr(e, name)
             if not t.is_contiguous() or t.numel() * t.element_size() < nbytes:
@@ -85,6 +106,7 @@ class OwnTokens:
 
     def __init__(self, params: HqmqParams, enc_k: EncodedBuffers, enc_v: EncodedBuffers, visible: torch.Tensor | None = None):
         _hold(params, (enc_k, enc_v))
+        params = HqmqParams.from_buffer_copy(params)  # as they were checked
         self.params = params
         self.visible = visible
         self.keep = (enc_k, enc_v, enc_k.as_struct(), enc_v.as_struct())
@@ -116,7 +138,7 @@ def hqmq_attend_shared(params: HqmqParams, q: torch.Tensor, scale: float, enc_k:
         _rows_of("visible", visible, torch.int32, rows)
     if lse is not None:
         _rows_of("lse", lse, torch.float32, rows)
-    _on_this_device(q, out, sec_k, sec_v, workspace, visible, lse, enc_k.codes, enc_v.codes)
+    _on_this_device(q, out, sec_k, sec_v, workspace, visible, lse, _hold_rows(params, enc_k), _hold_rows(params, enc_v))
     if own is not None:
         if own.visible is not None:
             _rows_of("the own tokens' visible", own.visible, torch.int32, rows)
@@ -149,7 +171,7 @@ def hqmq_attend_mass(params: HqmqParams, q: torch.Tensor, scale: float, enc_k: E
     _rows_of("sec", sec_k, torch.float32, (params.H, params.S, 4))
     if visible is not None:
         _rows_of("visible", visible, torch.int32, rows)
-    _on_this_device(q, sec_k, lse, mass, out, visible, enc_k.codes)
+    _on_this_device(q, sec_k, lse, mass, out, visible, _hold_rows(params, enc_k))
     rc = _load().hqmq_attend_mass(C.byref(params), n_share, rows[1], q.data_ptr(), float(scale),
                                   C.byref(enc_k.as_struct()), enc_k.outlier_capacity, sec_k.data_ptr(), lse.data_ptr(),
                                   None if visible is None else visible.data_ptr(), None if mass is None else mass.data_ptr(),
@@ -220,7 +242,7 @@ class CompactBatch:
         _on_this_device(*keeps, workspace)
         if not workspace.is_contiguous():
             raise ValueError("workspace must be contiguous")
-        self.params = params
+        self.params = HqmqParams.from_buffer_copy(params)  # as they were checked
         self.n = n
         self.n_keep = n_keep
         self.workspace = workspace

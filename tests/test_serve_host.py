@@ -217,3 +217,39 @@ def test_limits_far_below_zero(tmp_path):
     assert res.returncode == 0, res.stderr
     source = open(os.path.join(include, "hqmq_attend.hip")).read()
     assert source.count("a.visible[") == source.count("seen_tokens(a.visible[") == 2
+
+
+def _with(enc, **kw):
+    return hq.EncodedBuffers(**{**{n: getattr(enc, n) for n in ("codes", "sigma", "flags", "row_off", "outliers", "n_outliers", "status")}, **kw})
+
+
+def test_prefixes_of_short_buffers_are_refused():
+    """Every part that attention and weights read is looked at: fewer rows than params says, parts that only look long enough, a
+    list that has fewer bytes than payloads."""
+    p, fewer = _params(), _params(T=900, stride_b=4 * 900 * 128, stride_h=900 * 128)
+    full, short = hq.alloc_encoded(p, "cpu", 10), hq.alloc_encoded(fewer, "cpu", 10)
+    q, out, sec = torch.zeros(6, 8, 128, dtype=torch.float16), torch.zeros(6, 8, 128, dtype=torch.float16), torch.zeros(4, 64, 4)
+    ws = torch.zeros(1 << 20, dtype=torch.uint8)
+    bad = [short] + [_with(full, **{n: getattr(short, n)}) for n in ("codes", "sigma", "flags", "row_off")]
+    bad += [_with(full, flags=full.flags[:1].expand(full.flags.shape)), _with(full, row_off=full.row_off[:-1]),
+            _with(full, outliers=full.outliers[:, 0].contiguous()), _with(full, outliers=full.outliers[:, :2])]
+    for e in bad:
+        for k, v in ((e, full), (full, e)):
+            with pytest.raises(ValueError, match="hold"):
+                hq.hqmq_attend_shared(p, q, 0.1, k, sec, v, sec, out, ws)
+        with pytest.raises(ValueError, match="hold"):
+            hq.hqmq_attend_mass(p, q, 0.1, e, sec, torch.zeros(6, 8), torch.zeros(2, 4, 1000))
+    grown = _params()
+    for _ in range(2):
+        assert serving._hold_rows(grown, full) is full.codes
+    grown.T = 1001
+    with pytest.raises(ValueError, match="hold"):
+        serving._hold_rows(grown, full)
+
+
+def test_params_are_as_they_were_checked():
+    p = _params()
+    full = hq.alloc_encoded(p, "cpu", 10)
+    own = hq.OwnTokens(p, full, full)
+    p.T = 5000
+    assert own.params.T == 1000 and own.struct.params.contents.T == 1000
