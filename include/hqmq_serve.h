@@ -65,7 +65,8 @@ typedef struct hqmq_own_tokens {
  *               head saw, -infinity where that is nothing.
  *   workspace_dev  DEVICE, 256-byte aligned, hqmq_attend_shared_workspace_bytes().
  * Errors: INVALID_ARG (null / misaligned pointer, bad n_q_heads or n_share, non-finite scale, own tokens of another
- * shape), UNSUPPORTED (as hqmq_attend; B * n_share * H above 65535), BUFFER_TOO_SMALL, HIP. */
+ * shape), UNSUPPORTED (as hqmq_attend; B * n_share * H at 2^18 or above, with own tokens above 65535), BUFFER_TOO_SMALL,
+ * HIP. */
 int32_t hqmq_attend_shared(const hqmq_params *params, int32_t n_share, int32_t n_q_heads, const void *q_dev, float scale,
                            const hqmq_encoded *enc_k, uint64_t cap_k, const float *sec_k_dev,
                            const hqmq_encoded *enc_v, uint64_t cap_v, const float *sec_v_dev,
@@ -88,7 +89,7 @@ uint64_t hqmq_attend_shared_workspace_bytes(const hqmq_params *params, int32_t n
  *   mass_in_dev DEVICE, fp32 [B][H][T]; not read, and may be NULL, if decay is 0.
  *   decay       finite.
  *   mass_out_dev  DEVICE, out, fp32 [B][H][T]; may be mass_in_dev itself.
- * Errors: as hqmq_attend_shared. */
+ * Errors: as hqmq_attend_shared, but any B * n_share * H. */
 int32_t hqmq_attend_mass(const hqmq_params *params, int32_t n_share, int32_t n_q_heads, const void *q_dev, float scale,
                          const hqmq_encoded *enc_k, uint64_t cap_k, const float *sec_k_dev, const float *lse_dev,
                          const int32_t *visible_dev, const float *mass_in_dev, float decay, float *mass_out_dev,

@@ -912,9 +912,15 @@ static int32_t check_share(const hqmq_params *params, int32_t n_share, int32_t n
         return rc;
     if (n_share < 1 || n_share > HQMQ_MAX_SHARE)
         return HQMQ_ERR_INVALID_ARG;
-    if ((int64_t)params->B * n_share * params->H > 65535)
-        return HQMQ_ERR_UNSUPPORTED;  // grid.y of the own tokens
     return HQMQ_OK;
+}
+
+static int32_t check_shared(const hqmq_params *params, int32_t n_share, int32_t n_q_heads)
+{
+    const int32_t rc = check_share(params, n_share, n_q_heads);
+    if (rc == HQMQ_OK && (int64_t)params->B * n_share * params->H >= (1 << 18))
+        return HQMQ_ERR_UNSUPPORTED;  // the merge: up to 1024 threads for each of 16 query heads of these, fewer than 2^32
+    return rc;                        // own tokens: 65535 at most (check_own)
 }
 
 static int32_t check_own(const hqmq_params *params, int32_t n_share, const hqmq_params *own)
@@ -970,7 +976,7 @@ static SharedLayout shared_layout(const hqmq_params *params, int G, int n_share,
 extern "C" uint64_t hqmq_attend_shared_workspace_bytes(const hqmq_params *params, int32_t n_share, int32_t n_q_heads,
                                                        const hqmq_params *own_params)
 {
-    if (check_share(params, n_share, n_q_heads) != HQMQ_OK || (own_params && check_own(params, n_share, own_params) != HQMQ_OK))
+    if (check_shared(params, n_share, n_q_heads) != HQMQ_OK || (own_params && check_own(params, n_share, own_params) != HQMQ_OK))
         return 0;
     return shared_layout(params, n_q_heads / params->H, n_share, own_params).total;
 }
@@ -981,7 +987,7 @@ extern "C" int32_t hqmq_attend_shared(const hqmq_params *params, int32_t n_share
                                       const int32_t *visible_dev, const hqmq_own_tokens *own, void *out_dev, float *lse_dev,
                                       void *workspace_dev, uint64_t workspace_bytes, void *stream)
 {
-    int32_t rc = check_share(params, n_share, n_q_heads);
+    int32_t rc = check_shared(params, n_share, n_q_heads);
     if (rc != HQMQ_OK)
         return rc;
     if (!q_dev || !out_dev || !sec_k_dev || !sec_v_dev || !workspace_dev || !std::isfinite(scale))

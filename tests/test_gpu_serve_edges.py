@@ -215,3 +215,12 @@ def tight(monkeypatch):
 def test_shared_weights_of_many_rows(tight, M, G, own, D, gain):
     """One token with nearly all of the weight, and many: no query row's weights have fewer bits for there being more rows."""
     tight(2500 + M + D, 1, M, 2, G, 333, D, 24, own=own, gain=gain)
+
+
+# ---- many rows -----------------------------------------------------------------------------------------------------
+
+def test_windows_of_many_positions(tight):
+    """The last 1024 positions of two prompts: four workgroups' rows of each kv head, 65536 query heads in all."""
+    tight(2700, 2, 1024, 32, 1, 40, 64, 16, limits="ragged")
+    tight(2710, 1, 1024, 2, 2, 70, 128, 16)
+    serve._mass(2720, 2, 1024, 32, 1, 40, 64, 16, limits="ragged")

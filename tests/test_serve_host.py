@@ -253,3 +253,17 @@ def test_params_are_as_they_were_checked():
     own = hq.OwnTokens(p, full, full)
     p.T = 5000
     assert own.params.T == 1000 and own.struct.params.contents.T == 1000
+
+
+def test_windows_of_many_positions_are_taken(lib):
+    """Two prompts' last 1024 positions, 32 kv heads: 65536 times B * n_share * H, which only own tokens are too many for.  (The calls
+    end at a missing buffer, which is looked at later.)"""
+    p = _params(B=2, H=32, T=1000, stride_b=32 * 1000 * 128)
+    assert hq.hqmq_attend_shared_workspace_bytes(p, 1024, 32) > 0 and _shared(lib, params=p, n_share=1024, heads=32, ws_bytes=100) == SMALL
+    own = _params(B=2048, H=32, T=10, stride_b=32 * 10 * 128, stride_h=10 * 128)
+    assert hq.hqmq_attend_shared_workspace_bytes(p, 1024, 32, own) == 0
+    assert _shared(lib, params=p, n_share=1024, heads=32, own=_own(own)) == UNSUPPORTED
+    last = _params(B=255, H=257, T=10, stride_b=257 * 10 * 128, stride_h=10 * 128)  # 65535 heads
+    assert hq.hqmq_attend_shared_workspace_bytes(last, 4, 257) > 0 and hq.hqmq_attend_shared_workspace_bytes(last, 5, 257) == 0
+    for params, share, heads in ((p, 1024, 32), (last, 1024, 257 * 16)):
+        assert lib.hqmq_attend_mass(C.byref(params), share, heads, P, 0.1, C.byref(_enc(sigma=0)), 5, P, P, None, P, 1.0, P, None) == INVALID
