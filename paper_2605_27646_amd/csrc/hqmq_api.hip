@@ -1229,7 +1229,7 @@ extern "C" int32_t hqmq_evict_compact(const hqmq_params *params, int32_t n_keep,
         for (int32_t j = 0; j < n_tensors; ++j)
             if (out[i].codes == enc[j].codes || out[i].sigma == enc[j].sigma || out[i].flags == enc[j].flags ||
                 out[i].row_off == enc[j].row_off || (out_capacity[i] > 0 && out[i].outliers == enc[j].outliers) ||
-                out[i].status == enc[j].status ||
+                out[i].n_outliers == enc[j].n_outliers || out[i].status == enc[j].status ||
                 (i != j && (out[i].codes == out[j].codes || out[i].sigma == out[j].sigma || out[i].flags == out[j].flags ||
                             out[i].row_off == out[j].row_off || (out_capacity[i] > 0 && out[i].outliers == out[j].outliers) ||
                             out[i].n_outliers == out[j].n_outliers || out[i].status == out[j].status)))

@@ -267,3 +267,15 @@ def test_windows_of_many_positions_are_taken(lib):
     assert hq.hqmq_attend_shared_workspace_bytes(last, 4, 257) > 0 and hq.hqmq_attend_shared_workspace_bytes(last, 5, 257) == 0
     for params, share, heads in ((p, 1024, 32), (last, 1024, 257 * 16)):
         assert lib.hqmq_attend_mass(C.byref(params), share, heads, P, 0.1, C.byref(_enc(sigma=0)), 5, P, P, None, P, 1.0, P, None) == INVALID
+
+
+@pytest.mark.parametrize("name", ["codes", "sigma", "flags", "row_off", "outliers", "n_outliers", "status"])
+def test_compact_refuses_every_buffer_of_a_given_tensor(lib, name):
+    params, caps, keep = _params(), (C.c_uint64 * 2)(5, 5), (C.c_void_p * 2)(P, P)
+    enc = (binding._Encoded * 2)(_enc(P), _enc(2 * P))
+    at = getattr(enc[1], name)
+    out = (binding._Encoded * 2)(_enc(3 * P, **{name: at}), _enc(4 * P))
+    args = (C.byref(params), 10, 2, enc, caps, keep)
+    assert lib.hqmq_evict_compact(*args, out, caps, P, 1 << 40, None) == INVALID
+    out = (binding._Encoded * 2)(_enc(3 * P), _enc(4 * P))
+    assert lib.hqmq_evict_compact(*args, out, caps, P, 16, None) == SMALL  # apart: the next check is the workspace's
