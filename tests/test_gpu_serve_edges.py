@@ -224,3 +224,74 @@ def test_windows_of_many_positions(tight):
     tight(2700, 2, 1024, 32, 1, 40, 64, 16, limits="ragged")
     tight(2710, 1, 1024, 2, 2, 70, 128, 16)
     serve._mass(2720, 2, 1024, 32, 1, 40, 64, 16, limits="ragged")
+
+
+# ---- every form of the attention -----------------------------------------------------------------------------------
+
+def _shares(B, M, H, G, T, D, S):
+    """Workgroups along the prefix that the call plans: its workspace has 130 floats for each of them and query head."""
+    p = hq.HqmqParams(B, H, T, D, H * T * D, T * D, D, S, 6, 3.0, 0)
+    return hq.hqmq_attend_shared_workspace_bytes(p, M, H * G) // (B * M * H * G * 520)
+
+
+@pytest.mark.parametrize("M,G", [(3, 4), (25, 4), (35, 4), (65, 4)])
+@pytest.mark.parametrize("D", [128, 96, 64])
+@pytest.mark.parametrize("S", [5, 512, 700, 1024, 2730])
+def test_shared_codebooks_of_every_form(tight, M, G, D, S):
+    """Up to 64, 128, 256 query rows and more, of powers of two and others, with tables of directions and without (from 600 secondaries
+    on, more than 128 rows from 900)."""
+    tight(2800 + M + D + S, 1, M, 1, G, 170, D, S, 4 if S == 5 else 6)
+
+
+@pytest.mark.parametrize("M", [30, 40])
+@pytest.mark.parametrize("D", [128, 96, 64])
+@pytest.mark.parametrize("Cmul,capacity,kgain,gain", [
+    (0.3, None, 1.0, 1.0), (1.2, 37, 1.0, 1.0), (3.0, 0, 1.0, 1.0), (3.0, None, 9000.0, 1e-3), (3.0, None, 1e-4, 3.0),
+])
+def test_shared_outliers_and_ranges_of_many_rows(tight, M, D, Cmul, capacity, kgain, gain):
+    """The careful form beside more than 64 and 128 rows: saturating scales, payloads past the staged ones, lists too short."""
+    tight(2900 + M + D, 1, M, 2, 4, 321, D, 64, 6, Cmul=Cmul, capacity=capacity, kgain=kgain, gain=gain)
+
+
+@pytest.mark.parametrize("B,M,G,D,T,Cmul,limits", [
+    (64, 35, 4, 128, 333, 3.0, None), (64, 35, 4, 128, 257, 0.5, "ragged"), (64, 33, 4, 96, 333, 3.0, "some"), (64, 40, 4, 64, 500, 1.2, "ragged"),
+    (128, 25, 4, 128, 333, 1.2, "ragged"), (192, 3, 4, 128, 333, 1.2, "ragged"), (32, 70, 4, 128, 130, 1.2, "ragged"),
+])
+def test_shared_many_tiles_of_one_workgroup(tight, B, M, G, D, T, Cmul, limits):
+    """As many heads as the chip takes at once: a workgroup goes through all of its head's tiles."""
+    H = 4
+    assert _shares(B, M, H, G, T, D, 24) == 1
+    tight(3000 + M + D, B, M, H, G, T, D, 24, 6, limits=limits, Cmul=Cmul)
+
+
+@pytest.mark.parametrize("M,G,D,own", [(3, 4, 128, 20), (25, 4, 96, 200), (35, 4, 64, 90), (40, 8, 128, 300)])
+def test_shared_negative_scale(M, G, D, own):
+    """The scores of the negated queries: of the prefix to the bit, as its kernel takes the sign into the queries; hqmq_attend's, which own
+    tokens may take, into the product, whose fp32 sums need not round alike for both signs."""
+    H, T, S = 2, 270, 24
+    sk, sv = _secs(29, H, S)
+    k, v = Cache(3100, 1, H, T, D, sk), Cache(3101, 1, H, T, D, sv)
+    ok, ov = Cache(3102, M, H, own, D, sk), Cache(3103, M, H, own, D, sv)
+    q = torch.randn(M, H * G, D, generator=_gen(3104)).to(torch.float16)
+    ws = torch.empty(hq.hqmq_attend_shared_workspace_bytes(k.params, M, H * G, ok.params), dtype=torch.uint8, device=DEV)
+    tokens = hq.OwnTokens(ok.params, ok.bufs, ov.bufs)
+
+    def run(q, scale, tokens):
+        out, lse = torch.full(q.shape, float("nan"), dtype=torch.float16, device=DEV), torch.full((M, H * G), float("nan"), device=DEV)
+        hq.hqmq_attend_shared(k.params, q.to(DEV), scale, k.bufs, k.sec, v.bufs, v.sec, out, ws, own=tokens, lse=lse)
+        torch.cuda.synchronize()
+        return out.cpu(), lse.cpu()
+
+    got, want = run(q, -0.11, None), run(-q, 0.11, None)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    got = run(q, -0.11, tokens)
+    _check_by_sixty_four(got[0].numpy(), got[1].numpy().astype(np.float64), -q.numpy(), float(np.float32(0.11)), k.decoded(), v.decoded(), None,
+                         (ok.decoded(), ov.decoded()), None, 1, M, H, G)
+
+
+@pytest.mark.parametrize("B,M,H,G,D,T", [(140, 9, 6, 3, 128, 71), (129, 9, 6, 3, 96, 71), (65, 25, 8, 4, 64, 130), (66, 40, 4, 4, 128, 40), (1, 3, 2, 4, 64, 128)])
+@pytest.mark.parametrize("limits", [None, "some"])
+def test_shared_results_of_one_share(tight, B, M, H, G, D, T, limits):
+    """Where one workgroup has all of its rows' prefix it writes the result itself, without partial sums."""
+    assert _shares(B, M, H, G, T, D, 16) == 1
+    tight(3200 + B + M, B, M, H, G, T, D, 16, 4, limits=limits)
