@@ -216,7 +216,7 @@ def test_limits_far_below_zero(tmp_path):
     res = subprocess.run(["g++", "-std=c++17", "-fsyntax-only", "-I", include, str(src)], capture_output=True, text=True)
     assert res.returncode == 0, res.stderr
     source = open(os.path.join(include, "hqmq_attend.hip")).read()
-    assert source.count("a.visible[") == source.count("seen_tokens(a.visible[") == 2
+    assert source.count("a.visible[") == source.count("vis = seen_tokens(vis)") == 2
 
 
 def _with(enc, **kw):
