@@ -42,7 +42,8 @@ typedef struct hqmq_own_tokens {
 } hqmq_own_tokens;
 
 /* Attention of the generation step for a batch whose sequences share prefixes: sequence n = b * n_share + m reads the
- * packed prefix b, which is reconstructed once for all n_share of them, and then its own packed tokens:
+ * packed prefix b, which is reconstructed once for all n_share of them (up to 256 query rows n_share * n_q_heads / H of a kv
+ * head; once more for every further 256), and then its own packed tokens:
  *     o = (sum_t e^{s_t - M} V_hat_t + sum_u e^{s'_u - M} V_hat'_u) / (the same sums without V),  s = scale <q, K_hat>
  * K_hat and V_hat are the fp16 tensors hqmq_decode returns (up to the last fp32 bit before that rounding).  Products
  * are accumulated in fp32, the softmax subtracts a running maximum, the result is rounded once to fp16.  The softmax weights

@@ -6,12 +6,15 @@
 // stands.  Reconstructed keys and values (transposed) go through LDS, where the waves of a workgroup share them.  Workgroups split the
 // prefix; sums and maxima of the splits, in fp32, are joined by the merge of hqmq_attend where there is more than one.
 //
-// What bounds it depends on the rows.  Up to 64 of them: the reconstruction, 40 vector instructions and some 60 cycles of LDS per 64 chunks
-// (8 heads x 32771 tokens x 64, 24 rows a head: 27 us, of which the products take 2; 64 heads x 2049 x 96, 12 rows: 24).  256 rows: the
-// products beside the softmax's exponentials and roundings, 8 heads x 32768 x 128 in 74 us or 460 TFLOP/s, where a large product of two
-// matrices would take 30.  Measured at 256 rows, with one fp16 number per weight: two groups of four waves that reconstruct and multiply in
-// turn 124 us, eight alike 104, four that reconstruct for eight 86, and with a tile's weights computed between the last one's products and
-// rows written in whole lines 64.  64 columns per wave spill (247 us).
+// What bounds it depends on the rows.  Up to 64 of them the reconstruction, 40 vector instructions and some 60 cycles of LDS per 64 chunks,
+// but neither unit by itself: 8 heads x 32771 tokens x 64, 24 rows a head, 27 us, of which vector instructions issue for 48 % and the LDS
+// works for 43 %, while waves wait for 48 % of their cycles (reconstruct, barrier, multiply, barrier; 64 heads x 2049 x 96, 12 rows and
+// their own tokens: 31 us, 50, 37 and 49 %).  256 rows, 8 heads x 32768 x 128: 74 us for encoded normal values, 82 for channels of different
+// gain and uniformly drawn codewords, 420 to 460 TFLOP/s, where a large product of two matrices would take 30.  Of the 82 vector instructions
+// have 47 %, the matrix cores 25, the LDS 31, and waves wait for 44 % of their cycles: a barrier for every 32 tokens between those that
+// reconstruct and those that multiply.  Measured at 256 rows, with one fp16 number per weight: two groups of four waves that reconstruct and
+// multiply in turn 124 us, eight alike 104, four that reconstruct for eight 86, and with a tile's weights computed between the last one's
+// products and rows written in whole lines 64.  64 columns per wave spill (247 us).
 //
 // The weights enter the second product as fp16 pairs, 22 bits, whatever the number of rows.  One fp16 number each, 11 bits, would take
 // 63 us instead of 74 at 256 rows x 128, 42 instead of 47 x 64, 51 instead of 54 at 96 rows x 128, and a row in which one token has nearly all
@@ -66,7 +69,12 @@ __device__ __forceinline__ int value_row(int c, int e) { return 32 * (c >> 3) + 
 // waves reconstruct a tile and then multiply it, and the workgroups that share a compute unit fill each other's waits; with two, four
 // waves more reconstruct the next tile while these multiply.
 // By rows of a kv head: 16 columns per wave and three workgroups per compute unit up to 64 (two per compute unit, which spills nothing:
-// 24 rows x 64 27.5 -> 30 us, 12 x 96 25.2 -> 26.6, 130 tokens 6.8 -> 6.2), 32 columns up to 128, two tiles and eight waves of them above.
+// 24 rows x 64 27.5 -> 30 us, 12 x 96 25.2 -> 26.6, 130 tokens 6.8 -> 6.2), 32 columns up to 128, two tiles and eight waves of them above;
+// more than 256 rows are blocks of 256, each with a reconstruction of its own.
+// Both sides, 8 heads x 32768 x 128 in us: 48 rows small 49.3, middle 51.8; 64 rows 51.5, 51.9 (x 64: 33.1, 34.1); 65 rows 77.3, 52.3.
+// Middle / large: 65 rows 52.4 / 51.7, 128 rows 57.4 / 55.2 and, 128 rows, 8 x 2000 x 128 27.2 / 22.8, but 320 heads of 500 tokens 48.7 / 56.5, of 80
+// rows 46.6 / 54.9, 512 heads of 300 x 64 20.9 / 27.0, 8 of 500 13.2 / 14.5: two workgroups per compute unit take many heads and few tiles better.
+// 129 rows 86.7 / 62.0, 256 94.3 / 73.0.  Blocks of 256: 257 rows 110, 384 115, 512 127, 1024 240.
 template <int kTakers_, int kCols_, int kBufs_, int kPerSimd_>
 struct Form {
     static constexpr int kTakers = kTakers_, kCols = kCols_, kBufs = kBufs_, kPerSimd = kPerSimd_;
@@ -574,8 +582,7 @@ __global__ __launch_bounds__(F::kThreads, F::kPerSimd) void k_shared(Geometry g,
     l_run = over_lanes(l_run, [](float x, float y) { return x + y; });
     if (!has_cols)
         return;
-    // The only share writes the result itself: 256 x 8 heads of 64 tokens x 64, 64 rows, 25 us instead of 101 with partial sums and the merge;
-    // 40 x 8 of 500 x 128, 80 rows, 43 instead of 75.
+    // The only share writes the result itself: 256 x 8 heads of 64 tokens x 64, 64 rows, 25 us instead of 101 with partial sums and the merge.
     const float factor = !a.out ? 1.f : l_run > 0.f ? 1.f / l_run : 0.f;  // a row that saw no token: zeros
     if (a.out) {
         if (there && kgrp == 0 && a.lse)
