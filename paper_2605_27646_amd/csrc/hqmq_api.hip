@@ -6,6 +6,7 @@
 #include <cstring>
 #include <mutex>
 
+#include "hqmq_cache4_device.h"
 #include "hqmq_device.h"
 #include "hqmq_serve_device.h"
 
@@ -1255,4 +1256,237 @@ extern "C" int32_t hqmq_evict_compact(const hqmq_params *params, int32_t n_keep,
             return hip_failed(err);
     }
     return HQMQ_OK;
+}
+
+// ---- the paged 4-bit cache (include/hqmq_cache4.h) ------------------------------------------------------------------------
+
+static int32_t check_cache4(const hqmq_cache4_params *p)
+{
+    if (!p || p->n_pages <= 0 || p->H <= 0 || p->D <= 0 || p->page_size < 16 || p->page_size > (1 << 20) || (p->page_size & (p->page_size - 1)))
+        return HQMQ_ERR_INVALID_ARG;
+    if (p->D > 256 || p->H > 4096 || (p->format != HQMQ_CACHE4_FLOAT && p->format != HQMQ_CACHE4_INT))
+        return HQMQ_ERR_UNSUPPORTED;
+    return HQMQ_OK;
+}
+
+static Cache4 make_cache4(const hqmq_cache4_params *p, const hqmq_cache4_buffers *b)
+{
+    Cache4 c = {};
+    if (b) {
+        c.k_codes = static_cast<uint8_t *>(b->k_codes);
+        c.k_scales = static_cast<uint8_t *>(b->k_scales);
+        c.v_codes = static_cast<uint8_t *>(b->v_codes);
+        c.v_scales = static_cast<uint8_t *>(b->v_scales);
+    }
+    c.n_pages = p->n_pages;
+    c.page_shift = 0;
+    while ((1 << c.page_shift) < p->page_size)
+        ++c.page_shift;
+    c.H = p->H;
+    c.D = p->D;
+    c.NG = cache4_groups(p->D);
+    c.format = p->format;
+    return c;
+}
+
+extern "C" int32_t hqmq_cache4_sizes(const hqmq_cache4_params *params, uint64_t *code_bytes, uint64_t *scale_bytes)
+{
+    const int32_t rc = check_cache4(params);
+    if (rc != HQMQ_OK)
+        return rc;
+    if (!code_bytes || !scale_bytes)
+        return HQMQ_ERR_INVALID_ARG;
+    // 2^31 pages of 2^20 tokens of 2^12 heads of 2^3 groups are 2^66 of these
+    const uint64_t rows = (uint64_t)params->n_pages * (uint64_t)params->page_size;
+    if (rows > (1ull << 46) / (16ull * 8 * params->H))
+        return HQMQ_ERR_UNSUPPORTED;
+    const uint64_t groups = rows * params->H * cache4_groups(params->D);
+    *code_bytes = 16 * groups;
+    *scale_bytes = (params->format == HQMQ_CACHE4_FLOAT ? 1 : 4) * groups;
+    return HQMQ_OK;
+}
+
+static int32_t check_cache4_batch(const hqmq_cache4_params *p, const hqmq_cache4_batch *b, int32_t n_rows)
+{
+    if (!b || b->n_seqs <= 0 || b->pages_per_seq <= 0 || b->max_rows <= 0 || b->max_length <= 0 || n_rows < 0)
+        return HQMQ_ERR_INVALID_ARG;
+    if (!b->starts && n_rows % b->n_seqs)
+        return HQMQ_ERR_INVALID_ARG;
+    if (b->n_seqs > 65535 || (int64_t)b->pages_per_seq * p->page_size > (1 << 30) || n_rows > (1 << 30))
+        return HQMQ_ERR_UNSUPPORTED;
+    return HQMQ_OK;
+}
+
+// The cache's buffers and the batch's arrays.
+static int32_t check_cache4_pointers(const hqmq_cache4_params *p, const hqmq_cache4_buffers *c, const hqmq_cache4_batch *b)
+{
+    if (!c || !c->k_codes || !c->k_scales || !c->v_codes || !c->v_scales || !b->block_table || !b->lengths)
+        return HQMQ_ERR_INVALID_ARG;
+    uint64_t codes = 0, scales = 0;
+    const int32_t rc = hqmq_cache4_sizes(p, &codes, &scales);
+    if (rc != HQMQ_OK)
+        return rc;
+    const void *at[4] = {c->k_codes, c->v_codes, c->k_scales, c->v_scales};
+    for (int i = 0; i < 4; ++i) {
+        if (misaligned(at[i], 16))
+            return HQMQ_ERR_INVALID_ARG;
+        for (int j = 0; j < i; ++j) {
+            const uint64_t x = reinterpret_cast<uintptr_t>(at[i]), y = reinterpret_cast<uintptr_t>(at[j]);
+            if (x < y + (j < 2 ? codes : scales) && y < x + (i < 2 ? codes : scales))
+                return HQMQ_ERR_INVALID_ARG;
+        }
+    }
+    if (misaligned(b->block_table, 4) || misaligned(b->lengths, 4) || misaligned(b->starts, 4))
+        return HQMQ_ERR_INVALID_ARG;
+    return HQMQ_OK;
+}
+
+// out: rows that are written, where no element may be two rows'.
+static int32_t check_cache4_rows(const hqmq_cache4_rows *r, int32_t n_rows, int32_t heads, int32_t D, bool out)
+{
+    if (!r || r->stride_row < 0 || r->stride_head < 0)
+        return HQMQ_ERR_INVALID_ARG;
+    if (n_rows == 0)
+        return HQMQ_OK;
+    if (!r->data || misaligned(r->data, 2))
+        return HQMQ_ERR_INVALID_ARG;
+    constexpr int64_t kMost = (int64_t)1 << 30;  // 2^30 rows of them are 2^60 elements
+    if (r->stride_row > kMost || r->stride_head > kMost)
+        return HQMQ_ERR_UNSUPPORTED;
+    if (out) {
+        const bool heads_apart = heads == 1 || r->stride_head >= D, rows_apart = n_rows == 1 || r->stride_row >= D;
+        const bool head_major = rows_apart && (heads == 1 || r->stride_head >= (n_rows - 1) * r->stride_row + D);
+        const bool row_major = heads_apart && (n_rows == 1 || r->stride_row >= (heads - 1) * r->stride_head + D);
+        if (!head_major && !row_major)
+            return HQMQ_ERR_INVALID_ARG;
+    }
+    return HQMQ_OK;
+}
+
+static Cache4Seqs make_cache4_seqs(const hqmq_cache4_batch *b, int32_t n_rows)
+{
+    return Cache4Seqs{b->block_table, b->lengths, b->starts, b->n_seqs, n_rows, b->pages_per_seq, n_rows / b->n_seqs};
+}
+
+static int32_t cache4_most_rows(const hqmq_cache4_batch *b, int32_t n_rows)
+{
+    return std::max(1, b->starts ? std::min(b->max_rows, n_rows) : n_rows / b->n_seqs);
+}
+
+static Cache4Rows make_cache4_rows(const hqmq_cache4_rows *r, int32_t D)
+{
+    const bool wide = D % 8 == 0 && r->stride_row % 8 == 0 && r->stride_head % 8 == 0 && !misaligned(r->data, 16);
+    return Cache4Rows{static_cast<uint16_t *>(r->data), r->stride_row, r->stride_head, wide ? 1 : 0};
+}
+
+static int32_t cache4_move(bool write, const hqmq_cache4_params *params, const hqmq_cache4_buffers *cache, const hqmq_cache4_batch *batch,
+                           int32_t n_rows, int32_t type, const hqmq_cache4_rows *k, const hqmq_cache4_rows *v, void *stream)
+{
+    int32_t rc = check_cache4(params);
+    if (rc == HQMQ_OK)
+        rc = check_cache4_batch(params, batch, n_rows);
+    if (rc == HQMQ_OK)
+        rc = check_cache4_pointers(params, cache, batch);
+    if (rc == HQMQ_OK && type != HQMQ_TYPE_FP16 && type != HQMQ_TYPE_BF16)
+        rc = HQMQ_ERR_UNSUPPORTED;
+    if (rc == HQMQ_OK)
+        rc = check_cache4_rows(k, n_rows, params->H, params->D, !write);
+    if (rc == HQMQ_OK)
+        rc = check_cache4_rows(v, n_rows, params->H, params->D, !write);
+    if (rc != HQMQ_OK)
+        return rc;
+    if (!write && n_rows > 0 && k->data == v->data)
+        return HQMQ_ERR_INVALID_ARG;
+    if (n_rows == 0)
+        return HQMQ_OK;
+    const auto launch = write ? launch_cache4_write : launch_cache4_read;
+    const hipError_t err = launch(make_cache4(params, cache), make_cache4_seqs(batch, n_rows), cache4_most_rows(batch, n_rows),
+                                  type == HQMQ_TYPE_BF16, make_cache4_rows(k, params->D), make_cache4_rows(v, params->D),
+                                  static_cast<hipStream_t>(stream));
+    return err == hipSuccess ? HQMQ_OK : hip_failed(err);
+}
+
+extern "C" int32_t hqmq_cache4_write(const hqmq_cache4_params *params, const hqmq_cache4_buffers *cache, const hqmq_cache4_batch *batch,
+                                     int32_t n_rows, int32_t type, const hqmq_cache4_rows *k, const hqmq_cache4_rows *v, void *stream)
+{
+    return cache4_move(true, params, cache, batch, n_rows, type, k, v, stream);
+}
+
+extern "C" int32_t hqmq_cache4_read(const hqmq_cache4_params *params, const hqmq_cache4_buffers *cache, const hqmq_cache4_batch *batch,
+                                    int32_t n_rows, int32_t type, const hqmq_cache4_rows *k, const hqmq_cache4_rows *v, void *stream)
+{
+    return cache4_move(false, params, cache, batch, n_rows, type, k, v, stream);
+}
+
+static int32_t check_cache4_heads(const hqmq_cache4_params *p, int32_t n_rows, int32_t n_q_heads, int32_t window)
+{
+    if (n_q_heads <= 0 || n_q_heads % p->H || window < 0)
+        return HQMQ_ERR_INVALID_ARG;
+    return n_q_heads > 65535 || (int64_t)n_rows * n_q_heads > (1 << 30) ? HQMQ_ERR_UNSUPPORTED : HQMQ_OK;
+}
+
+static Cache4Plan cache4_plan(const hqmq_cache4_params *p, const hqmq_cache4_batch *b, int32_t n_rows, int32_t n_q_heads, int32_t window)
+{
+    const int32_t length = (int32_t)std::min<int64_t>(b->max_length, (int64_t)b->pages_per_seq * p->page_size);
+    return plan_cache4_attend(make_cache4(p, nullptr), make_cache4_seqs(b, n_rows), cache4_most_rows(b, n_rows), length, n_q_heads / p->H,
+                              std::min(window, 1 << 30));
+}
+
+extern "C" uint64_t hqmq_cache4_attend_workspace_bytes(const hqmq_cache4_params *params, const hqmq_cache4_batch *batch, int32_t n_rows,
+                                                       int32_t n_q_heads, int32_t window)
+{
+    if (check_cache4(params) != HQMQ_OK || check_cache4_batch(params, batch, n_rows) != HQMQ_OK ||
+        check_cache4_heads(params, n_rows, n_q_heads, window) != HQMQ_OK || n_rows == 0)
+        return 0;
+    const Cache4Plan plan = cache4_plan(params, batch, n_rows, n_q_heads, window);
+    return plan.ml_bytes + plan.acc_bytes;
+}
+
+extern "C" int32_t hqmq_cache4_attend(const hqmq_cache4_params *params, const hqmq_cache4_buffers *cache, const hqmq_cache4_batch *batch,
+                                      int32_t n_rows, int32_t n_q_heads, int32_t type, const hqmq_cache4_rows *q, float scale,
+                                      int32_t window, const hqmq_cache4_rows *out, float *lse_dev, void *workspace_dev,
+                                      uint64_t workspace_bytes, void *stream)
+{
+    int32_t rc = check_cache4(params);
+    if (rc == HQMQ_OK)
+        rc = check_cache4_batch(params, batch, n_rows);
+    if (rc == HQMQ_OK)
+        rc = check_cache4_heads(params, n_rows, n_q_heads, window);
+    if (rc == HQMQ_OK)
+        rc = check_cache4_pointers(params, cache, batch);
+    if (rc == HQMQ_OK && type != HQMQ_TYPE_FP16 && type != HQMQ_TYPE_BF16)
+        rc = HQMQ_ERR_UNSUPPORTED;
+    if (rc == HQMQ_OK)
+        rc = check_cache4_rows(q, n_rows, n_q_heads, params->D, false);
+    if (rc == HQMQ_OK)
+        rc = check_cache4_rows(out, n_rows, n_q_heads, params->D, true);
+    if (rc != HQMQ_OK)
+        return rc;
+    if (!std::isfinite(scale) || misaligned(lse_dev, 4) || misaligned(workspace_dev, 256))
+        return HQMQ_ERR_INVALID_ARG;
+    if (n_rows == 0)
+        return HQMQ_OK;
+    const Cache4Plan plan = cache4_plan(params, batch, n_rows, n_q_heads, window);
+    if (plan.ml_bytes + plan.acc_bytes > 0) {
+        if (!workspace_dev)
+            return HQMQ_ERR_INVALID_ARG;
+        if (workspace_bytes < plan.ml_bytes + plan.acc_bytes)
+            return HQMQ_ERR_BUFFER_TOO_SMALL;
+    }
+    Cache4Attend a;
+    a.c = make_cache4(params, cache);
+    a.b = make_cache4_seqs(batch, n_rows);
+    a.q = make_cache4_rows(q, params->D);
+    a.out = make_cache4_rows(out, params->D);
+    a.lse = lse_dev;
+    a.part_ml = static_cast<float *>(workspace_dev);
+    a.part_acc = reinterpret_cast<float *>(static_cast<unsigned char *>(workspace_dev) + plan.ml_bytes);
+    a.scale = scale;
+    a.G = n_q_heads / params->H;
+    a.window = std::min(window, 1 << 30);
+    a.n_tiles = plan.n_tiles;
+    a.n_splits = plan.n_splits;
+    a.split_tokens = plan.split_tokens;
+    const hipError_t err = launch_cache4_attend(a, plan, type == HQMQ_TYPE_BF16, static_cast<hipStream_t>(stream));
+    return err == hipSuccess ? HQMQ_OK : hip_failed(err);
 }

@@ -1,0 +1,118 @@
+// Declarations shared by the kernels of the paged 4-bit cache (hqmq_cache4_rows.hip, hqmq_cache4_attend.hip) and the C ABI
+// (hqmq_api.hip).  Not part of the public ABI (include/hqmq_cache4.h).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "hqmq_cache4.h"
+
+namespace hqmq {
+
+// Groups of 32 channels that a row of D channels takes: a part of the V layout is 4, 2 or 1 of them.
+constexpr int cache4_groups(int D) { return D <= 128 ? (D + 31) / 32 : (D + 63) / 64 * 2; }
+
+struct Cache4 {
+    uint8_t *k_codes, *k_scales, *v_codes, *v_scales;
+    int32_t n_pages, page_shift, H, D;
+    int32_t NG;      // groups of a row
+    int32_t format;
+};
+
+struct Cache4Seqs {
+    const int32_t *table, *lengths, *starts;  // starts: null for n_rows / n_seqs rows each
+    int32_t n_seqs, n_rows, pitch;
+    int32_t rows_each;                        // where starts is null
+};
+
+struct Cache4Rows {
+    uint16_t *data;
+    int64_t row, head;  // element strides
+    int32_t wide;       // every run of 8 channels that begins at a multiple of 8 is 16 aligned bytes inside the row
+};
+
+// Sequence i of a batch: its tokens, its rows and the position of the first of them (negative: more rows than tokens).
+struct Cache4Seq {
+    int32_t length, first_row, n, pos0;
+};
+__device__ __forceinline__ Cache4Seq cache4_seq(const Cache4Seqs &b, int page_shift, int i)
+{
+    Cache4Seq s;
+    const int most = b.pitch << page_shift;
+    s.length = min(max(b.lengths[i], 0), most);
+    if (b.starts) {  // inside the tensors, whatever they hold
+        s.first_row = min(max(b.starts[i], 0), b.n_rows);
+        s.n = min(max(b.starts[i + 1], s.first_row), b.n_rows) - s.first_row;
+    } else {
+        s.first_row = i * b.rows_each;
+        s.n = b.rows_each;
+    }
+    s.pos0 = s.length - s.n;
+    return s;
+}
+
+// ---- codes ------------------------------------------------------------------------------------------------------------
+
+typedef _Float16 cache4_h2 __attribute__((ext_vector_type(2)));
+
+// Two values of a byte of e2m1 codes times a power of two (exact in fp16), byte kByte of the word.
+template <int kByte>
+__device__ __forceinline__ cache4_h2 e2m1_pair(uint32_t word, float scale)
+{
+    return __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(word, scale, kByte);
+}
+
+// Integer codes, one at bits 0..3 and one at bits 16..19 (the others are ignored), times s plus m, rounded once: 1024 + c is the
+// fp16 number 0x6400 | c, and the difference is exact.
+__device__ __forceinline__ cache4_h2 int4_pair(uint32_t word, cache4_h2 s, cache4_h2 m)
+{
+    const cache4_h2 big = __builtin_bit_cast(cache4_h2, (word & 0x000f000fu) | 0x64006400u);
+    return __builtin_elementwise_fma(big - cache4_h2{(_Float16)1024.f, (_Float16)1024.f}, s, m);
+}
+
+__device__ __forceinline__ float e8m0(uint32_t byte) { return __uint_as_float(byte << 23); }
+
+// Where dword w (channels 8 w .. 8 w + 7) of token t of a block of four lies in the block of V codes: first byte, and how many runs
+// of how many bytes it is split into, kStep(t) apart.
+struct Cache4Place {
+    int32_t at, runs, bytes;  // run r at `at` + r * 4 * bytes
+};
+__device__ __forceinline__ Cache4Place cache4_v_place(int NG, int w, int t)
+{
+    const int whole = NG & ~3;  // groups in parts of 128 channels
+    const int w64 = 4 * whole, w32 = 4 * (NG & ~1);
+    if (w < w64)
+        return {16 * w + 4 * t, 1, 4};
+    if (w < w32)
+        return {16 * w64 + 16 * (w - w64) + 2 * t, 2, 2};
+    return {16 * w32 + 16 * (w - w32) + t, 4, 1};
+}
+
+// ---- launches ---------------------------------------------------------------------------------------------------------
+
+hipError_t launch_cache4_write(const Cache4 &c, const Cache4Seqs &b, int max_rows, bool bf16, const Cache4Rows &k, const Cache4Rows &v,
+                               hipStream_t stream);
+hipError_t launch_cache4_read(const Cache4 &c, const Cache4Seqs &b, int max_rows, bool bf16, const Cache4Rows &k, const Cache4Rows &v,
+                              hipStream_t stream);
+
+struct Cache4Attend {
+    Cache4 c;
+    Cache4Seqs b;
+    Cache4Rows q, out;
+    float *lse;                // [n_rows][H * G] or null
+    float *part_acc;           // [n_rows * H * G][n_splits][32 NG]: weighted sums of a split, relative to 2^part_ml[0]
+    float *part_ml;            // [n_rows * H * G][n_splits][2]: reference (log2 domain) and sum of the weights, 0: nothing seen
+    float scale;
+    int32_t G, window;
+    int32_t n_tiles, n_splits; // workgroups along the rows and along the tokens
+    int32_t split_tokens;      // of each split but the last, which goes to the end
+};
+struct Cache4Plan {
+    int32_t blocks;            // of 16 query rows that a workgroup takes at a time: 1, 2 or 4
+    int32_t n_tiles, n_splits, split_tokens;
+    uint64_t ml_bytes, acc_bytes;
+};
+Cache4Plan plan_cache4_attend(const Cache4 &c, const Cache4Seqs &b, int max_rows, int max_length, int G, int window);
+hipError_t launch_cache4_attend(const Cache4Attend &a, const Cache4Plan &plan, bool bf16, hipStream_t stream);
+
+}  // namespace hqmq

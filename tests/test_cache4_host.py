@@ -1,0 +1,220 @@
+"""Host-side checks of include/hqmq_cache4.h that need no GPU: what the library exports, sizes, refusals before anything is
+enqueued (pointers here are addresses that are never read), and the plain form's own properties."""
+import ctypes as C
+import os
+import re
+import subprocess
+
+import numpy as np
+import pytest
+import torch
+
+import cache4_ref as ref
+import paper_2605_27646_amd as hq
+from paper_2605_27646_amd import cache4
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+P = 1 << 40  # aligned addresses
+INVALID, UNSUPPORTED, SMALL = -1, -2, -3
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not os.path.exists(hq.library_path()):
+        from paper_2605_27646_amd import build
+        build.build()
+    return cache4._load()
+
+
+def test_header_and_library_agree(lib):
+    header = open(os.path.join(ROOT, "include", "hqmq_cache4.h")).read()
+    declared = set(re.findall(r"^(?:int32_t|uint64_t)\s+(hqmq_\w+)\s*\(", header, re.M))
+    assert declared == {"hqmq_cache4_sizes", "hqmq_cache4_write", "hqmq_cache4_read", "hqmq_cache4_attend",
+                        "hqmq_cache4_attend_workspace_bytes"}
+    for name in declared:
+        assert hasattr(lib, name) and hasattr(hq, name), name
+    for name in ("HQMQ_CACHE4_FLOAT", "HQMQ_CACHE4_INT"):
+        assert int(re.search(rf"#define {name} (\d+)", header).group(1)) == getattr(hq, name)
+    assert (C.sizeof(cache4.Cache4Params), C.sizeof(cache4._Buffers), C.sizeof(cache4._Batch), C.sizeof(cache4._Rows)) == (20, 32, 40, 24)
+
+
+def _params(**kw):
+    d = dict(n_pages=100, page_size=16, H=4, D=128, format=0)
+    d.update(kw)
+    return hq.Cache4Params(*d.values())
+
+
+@pytest.mark.parametrize("D,groups", [(1, 1), (32, 1), (33, 2), (96, 3), (100, 4), (128, 4), (129, 6), (192, 6), (193, 8), (256, 8)])
+@pytest.mark.parametrize("fmt", [0, 1])
+def test_sizes(lib, D, groups, fmt):
+    assert hq.hqmq_cache4_sizes(_params(D=D, format=fmt)) == (100 * 16 * 4 * groups * 16, 100 * 16 * 4 * groups * (4 if fmt else 1))
+    pages = ref.Pages(100, 16, 4, D, fmt)
+    assert (pages.k.size, pages.ks.size, pages.v.size, pages.vs.size) == hq.hqmq_cache4_sizes(_params(D=D, format=fmt)) * 2
+
+
+@pytest.mark.parametrize("want,kw", [
+    (INVALID, dict(n_pages=0)), (INVALID, dict(n_pages=-1)), (INVALID, dict(page_size=8)), (INVALID, dict(page_size=48)), (INVALID, dict(page_size=1 << 21)),
+    (INVALID, dict(H=0)), (UNSUPPORTED, dict(H=4097)), (INVALID, dict(D=0)), (UNSUPPORTED, dict(D=257)), (UNSUPPORTED, dict(format=2)),
+    (UNSUPPORTED, dict(format=-1)), (UNSUPPORTED, dict(n_pages=2 ** 31 - 1, page_size=1 << 20, H=4096)),
+])
+def test_sizes_refuse(lib, want, kw):
+    a, b = C.c_uint64(), C.c_uint64()
+    assert lib.hqmq_cache4_sizes(C.byref(_params(**kw)), C.byref(a), C.byref(b)) == want
+    assert _call(lib, "write", **{"params": _params(**kw)}) == want
+    with pytest.raises(hq.HqmqError):
+        hq.alloc_cache4(_params(**kw), "cpu")
+
+
+def _rows(data=P + (5 << 30), row=512, head=128):
+    return cache4._Rows(data, row, head)
+
+
+def _call(lib, what, params=None, cache=None, n_seqs=3, pages=10, max_rows=8, max_length=160, table=P, lengths=P, starts=P, n_rows=24, heads=8, type=0,
+          a=None, b=None, scale=0.1, window=0, lse=0, ws=P, ws_bytes=1 << 40):
+    params = params or _params()
+    cache = cache if cache is not None else cache4._Buffers(P, P + (1 << 30), P + (2 << 30), P + (3 << 30))
+    batch = cache4._Batch(n_seqs, pages, max_rows, max_length, table, lengths, starts or None)
+    if what == "attend":
+        a, b = a or _rows(row=1024), b or _rows(P + (6 << 30), row=1024)
+        return lib.hqmq_cache4_attend(C.byref(params), C.byref(cache), C.byref(batch), n_rows, heads, type, C.byref(a), scale, window, C.byref(b), lse or None, ws,
+                                      ws_bytes, None)
+    a, b = a or _rows(), b or _rows(P + (6 << 30))
+    return getattr(lib, "hqmq_cache4_" + what)(C.byref(params), C.byref(cache), C.byref(batch), n_rows, type, C.byref(a), C.byref(b), None)
+
+
+@pytest.mark.parametrize("what", ["write", "read", "attend"])
+@pytest.mark.parametrize("want,kw", [
+    (INVALID, dict(n_seqs=0)), (INVALID, dict(n_seqs=-1)), (UNSUPPORTED, dict(n_seqs=65536)), (INVALID, dict(pages=0)), (UNSUPPORTED, dict(pages=1 << 27)),
+    (INVALID, dict(max_rows=0)), (INVALID, dict(max_length=0)), (INVALID, dict(n_rows=-1)), (INVALID, dict(starts=0, n_rows=25)),
+    (INVALID, dict(table=None)), (INVALID, dict(lengths=None)), (INVALID, dict(table=P + 2)), (INVALID, dict(lengths=P + 1)), (INVALID, dict(starts=P + 3)),
+    (UNSUPPORTED, dict(type=2)), (UNSUPPORTED, dict(type=-1)), (UNSUPPORTED, dict(n_rows=(1 << 30) + 1)),
+    (INVALID, dict(cache=cache4._Buffers(None, P, P, P))), (INVALID, dict(cache=cache4._Buffers(P, P + 4096, P + (2 << 30), P + (3 << 30)))),
+    (INVALID, dict(cache=cache4._Buffers(P, P + (1 << 30), P, P + (3 << 30)))), (INVALID, dict(cache=cache4._Buffers(P + 8, P + (1 << 30), P + (2 << 30), P + (3 << 30)))),
+    (INVALID, dict(cache=cache4._Buffers(P, P + (1 << 30), P + (2 << 30), P + (1 << 30) + 16))),
+    (INVALID, dict(a=_rows(None))), (INVALID, dict(b=_rows(None))), (INVALID, dict(a=_rows(P + 1))), (INVALID, dict(a=_rows(row=-1))), (INVALID, dict(b=_rows(head=-128))),
+    (UNSUPPORTED, dict(a=_rows(row=1 << 31))),
+])
+def test_calls_refuse(lib, what, want, kw):
+    assert _call(lib, what, **kw) == want
+
+
+@pytest.mark.parametrize("what", ["read", "attend"])
+@pytest.mark.parametrize("row,head", [(512, 127), (512, 0), (0, 128), (384, 128), (100, 1 << 20), (128, 128 * 23)])
+def test_rows_that_share_elements_are_not_written(lib, what, row, head):
+    assert _call(lib, what, b=_rows(row=row, head=head)) == INVALID
+
+
+def test_read_refuses_one_place_for_both(lib):
+    assert _call(lib, "read", a=_rows(), b=_rows()) == INVALID
+
+
+@pytest.mark.parametrize("want,kw", [
+    (INVALID, dict(heads=0)), (INVALID, dict(heads=6)), (INVALID, dict(heads=-4)), (UNSUPPORTED, dict(heads=65536)), (INVALID, dict(window=-1)),
+    (INVALID, dict(scale=float("nan"))), (INVALID, dict(scale=float("inf"))), (INVALID, dict(lse=P + 2)), (INVALID, dict(ws=P + 128)),
+    (INVALID, dict(ws=None)), (SMALL, dict(ws_bytes=100)), (UNSUPPORTED, dict(n_rows=1 << 29)),
+])
+def test_attend_refuses(lib, want, kw):
+    kw = dict(dict(max_length=160000, pages=10000), **kw)
+    assert _call(lib, "attend", **kw) == want
+
+
+def test_calls_without_rows_enqueue_nothing(lib):
+    for what in ("write", "read", "attend"):
+        assert _call(lib, what, n_rows=0, a=_rows(None), b=_rows(None), ws=None, ws_bytes=0) == 0
+        assert _call(lib, what, n_rows=0, table=None) == INVALID
+
+
+def test_attend_workspace(lib):
+    table, lengths = torch.zeros(1, 4096, dtype=torch.int32), torch.zeros(1, dtype=torch.int32)
+    params = _params(n_pages=4096, H=8)
+    long = hq.Cache4Batch(table, lengths, max_length=65536)
+    n = hq.hqmq_cache4_attend_workspace_bytes(params, long, 1, 32)
+    assert n > 0 and _call(lib, "attend", params=params, n_seqs=1, pages=4096, max_length=65536, starts=0, n_rows=1, heads=32, ws_bytes=n - 1) == SMALL
+    assert hq.hqmq_cache4_attend_workspace_bytes(params, hq.Cache4Batch(table, lengths, max_length=100), 1, 32) == 0
+    assert hq.hqmq_cache4_attend_workspace_bytes(params, long, 1, 32, window=64) == 0
+    assert hq.hqmq_cache4_attend_workspace_bytes(params, long, 1, 31) == 0 and hq.hqmq_cache4_attend_workspace_bytes(_params(D=300), long, 1, 32) == 0
+    # what the table has room for is what counts where the hint is larger
+    assert hq.hqmq_cache4_attend_workspace_bytes(params, hq.Cache4Batch(table, lengths), 1, 32) == n
+
+
+def test_binding_refuses_shapes(lib):
+    i32 = dict(dtype=torch.int32)
+    table, lengths = torch.zeros(2, 5, **i32), torch.zeros(2, **i32)
+    for bad in ((table[0], lengths), (table.long(), lengths), (table, lengths[:1]), (table.t(), lengths), (table, lengths, torch.zeros(2, **i32)),
+                (table, lengths, torch.zeros(3))):
+        with pytest.raises(ValueError):
+            hq.Cache4Batch(*bad)
+    batch, params = hq.Cache4Batch(table, lengths), _params()
+    cache = hq.alloc_cache4(params, "cpu")
+    k = torch.zeros(4, 4, 128, dtype=torch.float16)
+    for kk, vv in ((k.float(), k.float()), (k[:, :3], k), (k, k[:2]), (k, k.bfloat16()), (k[0], k), (torch.zeros(4, 4, 129, dtype=torch.float16)[:, :, :-1].transpose(1, 2), k),
+                   (torch.zeros(4, 4, 256, dtype=torch.float16)[:, :, ::2], k)):
+        for call in (hq.hqmq_cache4_write, hq.hqmq_cache4_read):
+            with pytest.raises(ValueError):
+                call(params, cache, batch, kk, vv)
+    q = torch.zeros(4, 8, 128, dtype=torch.float16)
+    for kw in (dict(out=q[:, :4]), dict(out=q.bfloat16()), dict(q=q.float()), dict(lse=torch.zeros(4, 7)), dict(workspace=torch.zeros(4, 4).t())):
+        args = dict(q=q, out=q, workspace=None, lse=None)
+        args.update(kw)
+        with pytest.raises(ValueError):
+            hq.hqmq_cache4_attend(params, cache, batch, args["q"], 1.0, args["out"], args["workspace"], lse=args["lse"])
+    for field in ("k_codes", "k_scales", "v_codes", "v_scales"):
+        short = hq.alloc_cache4(params, "cpu")
+        setattr(short, field, getattr(short, field)[:-1])
+        with pytest.raises(ValueError, match="hold"):
+            hq.hqmq_cache4_write(params, short, batch, k, k.clone())
+
+
+PLACES = """
+#include <cstdio>
+#include <initializer_list>
+#define __device__
+#define __forceinline__ inline
+%s
+int main()
+{
+    for (int NG : {1, 2, 3, 4, 6, 8})
+        for (int w = 0; w < 4 * NG; ++w)
+            for (int t = 0; t < 4; ++t) {
+                const Cache4Place p = cache4_v_place(NG, w, t);
+                for (int r = 0; r < p.runs; ++r)
+                    for (int b = 0; b < p.bytes; ++b)
+                        printf("%%d %%d %%d %%d %%d\\n", NG, t, 8 * w + 2 * (r * p.bytes + b), p.at + r * 4 * p.bytes + b, p.runs * p.bytes);
+            }
+}
+"""
+
+
+def test_places_of_v(tmp_path):
+    """The kernels' address of every byte of V, compiled for the host, against the plain form's."""
+    source = open(os.path.join(ROOT, "paper_2605_27646_amd", "csrc", "hqmq_cache4_device.h")).read()
+    start, end = source.index("struct Cache4Place {"), source.index("// ---- launches")
+    code = tmp_path / "places.cpp"
+    code.write_text(PLACES % ("#include <cstdint>\n" + source[start:end]))
+    subprocess.run(["g++", "-std=c++17", "-o", str(tmp_path / "places"), str(code)], check=True)
+    out = subprocess.run([str(tmp_path / "places")], check=True, capture_output=True, text=True).stdout
+    rows = np.array([[int(x) for x in line.split()] for line in out.splitlines()])
+    assert (rows[:, 4] == 4).all()
+    for NG in (1, 2, 3, 4, 6, 8):
+        pages = ref.Pages(1, 16, 1, 32 * NG, 0)
+        mine = rows[rows[:, 0] == NG]
+        assert len(mine) == 4 * 16 * NG and len(set(mine[:, 3])) == len(mine)  # a place of its own for each
+        for t in range(4):
+            of = mine[mine[:, 1] == t]
+            assert np.array_equal(of[np.argsort(of[:, 2])][:, 3], pages._v_bytes(t))
+
+
+@pytest.mark.parametrize("fmt", [0, 1])
+def test_plain_form_is_within_half_a_step(fmt):
+    """What comes back is the nearest value that the group's scale allows."""
+    x = np.random.default_rng(fmt).standard_normal((50, 96)).astype(np.float16).astype(np.float64)
+    codes, scales = ref.quantise(fmt, x)
+    y = ref.dequantise(fmt, codes, scales, 96)
+    if fmt == 0:
+        unit = np.repeat(2.0 ** (scales[..., 0].astype(float) - 127), 32, -1)
+        gap = np.where(np.abs(x) <= 2 * unit, 0.25, np.where(np.abs(x) <= 4 * unit, 0.5, 1.0)) * unit  # 4 to 7 may be off by one unit
+        assert (np.abs(x - y) <= gap).all() and (scales[..., 0] >= 104).all() and (scales[..., 0] <= 140).all()
+    else:
+        step = np.repeat(np.ascontiguousarray(scales).view(np.float16)[..., 0].astype(float), 32, -1)
+        # half a step, 15 times the rounding of the step to fp16, and that of the value
+        assert (np.abs(x - y) <= step * (0.5 + 15 * 2.0 ** -11) + 2.0 ** -11 * np.abs(y)).all()
