@@ -34,7 +34,7 @@ constexpr int kJoinPitch = kPartChannels + 4;
 constexpr size_t attend_lds_bytes(int NG, int blocks)
 {
     const size_t queries = (size_t)blocks * NG * 64 * 16, join = (size_t)kWaves * 16 * kJoinPitch * 4;
-    return (queries > join ? queries : join) + (size_t)blocks * 16 * 4 + (size_t)kWaves * blocks * 16 * 2 * 4;
+    return (queries > join ? queries : join) + (size_t)blocks * 16 * 8 + (size_t)kWaves * blocks * 16 * 2 * 4;
 }
 
 // Maximum or sum over the four lanes that hold a query's column.
@@ -95,14 +95,26 @@ struct VStage {
     Words<kWords> scale[Parts<NG>::n];
 };
 
+// 16 tokens of a head in one page: where they begin in each of the cache's buffers (one address for the wave), and where the lane's
+// share lies behind that (the same for all).
+struct Tile {
+    const uint8_t *k_codes, *k_scales, *v_codes, *v_scales;
+};
 template <int kFormat, int NG>
-__device__ __forceinline__ void load_k(KStage<kFormat, NG> &s, const Cache4 &c, int64_t row0, int slot, int lane)
+__device__ __forceinline__ Tile tile_at(const Cache4 &c, int page, int h, int slot)
 {
-    const int64_t row = row0 + slot + (lane & 15);
-    const int quarter = lane >> 4, first = quarter * NG >> 2, last = (quarter * NG + NG - 1) >> 2;
-    s.code = load_words<NG>(c.k_codes + row * (16 * NG) + 4 * NG * quarter);
-    const auto scale_of = [&](int g) -> uint32_t {
-        return kFormat == HQMQ_CACHE4_FLOAT ? (uint32_t)c.k_scales[row * NG + g] : reinterpret_cast<const uint32_t *>(c.k_scales)[row * NG + g];
+    constexpr int kScale = kFormat == HQMQ_CACHE4_FLOAT ? 1 : 4;
+    const int64_t row = (((int64_t)page * c.H + h) << c.page_shift) + slot;
+    return Tile{c.k_codes + row * (16 * NG), c.k_scales + row * (kScale * NG), c.v_codes + row * (16 * NG), c.v_scales + row * (kScale * NG)};
+}
+
+template <int kFormat, int NG>
+__device__ __forceinline__ void load_k(KStage<kFormat, NG> &s, const Tile &tile, int lane)
+{
+    const uint32_t token = lane & 15, quarter = lane >> 4, first = quarter * NG >> 2, last = (quarter * NG + NG - 1) >> 2;
+    s.code = load_words<NG>(tile.k_codes + (token * (16 * NG) + 4 * NG * quarter));
+    const auto scale_of = [&](uint32_t g) -> uint32_t {
+        return kFormat == HQMQ_CACHE4_FLOAT ? (uint32_t)tile.k_scales[token * NG + g] : load_words<1>(tile.k_scales + 4 * (token * NG + g)).w[0];
     };
     s.scale[0] = scale_of(first);
     if (KStage<kFormat, NG>::kScales > 1)
@@ -110,28 +122,27 @@ __device__ __forceinline__ void load_k(KStage<kFormat, NG> &s, const Cache4 &c, 
 }
 
 template <int kFormat, int NG>
-__device__ __forceinline__ void load_v(VStage<kFormat, NG> &s, const Cache4 &c, int64_t row0, int slot, int lane)
+__device__ __forceinline__ void load_v(VStage<kFormat, NG> &s, const Tile &tile, int lane)
 {
-    const int64_t row = row0 + slot + 4 * (lane >> 4);  // the first of a block of four tokens
-    const int run = lane & 15;
+    constexpr uint32_t kScale = kFormat == HQMQ_CACHE4_FLOAT ? 1 : 4;
+    const uint32_t quarter = lane >> 4, run = lane & 15;
     using P = Parts<NG>;
 #pragma unroll
     for (int p = 0; p < P::n; ++p) {
-        const uint8_t *at = c.v_codes + row * (16 * NG) + 64 * P::before(p) + 4 * P::groups(p) * run;
-        const int64_t scale_at = row * NG + 4 * (P::before(p) + (run * P::groups(p) >> 4));
+        const uint8_t *at = tile.v_codes + (quarter * (64 * NG) + 4 * P::groups(p) * run + 64 * P::before(p));
         if (P::groups(p) == 4) {
             const Words<4> w = load_words<4>(at);
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                s.code.w[P::before(p) + i] = w.w[i];
+                s.code.w[(P::before(p) + i) % NG] = w.w[i];
         } else if (P::groups(p) == 2) {
             const Words<2> w = load_words<2>(at);
             s.code.w[P::before(p)] = w.w[0];
-            s.code.w[P::before(p) + (NG > 1 ? 1 : 0)] = w.w[1];
+            s.code.w[(P::before(p) + 1) % NG] = w.w[1];
         } else {
             s.code.w[P::before(p)] = load_words<1>(at).w[0];
         }
-        s.scale[p] = load_words<VStage<kFormat, NG>::kWords>(c.v_scales + scale_at * (kFormat == HQMQ_CACHE4_FLOAT ? 1 : 4));
+        s.scale[p] = load_words<VStage<kFormat, NG>::kWords>(tile.v_scales + kScale * (4 * (quarter * NG + P::before(p) + (run * P::groups(p) >> 4))));
     }
 }
 
@@ -260,20 +271,64 @@ __global__ __launch_bounds__(kThreads4, attend_occupancy(NG, kBlocks)) void k_ca
     half8_t *const queries = reinterpret_cast<half8_t *>(lds);           // [kBlocks][NG][lane]
     float *const join = reinterpret_cast<float *>(lds);                  // [kWaves][16][kJoinPitch], when the queries are done with
     float *const factor = reinterpret_cast<float *>(lds + kShared);      // [kRows]: from products to exponents of 2
-    float *const stats = factor + kRows;                                 // [kWaves][kRows][2]
+    int *const position = reinterpret_cast<int *>(factor + kRows);       // [kRows]: -1 - 2^30 and less: no row
+    float *const stats = reinterpret_cast<float *>(position + kRows);    // [kWaves][kRows][2]
 
     const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, quarter = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const Cache4 &c = a.c;
     const int h = (int)(blockIdx.x % (uint32_t)c.H), rest = (int)(blockIdx.x / (uint32_t)c.H);
     const int split = rest % a.n_splits, seq = blockIdx.y;
-    const Cache4Seq s = cache4_seq(a.b, c.page_shift, seq);
     const int page_mask = (1 << c.page_shift) - 1;
-    const int32_t *const table = a.b.table + (int64_t)seq * a.b.pitch;
+    const ConstInts table = const_ints(a.b.table + (int64_t)seq * a.b.pitch);
+    const Cache4Seq s = cache4_seq(a.b, c.page_shift, seq);
     const int n_rows = s.n * a.G, n_heads = c.H * a.G;
 
-    for (int tile = rest / a.n_splits; tile * kRows < n_rows; tile += a.n_tiles) {
+    // the longest first: a causal prompt's last rows see the most
+    for (int tile = a.n_tiles - 1 - rest / a.n_splits; tile * kRows < n_rows; tile += a.n_tiles) {
         const int r0 = tile * kRows;
+        // ---- what the rows see -----------------------------------------------------------------------------------------
+        const int j_first = r0 / a.G, j_last = min((r0 + kRows - 1) / a.G, s.n - 1);
+        const int end = s.pos0 + j_last + 1, all_end = s.pos0 + j_first + 1;  // all_end: every row sees what is before it,
+        const int begin = a.window ? max(0, s.pos0 + j_first + 1 - a.window) & ~(kStep - 1) : 0;
+        const int all_begin = a.window ? s.pos0 + j_last + 1 - a.window : 0;  // and from here on
+        const int64_t share = (int64_t)begin + (int64_t)split * a.split_tokens;
+        const int from = (int)min(share, (int64_t)max(end, 0));
+        const int to = split == a.n_splits - 1 ? end : (int)min(share + a.split_tokens, (int64_t)max(end, 0));
+        const int n_steps = to > from ? (to - from + kStep - 1) / kStep : 0;
+
+        // Pages of a step's two halves; -1 for none.  Past the share's end: those of its last step.
+        const int last = from + kStep * max(n_steps - 1, 0);
+        int page[2];
+        const auto look_up = [&](int step) {
+            const int token = min(from + kStep * step, last);
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+                page[x] = __builtin_amdgcn_readfirstlane(table[min((token + 16 * x) >> c.page_shift, a.b.pitch - 1)]);
+        };
+        KStage<kFormat, NG> ks[2];
+        VStage<kFormat, NG> vs[2];
+        Tile tiles[2];
+        bool bad[2];
+        const auto tiles_of = [&](int token) {  // of the pages that were looked up last
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                bad[x] = (uint32_t)page[x] >= (uint32_t)c.n_pages;
+                tiles[x] = tile_at<kFormat, NG>(c, bad[x] ? 0 : page[x], h, (token + 16 * x) & page_mask);
+            }
+        };
+        if (wave < n_steps) {
+            look_up(wave);
+            tiles_of(from + kStep * wave);
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+                load_k(ks[x], tiles[x], lane);
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+                load_v(vs[x], tiles[x], lane);
+            look_up(wave + kWaves);
+        }
+
         // ---- queries to LDS, as operands -------------------------------------------------------------------------------
         for (int nb = wave; nb < kBlocks; nb += kWaves) {
             const int r = r0 + 16 * nb + col;
@@ -325,30 +380,17 @@ __global__ __launch_bounds__(kThreads4, attend_occupancy(NG, kBlocks)) void k_ca
                                __builtin_amdgcn_perm(x[3], x[1], 0x05040100u), __builtin_amdgcn_perm(x[3], x[1], 0x07060302u)};
                 queries[(nb * NG + w) * 64 + lane] = __builtin_bit_cast(half8_t, x);
             }
-            if (quarter == 0)
-                factor[16 * nb + col] = f;
+            if (quarter == 0) {
+                // Products stay below 2^40: with a factor this small they all become 0, but minus infinity stays what it is.
+                factor[16 * nb + col] = fmaxf(f, 0x1p-120f);
+                position[16 * nb + col] = there ? s.pos0 + j : -0x7fffffff;
+            }
         }
         __syncthreads();
-
-        // ---- what the rows see -----------------------------------------------------------------------------------------
-        const int j_first = r0 / a.G, j_last = min((r0 + kRows - 1) / a.G, s.n - 1);
-        const int end = s.pos0 + j_last + 1, all_end = s.pos0 + j_first + 1;  // all_end: every row sees what is before it,
-        const int begin = a.window ? max(0, s.pos0 + j_first + 1 - a.window) & ~(kStep - 1) : 0;
-        const int all_begin = a.window ? s.pos0 + j_last + 1 - a.window : 0;  // and from here on
-        const int64_t share = (int64_t)begin + (int64_t)split * a.split_tokens;
-        const int from = (int)min(share, (int64_t)max(end, 0));
-        const int to = split == a.n_splits - 1 ? end : (int)min(share + a.split_tokens, (int64_t)max(end, 0));
-        const int n_steps = to > from ? (to - from + kStep - 1) / kStep : 0;
-
         float scale[kBlocks];
-        int limit[kBlocks], low[kBlocks];
 #pragma unroll
-        for (int nb = 0; nb < kBlocks; ++nb) {
-            const int r = r0 + 16 * nb + col, p = s.pos0 + r / a.G;
+        for (int nb = 0; nb < kBlocks; ++nb)
             scale[nb] = factor[16 * nb + col];
-            limit[nb] = r < n_rows ? p + 1 : 0;
-            low[nb] = a.window ? p + 1 - a.window : 0;
-        }
 
         f4 o[kChannels][kBlocks];
         float ref[kBlocks], sum[kBlocks];
@@ -361,42 +403,13 @@ __global__ __launch_bounds__(kThreads4, attend_occupancy(NG, kBlocks)) void k_ca
                 o[e][nb] = f4{0.f, 0.f, 0.f, 0.f};
         }
 
-        // Pages of a step's two halves; -1 for none.  Past the share's end: those of its last step.
-        const auto page_of = [&](int token) { return table[min(token >> c.page_shift, a.b.pitch - 1)]; };
-        const int last = from + kStep * max(n_steps - 1, 0);
-        int page[2];
-        const auto look_up = [&](int step) {
-            const int token = min(from + kStep * step, last);
-#pragma unroll
-            for (int x = 0; x < 2; ++x)
-                page[x] = __builtin_amdgcn_readfirstlane(page_of(token + 16 * x));
-        };
-        KStage<kFormat, NG> ks[2];
-        VStage<kFormat, NG> vs[2];
-        bool bad[2];
-        int64_t row0[2];
-        const auto rows_of = [&]() {  // first rows of the head's pages that were looked up last
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                bad[x] = (uint32_t)page[x] >= (uint32_t)c.n_pages;
-                row0[x] = ((int64_t)(bad[x] ? 0 : page[x]) * c.H + h) << c.page_shift;
-            }
-        };
-        if (wave < n_steps) {
-            look_up(wave);
-            rows_of();
-            const int token = from + kStep * wave;
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                load_k(ks[x], c, row0[x], (token + 16 * x) & page_mask, lane);
-                load_v(vs[x], c, row0[x], (token + 16 * x) & page_mask, lane);
-            }
-            look_up(wave + kWaves);
-        }
         for (int step = wave; step < n_steps; step += kWaves) {
-            const int token = from + kStep * step, next = min(token + kStep * kWaves, last);
+            const int token = from + kStep * step;
             const bool bad_now[2] = {bad[0], bad[1]};
             // ---- scores
+            int at = lane;
+            if (kBlocks * NG > 8)
+                asm volatile("" : "+v"(at));  // the operands of many queries are read again, not kept in registers
             f4 x[2][kBlocks];
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
@@ -408,55 +421,46 @@ __global__ __launch_bounds__(kThreads4, attend_occupancy(NG, kBlocks)) void k_ca
                     const half8_t key = k_operand(ks[i], w, lane);
 #pragma unroll
                     for (int nb = 0; nb < kBlocks; ++nb)
-                        x[i][nb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(key, queries[(nb * NG + w) * 64 + lane], x[i][nb], 0, 0, 0);
+                        x[i][nb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(key, queries[(nb * NG + w) * 64 + at], x[i][nb], 0, 0, 0);
                 }
             }
-            rows_of();
+            tiles_of(min(token + kStep * kWaves, last));
 #pragma unroll
             for (int i = 0; i < 2; ++i)
-                load_k(ks[i], c, row0[i], (next + 16 * i) & page_mask, lane);
-            // ---- exponents; a row's unseen tokens get minus infinity
-            const bool whole = token + kStep <= all_end && token >= all_begin && !bad_now[0] && !bad_now[1];
-            float most = -__builtin_inff();
-            const auto seen = [&](int nb, int i, int r) {
-                const int t = token + 16 * i + 4 * quarter + r;
-                return t < limit[nb] && t >= low[nb] && !bad_now[i];
-            };
-            const auto exponents = [&](int nb, int i, int r) {
-                const float y = fmaf(x[i][nb][r], scale[nb], -ref[nb]);
-                return whole || seen(nb, i, r) ? y : -__builtin_inff();
-            };
-            f4 y[2][kBlocks];
-#pragma unroll
-            for (int nb = 0; nb < kBlocks; ++nb)
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        y[i][nb][r] = exponents(nb, i, r);
-                        most = fmaxf(most, y[i][nb][r]);
-                    }
-            if (__any(most > kRise4)) {  // rare but for a wave's first step
+                load_k(ks[i], tiles[i], lane);
+            // ---- unseen tokens
+            if (token + kStep > all_end || token < all_begin || bad_now[0] || bad_now[1]) {
 #pragma unroll
                 for (int nb = 0; nb < kBlocks; ++nb) {
-                    float top = -__builtin_inff();
+                    const int pos = position[16 * nb + col], low = a.window ? max(pos, -1) + 1 - a.window : 0;
 #pragma unroll
                     for (int i = 0; i < 2; ++i)
 #pragma unroll
-                        for (int r = 0; r < 4; ++r)
-                            top = fmaxf(top, whole || seen(nb, i, r) ? x[i][nb][r] * scale[nb] : -__builtin_inff());
-                    const float newer = fmaxf(ref[nb], column_max(top) - kTop4);
+                        for (int r = 0; r < 4; ++r) {
+                            const int t = token + 16 * i + 4 * quarter + r;
+                            x[i][nb][r] = t <= pos && t >= low && !bad_now[i] ? x[i][nb][r] : -__builtin_inff();
+                        }
+                }
+            }
+            // ---- a newer reference for the weights: rare but for a wave's first step
+            float top[kBlocks];
+            bool rise = false;
+#pragma unroll
+            for (int nb = 0; nb < kBlocks; ++nb) {
+                top[nb] = fmaxf(fmaxf(fmaxf(x[0][nb][0], x[0][nb][1]), fmaxf(x[0][nb][2], x[0][nb][3])),
+                                fmaxf(fmaxf(x[1][nb][0], x[1][nb][1]), fmaxf(x[1][nb][2], x[1][nb][3])));
+                rise |= fmaf(top[nb], scale[nb], -ref[nb]) > kRise4;
+            }
+            if (__any(rise)) {
+#pragma unroll
+                for (int nb = 0; nb < kBlocks; ++nb) {
+                    const float newer = fmaxf(ref[nb], column_max(top[nb] * scale[nb]) - kTop4);
                     const float f = __builtin_amdgcn_exp2f(ref[nb] - newer);
                     ref[nb] = newer;
                     sum[nb] *= f;
 #pragma unroll
                     for (int e = 0; e < kChannels; ++e)
                         o[e][nb] *= f4{f, f, f, f};
-#pragma unroll
-                    for (int i = 0; i < 2; ++i)
-#pragma unroll
-                        for (int r = 0; r < 4; ++r)
-                            y[i][nb][r] = exponents(nb, i, r);
                 }
             }
             // ---- weights
@@ -467,7 +471,7 @@ __global__ __launch_bounds__(kThreads4, attend_occupancy(NG, kBlocks)) void k_ca
                 for (int i = 0; i < 2; ++i)
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
-                        const float p = __builtin_amdgcn_exp2f(y[i][nb][r]);
+                        const float p = __builtin_amdgcn_exp2f(fmaf(x[i][nb][r], scale[nb], -ref[nb]));
                         sum[nb] += p;
                         const _Float16 rounded = (_Float16)p;
                         hi[nb][4 * i + r] = rounded;
@@ -492,7 +496,10 @@ __global__ __launch_bounds__(kThreads4, attend_occupancy(NG, kBlocks)) void k_ca
                     for (int nb = 0; nb < kBlocks; ++nb) {
                         o[e][nb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(even, hi[nb], o[e][nb], 0, 0, 0);
                         o[e + 1][nb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(odd, hi[nb], o[e + 1][nb], 0, 0, 0);
-                        if (kFine) {
+                    }
+                    if (kFine) {
+#pragma unroll
+                        for (int nb = 0; nb < kBlocks; ++nb) {
                             o[e][nb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(even, lo[nb], o[e][nb], 0, 0, 0);
                             o[e + 1][nb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(odd, lo[nb], o[e + 1][nb], 0, 0, 0);
                         }
@@ -501,7 +508,7 @@ __global__ __launch_bounds__(kThreads4, attend_occupancy(NG, kBlocks)) void k_ca
             });
 #pragma unroll
             for (int i = 0; i < 2; ++i)
-                load_v(vs[i], c, row0[i], (next + 16 * i) & page_mask, lane);
+                load_v(vs[i], tiles[i], lane);
             look_up(step + 2 * kWaves);
         }
 
@@ -597,44 +604,77 @@ __global__ __launch_bounds__(kThreads4, attend_occupancy(NG, kBlocks)) void k_ca
     }
 }
 
-// The splits' sums of a row, relative to the largest reference.  One wave a row and head.
+// The splits' sums of a row, relative to the largest reference.  A workgroup takes one row and head: its four waves take splits in
+// turn, as many at a time as rows of 4-channel lanes fit a wave, and join their sums in LDS.
+constexpr int kMostSplits = 128;
 template <bool kBf16>
-__global__ __launch_bounds__(64) void k_cache4_merge(Cache4Attend a)
+__global__ __launch_bounds__(kThreads4) void k_cache4_merge(Cache4Attend a)
 {
-    const int lane = threadIdx.x, n_heads = a.c.H * a.G, width = 32 * a.c.NG, ch = 4 * lane;
+    __shared__ __align__(16) float weight[kMostSplits];
+    __shared__ __align__(16) f4 partial[kThreads4];
+    __shared__ float whole[2];
+    const int tid = threadIdx.x, n_heads = a.c.H * a.G, width = 32 * a.c.NG, lanes = width / 4, at_once = kThreads4 / lanes;
+    const int mine = tid / lanes, ch = 4 * (tid - mine * lanes);
     const int64_t n = (int64_t)a.b.n_rows * n_heads;
     for (int64_t row_at = blockIdx.x; row_at < n; row_at += gridDim.x) {
         const int row = (int)(row_at / n_heads), head = (int)(row_at - (int64_t)row * n_heads);
         if (a.b.starts && (row < a.b.starts[0] || row >= a.b.starts[a.b.n_seqs]))
             continue;
-        const float *ml = a.part_ml + 2 * row_at * a.n_splits;
-        float m = kNothing, l = 0.f;
-        for (int s = lane; s < a.n_splits; s += 64)
-            if (ml[2 * s + 1] > 0.f)
-                m = fmaxf(m, ml[2 * s]);
+        __syncthreads();
+        if (tid < 64) {
+            const float2 *ml = reinterpret_cast<const float2 *>(a.part_ml) + row_at * a.n_splits;
+            float2 y[kMostSplits / 64];
+            float m = kNothing, l = 0.f;
 #pragma unroll
-        for (int d = 32; d; d >>= 1)
-            m = fmaxf(m, __shfl_xor(m, d));
-        f4 total = f4{0.f, 0.f, 0.f, 0.f};
-        for (int s = 0; s < a.n_splits; ++s) {
-            const float part = ml[2 * s + 1];
-            if (part > 0.f) {
-                const float f = __builtin_amdgcn_exp2f(ml[2 * s] - m);
-                l = fmaf(part, f, l);
-                if (ch < width)
-                    total += f4{f, f, f, f} * *reinterpret_cast<const f4 *>(a.part_acc + (row_at * a.n_splits + s) * width + ch);
+            for (int i = 0; i < kMostSplits / 64; ++i) {
+                y[i] = tid + 64 * i < a.n_splits ? ml[tid + 64 * i] : make_float2(kNothing, 0.f);
+                m = fmaxf(m, y[i].y > 0.f ? y[i].x : kNothing);
+            }
+#pragma unroll
+            for (int d = 32; d; d >>= 1)
+                m = fmaxf(m, __shfl_xor(m, d));
+#pragma unroll
+            for (int i = 0; i < kMostSplits / 64; ++i) {
+                const float f = y[i].y > 0.f ? __builtin_amdgcn_exp2f(y[i].x - m) : 0.f;
+                weight[tid + 64 * i] = f;
+                l = fmaf(y[i].y, f, l);
+            }
+#pragma unroll
+            for (int d = 32; d; d >>= 1)
+                l += __shfl_xor(l, d);
+            if (tid == 0) {
+                whole[0] = m;
+                whole[1] = l;
             }
         }
-        const float inverse = l > 0.f ? 1.f / l : 0.f;
-        uint16_t *dst = a.out.data + (int64_t)row * a.out.row + (int64_t)head * a.out.head + ch;
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (ch + e < a.c.D) {
-                const float y = total[e] * inverse;
-                dst[e] = kBf16 ? __builtin_bit_cast(uint16_t, (__bf16)y) : __builtin_bit_cast(uint16_t, (_Float16)y);
+        __syncthreads();
+        f4 total = f4{0.f, 0.f, 0.f, 0.f};
+        if (mine < at_once) {
+            const float *acc = a.part_acc + row_at * a.n_splits * width + ch;
+#pragma unroll 4
+            for (int s = mine; s < a.n_splits; s += at_once) {
+                const float f = weight[s];
+                const f4 y = *reinterpret_cast<const f4 *>(acc + (int64_t)s * width);
+                if (f > 0.f)  // of a split that saw nothing there are no sums
+                    total += f4{f, f, f, f} * y;
             }
-        if (a.lse && lane == 0)
-            a.lse[row_at] = l > 0.f ? kLn2 * (m + __builtin_amdgcn_logf(l)) : -__builtin_inff();
+        }
+        partial[tid] = total;
+        __syncthreads();
+        if (tid < lanes) {
+            for (int i = 1; i < at_once; ++i)
+                total += partial[tid + i * lanes];
+            const float l = whole[1], inverse = l > 0.f ? 1.f / l : 0.f;
+            uint16_t *dst = a.out.data + (int64_t)row * a.out.row + (int64_t)head * a.out.head + ch;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (ch + e < a.c.D) {
+                    const float y = total[e] * inverse;
+                    dst[e] = kBf16 ? __builtin_bit_cast(uint16_t, (__bf16)y) : __builtin_bit_cast(uint16_t, (_Float16)y);
+                }
+            if (a.lse && tid == 0)
+                a.lse[row_at] = l > 0.f ? kLn2 * (whole[0] + __builtin_amdgcn_logf(l)) : -__builtin_inff();
+        }
     }
 }
 
@@ -649,9 +689,9 @@ Cache4Plan plan_cache4_attend(const Cache4 &c, const Cache4Seqs &b, int max_rows
     int64_t span = max_length;
     if (window)
         span = std::min(span, (int64_t)window + std::min<int64_t>(max_rows, 16 * p.blocks / G + 1));
-    const int64_t round = kStep * kWaves, most = std::max<int64_t>((span + 2 * round - 1) / (2 * round), 1);
-    const int64_t wanted = 512 / std::max<int64_t>(p.n_tiles * heads, 1);
-    p.n_splits = (int32_t)std::max<int64_t>(std::min<int64_t>(std::min(wanted, most), 128), 1);
+    const int64_t round = kStep * kWaves, rr = getenv("HQ_R") ? atoi(getenv("HQ_R")) : 2, most = std::max<int64_t>((span + rr * round - 1) / (rr * round), 1);
+    const int64_t wanted = (getenv("HQ_S") ? atoi(getenv("HQ_S")) : 512) / std::max<int64_t>(p.n_tiles * heads, 1);
+    p.n_splits = (int32_t)std::max<int64_t>(std::min<int64_t>(std::min(wanted, most), kMostSplits), 1);
     p.split_tokens = (int32_t)((span + p.n_splits * round - 1) / (p.n_splits * round) * round);
     p.n_splits = (int32_t)std::max<int64_t>((span + p.split_tokens - 1) / p.split_tokens, 1);
     p.ml_bytes = p.acc_bytes = 0;
@@ -704,9 +744,9 @@ hipError_t launch_cache4_attend(const Cache4Attend &a, const Cache4Plan &plan, b
         return err;
     const dim3 rows((unsigned)std::min<int64_t>((int64_t)a.b.n_rows * a.c.H * a.G, 1 << 20));
     if (bf16)
-        k_cache4_merge<true><<<rows, 64, 0, stream>>>(args);
+        k_cache4_merge<true><<<rows, kThreads4, 0, stream>>>(args);
     else
-        k_cache4_merge<false><<<rows, 64, 0, stream>>>(args);
+        k_cache4_merge<false><<<rows, kThreads4, 0, stream>>>(args);
     return hipGetLastError();
 }
 

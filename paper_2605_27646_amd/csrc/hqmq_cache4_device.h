@@ -31,6 +31,10 @@ struct Cache4Rows {
     int32_t wide;       // every run of 8 channels that begins at a multiple of 8 is 16 aligned bytes inside the row
 };
 
+// What no kernel writes while it runs, so that uniform loads of it are scalar ones (which do not wait for the vector loads before them).
+typedef const __attribute__((address_space(4))) int32_t *ConstInts;
+__device__ __forceinline__ ConstInts const_ints(const int32_t *p) { return (ConstInts)p; }
+
 // Sequence i of a batch: its tokens, its rows and the position of the first of them (negative: more rows than tokens).
 struct Cache4Seq {
     int32_t length, first_row, n, pos0;
@@ -39,10 +43,10 @@ __device__ __forceinline__ Cache4Seq cache4_seq(const Cache4Seqs &b, int page_sh
 {
     Cache4Seq s;
     const int most = b.pitch << page_shift;
-    s.length = min(max(b.lengths[i], 0), most);
+    s.length = min(max(const_ints(b.lengths)[i], 0), most);
     if (b.starts) {  // inside the tensors, whatever they hold
-        s.first_row = min(max(b.starts[i], 0), b.n_rows);
-        s.n = min(max(b.starts[i + 1], s.first_row), b.n_rows) - s.first_row;
+        s.first_row = min(max(const_ints(b.starts)[i], 0), b.n_rows);
+        s.n = min(max(const_ints(b.starts)[i + 1], s.first_row), b.n_rows) - s.first_row;
     } else {
         s.first_row = i * b.rows_each;
         s.n = b.rows_each;
