@@ -28,7 +28,7 @@
  * place t % page_size; its n_i rows are the rows starts[i] .. starts[i + 1] - 1 of the tensors passed, and row j of them
  * stands at position length_i - n_i + j.  Several sequences may share pages that are only read.
  *
- * None of the calls allocates or synchronises; all of them can be recorded into a graph.  Workspaces hold nothing between
+ * None of the calls allocates or synchronises; all of them can be recorded into a graph (hqmq_init first).  Workspaces hold nothing between
  * calls; calls that may overlap need one each.
  */
 #ifndef HQMQ_CACHE4_H

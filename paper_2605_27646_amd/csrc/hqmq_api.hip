@@ -49,6 +49,8 @@ static hipError_t ensure_device_setup(void **scratch_out = nullptr)
                 err = prepare_shared_kernels();
             if (err == hipSuccess)
                 err = prepare_mass_kernels();
+            if (err == hipSuccess)
+                err = prepare_cache4_kernels();
             if (err != hipSuccess)
                 return err;
             void *ptr = nullptr;
@@ -1473,6 +1475,9 @@ extern "C" int32_t hqmq_cache4_attend(const hqmq_cache4_params *params, const hq
         if (workspace_bytes < plan.ml_bytes + plan.acc_bytes)
             return HQMQ_ERR_BUFFER_TOO_SMALL;
     }
+    const hipError_t ready = ensure_device_setup();
+    if (ready != hipSuccess)
+        return hip_failed(ready);
     Cache4Attend a;
     a.c = make_cache4(params, cache);
     a.b = make_cache4_seqs(batch, n_rows);
@@ -1484,6 +1489,8 @@ extern "C" int32_t hqmq_cache4_attend(const hqmq_cache4_params *params, const hq
     a.scale = scale;
     a.G = n_q_heads / params->H;
     a.window = std::min(window, 1 << 30);
+    a.by_G = make_divisor((uint32_t)a.G);
+    a.by_splits = make_divisor((uint32_t)plan.n_splits);
     a.n_tiles = plan.n_tiles;
     a.n_splits = plan.n_splits;
     a.split_tokens = plan.split_tokens;

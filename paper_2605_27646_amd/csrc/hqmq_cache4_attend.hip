@@ -1,7 +1,7 @@
 // Causal attention over a paged cache held in 4 bits (include/hqmq_cache4.h, hqmq_cache4_attend).
 //
 // A workgroup takes 16, 32 or 64 query rows of a kv head (row r = j G + g is query head g of the sequence's row j) and a share of
-// the tokens; its four waves take steps of 32 tokens in turn and join their sums in LDS at the end.  The codes go from memory to
+// the tokens; its waves take steps of 32 tokens in turn and join their sums in LDS at the end.  The codes go from memory to
 // the operands of v_mfma_f32_16x16x32_f16 without crossing lanes, by three choices of order:
 //   S^T = K Q^T   lane (token l % 16, quarter l / 16) reads a quarter of a key's codes, a run of 8 NG channels, and the query operand
 //                 has the same channels in the same places;
@@ -11,6 +11,7 @@
 //                 tokens of the V layout, and product e takes channel e of every run.
 // A query's maximum and sum belong to one column, so every factor is one per lane.
 #include <algorithm>
+#include <type_traits>
 
 #include "hqmq_cache4_device.h"
 
@@ -23,18 +24,30 @@ typedef cache4_h2 half2_t;
 typedef float f4 __attribute__((ext_vector_type(4)));
 typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
 
-constexpr int kWaves = 4, kThreads4 = 64 * kWaves, kStep = 32;
+constexpr int kStep = 32;             // tokens that a wave takes at a time
+constexpr int kMergeThreads = 256;
 constexpr float kNothing = -1.0e30f;  // "no token seen yet": finite, so that differences stay finite
 constexpr float kTop4 = 7.f;          // weights are taken relative to 2^-kTop4 of the largest score,
 constexpr float kRise4 = 15.f;        // and relative to a newer one once they would pass 2^kRise4 (fp16 ends at 2^16)
 constexpr float kLog2e4 = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
-constexpr int kPartChannels = 128;    // of V at most, as a part of its layout
-constexpr int kJoinPitch = kPartChannels + 4;
 
+// Waves of a workgroup.  For up to 16 rows eight, of which two workgroups fill a compute unit's registers.
+constexpr int attend_waves(int blocks) { return blocks == 1 ? 8 : 4; }
+
+// Blocks of rows whose sums are joined at a time: two workgroups fit a compute unit's LDS, heads of more than 128 channels one of eight waves.
+constexpr int attend_pass(int NG, int blocks) { return blocks == 1 || NG > 4 ? 1 : 2; }
+// A row's pitch there: 4 banks past a multiple of all, so that the 16 rows of a wave's store go to all banks once.
+constexpr int attend_pitch(int NG) { return 32 * NG + 4 + 32 * (NG & 1); }
+
+constexpr size_t attend_shared_bytes(int NG, int blocks)  // queries, then the waves' sums of the rows that are joined
+{
+    const size_t queries = (size_t)blocks * NG * 64 * 16;
+    const size_t join = (size_t)attend_waves(blocks) * attend_pass(NG, blocks) * 16 * attend_pitch(NG) * 4;
+    return queries > join ? queries : join;
+}
 constexpr size_t attend_lds_bytes(int NG, int blocks)
 {
-    const size_t queries = (size_t)blocks * NG * 64 * 16, join = (size_t)kWaves * 16 * kJoinPitch * 4;
-    return (queries > join ? queries : join) + (size_t)blocks * 16 * 8 + (size_t)kWaves * blocks * 16 * 2 * 4;
+    return attend_shared_bytes(NG, blocks) + (size_t)blocks * 16 * 8 + (size_t)attend_waves(blocks) * blocks * 16 * 2 * 4;
 }
 
 // Maximum or sum over the four lanes that hold a query's column.
@@ -54,21 +67,37 @@ __device__ __forceinline__ float column_sum(float x)
 }
 
 // n words from an address that is a multiple of 4 n bytes from one of 16.
+#define HQMQ_GLOBAL __attribute__((address_space(1)))
+typedef const HQMQ_GLOBAL uint8_t *Bytes;  // of the cache: an address that the compiler knows to be in memory, though it is made opaque
 template <int n>
 struct Words {
     uint32_t w[n];
 };
 template <int n>
-__device__ __forceinline__ Words<n> load_words(const uint8_t *p)
+__device__ __forceinline__ Words<n> load_words(Bytes p)
 {
-    struct __attribute__((packed, aligned(n % 4 == 0 ? 16 : n % 2 == 0 ? 8 : 4))) Raw {
-        uint32_t w[n];
-    };
-    const Raw r = *reinterpret_cast<const Raw *>(p);
+    typedef uint32_t uint2v __attribute__((ext_vector_type(2)));
     Words<n> out;
+    if constexpr (n % 4 == 0) {
 #pragma unroll
-    for (int i = 0; i < n; ++i)
-        out.w[i] = r.w[i];
+        for (int i = 0; i < n / 4; ++i) {
+            const uint4v y = reinterpret_cast<const HQMQ_GLOBAL uint4v *>(p)[i];
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                out.w[4 * i + e] = y[e];
+        }
+    } else if constexpr (n % 2 == 0) {
+#pragma unroll
+        for (int i = 0; i < n / 2; ++i) {
+            const uint2v y = reinterpret_cast<const HQMQ_GLOBAL uint2v *>(p)[i];
+            out.w[2 * i] = y[0];
+            out.w[2 * i + 1] = y[1];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < n; ++i)
+            out.w[i] = reinterpret_cast<const HQMQ_GLOBAL uint32_t *>(p)[i];
+    }
     return out;
 }
 
@@ -85,8 +114,10 @@ struct Parts {
 template <int kFormat, int NG>
 struct KStage {
     static constexpr int kScales = NG == 1 || NG == 2 || NG == 4 ? 1 : 2;
+    // a byte stays one until it is used: widening it where it is loaded would wait for it
+    typedef std::conditional_t<kFormat == HQMQ_CACHE4_FLOAT, uint8_t, uint32_t> Scale;
     Words<NG> code;
-    uint32_t scale[kScales];
+    Scale scale[kScales];
 };
 template <int kFormat, int NG>
 struct VStage {
@@ -95,41 +126,74 @@ struct VStage {
     Words<kWords> scale[Parts<NG>::n];
 };
 
-// 16 tokens of a head in one page: where they begin in each of the cache's buffers (one address for the wave), and where the lane's
-// share lies behind that (the same for all).
+// 16 tokens of a head in one page: where they begin in each of the cache's buffers, one address for the wave.
 struct Tile {
-    const uint8_t *k_codes, *k_scales, *v_codes, *v_scales;
+    Bytes k_codes, k_scales, v_codes, v_scales;
 };
+// head: the first token of the head in page 0
 template <int kFormat, int NG>
-__device__ __forceinline__ Tile tile_at(const Cache4 &c, int page, int h, int slot)
+__device__ __forceinline__ Tile tile_at(const Tile &head, const Cache4 &c, int page, int slot)
 {
-    constexpr int kScale = kFormat == HQMQ_CACHE4_FLOAT ? 1 : 4;
-    const int64_t row = (((int64_t)page * c.H + h) << c.page_shift) + slot;
-    return Tile{c.k_codes + row * (16 * NG), c.k_scales + row * (kScale * NG), c.v_codes + row * (16 * NG), c.v_scales + row * (kScale * NG)};
+    const uint64_t codes = ((uint64_t)(uint32_t)page * (uint32_t)(c.H * NG) << (c.page_shift + 4)) + (uint32_t)(16 * NG * slot);
+    const uint64_t scales = codes >> (kFormat == HQMQ_CACHE4_FLOAT ? 4 : 2);
+    Tile t = {head.k_codes + codes, head.k_scales + scales, head.v_codes + codes, head.v_scales + scales};
+    asm("" : "+s"(t.k_codes), "+s"(t.k_scales), "+s"(t.v_codes), "+s"(t.v_scales));  // scalar bases: a lane's share is a 32-bit offset
+    return t;
+}
+
+// A lane's places behind a tile's addresses.
+template <int kFormat, int NG>
+struct Places {
+    static constexpr uint32_t kScale = kFormat == HQMQ_CACHE4_FLOAT ? 1 : 4;
+    using P = Parts<NG>;
+    uint32_t k_code, k_scale[KStage<kFormat, NG>::kScales], v_code[P::n], v_scale[P::n];
+    __device__ __forceinline__ explicit Places(uint32_t lane)
+    {
+        const uint32_t token = lane & 15, run = token, quarter = lane >> 4;
+        k_code = token * (16 * NG) + 4 * NG * quarter;
+        k_scale[0] = kScale * (token * NG + (quarter * NG >> 2));
+        k_scale[KStage<kFormat, NG>::kScales - 1] = kScale * (token * NG + ((quarter * NG + (KStage<kFormat, NG>::kScales > 1 ? NG - 1 : 0)) >> 2));
+#pragma unroll
+        for (int p = 0; p < P::n; ++p) {
+            v_code[p] = quarter * (64 * NG) + 4 * P::groups(p) * run + 64 * P::before(p);
+            v_scale[p] = kScale * (4 * (quarter * NG + P::before(p) + (run * P::groups(p) >> 4)));
+        }
+    }
+    // Widening an offset where it is used, in every step, makes it an offset to a scalar base; kept as 64 bits it would be added to each.
+    __device__ __forceinline__ void keep_narrow_k()
+    {
+        asm volatile("" : "+v"(k_code));
+#pragma unroll
+        for (int i = 0; i < KStage<kFormat, NG>::kScales; ++i)
+            asm volatile("" : "+v"(k_scale[i]));
+    }
+    __device__ __forceinline__ void keep_narrow_v()
+    {
+#pragma unroll
+        for (int p = 0; p < P::n; ++p) {
+            asm volatile("" : "+v"(v_code[p]));
+            asm volatile("" : "+v"(v_scale[p]));
+        }
+    }
+};
+
+template <int kFormat, int NG>
+__device__ __forceinline__ void load_k(KStage<kFormat, NG> &s, const Tile &tile, const Places<kFormat, NG> &at)
+{
+    typedef typename KStage<kFormat, NG>::Scale Scale;
+    s.code = load_words<NG>(tile.k_codes + at.k_code);
+#pragma unroll
+    for (int i = 0; i < KStage<kFormat, NG>::kScales; ++i)
+        s.scale[i] = *reinterpret_cast<const HQMQ_GLOBAL Scale *>(tile.k_scales + at.k_scale[i]);
 }
 
 template <int kFormat, int NG>
-__device__ __forceinline__ void load_k(KStage<kFormat, NG> &s, const Tile &tile, int lane)
+__device__ __forceinline__ void load_v(VStage<kFormat, NG> &s, const Tile &tile, const Places<kFormat, NG> &place)
 {
-    const uint32_t token = lane & 15, quarter = lane >> 4, first = quarter * NG >> 2, last = (quarter * NG + NG - 1) >> 2;
-    s.code = load_words<NG>(tile.k_codes + (token * (16 * NG) + 4 * NG * quarter));
-    const auto scale_of = [&](uint32_t g) -> uint32_t {
-        return kFormat == HQMQ_CACHE4_FLOAT ? (uint32_t)tile.k_scales[token * NG + g] : load_words<1>(tile.k_scales + 4 * (token * NG + g)).w[0];
-    };
-    s.scale[0] = scale_of(first);
-    if (KStage<kFormat, NG>::kScales > 1)
-        s.scale[KStage<kFormat, NG>::kScales - 1] = scale_of(last);
-}
-
-template <int kFormat, int NG>
-__device__ __forceinline__ void load_v(VStage<kFormat, NG> &s, const Tile &tile, int lane)
-{
-    constexpr uint32_t kScale = kFormat == HQMQ_CACHE4_FLOAT ? 1 : 4;
-    const uint32_t quarter = lane >> 4, run = lane & 15;
     using P = Parts<NG>;
 #pragma unroll
     for (int p = 0; p < P::n; ++p) {
-        const uint8_t *at = tile.v_codes + (quarter * (64 * NG) + 4 * P::groups(p) * run + 64 * P::before(p));
+        const Bytes at = tile.v_codes + place.v_code[p];
         if (P::groups(p) == 4) {
             const Words<4> w = load_words<4>(at);
 #pragma unroll
@@ -142,7 +206,7 @@ __device__ __forceinline__ void load_v(VStage<kFormat, NG> &s, const Tile &tile,
         } else {
             s.code.w[P::before(p)] = load_words<1>(at).w[0];
         }
-        s.scale[p] = load_words<VStage<kFormat, NG>::kWords>(tile.v_scales + kScale * (4 * (quarter * NG + P::before(p) + (run * P::groups(p) >> 4))));
+        s.scale[p] = load_words<VStage<kFormat, NG>::kWords>(tile.v_scales + place.v_scale[p]);
     }
 }
 
@@ -176,7 +240,7 @@ template <int kFormat, int NG>
 __device__ __forceinline__ half8_t k_operand(const KStage<kFormat, NG> &s, int w, int lane)
 {
     const int quarter = lane >> 4;
-    uint32_t scale = s.scale[0];
+    auto scale = s.scale[0];
     if (KStage<kFormat, NG>::kScales > 1)
         scale = (quarter * NG + w) >> 2 == quarter * NG >> 2 ? scale : s.scale[KStage<kFormat, NG>::kScales - 1];
     const uint32_t code = s.code.w[w];
@@ -188,7 +252,7 @@ __device__ __forceinline__ half8_t k_operand(const KStage<kFormat, NG> &s, int w
         y[2] = e2m1_pair<2>(code, unit);
         y[3] = e2m1_pair<3>(code, unit);
     } else {
-        const half2_t sm = __builtin_bit_cast(half2_t, scale), ss = {sm[0], sm[0]}, mm = {sm[1], sm[1]};
+        const half2_t sm = __builtin_bit_cast(half2_t, (uint32_t)scale), ss = {sm[0], sm[0]}, mm = {sm[1], sm[1]};
 #pragma unroll
         for (int e = 0; e < 4; ++e)
             y[e] = int4_pair(code >> (4 * e), ss, mm);
@@ -255,21 +319,53 @@ __device__ __forceinline__ void unrolled(F &&f)
     }
 }
 
-// Workgroups of a compute unit that the registers are to leave room for.
-constexpr int attend_occupancy(int NG, int blocks) { return blocks == 1 ? (NG <= 4 ? 4 : 2) : 2; }
+// Waves of a SIMD that the registers are to leave room for.
+constexpr int attend_occupancy(int NG, int blocks) { return blocks == 1 && NG <= 4 ? 4 : 2; }
 
 }  // namespace
 
+// Four channels of a result: the weighted sum divided by the weights' sum l, relative to 2^m.
+template <bool kBf16>
+__device__ __forceinline__ void store_row(const Cache4Attend &a, int row, int head, int ch, f4 total, float m, float l, int64_t row_at)
+{
+    const float inverse = l > 0.f ? 1.f / l : 0.f;
+    uint32_t bits[2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        const float u = total[2 * e] * inverse, v = total[2 * e + 1] * inverse;
+        if (kBf16) {
+            typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+            bits[e] = __builtin_bit_cast(uint32_t, b2{(__bf16)u, (__bf16)v});
+        } else {
+            bits[e] = __builtin_bit_cast(uint32_t, half2_t{(_Float16)u, (_Float16)v});
+        }
+    }
+    uint16_t *dst = a.out.data + (int64_t)row * a.out.row + (int64_t)head * a.out.head + ch;
+    if (a.out.wide) {  // a head is a multiple of 8 channels
+        if (ch < a.c.D)
+            *reinterpret_cast<uint2 *>(dst) = make_uint2(bits[0], bits[1]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (ch + e < a.c.D)
+                dst[e] = (uint16_t)(bits[e / 2] >> (16 * (e & 1)));
+    }
+    if (a.lse && ch == 0)
+        a.lse[row_at] = l > 0.f ? kLn2 * (m + __builtin_amdgcn_logf(l)) : -__builtin_inff();
+}
+
 template <int kFormat, int NG, int kBlocks, bool kBf16>
-__global__ __launch_bounds__(kThreads4, attend_occupancy(NG, kBlocks)) void k_cache4_attend(Cache4Attend a)
+__global__ __launch_bounds__(64 * attend_waves(kBlocks), attend_occupancy(NG, kBlocks)) void k_cache4_attend(Cache4Attend a)
 {
     using P = Parts<NG>;
     constexpr int kRows = 16 * kBlocks, kChannels = 2 * NG;  // of a lane
+    constexpr int kWaves = attend_waves(kBlocks), kPitch = attend_pitch(NG);
+    static_assert(kBlocks <= kWaves, "a wave stages a block of queries");
     constexpr bool kFine = !kBf16;
     extern __shared__ __align__(16) unsigned char lds[];
-    constexpr size_t kShared = std::max((size_t)kBlocks * NG * 64 * 16, (size_t)kWaves * 16 * kJoinPitch * 4);
+    constexpr size_t kShared = attend_shared_bytes(NG, kBlocks);
     half8_t *const queries = reinterpret_cast<half8_t *>(lds);           // [kBlocks][NG][lane]
-    float *const join = reinterpret_cast<float *>(lds);                  // [kWaves][16][kJoinPitch], when the queries are done with
+    float *const join = reinterpret_cast<float *>(lds);                  // [kWaves][kPass][16][kPitch], when the queries are done with
     float *const factor = reinterpret_cast<float *>(lds + kShared);      // [kRows]: from products to exponents of 2
     int *const position = reinterpret_cast<int *>(factor + kRows);       // [kRows]: -1 - 2^30 and less: no row
     float *const stats = reinterpret_cast<float *>(position + kRows);    // [kWaves][kRows][2]
@@ -277,80 +373,89 @@ __global__ __launch_bounds__(kThreads4, attend_occupancy(NG, kBlocks)) void k_ca
     const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, quarter = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const Cache4 &c = a.c;
-    const int h = (int)(blockIdx.x % (uint32_t)c.H), rest = (int)(blockIdx.x / (uint32_t)c.H);
-    const int split = rest % a.n_splits, seq = blockIdx.y;
+    const int h = blockIdx.x, seq = blockIdx.z, rest = divided((int)blockIdx.y, a.by_splits), split = (int)blockIdx.y - rest * a.n_splits;
     const int page_mask = (1 << c.page_shift) - 1;
+    const uint64_t head_rows = (uint64_t)h << c.page_shift;
+    constexpr int kScale = kFormat == HQMQ_CACHE4_FLOAT ? 1 : 4;
+    const Tile head = {(Bytes)c.k_codes + head_rows * (16 * NG), (Bytes)c.k_scales + head_rows * (kScale * NG),
+                       (Bytes)c.v_codes + head_rows * (16 * NG), (Bytes)c.v_scales + head_rows * (kScale * NG)};
     const ConstInts table = const_ints(a.b.table + (int64_t)seq * a.b.pitch);
     const Cache4Seq s = cache4_seq(a.b, c.page_shift, seq);
     const int n_rows = s.n * a.G, n_heads = c.H * a.G;
 
     // the longest first: a causal prompt's last rows see the most
-    for (int tile = a.n_tiles - 1 - rest / a.n_splits; tile * kRows < n_rows; tile += a.n_tiles) {
+    for (int tile = a.n_tiles - 1 - rest; tile * kRows < n_rows; tile += a.n_tiles) {
         const int r0 = tile * kRows;
         // ---- what the rows see -----------------------------------------------------------------------------------------
-        const int j_first = r0 / a.G, j_last = min((r0 + kRows - 1) / a.G, s.n - 1);
+        const int j_first = divided(r0, a.by_G), j_last = min(divided(r0 + kRows - 1, a.by_G), s.n - 1);
         const int end = s.pos0 + j_last + 1, all_end = s.pos0 + j_first + 1;  // all_end: every row sees what is before it,
         const int begin = a.window ? max(0, s.pos0 + j_first + 1 - a.window) & ~(kStep - 1) : 0;
         const int all_begin = a.window ? s.pos0 + j_last + 1 - a.window : 0;  // and from here on
+        // Without a window the first pages are looked up before the length is there: no length puts them past the table.
         const int64_t share = (int64_t)begin + (int64_t)split * a.split_tokens;
-        const int from = (int)min(share, (int64_t)max(end, 0));
-        const int to = split == a.n_splits - 1 ? end : (int)min(share + a.split_tokens, (int64_t)max(end, 0));
-        const int n_steps = to > from ? (to - from + kStep - 1) / kStep : 0;
-
-        // Pages of a step's two halves; -1 for none.  Past the share's end: those of its last step.
-        const int last = from + kStep * max(n_steps - 1, 0);
+        const int from = (int)min(share, (int64_t)(a.b.pitch << c.page_shift));
         int page[2];
-        const auto look_up = [&](int step) {
+        const auto look_up = [&](int step, int last) {  // pages of a step's two halves; past the share's end: those of its last step
             const int token = min(from + kStep * step, last);
 #pragma unroll
             for (int x = 0; x < 2; ++x)
-                page[x] = __builtin_amdgcn_readfirstlane(table[min((token + 16 * x) >> c.page_shift, a.b.pitch - 1)]);
+                page[x] = table[min((token + 16 * x) >> c.page_shift, a.b.pitch - 1)];
         };
+        look_up(wave, 0x7fffffdf);
+        const int to = split == a.n_splits - 1 ? end : (int)min(share + a.split_tokens, (int64_t)end);
+        const int n_steps = to > from ? (to - from + kStep - 1) / kStep : 0;
+        const int last = from + kStep * max(n_steps - 1, 0);
         KStage<kFormat, NG> ks[2];
         VStage<kFormat, NG> vs[2];
+        Places<kFormat, NG> places(lane);
         Tile tiles[2];
         bool bad[2];
         const auto tiles_of = [&](int token) {  // of the pages that were looked up last
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
                 bad[x] = (uint32_t)page[x] >= (uint32_t)c.n_pages;
-                tiles[x] = tile_at<kFormat, NG>(c, bad[x] ? 0 : page[x], h, (token + 16 * x) & page_mask);
+                tiles[x] = tile_at<kFormat, NG>(head, c, bad[x] ? 0 : page[x], (token + 16 * x) & page_mask);
             }
         };
+        // ---- the wave's block of queries and its first step are on their way together --------------------------------------
+        const int query = r0 + 16 * wave + col, query_j = divided(query, a.by_G);
+        const bool there = wave < kBlocks && query < n_rows;
+        uint4v bits[NG];
+#pragma unroll
+        for (int w = 0; w < NG; ++w)
+            bits[w] = uint4v{0u, 0u, 0u, 0u};
+        if (there) {
+            const uint16_t *src = a.q.data + (int64_t)(s.first_row + query_j) * a.q.row + (int64_t)(h * a.G + (query - query_j * a.G)) * a.q.head;
+            int D = c.D, ch = 8 * NG * quarter;
+            asm volatile("" : "+s"(D));  // what is compared with it is not kept in registers from tile to tile
+            if (a.q.wide) {
+#pragma unroll
+                for (int w = 0; w < NG; ++w)
+                    if (ch + 8 * w < D)
+                        bits[w] = *reinterpret_cast<const uint4v *>(src + (ch + 8 * w));
+            } else {  // element by element through the lane's own places in LDS
+                uint16_t *const mine = reinterpret_cast<uint16_t *>(queries + wave * NG * 64 + lane);
+#pragma unroll 1
+                for (int e = 0; e < 8 * NG; ++e)
+                    mine[512 * (e >> 3) + (e & 7)] = ch + e < D ? src[ch + e] : (uint16_t)0;
+                asm volatile("" : : : "memory");
+#pragma unroll
+                for (int w = 0; w < NG; ++w)
+                    bits[w] = *reinterpret_cast<const uint4v *>(mine + 512 * w);
+            }
+        }
         if (wave < n_steps) {
-            look_up(wave);
             tiles_of(from + kStep * wave);
 #pragma unroll
             for (int x = 0; x < 2; ++x)
-                load_k(ks[x], tiles[x], lane);
+                load_k(ks[x], tiles[x], places);
 #pragma unroll
             for (int x = 0; x < 2; ++x)
-                load_v(vs[x], tiles[x], lane);
-            look_up(wave + kWaves);
+                load_v(vs[x], tiles[x], places);
+            look_up(wave + kWaves, last);
         }
-
-        // ---- queries to LDS, as operands -------------------------------------------------------------------------------
-        for (int nb = wave; nb < kBlocks; nb += kWaves) {
-            const int r = r0 + 16 * nb + col;
-            const bool there = r < n_rows;
-            const int j = r / a.G;
-            const uint16_t *src = a.q.data + (int64_t)(s.first_row + j) * a.q.row + (int64_t)(h * a.G + (r - j * a.G)) * a.q.head;
-            uint4v bits[NG];
-#pragma unroll
-            for (int w = 0; w < NG; ++w) {
-                const int ch = 8 * (quarter * NG + w);
-                bits[w] = uint4v{0u, 0u, 0u, 0u};
-                if (there && ch < c.D) {
-                    if (a.q.wide) {
-                        bits[w] = *reinterpret_cast<const uint4v *>(src + ch);
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            if (ch + e < c.D)
-                                bits[w][e / 2] |= (uint32_t)src[ch + e] << (16 * (e & 1));
-                    }
-                }
-            }
+        // ---- queries to LDS, as operands
+        if (wave < kBlocks) {
             float f = fabsf(a.scale) * kLog2e4;
             const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;  // a negative scale goes into the queries' signs
             if (kBf16) {
@@ -378,12 +483,12 @@ __global__ __launch_bounds__(kThreads4, attend_occupancy(NG, kBlocks)) void k_ca
                 if (kFormat == HQMQ_CACHE4_INT)  // channels 0 4 1 5 2 6 3 7
                     x = uint4v{__builtin_amdgcn_perm(x[2], x[0], 0x05040100u), __builtin_amdgcn_perm(x[2], x[0], 0x07060302u),
                                __builtin_amdgcn_perm(x[3], x[1], 0x05040100u), __builtin_amdgcn_perm(x[3], x[1], 0x07060302u)};
-                queries[(nb * NG + w) * 64 + lane] = __builtin_bit_cast(half8_t, x);
+                queries[(wave * NG + w) * 64 + lane] = __builtin_bit_cast(half8_t, x);
             }
             if (quarter == 0) {
                 // Products stay below 2^40: with a factor this small they all become 0, but minus infinity stays what it is.
-                factor[16 * nb + col] = fmaxf(f, 0x1p-120f);
-                position[16 * nb + col] = there ? s.pos0 + j : -0x7fffffff;
+                factor[16 * wave + col] = fmaxf(f, 0x1p-120f);
+                position[16 * wave + col] = there ? s.pos0 + query_j : -0x7fffffff;
             }
         }
         __syncthreads();
@@ -425,9 +530,10 @@ __global__ __launch_bounds__(kThreads4, attend_occupancy(NG, kBlocks)) void k_ca
                 }
             }
             tiles_of(min(token + kStep * kWaves, last));
+            places.keep_narrow_k();
 #pragma unroll
             for (int i = 0; i < 2; ++i)
-                load_k(ks[i], tiles[i], lane);
+                load_k(ks[i], tiles[i], places);
             // ---- unseen tokens
             if (token + kStep > all_end || token < all_begin || bad_now[0] || bad_now[1]) {
 #pragma unroll
@@ -464,19 +570,27 @@ __global__ __launch_bounds__(kThreads4, attend_occupancy(NG, kBlocks)) void k_ca
                 }
             }
             // ---- weights
+            float minus = -1.f;
+            asm("" : "+s"(minus));  // a product that the compiler keeps: one instruction takes the fp16 factor as it is
             half8_t hi[kBlocks], lo[kBlocks];
 #pragma unroll
             for (int nb = 0; nb < kBlocks; ++nb) {
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
+                    for (int r = 0; r < 4; r += 2) {
                         const float p = __builtin_amdgcn_exp2f(fmaf(x[i][nb][r], scale[nb], -ref[nb]));
+                        const float q = __builtin_amdgcn_exp2f(fmaf(x[i][nb][r + 1], scale[nb], -ref[nb]));
                         sum[nb] += p;
-                        const _Float16 rounded = (_Float16)p;
-                        hi[nb][4 * i + r] = rounded;
-                        if (kFine)
-                            lo[nb][4 * i + r] = (_Float16)(p - (float)rounded);
+                        sum[nb] += q;
+                        const half2_t rounded = {(_Float16)p, (_Float16)q};
+                        hi[nb][4 * i + r] = rounded[0];
+                        hi[nb][4 * i + r + 1] = rounded[1];
+                        if (kFine) {
+                            const half2_t rest = {(_Float16)fmaf((float)rounded[0], minus, p), (_Float16)fmaf((float)rounded[1], minus, q)};
+                            lo[nb][4 * i + r] = rest[0];
+                            lo[nb][4 * i + r + 1] = rest[1];
+                        }
                     }
             }
             // ---- values: a token that is none of the sequence's may hold anything
@@ -506,101 +620,84 @@ __global__ __launch_bounds__(kThreads4, attend_occupancy(NG, kBlocks)) void k_ca
                     }
                 });
             });
+            places.keep_narrow_v();
 #pragma unroll
             for (int i = 0; i < 2; ++i)
-                load_v(vs[i], tiles[i], lane);
-            look_up(step + 2 * kWaves);
+                load_v(vs[i], tiles[i], places);
+            look_up(step + 2 * kWaves, last);
         }
 
-        // ---- the four waves' sums joined -------------------------------------------------------------------------------
+        // ---- the waves' sums joined, kPass blocks of rows at a time -----------------------------------------------------------
 #pragma unroll
         for (int nb = 0; nb < kBlocks; ++nb) {
             const float total = column_sum(sum[nb]);
-            if (quarter == 0) {
-                stats[(wave * kRows + 16 * nb + col) * 2] = ref[nb];
-                stats[(wave * kRows + 16 * nb + col) * 2 + 1] = total;
-            }
+            if (quarter == 0)
+                *reinterpret_cast<float2 *>(stats + (wave * kRows + 16 * nb + col) * 2) = make_float2(ref[nb], total);
         }
-        __syncthreads();
-        const bool whole_result = a.n_splits == 1;
-        unrolled<0, kBlocks>([&](auto block) {
-            constexpr int nb = decltype(block)::value;
-            const auto joined = [&](int row, float &ref_all, float &sum_all) {
-                ref_all = kNothing;
+        __syncthreads();  // the queries are done with
+        constexpr int kPass = attend_pass(NG, kBlocks), kUnits = 8 * NG;  // a thread takes 4 channels of a row
+#pragma unroll 1
+        for (int first = 0; first < kBlocks; first += kPass) {
+            unrolled<0, kBlocks>([&](auto t) {
+                constexpr int nb = decltype(t)::value;
+                if (first == nb / kPass * kPass) {
+                    float *const mine = join + ((wave * kPass + nb % kPass) * 16 + col) * kPitch;
+                    unrolled<0, P::n>([&](auto part) {
+                        constexpr int p = decltype(part)::value, kRun = 2 * P::groups(p), kWide = kRun < 4 ? 2 : 4;
+                        typedef float wide __attribute__((ext_vector_type(kWide)));
 #pragma unroll
-                for (int w = 0; w < kWaves; ++w)
-                    ref_all = fmaxf(ref_all, stats[(w * kRows + row) * 2]);
-                sum_all = 0.f;
+                        for (int r = 0; r < 4; ++r)
 #pragma unroll
-                for (int w = 0; w < kWaves; ++w)
-                    sum_all += stats[(w * kRows + row) * 2 + 1] * __builtin_amdgcn_exp2f(stats[(w * kRows + row) * 2] - ref_all);
-            };
-            float ref_all, sum_all;
-            joined(16 * nb + col, ref_all, sum_all);
-            const float f = __builtin_amdgcn_exp2f(ref[nb] - ref_all);
-            unrolled<0, P::n>([&](auto part) {
-                constexpr int p = decltype(part)::value, kRun = 2 * P::groups(p), kUnits = 4 * P::groups(p);
+                            for (int e0 = 0; e0 < kRun; e0 += kWide) {
+                                wide y;
 #pragma unroll
-                for (int r = 0; r < 4; ++r)
-#pragma unroll
-                    for (int e = 0; e < kRun; ++e)
-                        join[(wave * 16 + col) * kJoinPitch + kRun * (4 * quarter + r) + e] = f * o[2 * P::before(p) + e][nb][r];
-                __syncthreads();
-                if (tid < 16 * kUnits) {
-                    const int row = tid / kUnits, ch0 = 8 * (tid % kUnits), r = r0 + 16 * nb + row;
-                    float m, l;
-                    joined(16 * nb + row, m, l);
-                    f4 total[2] = {f4{0.f, 0.f, 0.f, 0.f}, f4{0.f, 0.f, 0.f, 0.f}};
-#pragma unroll
-                    for (int w = 0; w < kWaves; ++w)
-#pragma unroll
-                        for (int i = 0; i < 2; ++i)
-                            total[i] += *reinterpret_cast<const f4 *>(join + (w * 16 + row) * kJoinPitch + ch0 + 4 * i);
-                    if (r < n_rows) {
-                        const int j = r / a.G, head = h * a.G + (r - j * a.G), ch = 32 * P::before(p) + ch0;
-                        const int64_t row_at = (int64_t)(s.first_row + j) * n_heads + head;
-                        if (!whole_result) {
-                            const int64_t at = row_at * a.n_splits + split;
-                            if (l > 0.f) {
-                                f4 *dst = reinterpret_cast<f4 *>(a.part_acc + at * (32 * NG) + ch);
-                                dst[0] = total[0];
-                                dst[1] = total[1];
+                                for (int e = 0; e < kWide; ++e)
+                                    y[e] = o[2 * P::before(p) + e0 + e][nb][r];
+                                *reinterpret_cast<wide *>(mine + 32 * P::before(p) + kRun * (4 * quarter + r) + e0) = y;
                             }
-                            if (ch == 0) {
-                                a.part_ml[2 * at] = m;
-                                a.part_ml[2 * at + 1] = l;
-                            }
-                        } else {
-                            const float inverse = l > 0.f ? 1.f / l : 0.f;
-                            uint4v bits;
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                const float u = total[e / 2][2 * (e & 1)] * inverse, v = total[e / 2][2 * (e & 1) + 1] * inverse;
-                                if (kBf16) {
-                                    typedef __bf16 b2 __attribute__((ext_vector_type(2)));
-                                    bits[e] = __builtin_bit_cast(uint32_t, b2{(__bf16)u, (__bf16)v});
-                                } else {
-                                    bits[e] = __builtin_bit_cast(uint32_t, half2_t{(_Float16)u, (_Float16)v});
-                                }
-                            }
-                            uint16_t *dst = a.out.data + (int64_t)(s.first_row + j) * a.out.row + (int64_t)head * a.out.head + ch;
-                            if (a.out.wide) {
-                                if (ch < c.D)
-                                    *reinterpret_cast<uint4v *>(dst) = bits;
-                            } else {
-#pragma unroll
-                                for (int e = 0; e < 8; ++e)
-                                    if (ch + e < c.D)
-                                        dst[e] = (uint16_t)(bits[e / 2] >> (16 * (e & 1)));
-                            }
-                            if (a.lse && ch == 0)
-                                a.lse[row_at] = l > 0.f ? kLn2 * (m + __builtin_amdgcn_logf(l)) : -__builtin_inff();
-                        }
-                    }
+                    });
                 }
-                __syncthreads();
             });
-        });
+            __syncthreads();
+#pragma unroll 1
+            for (int unit = tid; unit < kPass * 16 * kUnits; unit += 64 * kWaves) {
+                const int row = unit / kUnits, ch = 4 * (unit - row * kUnits), r = r0 + 16 * first + row;
+                if (r >= n_rows)
+                    break;
+                float2 part[kWaves];
+                f4 y[kWaves];
+#pragma unroll
+                for (int w = 0; w < kWaves; ++w) {
+                    part[w] = *reinterpret_cast<const float2 *>(stats + (w * kRows + 16 * first + row) * 2);
+                    y[w] = *reinterpret_cast<const f4 *>(join + (w * kPass * 16 + row) * kPitch + ch);
+                }
+                float m = kNothing, l = 0.f;
+#pragma unroll
+                for (int w = 0; w < kWaves; ++w)
+                    m = fmaxf(m, part[w].x);
+                f4 total = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int w = 0; w < kWaves; ++w) {
+                    const float f = __builtin_amdgcn_exp2f(part[w].x - m);
+                    l = fmaf(part[w].y, f, l);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        total[e] = fmaf(f, y[w][e], total[e]);
+                }
+                const int j = divided(r, a.by_G), in_head = h * a.G + (r - j * a.G);
+                const int64_t row_at = (int64_t)(s.first_row + j) * n_heads + in_head;
+                if (a.n_splits > 1) {
+                    const int64_t at = row_at * a.n_splits + split;
+                    if (l > 0.f)
+                        *reinterpret_cast<f4 *>(a.part_acc + at * (32 * NG) + ch) = total;
+                    if (ch == 0)
+                        *reinterpret_cast<float2 *>(a.part_ml + 2 * at) = make_float2(m, l);
+                } else {
+                    store_row<kBf16>(a, s.first_row + j, in_head, ch, total, m, l, row_at);
+                }
+            }
+            __syncthreads();
+        }
     }
 }
 
@@ -608,36 +705,46 @@ __global__ __launch_bounds__(kThreads4, attend_occupancy(NG, kBlocks)) void k_ca
 // turn, as many at a time as rows of 4-channel lanes fit a wave, and join their sums in LDS.
 constexpr int kMostSplits = 128;
 template <bool kBf16>
-__global__ __launch_bounds__(kThreads4) void k_cache4_merge(Cache4Attend a)
+__global__ __launch_bounds__(kMergeThreads) void k_cache4_merge(Cache4Attend a)
 {
+    constexpr int kAhead = 8;
     __shared__ __align__(16) float weight[kMostSplits];
-    __shared__ __align__(16) f4 partial[kThreads4];
+    __shared__ __align__(16) f4 partial[kMergeThreads];
     __shared__ float whole[2];
-    const int tid = threadIdx.x, n_heads = a.c.H * a.G, width = 32 * a.c.NG, lanes = width / 4, at_once = kThreads4 / lanes;
+    const int tid = threadIdx.x, n_heads = a.c.H * a.G, width = 32 * a.c.NG, lanes = width / 4, at_once = kMergeThreads / lanes;
     const int mine = tid / lanes, ch = 4 * (tid - mine * lanes);
     const int64_t n = (int64_t)a.b.n_rows * n_heads;
+    const int first_row = a.b.starts ? const_ints(a.b.starts)[0] : 0, end_row = a.b.starts ? const_ints(a.b.starts)[a.b.n_seqs] : a.b.n_rows;
     for (int64_t row_at = blockIdx.x; row_at < n; row_at += gridDim.x) {
-        const int row = (int)(row_at / n_heads), head = (int)(row_at - (int64_t)row * n_heads);
-        if (a.b.starts && (row < a.b.starts[0] || row >= a.b.starts[a.b.n_seqs]))
+        const int row = (int)((uint32_t)row_at / (uint32_t)n_heads), head = (int)row_at - row * n_heads;
+        if (row < first_row || row >= end_row)
             continue;
-        __syncthreads();
+        const float *acc = a.part_acc + row_at * a.n_splits * width + ch;
+        const auto load = [&](int s) { return *reinterpret_cast<const f4 *>(acc + (int64_t)s * width); };
+        const int n_mine = mine < at_once ? (a.n_splits - mine + at_once - 1) / at_once : 0;  // splits mine, mine + at_once, ..
+        f4 y[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+            if (i < n_mine)
+                y[i] = load(mine + i * at_once);
         if (tid < 64) {
             const float2 *ml = reinterpret_cast<const float2 *>(a.part_ml) + row_at * a.n_splits;
-            float2 y[kMostSplits / 64];
+            float2 z[kMostSplits / 64];
             float m = kNothing, l = 0.f;
 #pragma unroll
-            for (int i = 0; i < kMostSplits / 64; ++i) {
-                y[i] = tid + 64 * i < a.n_splits ? ml[tid + 64 * i] : make_float2(kNothing, 0.f);
-                m = fmaxf(m, y[i].y > 0.f ? y[i].x : kNothing);
-            }
+            for (int i = 0; i < kMostSplits / 64; ++i)
+                z[i] = tid + 64 * i < a.n_splits ? ml[tid + 64 * i] : make_float2(kNothing, 0.f);
+#pragma unroll
+            for (int i = 0; i < kMostSplits / 64; ++i)
+                m = fmaxf(m, z[i].y > 0.f ? z[i].x : kNothing);
 #pragma unroll
             for (int d = 32; d; d >>= 1)
                 m = fmaxf(m, __shfl_xor(m, d));
 #pragma unroll
             for (int i = 0; i < kMostSplits / 64; ++i) {
-                const float f = y[i].y > 0.f ? __builtin_amdgcn_exp2f(y[i].x - m) : 0.f;
+                const float f = z[i].y > 0.f ? __builtin_amdgcn_exp2f(z[i].x - m) : 0.f;
                 weight[tid + 64 * i] = f;
-                l = fmaf(y[i].y, f, l);
+                l = fmaf(z[i].y, f, l);
             }
 #pragma unroll
             for (int d = 32; d; d >>= 1)
@@ -649,34 +756,30 @@ __global__ __launch_bounds__(kThreads4) void k_cache4_merge(Cache4Attend a)
         }
         __syncthreads();
         f4 total = f4{0.f, 0.f, 0.f, 0.f};
-        if (mine < at_once) {
-            const float *acc = a.part_acc + row_at * a.n_splits * width + ch;
-#pragma unroll 4
-            for (int s = mine; s < a.n_splits; s += at_once) {
-                const float f = weight[s];
-                const f4 y = *reinterpret_cast<const f4 *>(acc + (int64_t)s * width);
-                if (f > 0.f)  // of a split that saw nothing there are no sums
-                    total += f4{f, f, f, f} * y;
-            }
-        }
+        const auto add = [&](int s, f4 z) {
+            const float f = weight[s];
+            if (f > 0.f)  // of a split that saw nothing there are no sums
+                total += f4{f, f, f, f} * z;
+        };
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+            if (i < n_mine)
+                add(mine + i * at_once, y[i]);
+        for (int i = kAhead; i < n_mine; ++i)
+            add(mine + i * at_once, load(mine + i * at_once));
         partial[tid] = total;
         __syncthreads();
         if (tid < lanes) {
             for (int i = 1; i < at_once; ++i)
                 total += partial[tid + i * lanes];
-            const float l = whole[1], inverse = l > 0.f ? 1.f / l : 0.f;
-            uint16_t *dst = a.out.data + (int64_t)row * a.out.row + (int64_t)head * a.out.head + ch;
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (ch + e < a.c.D) {
-                    const float y = total[e] * inverse;
-                    dst[e] = kBf16 ? __builtin_bit_cast(uint16_t, (__bf16)y) : __builtin_bit_cast(uint16_t, (_Float16)y);
-                }
-            if (a.lse && tid == 0)
-                a.lse[row_at] = l > 0.f ? kLn2 * (whole[0] + __builtin_amdgcn_logf(l)) : -__builtin_inff();
+            store_row<kBf16>(a, row, head, ch, total, whole[0], whole[1], row_at);
         }
+        __syncthreads();
     }
 }
+
+constexpr int kWantedGroups = 512;
+constexpr int kLeastRounds = 2;
 
 Cache4Plan plan_cache4_attend(const Cache4 &c, const Cache4Seqs &b, int max_rows, int max_length, int G, int window)
 {
@@ -684,13 +787,12 @@ Cache4Plan plan_cache4_attend(const Cache4 &c, const Cache4Seqs &b, int max_rows
     const int64_t rows = (int64_t)max_rows * G;
     p.blocks = rows <= 16 ? 1 : rows <= 32 || c.NG > 4 ? 2 : 4;
     const int64_t heads = (int64_t)c.H * b.n_seqs;
-    const int64_t most_tiles = ((int64_t)1 << 22) / c.H > 0 ? ((int64_t)1 << 22) / c.H : 1;
-    p.n_tiles = (int32_t)std::min((rows + 16 * p.blocks - 1) / (16 * p.blocks), most_tiles);
+    p.n_tiles = (int32_t)std::min<int64_t>((rows + 16 * p.blocks - 1) / (16 * p.blocks), 512);  // more take turns
     int64_t span = max_length;
     if (window)
         span = std::min(span, (int64_t)window + std::min<int64_t>(max_rows, 16 * p.blocks / G + 1));
-    const int64_t round = kStep * kWaves, rr = getenv("HQ_R") ? atoi(getenv("HQ_R")) : 2, most = std::max<int64_t>((span + rr * round - 1) / (rr * round), 1);
-    const int64_t wanted = (getenv("HQ_S") ? atoi(getenv("HQ_S")) : 512) / std::max<int64_t>(p.n_tiles * heads, 1);
+    const int64_t round = kStep * attend_waves(p.blocks), most = std::max<int64_t>((span + kLeastRounds * round - 1) / (kLeastRounds * round), 1);
+    const int64_t wanted = kWantedGroups / std::max<int64_t>(p.n_tiles * heads, 1);
     p.n_splits = (int32_t)std::max<int64_t>(std::min<int64_t>(std::min(wanted, most), kMostSplits), 1);
     p.split_tokens = (int32_t)((span + p.n_splits * round - 1) / (p.n_splits * round) * round);
     p.n_splits = (int32_t)std::max<int64_t>((span + p.split_tokens - 1) / p.split_tokens, 1);
@@ -731,22 +833,43 @@ const void *attend_kernel(int NG, int blocks)
 
 }  // namespace
 
+static const void *attend_kernel(int format, bool bf16, int NG, int blocks)
+{
+    if (format == HQMQ_CACHE4_FLOAT)
+        return bf16 ? attend_kernel<HQMQ_CACHE4_FLOAT, true>(NG, blocks) : attend_kernel<HQMQ_CACHE4_FLOAT, false>(NG, blocks);
+    return bf16 ? attend_kernel<HQMQ_CACHE4_INT, true>(NG, blocks) : attend_kernel<HQMQ_CACHE4_INT, false>(NG, blocks);
+}
+
+hipError_t prepare_cache4_kernels()
+{
+    for (int format : {HQMQ_CACHE4_FLOAT, HQMQ_CACHE4_INT})
+        for (int NG : {1, 2, 3, 4, 6, 8})
+            for (int blocks : {1, 2, 4})
+                for (int bf16 = 0; bf16 < 2; ++bf16) {
+                    if (attend_lds_bytes(NG, blocks) <= 64 * 1024 || (NG > 4 && blocks > 2))
+                        continue;
+                    const hipError_t err = hipFuncSetAttribute(attend_kernel(format, bf16 != 0, NG, blocks), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                                               (int)attend_lds_bytes(NG, blocks));
+                    if (err != hipSuccess)
+                        return err;
+                }
+    return hipSuccess;
+}
+
 hipError_t launch_cache4_attend(const Cache4Attend &a, const Cache4Plan &plan, bool bf16, hipStream_t stream)
 {
-    const bool f = a.c.format == HQMQ_CACHE4_FLOAT;
-    const void *kernel = f ? (bf16 ? attend_kernel<HQMQ_CACHE4_FLOAT, true>(a.c.NG, plan.blocks) : attend_kernel<HQMQ_CACHE4_FLOAT, false>(a.c.NG, plan.blocks))
-                           : (bf16 ? attend_kernel<HQMQ_CACHE4_INT, true>(a.c.NG, plan.blocks) : attend_kernel<HQMQ_CACHE4_INT, false>(a.c.NG, plan.blocks));
-    const dim3 grid((unsigned)((int64_t)a.c.H * plan.n_tiles * plan.n_splits), (unsigned)a.b.n_seqs);
+    const void *kernel = attend_kernel(a.c.format, bf16, a.c.NG, plan.blocks);
+    const dim3 grid((unsigned)a.c.H, (unsigned)(plan.n_tiles * plan.n_splits), (unsigned)a.b.n_seqs);
     Cache4Attend args = a;
     void *list[] = {&args};
-    hipError_t err = hipLaunchKernel(kernel, grid, dim3(kThreads4), list, attend_lds_bytes(a.c.NG, plan.blocks), stream);
+    hipError_t err = hipLaunchKernel(kernel, grid, dim3(64 * attend_waves(plan.blocks)), list, attend_lds_bytes(a.c.NG, plan.blocks), stream);
     if (err != hipSuccess || plan.n_splits == 1)
         return err;
     const dim3 rows((unsigned)std::min<int64_t>((int64_t)a.b.n_rows * a.c.H * a.G, 1 << 20));
     if (bf16)
-        k_cache4_merge<true><<<rows, kThreads4, 0, stream>>>(args);
+        k_cache4_merge<true><<<rows, kMergeThreads, 0, stream>>>(args);
     else
-        k_cache4_merge<false><<<rows, kThreads4, 0, stream>>>(args);
+        k_cache4_merge<false><<<rows, kMergeThreads, 0, stream>>>(args);
     return hipGetLastError();
 }
 

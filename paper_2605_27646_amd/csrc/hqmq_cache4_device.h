@@ -70,7 +70,9 @@ __device__ __forceinline__ cache4_h2 e2m1_pair(uint32_t word, float scale)
 // fp16 number 0x6400 | c, and the difference is exact.
 __device__ __forceinline__ cache4_h2 int4_pair(uint32_t word, cache4_h2 s, cache4_h2 m)
 {
-    const cache4_h2 big = __builtin_bit_cast(cache4_h2, (word & 0x000f000fu) | 0x64006400u);
+    uint32_t magic = 0x64006400u;
+    asm("" : "+v"(magic));  // in a vector register: one instruction masks and adds it, which takes one scalar operand only
+    const cache4_h2 big = __builtin_bit_cast(cache4_h2, (word & 0x000f000fu) | magic);
     return __builtin_elementwise_fma(big - cache4_h2{(_Float16)1024.f, (_Float16)1024.f}, s, m);
 }
 
@@ -99,6 +101,20 @@ hipError_t launch_cache4_write(const Cache4 &c, const Cache4Seqs &b, int max_row
 hipError_t launch_cache4_read(const Cache4 &c, const Cache4Seqs &b, int max_rows, bool bf16, const Cache4Rows &k, const Cache4Rows &v,
                               hipStream_t stream);
 
+// Division of numbers below 2^30 by one that the host knows: with l = ceil(log2 d) and m = ceil(2^(30 + l) / d), which is at most 2^30 + 1,
+// n m / 2^(30 + l) exceeds n / d by less than 2^l / 2^(30 + l) * n < 1 / d, and so has the same whole part.
+struct Divisor {
+    uint32_t mul, shift;
+};
+inline Divisor make_divisor(uint32_t d)
+{
+    uint32_t l = 0;
+    while ((1u << l) < d)
+        ++l;
+    return Divisor{(uint32_t)(((1ull << (30 + l)) + d - 1) / d), 30 + l};
+}
+__host__ __device__ __forceinline__ int divided(int n, Divisor d) { return (int)((uint64_t)(uint32_t)n * d.mul >> d.shift); }
+
 struct Cache4Attend {
     Cache4 c;
     Cache4Seqs b;
@@ -108,6 +124,7 @@ struct Cache4Attend {
     float *part_ml;            // [n_rows * H * G][n_splits][2]: reference (log2 domain) and sum of the weights, 0: nothing seen
     float scale;
     int32_t G, window;
+    Divisor by_G, by_splits;
     int32_t n_tiles, n_splits; // workgroups along the rows and along the tokens
     int32_t split_tokens;      // of each split but the last, which goes to the end
 };
@@ -117,6 +134,7 @@ struct Cache4Plan {
     uint64_t ml_bytes, acc_bytes;
 };
 Cache4Plan plan_cache4_attend(const Cache4 &c, const Cache4Seqs &b, int max_rows, int max_length, int G, int window);
+hipError_t prepare_cache4_kernels();  // once per device, before the first launch_cache4_attend on it
 hipError_t launch_cache4_attend(const Cache4Attend &a, const Cache4Plan &plan, bool bf16, hipStream_t stream);
 
 }  // namespace hqmq
