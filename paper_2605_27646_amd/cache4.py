@@ -4,13 +4,12 @@ from __future__ import annotations
 
 import ctypes as C
 import functools
-from dataclasses import dataclass
 
 import torch
 
 from . import binding
-from .binding import _check, _stream_ptr
-from .serving import _on_this_device, _rows_of
+from .binding import _check, _raw_stream, _stream_ptr
+from .serving import _rows_of
 
 HQMQ_CACHE4_FLOAT = 0
 HQMQ_CACHE4_INT = 1
@@ -69,16 +68,33 @@ def hqmq_cache4_sizes(params: Cache4Params) -> tuple:
     return _sizes(bytes(params))
 
 
-@dataclass
 class Cache4Buffers:
-    """The pages: uint8 tensors of hqmq_cache4_sizes(params) bytes (any shape, contiguous)."""
-    k_codes: torch.Tensor
-    k_scales: torch.Tensor
-    v_codes: torch.Tensor
-    v_scales: torch.Tensor
+    """The pages: uint8 tensors of hqmq_cache4_sizes(params) bytes (any shape, contiguous), of one device.  They are looked at when
+    they are set and with the first call of other params; they have to stay in place from then on."""
+
+    def __init__(self, k_codes: torch.Tensor, k_scales: torch.Tensor, v_codes: torch.Tensor, v_scales: torch.Tensor):
+        self.k_codes, self.k_scales, self.v_codes, self.v_scales = k_codes, k_scales, v_codes, v_scales
+
+    def __setattr__(self, name, value):
+        object.__setattr__(self, name, value)
+        object.__setattr__(self, "_held", None)  # params, and the calls' argument and device for them
 
     def as_struct(self) -> _Buffers:
         return _Buffers(self.k_codes.data_ptr(), self.k_scales.data_ptr(), self.v_codes.data_ptr(), self.v_scales.data_ptr())
+
+    def _argument(self, params: Cache4Params) -> tuple:
+        key, held = bytes(params), self._held
+        if held is None or held[0] != key:
+            codes, scales = hqmq_cache4_sizes(params)
+            tensors = ((self.k_codes, codes), (self.v_codes, codes), (self.k_scales, scales), (self.v_scales, scales))
+            if any(t.nbytes < n or not t.is_contiguous() for t, n in tensors):
+                raise ValueError(f"the cache's codes must be contiguous and hold {codes} bytes, its scales {scales}")
+            device = self.k_codes.get_device()
+            if any(t.get_device() != device for t, _ in tensors):
+                raise ValueError("the cache's tensors must be on one device")
+            held = (key, (C.byref(self.as_struct()), device))
+            object.__setattr__(self, "_held", held)
+        return held[1]
 
 
 def alloc_cache4(params: Cache4Params, device) -> Cache4Buffers:
@@ -90,7 +106,7 @@ class Cache4Batch:
     """Which rows a call has and where their tokens lie: block_table (int32 [n_seqs, pages_per_seq]), lengths (int32 [n_seqs], the
     call's rows included), starts (int32 [n_seqs + 1], ascending; None: equal shares).  max_rows and max_length: the largest as
     far as the host knows them, by default all rows (of starts) and all that the table has room for; they shape the launch, not
-    the results.  The tensors are read when the calls run, so that one batch serves many steps."""
+    the results.  The tensors are read when the calls run, so that one batch serves many steps; they have to stay in place."""
 
     def __init__(self, block_table: torch.Tensor, lengths: torch.Tensor, starts: torch.Tensor | None = None, max_rows: int | None = None,
                  max_length: int | None = None):
@@ -101,38 +117,41 @@ class Cache4Batch:
         _rows_of("lengths", lengths, torch.int32, (n,))
         if starts is not None:
             _rows_of("starts", starts, torch.int32, (n + 1,))
-        self.tensors = (block_table, lengths, starts)
+        self._tensors = (block_table, lengths, starts)
+        self._device = block_table.get_device()
+        if any(t is not None and t.get_device() != self._device for t in self._tensors):
+            raise ValueError("block_table, lengths and starts must be on one device")
         self.struct = _Batch(n, pages, 2 ** 30 if max_rows is None else int(max_rows), 2 ** 30 if max_length is None else int(max_length),
                              block_table.data_ptr(), lengths.data_ptr(), None if starts is None else starts.data_ptr())
+        self._argument = C.byref(self.struct)
 
 
-def _rows_struct(name: str, x: torch.Tensor, heads: int | None, D: int, like: torch.Tensor | None = None) -> _Rows:
-    """x [n_rows, heads, D] with contiguous channels; like: a tensor that has its type and number of rows."""
-    if (x.dim() != 3 or x.dtype not in _TYPES or x.shape[2] != D or (heads is not None and x.shape[1] != heads)
-            or (D > 1 and x.shape[0] and x.shape[1] and x.stride(2) != 1)):
-        raise ValueError(f"{name} must be fp16 or bf16 [n_rows, {'n_q_heads' if heads is None else heads}, {D}] with contiguous channels")
-    if like is not None and (x.dtype is not like.dtype or x.shape[0] != like.shape[0]):
-        raise ValueError(f"{name} must have the type and the number of rows of the other rows")
-    return _Rows(x.data_ptr(), x.stride(0), x.stride(1))
+_ELSEWHERE = "every tensor must be on torch's current device"
 
 
-def _hold_cache(params: Cache4Params, cache: Cache4Buffers, batch: Cache4Batch, *rows) -> _Buffers:
-    """The buffers are as long as params says, which the library cannot know, and everything is on the current device."""
-    codes, scales = hqmq_cache4_sizes(params)
-    for t, n in ((cache.k_codes, codes), (cache.v_codes, codes), (cache.k_scales, scales), (cache.v_scales, scales)):
-        if t.nbytes < n or not t.is_contiguous():
-            raise ValueError(f"the cache's codes must be contiguous and hold {codes} bytes, its scales {scales}")
-    _on_this_device(cache.k_codes, cache.k_scales, cache.v_codes, cache.v_scales, *batch.tensors, *rows)
-    return cache.as_struct()
+def _rows(name: str, x: torch.Tensor, D: int) -> tuple:
+    """x [n_rows, heads, D] with contiguous channels: (argument of the calls, its shape, its type)."""
+    shape, stride, code = x.shape, x.stride(), _TYPES.get(x.dtype)
+    if code is None or len(shape) != 3 or shape[2] != D or (stride[2] != 1 and D > 1 and x.numel()):
+        raise ValueError(f"{name} must be fp16 or bf16 [n_rows, heads, {D}] with contiguous channels")
+    return C.byref(_Rows(x.data_ptr(), stride[0], stride[1])), shape, code
+
+
+def _stream(stream, device: int) -> int:
+    return _raw_stream(device) if stream is None and _raw_stream is not None else _stream_ptr(stream)
 
 
 def _move(name, params, cache, batch, k, v, stream) -> None:
-    k_rows = _rows_struct("k", k, params.H, params.D)
-    v_rows = _rows_struct("v", v, params.H, params.D, k)
-    buffers = _hold_cache(params, cache, batch, k, v)
-    rc = getattr(_load(), name)(C.byref(params), C.byref(buffers), C.byref(batch.struct), k.shape[0], _TYPES[k.dtype], C.byref(k_rows),
-                                C.byref(v_rows), _stream_ptr(stream))
-    _check(rc, name)
+    k_rows, shape, code = _rows("k", k, params.D)
+    v_rows, v_shape, v_code = _rows("v", v, params.D)
+    if shape[1] != params.H or v_shape != shape or v_code != code:
+        raise ValueError(f"k and v must be of one type, [n_rows, {params.H}, {params.D}] both")
+    buffers, device = cache._argument(params)
+    if not (device == batch._device == k.get_device() == v.get_device() == torch.cuda.current_device()):
+        raise ValueError(_ELSEWHERE)
+    rc = getattr(_lib or _load(), name)(params, buffers, batch._argument, shape[0], code, k_rows, v_rows, _stream(stream, device))
+    if rc:
+        _check(rc, name)
 
 
 def hqmq_cache4_write(params: Cache4Params, cache: Cache4Buffers, batch: Cache4Batch, k: torch.Tensor, v: torch.Tensor, stream=None) -> None:
@@ -153,15 +172,20 @@ def hqmq_cache4_attend(params: Cache4Params, cache: Cache4Buffers, batch: Cache4
                        workspace: torch.Tensor | None = None, window: int = 0, lse: torch.Tensor | None = None, stream=None) -> None:
     """Enqueue the causal attention of q (fp16 or bf16 [n_rows, n_q_heads, D]) over the pages of the batch's sequences, with a
     window of that many tokens if it is not 0.  lse: optional fp32 output [n_rows, n_q_heads]."""
-    q_rows = _rows_struct("q", q, None, params.D)
-    out_rows = _rows_struct("out", out, q.shape[1], params.D, q)
+    q_rows, shape, code = _rows("q", q, params.D)
+    out_rows, out_shape, out_code = _rows("out", out, params.D)
+    if out_shape != shape or out_code != code:
+        raise ValueError("out must have the shape and the type of q")
     if lse is not None:
-        _rows_of("lse", lse, torch.float32, q.shape[:2])
+        _rows_of("lse", lse, torch.float32, shape[:2])
     if workspace is not None and not workspace.is_contiguous():
         raise ValueError("workspace must be contiguous")
-    buffers = _hold_cache(params, cache, batch, q, out, lse, workspace)
-    rc = _load().hqmq_cache4_attend(C.byref(params), C.byref(buffers), C.byref(batch.struct), q.shape[0], q.shape[1], _TYPES[q.dtype],
-                                    C.byref(q_rows), float(scale), int(window), C.byref(out_rows), None if lse is None else lse.data_ptr(),
-                                    None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.nbytes,
-                                    _stream_ptr(stream))
-    _check(rc, "hqmq_cache4_attend")
+    buffers, device = cache._argument(params)
+    if (not (device == batch._device == q.get_device() == out.get_device() == torch.cuda.current_device())
+            or (lse is not None and lse.get_device() != device) or (workspace is not None and workspace.get_device() != device)):
+        raise ValueError(_ELSEWHERE)
+    rc = (_lib or _load()).hqmq_cache4_attend(params, buffers, batch._argument, shape[0], shape[1], code, q_rows, scale, window, out_rows,
+                                              None if lse is None else lse.data_ptr(), None if workspace is None else workspace.data_ptr(),
+                                              0 if workspace is None else workspace.nbytes, _stream(stream, device))
+    if rc:
+        _check(rc, "hqmq_cache4_attend")

@@ -1375,10 +1375,9 @@ static int32_t cache4_most_rows(const hqmq_cache4_batch *b, int32_t n_rows)
     return std::max(1, b->starts ? std::min(b->max_rows, n_rows) : n_rows / b->n_seqs);
 }
 
-static Cache4Rows make_cache4_rows(const hqmq_cache4_rows *r, int32_t D)
+static Cache4Rows make_cache4_rows(const hqmq_cache4_rows *r)
 {
-    const bool wide = D % 8 == 0 && r->stride_row % 8 == 0 && r->stride_head % 8 == 0 && !misaligned(r->data, 16);
-    return Cache4Rows{static_cast<uint16_t *>(r->data), r->stride_row, r->stride_head, wide ? 1 : 0};
+    return Cache4Rows{static_cast<uint16_t *>(r->data), r->stride_row, r->stride_head};
 }
 
 static int32_t cache4_move(bool write, const hqmq_cache4_params *params, const hqmq_cache4_buffers *cache, const hqmq_cache4_batch *batch,
@@ -1403,7 +1402,7 @@ static int32_t cache4_move(bool write, const hqmq_cache4_params *params, const h
         return HQMQ_OK;
     const auto launch = write ? launch_cache4_write : launch_cache4_read;
     const hipError_t err = launch(make_cache4(params, cache), make_cache4_seqs(batch, n_rows), cache4_most_rows(batch, n_rows),
-                                  type == HQMQ_TYPE_BF16, make_cache4_rows(k, params->D), make_cache4_rows(v, params->D),
+                                  type == HQMQ_TYPE_BF16, make_cache4_rows(k), make_cache4_rows(v),
                                   static_cast<hipStream_t>(stream));
     return err == hipSuccess ? HQMQ_OK : hip_failed(err);
 }
@@ -1481,8 +1480,8 @@ extern "C" int32_t hqmq_cache4_attend(const hqmq_cache4_params *params, const hq
     Cache4Attend a;
     a.c = make_cache4(params, cache);
     a.b = make_cache4_seqs(batch, n_rows);
-    a.q = make_cache4_rows(q, params->D);
-    a.out = make_cache4_rows(out, params->D);
+    a.q = make_cache4_rows(q);
+    a.out = make_cache4_rows(out);
     a.lse = lse_dev;
     a.part_ml = static_cast<float *>(workspace_dev);
     a.part_acc = reinterpret_cast<float *>(static_cast<unsigned char *>(workspace_dev) + plan.ml_bytes);

@@ -341,12 +341,14 @@ __device__ __forceinline__ void store_row(const Cache4Attend &a, int row, int he
         }
     }
     uint16_t *dst = a.out.data + (int64_t)row * a.out.row + (int64_t)head * a.out.head + ch;
-    if (a.out.wide) {  // a head is a multiple of 8 channels
-        if (ch < a.c.D)
-            *reinterpret_cast<uint2 *>(dst) = make_uint2(bits[0], bits[1]);
+    if (ch + 4 <= a.c.D) {
+        struct __attribute__((packed, aligned(2))) Four {
+            uint64_t bits;
+        };
+        reinterpret_cast<Four *>(dst)->bits = (uint64_t)bits[1] << 32 | bits[0];
     } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
+        for (int e = 0; e < 3; ++e)
             if (ch + e < a.c.D)
                 dst[e] = (uint16_t)(bits[e / 2] >> (16 * (e & 1)));
     }
@@ -370,7 +372,7 @@ __global__ __launch_bounds__(64 * attend_waves(kBlocks), attend_occupancy(NG, kB
     int *const position = reinterpret_cast<int *>(factor + kRows);       // [kRows]: -1 - 2^30 and less: no row
     float *const stats = reinterpret_cast<float *>(position + kRows);    // [kWaves][kRows][2]
 
-    const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, quarter = lane >> 4;
+    const int tid = threadIdx.x;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const Cache4 &c = a.c;
     const int h = blockIdx.x, seq = blockIdx.z, rest = divided((int)blockIdx.y, a.by_splits), split = (int)blockIdx.y - rest * a.n_splits;
@@ -386,6 +388,9 @@ __global__ __launch_bounds__(64 * attend_waves(kBlocks), attend_occupancy(NG, kB
     // the longest first: a causal prompt's last rows see the most
     for (int tile = a.n_tiles - 1 - rest; tile * kRows < n_rows; tile += a.n_tiles) {
         const int r0 = tile * kRows;
+        int lane = tid & 63;
+        asm volatile("" : "+v"(lane));  // what is made of it stays inside a tile's turn, of which there is one as a rule
+        const int col = lane & 15, quarter = lane >> 4;
         // ---- what the rows see -----------------------------------------------------------------------------------------
         const int j_first = divided(r0, a.by_G), j_last = min(divided(r0 + kRows - 1, a.by_G), s.n - 1);
         const int end = s.pos0 + j_last + 1, all_end = s.pos0 + j_first + 1;  // all_end: every row sees what is before it,
@@ -405,8 +410,8 @@ __global__ __launch_bounds__(64 * attend_waves(kBlocks), attend_occupancy(NG, kB
         const int to = split == a.n_splits - 1 ? end : (int)min(share + a.split_tokens, (int64_t)end);
         const int n_steps = to > from ? (to - from + kStep - 1) / kStep : 0;
         const int last = from + kStep * max(n_steps - 1, 0);
-        KStage<kFormat, NG> ks[2];
-        VStage<kFormat, NG> vs[2];
+        KStage<kFormat, NG> ks[2] = {};
+        VStage<kFormat, NG> vs[2] = {};
         Places<kFormat, NG> places(lane);
         Tile tiles[2];
         bool bad[2];
@@ -418,7 +423,7 @@ __global__ __launch_bounds__(64 * attend_waves(kBlocks), attend_occupancy(NG, kB
             }
         };
         // ---- the wave's block of queries and its first step are on their way together --------------------------------------
-        const int query = r0 + 16 * wave + col, query_j = divided(query, a.by_G);
+        const int query = r0 + 16 * wave + col, query_j = divided(query, a.by_G), first_ch = 8 * NG * quarter;
         const bool there = wave < kBlocks && query < n_rows;
         uint4v bits[NG];
 #pragma unroll
@@ -426,18 +431,18 @@ __global__ __launch_bounds__(64 * attend_waves(kBlocks), attend_occupancy(NG, kB
             bits[w] = uint4v{0u, 0u, 0u, 0u};
         if (there) {
             const uint16_t *src = a.q.data + (int64_t)(s.first_row + query_j) * a.q.row + (int64_t)(h * a.G + (query - query_j * a.G)) * a.q.head;
-            int D = c.D, ch = 8 * NG * quarter;
+            int D = c.D;
             asm volatile("" : "+s"(D));  // what is compared with it is not kept in registers from tile to tile
-            if (a.q.wide) {
+            if (D % 8 == 0) {
 #pragma unroll
                 for (int w = 0; w < NG; ++w)
-                    if (ch + 8 * w < D)
-                        bits[w] = *reinterpret_cast<const uint4v *>(src + (ch + 8 * w));
-            } else {  // element by element through the lane's own places in LDS
+                    if (first_ch + 8 * w < D)
+                        bits[w] = load8(src + (first_ch + 8 * w));
+            } else {  // element by element, through the lane's own places in LDS
                 uint16_t *const mine = reinterpret_cast<uint16_t *>(queries + wave * NG * 64 + lane);
 #pragma unroll 1
                 for (int e = 0; e < 8 * NG; ++e)
-                    mine[512 * (e >> 3) + (e & 7)] = ch + e < D ? src[ch + e] : (uint16_t)0;
+                    mine[512 * (e >> 3) + (e & 7)] = first_ch + e < D ? src[first_ch + e] : (uint16_t)0;
                 asm volatile("" : : : "memory");
 #pragma unroll
                 for (int w = 0; w < NG; ++w)
@@ -628,11 +633,14 @@ __global__ __launch_bounds__(64 * attend_waves(kBlocks), attend_occupancy(NG, kB
         }
 
         // ---- the waves' sums joined, kPass blocks of rows at a time -----------------------------------------------------------
+        int thread = tid;
+        asm volatile("" : "+v"(thread));  // addresses are formed here, not kept in registers through the steps
+        const int col_now = thread & 15, quarter_now = (thread & 63) >> 4;
 #pragma unroll
         for (int nb = 0; nb < kBlocks; ++nb) {
             const float total = column_sum(sum[nb]);
-            if (quarter == 0)
-                *reinterpret_cast<float2 *>(stats + (wave * kRows + 16 * nb + col) * 2) = make_float2(ref[nb], total);
+            if (quarter_now == 0)
+                *reinterpret_cast<float2 *>(stats + (wave * kRows + 16 * nb + col_now) * 2) = make_float2(ref[nb], total);
         }
         __syncthreads();  // the queries are done with
         constexpr int kPass = attend_pass(NG, kBlocks), kUnits = 8 * NG;  // a thread takes 4 channels of a row
@@ -641,7 +649,7 @@ __global__ __launch_bounds__(64 * attend_waves(kBlocks), attend_occupancy(NG, kB
             unrolled<0, kBlocks>([&](auto t) {
                 constexpr int nb = decltype(t)::value;
                 if (first == nb / kPass * kPass) {
-                    float *const mine = join + ((wave * kPass + nb % kPass) * 16 + col) * kPitch;
+                    float *const mine = join + ((wave * kPass + nb % kPass) * 16 + col_now) * kPitch;
                     unrolled<0, P::n>([&](auto part) {
                         constexpr int p = decltype(part)::value, kRun = 2 * P::groups(p), kWide = kRun < 4 ? 2 : 4;
                         typedef float wide __attribute__((ext_vector_type(kWide)));
@@ -653,14 +661,14 @@ __global__ __launch_bounds__(64 * attend_waves(kBlocks), attend_occupancy(NG, kB
 #pragma unroll
                                 for (int e = 0; e < kWide; ++e)
                                     y[e] = o[2 * P::before(p) + e0 + e][nb][r];
-                                *reinterpret_cast<wide *>(mine + 32 * P::before(p) + kRun * (4 * quarter + r) + e0) = y;
+                                *reinterpret_cast<wide *>(mine + 32 * P::before(p) + kRun * (4 * quarter_now + r) + e0) = y;
                             }
                     });
                 }
             });
             __syncthreads();
 #pragma unroll 1
-            for (int unit = tid; unit < kPass * 16 * kUnits; unit += 64 * kWaves) {
+            for (int unit = thread; unit < kPass * 16 * kUnits; unit += 64 * kWaves) {
                 const int row = unit / kUnits, ch = 4 * (unit - row * kUnits), r = r0 + 16 * first + row;
                 if (r >= n_rows)
                     break;

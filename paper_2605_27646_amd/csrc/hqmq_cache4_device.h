@@ -28,8 +28,29 @@ struct Cache4Seqs {
 struct Cache4Rows {
     uint16_t *data;
     int64_t row, head;  // element strides
-    int32_t wide;       // every run of 8 channels that begins at a multiple of 8 is 16 aligned bytes inside the row
 };
+
+// 8 channels of a row, at any address that is a multiple of 2 (memory takes vector accesses of any alignment here).
+typedef uint32_t cache4_u4 __attribute__((ext_vector_type(4)));
+struct __attribute__((packed, aligned(2))) Cache4Eight {
+    cache4_u4 bits;
+};
+__device__ __forceinline__ cache4_u4 load8(const uint16_t *p) { return reinterpret_cast<const Cache4Eight *>(p)->bits; }
+__device__ __forceinline__ void store8(uint16_t *p, cache4_u4 bits) { reinterpret_cast<Cache4Eight *>(p)->bits = bits; }
+
+// Division of numbers below 2^30 by one that the host knows: with l = ceil(log2 d) and m = ceil(2^(30 + l) / d), which is at most 2^30 + 1,
+// n m / 2^(30 + l) exceeds n / d by less than 2^l / 2^(30 + l) * n < 1 / d, and so has the same whole part.
+struct Divisor {
+    uint32_t mul, shift;
+};
+inline Divisor make_divisor(uint32_t d)
+{
+    uint32_t l = 0;
+    while ((1u << l) < d)
+        ++l;
+    return Divisor{(uint32_t)(((1ull << (30 + l)) + d - 1) / d), 30 + l};
+}
+__host__ __device__ __forceinline__ int divided(int n, Divisor d) { return (int)((uint64_t)(uint32_t)n * d.mul >> d.shift); }
 
 // What no kernel writes while it runs, so that uniform loads of it are scalar ones (which do not wait for the vector loads before them).
 typedef const __attribute__((address_space(4))) int32_t *ConstInts;
@@ -100,20 +121,6 @@ hipError_t launch_cache4_write(const Cache4 &c, const Cache4Seqs &b, int max_row
                                hipStream_t stream);
 hipError_t launch_cache4_read(const Cache4 &c, const Cache4Seqs &b, int max_rows, bool bf16, const Cache4Rows &k, const Cache4Rows &v,
                               hipStream_t stream);
-
-// Division of numbers below 2^30 by one that the host knows: with l = ceil(log2 d) and m = ceil(2^(30 + l) / d), which is at most 2^30 + 1,
-// n m / 2^(30 + l) exceeds n / d by less than 2^l / 2^(30 + l) * n < 1 / d, and so has the same whole part.
-struct Divisor {
-    uint32_t mul, shift;
-};
-inline Divisor make_divisor(uint32_t d)
-{
-    uint32_t l = 0;
-    while ((1u << l) < d)
-        ++l;
-    return Divisor{(uint32_t)(((1ull << (30 + l)) + d - 1) / d), 30 + l};
-}
-__host__ __device__ __forceinline__ int divided(int n, Divisor d) { return (int)((uint64_t)(uint32_t)n * d.mul >> d.shift); }
 
 struct Cache4Attend {
     Cache4 c;

@@ -1,8 +1,13 @@
 // Rows into the pages of a 4-bit cache and back (include/hqmq_cache4.h, hqmq_cache4_write and hqmq_cache4_read).
 //
-// A lane takes 8 channels (16 bytes of a row, one dword of codes) of one token.  Four consecutive positions, which are one block of
-// the V layout, lie beside each other in a wave, so that the 64 dwords of a 128-channel head and four tokens are 256 bytes in a
-// row of the cache; the four lanes of a group are 4 lanes apart and share their extrema by rotations inside 16 lanes.
+// A lane takes 8 channels (16 bytes of a row, a dword of codes) of the four tokens of one block of the V layout: rows are moved
+// 1 KB a wave and instruction, V's codes of the four tokens are 16 consecutive bytes, and the four lanes of a group lie beside each
+// other.  One token a lane, the four of a block in lanes of their own, wrote rows in pieces of 256 bytes: 2 x 32768 tokens of 8 heads
+// x 96 read back in 100 us instead of the time below.
+//
+// Bound by memory for prompts, by launch and latency for a step's rows.
+#include <type_traits>
+
 #include "hqmq_cache4_device.h"
 
 namespace hqmq {
@@ -13,16 +18,11 @@ constexpr int kRowThreads = 256;
 constexpr int kMostBlocks = 1 << 16;  // of a grid along the positions
 typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
 
-// Extremum over lanes l, l + 4, l + 8, l + 12 of 16.
-template <int kCtrl>
-__device__ __forceinline__ float rotated(float x)
-{
-    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), kCtrl, 0xf, 0xf, false));
-}
+// Maximum over the four lanes of a group.
 __device__ __forceinline__ float group_max(float x)
 {
-    x = fmaxf(x, rotated<0x124>(x));
-    return fmaxf(x, rotated<0x128>(x));
+    x = fmaxf(x, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0xb1, 0xf, 0xf, false)));  // lanes 1 0 3 2
+    return fmaxf(x, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x4e, 0xf, 0xf, false)));  // lanes 2 3 0 1
 }
 
 template <bool kBf16>
@@ -33,211 +33,292 @@ __device__ __forceinline__ float widened(uint32_t bits)
     return __builtin_amdgcn_fmed3f(x, -49152.f, 49152.f);
 }
 
-// What a thread works on: 8 channels of kv head h, the same for every block of positions that it goes through.
+// What a thread works on: 8 channels of a kv head, the same for every block of positions that it goes through.
 struct Unit {
-    int h, w, t;    // head, dword of the row, token of four
+    int h, w;  // head, dword of the row
     bool there, is_v;
 };
-__device__ __forceinline__ Unit unit_of(const Cache4 &c)
+__device__ __forceinline__ Unit unit_of(const Cache4 &c, Divisor by_row)
 {
-    const int per_head = 16 * c.NG;  // 4 tokens of 4 NG dwords
-    const int per_role = (c.H * per_head + kRowThreads - 1) / kRowThreads;
+    const int words = 4 * c.NG, n = c.H * words;
+    int i = (int)(blockIdx.y * kRowThreads + threadIdx.x);
     Unit u;
-    u.is_v = (int)blockIdx.y >= per_role;
-    const int i = ((int)blockIdx.y - (u.is_v ? per_role : 0)) * kRowThreads + (int)threadIdx.x;
-    u.t = i & 3;
-    u.h = i / per_head;
-    u.w = (i - u.h * per_head) >> 2;
+    u.is_v = i >= n;
+    i -= u.is_v ? n : 0;
+    u.h = divided(i, by_row);
+    u.w = i - u.h * words;
     u.there = u.h < c.H;
     return u;
 }
 
-// The cache's page of a position, or -1.
+// The page of the block of four positions that begins at pos (0 or above), or -1: a page holds whole blocks.
 __device__ __forceinline__ int page_of(const Cache4 &c, const Cache4Seqs &b, int seq, int pos)
 {
-    const int page = b.table[(int64_t)seq * b.pitch + (pos >> c.page_shift)];
+    const int page = const_ints(b.table)[(int64_t)seq * b.pitch + (pos >> c.page_shift)];
     return (uint32_t)page < (uint32_t)c.n_pages ? page : -1;
+}
+
+// V's dwords of four tokens in the order of its layout, and back (the same exchange): whole, by halves or by bytes.
+__device__ __forceinline__ uint4v interleaved(uint4v x, int bytes)
+{
+    const auto perm = [](uint32_t hi, uint32_t lo, uint32_t sel) { return __builtin_amdgcn_perm(hi, lo, sel); };
+    if (bytes == 4)
+        return x;
+    if (bytes == 2)  // run r: halves r of the four
+        return uint4v{perm(x[1], x[0], 0x05040100u), perm(x[3], x[2], 0x05040100u), perm(x[1], x[0], 0x07060302u), perm(x[3], x[2], 0x07060302u)};
+    const uint32_t a = perm(x[1], x[0], 0x05010400u), b = perm(x[1], x[0], 0x07030602u);  // bytes 0 0 1 1, 2 2 3 3 of two
+    const uint32_t d = perm(x[3], x[2], 0x05010400u), e = perm(x[3], x[2], 0x07030602u);
+    return uint4v{perm(d, a, 0x05040100u), perm(d, a, 0x07060302u), perm(e, b, 0x05040100u), perm(e, b, 0x07060302u)};
+}
+__device__ __forceinline__ uint4v separated(uint4v y, int bytes)
+{
+    if (bytes != 2)
+        return interleaved(y, bytes);  // a transposition of 4 x 4 bytes
+    const auto perm = [](uint32_t hi, uint32_t lo, uint32_t sel) { return __builtin_amdgcn_perm(hi, lo, sel); };
+    return uint4v{perm(y[2], y[0], 0x05040100u), perm(y[2], y[0], 0x07060302u), perm(y[3], y[1], 0x05040100u), perm(y[3], y[1], 0x07060302u)};
+}
+
+// 8 channels as a dword of codes and the group's scale (a byte, or step and minimum).
+template <int kFormat, bool kBf16>
+__device__ __forceinline__ uint2 quantised(uint4v bits, int n)  // n: how many of them there are, others are zeros
+{
+    float x[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        x[e] = widened<kBf16>((bits[e / 2] >> (16 * (e & 1))) & 0xffffu);
+    uint32_t code = 0;
+    if (kFormat == HQMQ_CACHE4_FLOAT) {
+        float top = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            top = fmaxf(top, fabsf(x[e]));
+        top = group_max(top);
+        // 7 / 4 has the fraction bits 0x600000: an exponent more for anything above
+        const int exponent = min(max((int)((__float_as_uint(top) + 0x1fffffu) >> 23) - 2, 127 - 23), 127 + 13);
+        const float unit = e8m0((uint32_t)exponent);
+        code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x[0], x[1], unit, 0);
+        code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x[2], x[3], unit, 1);
+        code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x[4], x[5], unit, 2);
+        code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x[6], x[7], unit, 3);
+        return make_uint2(code, (uint32_t)exponent);
+    }
+    float high = -1.0e30f, low = 1.0e30f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (e < n) {
+            high = fmaxf(high, x[e]);
+            low = fminf(low, x[e]);
+        }
+    high = group_max(high);
+    low = -group_max(-low);
+    if (low > high)  // channels past the head's only
+        low = high = 0.f;
+    float fifteenth = (high - low) * (1.f / 15.f);
+    asm("" : "+v"(fifteenth));  // rounded to fp32 before fp16: v_fma_mixlo_f16 would round the product once
+    const _Float16 s16 = (_Float16)fifteenth, m16 = (_Float16)low;
+    const float step = (float)s16, least = (float)m16, inverse = step > 0.f ? 1.f / step : 0.f;
+    float r[8], near = 1.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float q = (x[e] - least) * inverse;
+        r[e] = rintf(q);
+        near = fminf(near, fabsf(fabsf(q - r[e]) - 0.5f));
+    }
+    // Three roundings put q up to 16 * 3 * 2^-24 off.  Next to the middle of two codes the exact difference d + rest from it decides:
+    // the middle has 5 bits and the step 11, and d is within a factor of two of their product.
+    if (near < 1.0e-5f) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float d = x[e] - least, back = d - x[e], rest = (x[e] - (d - back)) - (least + back);
+            const float lower = floorf(d * inverse), over = (d - (lower + 0.5f) * step) + rest;
+            const bool up = over > 0.f || (over == 0.f && ((int)lower & 1));
+            r[e] = step > 0.f ? lower + (up ? 1.f : 0.f) : 0.f;
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        code |= (e < n ? (uint32_t)__builtin_amdgcn_fmed3f(r[e], 0.f, 15.f) : 0u) << (4 * e);
+    return make_uint2(code, __builtin_bit_cast(uint32_t, cache4_h2{s16, m16}));
+}
+
+// And back, in the rows' type.
+template <int kFormat, bool kBf16>
+__device__ __forceinline__ uint4v values(uint32_t code, uint32_t scale)
+{
+    cache4_h2 y[4];
+    if (kFormat == HQMQ_CACHE4_FLOAT) {
+        const float unit = e8m0(scale);
+        y[0] = e2m1_pair<0>(code, unit);
+        y[1] = e2m1_pair<1>(code, unit);
+        y[2] = e2m1_pair<2>(code, unit);
+        y[3] = e2m1_pair<3>(code, unit);
+    } else {
+        const cache4_h2 sm = __builtin_bit_cast(cache4_h2, scale), ss = {sm[0], sm[0]}, mm = {sm[1], sm[1]};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t two = code >> (8 * e);
+            y[e] = int4_pair((two & 0xfu) | (two & 0xf0u) << 12, ss, mm);
+        }
+    }
+    uint4v bits;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        if (kBf16) {
+            typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+            bits[e] = __builtin_bit_cast(uint32_t, b2{(__bf16)(float)y[e][0], (__bf16)(float)y[e][1]});
+        } else {
+            bits[e] = __builtin_bit_cast(uint32_t, y[e]);
+        }
+    }
+    return bits;
 }
 
 }  // namespace
 
-// Bound by memory for prompts, by launch and latency for a step's rows.
 template <int kFormat, bool kBf16>
-__global__ __launch_bounds__(kRowThreads) void k_cache4_write(Cache4 c, Cache4Seqs b, Cache4Rows k, Cache4Rows v)
+__global__ __launch_bounds__(kRowThreads) void k_cache4_write(Cache4 c, Cache4Seqs b, Cache4Rows k, Cache4Rows v, Divisor by_row)
 {
+    typedef std::conditional_t<kFormat == HQMQ_CACHE4_FLOAT, uint8_t, uint32_t> Scale;
     const int seq = blockIdx.z;
     const Cache4Seq s = cache4_seq(b, c.page_shift, seq);
-    const Unit u = unit_of(c);
-    const Cache4Rows &rows = u.is_v ? v : k;
+    const Unit u = unit_of(c, by_row);
+    const Cache4Rows rows = u.is_v ? v : k;
     uint8_t *const codes = u.is_v ? c.v_codes : c.k_codes;
-    uint8_t *const scales = u.is_v ? c.v_scales : c.k_scales;
-    const int ch = 8 * u.w, row_bytes = 16 * c.NG;
+    Scale *const scales = reinterpret_cast<Scale *>(u.is_v ? c.v_scales : c.k_scales);
+    const int ch = 8 * u.w, row_bytes = 16 * c.NG, n_ch = min(max(c.D - ch, 0), 8);
+    const uint16_t *const src = rows.data + u.h * rows.head + ch;
     for (int block = (max(s.pos0, 0) >> 2) + (int)blockIdx.x; 4 * block < s.length && s.n > 0; block += (int)gridDim.x) {
-        const int pos = 4 * block + u.t;
-        const int page = u.there && pos >= s.pos0 && pos < s.length ? page_of(c, b, seq, pos) : -1;
-        uint4v bits = uint4v{0u, 0u, 0u, 0u};
-        if (page >= 0 && ch < c.D) {
-            const uint16_t *src = rows.data + (int64_t)(s.first_row + (pos - s.pos0)) * rows.row + u.h * rows.head + ch;
-            if (rows.wide) {
-                bits = *reinterpret_cast<const uint4v *>(src);
-            } else {
+        const int pos = 4 * block, first = max(s.pos0 - pos, 0), end = min(s.length - pos, 4);  // the block's tokens first .. end - 1
+        const int page = page_of(c, b, seq, pos);
+        if (page < 0)  // uniform
+            continue;
+        uint4v bits[4];
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (ch + e < c.D)
-                        bits[e / 2] |= (uint32_t)src[e] << (16 * (e & 1));
-            }
-        }
-        float x[8];
+        for (int t = 0; t < 4; ++t) {
+            bits[t] = uint4v{0u, 0u, 0u, 0u};
+            if (t >= first && t < end && u.there && n_ch > 0) {
+                const uint16_t *at = src + (int64_t)(s.first_row + (pos + t - s.pos0)) * rows.row;
+                if (n_ch == 8) {
+                    bits[t] = load8(at);
+                } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            x[e] = widened<kBf16>((bits[e / 2] >> (16 * (e & 1))) & 0xffffu);
-        uint32_t code = 0, scale;
-        if (kFormat == HQMQ_CACHE4_FLOAT) {
-            float top = 0.f;
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                top = fmaxf(top, fabsf(x[e]));
-            top = group_max(top);
-            // 7 / 4 has the fraction bits 0x600000: an exponent more for anything above
-            const int exponent = min(max((int)((__float_as_uint(top) + 0x1fffffu) >> 23) - 2, 127 - 23), 127 + 13);
-            scale = (uint32_t)exponent;
-            const float unit = e8m0(scale);
-            code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x[0], x[1], unit, 0);
-            code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x[2], x[3], unit, 1);
-            code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x[4], x[5], unit, 2);
-            code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x[6], x[7], unit, 3);
-        } else {
-            const int n = min(max(c.D - ch, 0), 8);
-            float high = -1.0e30f, low = 1.0e30f;
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (e < n) {
-                    high = fmaxf(high, x[e]);
-                    low = fminf(low, x[e]);
+                    for (int e = 0; e < 7; ++e)
+                        if (e < n_ch)
+                            bits[t][e / 2] |= (uint32_t)at[e] << (16 * (e & 1));
                 }
-            high = group_max(high);
-            low = -group_max(-low);
-            if (low > high)  // channels past the head's only
-                low = high = 0.f;
-            float fifteenth = (high - low) * (1.f / 15.f);
-            asm("" : "+v"(fifteenth));  // rounded to fp32 before fp16: v_fma_mixlo_f16 would round the product once
-            const _Float16 s16 = (_Float16)fifteenth, m16 = (_Float16)low;
-            scale = __builtin_bit_cast(uint32_t, cache4_h2{s16, m16});
-            const float step = (float)s16, least = (float)m16, inverse = step > 0.f ? 1.f / step : 0.f;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float q = (x[e] - least) * inverse;
-                float r = rintf(q);
-                // three roundings put q up to 16 * 3 * 2^-24 off: next to the middle of two codes the exact quotient decides
-                if (fabsf(fabsf(q - r) - 0.5f) < 1.0e-5f)
-                    r = (float)rint(((double)x[e] - (double)least) / (double)step);
-                const uint32_t q4 = (uint32_t)__builtin_amdgcn_fmed3f(r, 0.f, 15.f);
-                code |= (e < n ? q4 : 0u) << (4 * e);
             }
         }
-        if (page < 0)
+        uint4v code, scale;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            const uint2 y = quantised<kFormat, kBf16>(bits[t], n_ch);
+            code[t] = y.x;
+            scale[t] = y.y;
+        }
+        if (!u.there)
             continue;
         const int slot = pos & ((1 << c.page_shift) - 1);
-        const int64_t row0 = ((int64_t)page * c.H + u.h) << c.page_shift;  // of the head's page
-        int64_t scale_at = row0 * c.NG;
+        const int64_t row0 = (((int64_t)page * c.H + u.h) << c.page_shift) + slot;  // the block's first token
+        const int group = u.w >> 2;
+        const bool leads = (u.w & 3) == 0;  // of its group
         if (!u.is_v) {
-            *reinterpret_cast<uint32_t *>(codes + (row0 + slot) * row_bytes + 4 * u.w) = code;
-            scale_at += slot * c.NG + (u.w >> 2);
-        } else {
-            const Cache4Place p = cache4_v_place(c.NG, u.w, u.t);
-            uint8_t *at = codes + (row0 + (slot & ~3)) * row_bytes + p.at;
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+                if (t >= first && t < end) {
+                    *reinterpret_cast<uint32_t *>(codes + (row0 + t) * row_bytes + 4 * u.w) = code[t];
+                    if (leads)
+                        scales[(row0 + t) * c.NG + group] = (Scale)scale[t];
+                }
+            continue;
+        }
+        const Cache4Place p = cache4_v_place(c.NG, u.w, 0);
+        uint8_t *const at = codes + row0 * row_bytes + p.at;
+        Scale *const scale_at = scales + row0 * c.NG + 4 * group;
+        if (end - first == 4) {
+            *reinterpret_cast<uint4v *>(at) = interleaved(code, p.bytes);
+            if (leads) {
+                if (kFormat == HQMQ_CACHE4_FLOAT)
+                    *reinterpret_cast<uint32_t *>(scale_at) = scale[0] | scale[1] << 8 | scale[2] << 16 | scale[3] << 24;
+                else
+                    *reinterpret_cast<uint4v *>(scale_at) = scale;
+            }
+            continue;
+        }
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            if (t < first || t >= end)
+                continue;
             if (p.bytes == 4) {
-                *reinterpret_cast<uint32_t *>(at) = code;
+                *reinterpret_cast<uint32_t *>(at + 4 * t) = code[t];
             } else if (p.bytes == 2) {
-                *reinterpret_cast<uint16_t *>(at) = (uint16_t)code;
-                *reinterpret_cast<uint16_t *>(at + 8) = (uint16_t)(code >> 16);
+                *reinterpret_cast<uint16_t *>(at + 2 * t) = (uint16_t)code[t];
+                *reinterpret_cast<uint16_t *>(at + 2 * t + 8) = (uint16_t)(code[t] >> 16);
             } else {
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
-                    at[4 * r] = (uint8_t)(code >> (8 * r));
+                    at[t + 4 * r] = (uint8_t)(code[t] >> (8 * r));
             }
-            scale_at += (slot & ~3) * c.NG + (u.w >> 2) * 4 + u.t;
-        }
-        if ((u.w & 3) == 0) {
-            if (kFormat == HQMQ_CACHE4_FLOAT)
-                scales[scale_at] = (uint8_t)scale;
-            else
-                reinterpret_cast<uint32_t *>(scales)[scale_at] = scale;
+            if (leads)
+                scale_at[t] = (Scale)scale[t];
         }
     }
 }
 
 template <int kFormat, bool kBf16>
-__global__ __launch_bounds__(kRowThreads) void k_cache4_read(Cache4 c, Cache4Seqs b, Cache4Rows k, Cache4Rows v)
+__global__ __launch_bounds__(kRowThreads) void k_cache4_read(Cache4 c, Cache4Seqs b, Cache4Rows k, Cache4Rows v, Divisor by_row)
 {
+    typedef std::conditional_t<kFormat == HQMQ_CACHE4_FLOAT, uint8_t, uint32_t> Scale;
     const int seq = blockIdx.z;
     const Cache4Seq s = cache4_seq(b, c.page_shift, seq);
-    const Unit u = unit_of(c);
-    const Cache4Rows &rows = u.is_v ? v : k;
+    const Unit u = unit_of(c, by_row);
+    const Cache4Rows rows = u.is_v ? v : k;
     const uint8_t *const codes = u.is_v ? c.v_codes : c.k_codes;
-    const uint8_t *const scales = u.is_v ? c.v_scales : c.k_scales;
+    const Scale *const scales = reinterpret_cast<const Scale *>(u.is_v ? c.v_scales : c.k_scales);
     const int ch = 8 * u.w, row_bytes = 16 * c.NG;
     if (!u.there || ch >= c.D)
         return;
+    uint16_t *const dst = rows.data + u.h * rows.head + ch;
     for (int block = (s.pos0 >> 2) + (int)blockIdx.x; 4 * block < s.length; block += (int)gridDim.x) {
-        const int pos = 4 * block + u.t;
-        if (pos < s.pos0 || pos >= s.length)
-            continue;
+        const int pos = 4 * block, first = max(s.pos0 - pos, 0), end = min(s.length - pos, 4);
         const int page = pos >= 0 ? page_of(c, b, seq, pos) : -1;
-        uint4v bits = uint4v{0u, 0u, 0u, 0u};
-        if (page >= 0) {
+        uint4v code = uint4v{0u, 0u, 0u, 0u}, scale = code;
+        if (page >= 0) {  // uniform; all of the block's four tokens lie in the cache
             const int slot = pos & ((1 << c.page_shift) - 1);
-            const int64_t row0 = ((int64_t)page * c.H + u.h) << c.page_shift;
-            int64_t scale_at = row0 * c.NG;
-            uint32_t code;
+            const int64_t row0 = (((int64_t)page * c.H + u.h) << c.page_shift) + slot;
             if (!u.is_v) {
-                code = *reinterpret_cast<const uint32_t *>(codes + (row0 + slot) * row_bytes + 4 * u.w);
-                scale_at += slot * c.NG + (u.w >> 2);
-            } else {
-                const Cache4Place p = cache4_v_place(c.NG, u.w, u.t);
-                const uint8_t *at = codes + (row0 + (slot & ~3)) * row_bytes + p.at;
-                if (p.bytes == 4)
-                    code = *reinterpret_cast<const uint32_t *>(at);
-                else if (p.bytes == 2)
-                    code = *reinterpret_cast<const uint16_t *>(at) | (uint32_t) * reinterpret_cast<const uint16_t *>(at + 8) << 16;
-                else
-                    code = at[0] | (uint32_t)at[4] << 8 | (uint32_t)at[8] << 16 | (uint32_t)at[12] << 24;
-                scale_at += (slot & ~3) * c.NG + (u.w >> 2) * 4 + u.t;
-            }
-            cache4_h2 y[4];
-            if (kFormat == HQMQ_CACHE4_FLOAT) {
-                const float unit = e8m0(scales[scale_at]);
-                y[0] = e2m1_pair<0>(code, unit);
-                y[1] = e2m1_pair<1>(code, unit);
-                y[2] = e2m1_pair<2>(code, unit);
-                y[3] = e2m1_pair<3>(code, unit);
-            } else {
-                const cache4_h2 sm = __builtin_bit_cast(cache4_h2, reinterpret_cast<const uint32_t *>(scales)[scale_at]);
-                const cache4_h2 ss = {sm[0], sm[0]}, mm = {sm[1], sm[1]};
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const uint32_t two = code >> (8 * e);
-                    y[e] = int4_pair((two & 0xfu) | (two & 0xf0u) << 12, ss, mm);
+                for (int t = 0; t < 4; ++t) {
+                    code[t] = *reinterpret_cast<const uint32_t *>(codes + (row0 + t) * row_bytes + 4 * u.w);
+                    scale[t] = scales[(row0 + t) * c.NG + (u.w >> 2)];
                 }
-            }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                if (kBf16) {
-                    typedef __bf16 b2 __attribute__((ext_vector_type(2)));
-                    bits[e] = __builtin_bit_cast(uint32_t, b2{(__bf16)(float)y[e][0], (__bf16)(float)y[e][1]});
+            } else {
+                const Cache4Place p = cache4_v_place(c.NG, u.w, 0);
+                code = separated(*reinterpret_cast<const uint4v *>(codes + row0 * row_bytes + p.at), p.bytes);
+                const Scale *const scale_at = scales + row0 * c.NG + 4 * (u.w >> 2);
+                if (kFormat == HQMQ_CACHE4_FLOAT) {
+                    const uint32_t y = *reinterpret_cast<const uint32_t *>(scale_at);
+                    scale = uint4v{y & 0xffu, y >> 8 & 0xffu, y >> 16 & 0xffu, y >> 24};
                 } else {
-                    bits[e] = __builtin_bit_cast(uint32_t, y[e]);
+                    scale = *reinterpret_cast<const uint4v *>(scale_at);
                 }
             }
         }
-        uint16_t *dst = rows.data + (int64_t)(s.first_row + (pos - s.pos0)) * rows.row + u.h * rows.head + ch;
-        if (rows.wide) {
-            *reinterpret_cast<uint4v *>(dst) = bits;
-        } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (ch + e < c.D)
-                    dst[e] = (uint16_t)(bits[e / 2] >> (16 * (e & 1)));
+        for (int t = 0; t < 4; ++t) {
+            if (t < first || t >= end)
+                continue;
+            uint4v bits = uint4v{0u, 0u, 0u, 0u};
+            if (page >= 0)
+                bits = values<kFormat, kBf16>(code[t], scale[t]);
+            uint16_t *const at = dst + (int64_t)(s.first_row + (pos + t - s.pos0)) * rows.row;
+            if (ch + 8 <= c.D) {
+                store8(at, bits);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 7; ++e)
+                    if (ch + e < c.D)
+                        at[e] = (uint16_t)(bits[e / 2] >> (16 * (e & 1)));
+            }
         }
     }
 }
@@ -246,9 +327,9 @@ namespace {
 
 dim3 rows_grid(const Cache4 &c, const Cache4Seqs &b, int max_rows)
 {
-    const int per_role = (c.H * 16 * c.NG + kRowThreads - 1) / kRowThreads;
     const int blocks = max_rows == 1 ? 1 : (max_rows - 1) / 4 + 2;  // wherever in a block of four the first position lies
-    return dim3((unsigned)(blocks < kMostBlocks ? blocks : kMostBlocks), (unsigned)(2 * per_role), (unsigned)b.n_seqs);
+    return dim3((unsigned)(blocks < kMostBlocks ? blocks : kMostBlocks), (unsigned)((2 * c.H * 4 * c.NG + kRowThreads - 1) / kRowThreads),
+                (unsigned)b.n_seqs);
 }
 
 }  // namespace
@@ -256,20 +337,18 @@ dim3 rows_grid(const Cache4 &c, const Cache4Seqs &b, int max_rows)
 hipError_t launch_cache4_write(const Cache4 &c, const Cache4Seqs &b, int max_rows, bool bf16, const Cache4Rows &k, const Cache4Rows &v,
                                hipStream_t stream)
 {
-    const dim3 grid = rows_grid(c, b, max_rows);
     const auto kernel = c.format == HQMQ_CACHE4_FLOAT ? (bf16 ? k_cache4_write<HQMQ_CACHE4_FLOAT, true> : k_cache4_write<HQMQ_CACHE4_FLOAT, false>)
                                                       : (bf16 ? k_cache4_write<HQMQ_CACHE4_INT, true> : k_cache4_write<HQMQ_CACHE4_INT, false>);
-    kernel<<<grid, kRowThreads, 0, stream>>>(c, b, k, v);
+    kernel<<<rows_grid(c, b, max_rows), kRowThreads, 0, stream>>>(c, b, k, v, make_divisor((uint32_t)(4 * c.NG)));
     return hipGetLastError();
 }
 
 hipError_t launch_cache4_read(const Cache4 &c, const Cache4Seqs &b, int max_rows, bool bf16, const Cache4Rows &k, const Cache4Rows &v,
                               hipStream_t stream)
 {
-    const dim3 grid = rows_grid(c, b, max_rows);
     const auto kernel = c.format == HQMQ_CACHE4_FLOAT ? (bf16 ? k_cache4_read<HQMQ_CACHE4_FLOAT, true> : k_cache4_read<HQMQ_CACHE4_FLOAT, false>)
                                                       : (bf16 ? k_cache4_read<HQMQ_CACHE4_INT, true> : k_cache4_read<HQMQ_CACHE4_INT, false>);
-    kernel<<<grid, kRowThreads, 0, stream>>>(c, b, k, v);
+    kernel<<<rows_grid(c, b, max_rows), kRowThreads, 0, stream>>>(c, b, k, v, make_divisor((uint32_t)(4 * c.NG)));
     return hipGetLastError();
 }
 
