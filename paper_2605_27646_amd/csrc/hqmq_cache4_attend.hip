@@ -462,7 +462,8 @@ __global__ __launch_bounds__(64 * attend_waves(kBlocks), attend_occupancy(NG, kB
         // ---- queries to LDS, as operands
         if (wave < kBlocks) {
             float f = fabsf(a.scale) * kLog2e4;
-            const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;  // a negative scale goes into the queries' signs
+            uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;  // a negative scale goes into the queries' signs
+            asm volatile("" : "+s"(flip));
             if (kBf16) {
                 // A power of two brings the row's largest magnitude to 2^14 .. 2^15, where fp16 has all its bits down to 2^-28 of it.
                 uint32_t top = 0;
@@ -709,101 +710,143 @@ __global__ __launch_bounds__(64 * attend_waves(kBlocks), attend_occupancy(NG, kB
     }
 }
 
+// Maximum, or sum, over a wave: inside rows of 16 lanes and then across them, without LDS.
+template <int kCtrl, int kRows>
+__device__ __forceinline__ float moved(float x, float otherwise)
+{
+    return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(otherwise), __float_as_int(x), kCtrl, kRows, 0xf, false));
+}
+__device__ __forceinline__ float wave_max(float x)
+{
+    x = fmaxf(x, moved<0x111, 0xf>(x, kNothing));  // shifted right by 1, 2, 4, 8 lanes of a row
+    x = fmaxf(x, moved<0x112, 0xf>(x, kNothing));
+    x = fmaxf(x, moved<0x114, 0xf>(x, kNothing));
+    x = fmaxf(x, moved<0x118, 0xf>(x, kNothing));
+    x = fmaxf(x, moved<0x142, 0xa>(x, kNothing));  // lane 15 to the next row, lane 31 to the last two
+    x = fmaxf(x, moved<0x143, 0xc>(x, kNothing));
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
+}
+__device__ __forceinline__ float wave_sum(float x)
+{
+    x += moved<0x111, 0xf>(x, 0.f);
+    x += moved<0x112, 0xf>(x, 0.f);
+    x += moved<0x114, 0xf>(x, 0.f);
+    x += moved<0x118, 0xf>(x, 0.f);
+    x += moved<0x142, 0xa>(x, 0.f);
+    x += moved<0x143, 0xc>(x, 0.f);
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
+}
+
 // The splits' sums of a row, relative to the largest reference.  A workgroup takes one row and head: its four waves take splits in
-// turn, as many at a time as rows of 4-channel lanes fit a wave, and join their sums in LDS.
+// turn, as many at a time as rows of 4-channel lanes fit a wave, and join their sums in LDS.  Every wave forms the factors by itself
+// and asks for the sums before it has them.
 constexpr int kMostSplits = 128;
-template <bool kBf16>
+template <int NG, bool kBf16>
 __global__ __launch_bounds__(kMergeThreads) void k_cache4_merge(Cache4Attend a)
 {
-    constexpr int kAhead = 8;
-    __shared__ __align__(16) float weight[kMostSplits];
-    __shared__ __align__(16) f4 partial[kMergeThreads];
-    __shared__ float whole[2];
-    const int tid = threadIdx.x, n_heads = a.c.H * a.G, width = 32 * a.c.NG, lanes = width / 4, at_once = kMergeThreads / lanes;
-    const int mine = tid / lanes, ch = 4 * (tid - mine * lanes);
+    constexpr int kLanes = 8 * NG, kInWave = 64 / kLanes, kAtOnce = kInWave * (kMergeThreads / 64);  // lanes of a split, splits at once
+    constexpr int kAhead = NG <= 4 ? 8 : 4, kMls = kMostSplits / 64;
+    __shared__ __align__(16) f4 partial[kAtOnce][kLanes];
+    const int tid = threadIdx.x, lane = tid & 63, n_heads = a.c.H * a.G;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int in_wave = lane / kLanes, ch = 4 * (lane - in_wave * kLanes);
+    const bool works = in_wave < kInWave;
+    const int mine = kInWave * wave + in_wave;  // splits mine, mine + kAtOnce, ..
     const int64_t n = (int64_t)a.b.n_rows * n_heads;
     const int first_row = a.b.starts ? const_ints(a.b.starts)[0] : 0, end_row = a.b.starts ? const_ints(a.b.starts)[a.b.n_seqs] : a.b.n_rows;
     for (int64_t row_at = blockIdx.x; row_at < n; row_at += gridDim.x) {
         const int row = (int)((uint32_t)row_at / (uint32_t)n_heads), head = (int)row_at - row * n_heads;
         if (row < first_row || row >= end_row)
             continue;
-        const float *acc = a.part_acc + row_at * a.n_splits * width + ch;
-        const auto load = [&](int s) { return *reinterpret_cast<const f4 *>(acc + (int64_t)s * width); };
-        const int n_mine = mine < at_once ? (a.n_splits - mine + at_once - 1) / at_once : 0;  // splits mine, mine + at_once, ..
+        const float *acc = a.part_acc + row_at * a.n_splits * (32 * NG) + ch;
+        const auto load = [&](int s) { return *reinterpret_cast<const f4 *>(acc + (int64_t)min(s, a.n_splits - 1) * (32 * NG)); };
+        const float2 *ml = reinterpret_cast<const float2 *>(a.part_ml) + row_at * a.n_splits;
+        float2 z[kMls];
+#pragma unroll
+        for (int i = 0; i < kMls; ++i)
+            z[i] = ml[min(lane + 64 * i, a.n_splits - 1)];
         f4 y[kAhead];
 #pragma unroll
         for (int i = 0; i < kAhead; ++i)
-            if (i < n_mine)
-                y[i] = load(mine + i * at_once);
-        if (tid < 64) {
-            const float2 *ml = reinterpret_cast<const float2 *>(a.part_ml) + row_at * a.n_splits;
-            float2 z[kMostSplits / 64];
-            float m = kNothing, l = 0.f;
+            y[i] = load(mine + i * kAtOnce);
+        float m = kNothing, l = 0.f, f[kMls];
 #pragma unroll
-            for (int i = 0; i < kMostSplits / 64; ++i)
-                z[i] = tid + 64 * i < a.n_splits ? ml[tid + 64 * i] : make_float2(kNothing, 0.f);
+        for (int i = 0; i < kMls; ++i)
+            m = fmaxf(m, lane + 64 * i < a.n_splits && z[i].y > 0.f ? z[i].x : kNothing);
+        m = wave_max(m);
 #pragma unroll
-            for (int i = 0; i < kMostSplits / 64; ++i)
-                m = fmaxf(m, z[i].y > 0.f ? z[i].x : kNothing);
-#pragma unroll
-            for (int d = 32; d; d >>= 1)
-                m = fmaxf(m, __shfl_xor(m, d));
-#pragma unroll
-            for (int i = 0; i < kMostSplits / 64; ++i) {
-                const float f = z[i].y > 0.f ? __builtin_amdgcn_exp2f(z[i].x - m) : 0.f;
-                weight[tid + 64 * i] = f;
-                l = fmaf(z[i].y, f, l);
-            }
-#pragma unroll
-            for (int d = 32; d; d >>= 1)
-                l += __shfl_xor(l, d);
-            if (tid == 0) {
-                whole[0] = m;
-                whole[1] = l;
-            }
+        for (int i = 0; i < kMls; ++i) {
+            const bool there = lane + 64 * i < a.n_splits && z[i].y > 0.f;  // of a split that saw nothing there are no sums
+            f[i] = there ? __builtin_amdgcn_exp2f(z[i].x - m) : 0.f;
+            l = fmaf(there ? z[i].y : 0.f, f[i], l);
         }
-        __syncthreads();
+        l = wave_sum(l);
         f4 total = f4{0.f, 0.f, 0.f, 0.f};
-        const auto add = [&](int s, f4 z) {
-            const float f = weight[s];
-            if (f > 0.f)  // of a split that saw nothing there are no sums
-                total += f4{f, f, f, f} * z;
+        const auto add = [&](int s, f4 x) {
+            float w = __shfl(f[0], s & 63);
+#pragma unroll
+            for (int i = 1; i < kMls; ++i) {
+                const float v = __shfl(f[i], s & 63);
+                w = s >> 6 == i ? v : w;
+            }
+            w = works && s < a.n_splits ? w : 0.f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                total[e] = fmaf(w, w > 0.f ? x[e] : 0.f, total[e]);
         };
 #pragma unroll
         for (int i = 0; i < kAhead; ++i)
-            if (i < n_mine)
-                add(mine + i * at_once, y[i]);
-        for (int i = kAhead; i < n_mine; ++i)
-            add(mine + i * at_once, load(mine + i * at_once));
-        partial[tid] = total;
+            add(mine + i * kAtOnce, y[i]);
+        for (int s = kAhead * kAtOnce; s < a.n_splits; s += kAtOnce)  // as often for every lane: they ask each other for factors
+            add(s + mine, load(s + mine));
+        if (works)
+            partial[mine][ch / 4] = total;
         __syncthreads();
-        if (tid < lanes) {
-            for (int i = 1; i < at_once; ++i)
-                total += partial[tid + i * lanes];
-            store_row<kBf16>(a, row, head, ch, total, whole[0], whole[1], row_at);
+        if (tid < kLanes) {
+            total = partial[0][tid];
+#pragma unroll
+            for (int i = 1; i < kAtOnce; ++i)
+                total += partial[i][tid];
+            store_row<kBf16>(a, row, head, 4 * tid, total, m, l, row_at);
         }
         __syncthreads();
     }
 }
 
-constexpr int kWantedGroups = 512;
+// How a call is cut.  Times are of 8 kv heads x 128 channels in the float format, 4 query heads a kv head, unless said otherwise.
+//   - Rows of a workgroup: 16 as long as that makes no more than a workgroup for each compute unit, 32 up to twice that many, then 64;
+//     never so many that a smaller form would hold all rows of a sequence.  More rows share the reconstruction, fewer keep more units
+//     at work.  16 / 32 / 64 rows: 20 new tokens behind 2000 12.7 / 14.3 / 17.7 us, 128 behind 8000 38 / 41 / 43, 512 behind 8000
+//     112 / 88 / 87, 1024 of two sequences behind 15000 728 / 565 / 481.  Heads of more than 128 channels have no room for 64.
+//   - Tokens are split only where there are fewer workgroups than compute units, which the second kernel costs 4 us and more for many
+//     rows (32 sequences of 4000 tokens, 2 x 16 rows, 4 heads: 22 us as they are, 29 in two): into enough for two workgroups a unit
+//     (6 sequences of up to 12345 tokens, 5 rows x 8 query heads, 4 heads x 96 integers: 28 us, with one a unit 31), but no more than
+//     32 where that is enough for one (one sequence of 32768 tokens: 64 parts 16.0 us, 32 14.9), and of two steps of each wave at
+//     least (two of 8000: 13.3 us, with one step 14.4, with four 14.8).
+constexpr int kUnits = 256;  // compute units
+constexpr int kFewSplits = 32;
 constexpr int kLeastRounds = 2;
 
 Cache4Plan plan_cache4_attend(const Cache4 &c, const Cache4Seqs &b, int max_rows, int max_length, int G, int window)
 {
     Cache4Plan p;
-    const int64_t rows = (int64_t)max_rows * G;
-    p.blocks = rows <= 16 ? 1 : rows <= 32 || c.NG > 4 ? 2 : 4;
-    const int64_t heads = (int64_t)c.H * b.n_seqs;
-    p.n_tiles = (int32_t)std::min<int64_t>((rows + 16 * p.blocks - 1) / (16 * p.blocks), 512);  // more take turns
+    const int64_t rows = (int64_t)max_rows * G, heads = (int64_t)c.H * b.n_seqs;
+    const auto tiles_of = [&](int blocks) { return (rows + 16 * blocks - 1) / (16 * blocks); };
+    p.blocks = 1;
+    while (p.blocks < (c.NG > 4 ? 2 : 4) && tiles_of(p.blocks) > 1 && tiles_of(p.blocks) * heads > kUnits * p.blocks)
+        p.blocks *= 2;
+    p.n_tiles = (int32_t)std::min<int64_t>(tiles_of(p.blocks), 512);  // more take turns
     int64_t span = max_length;
     if (window)
         span = std::min(span, (int64_t)window + std::min<int64_t>(max_rows, 16 * p.blocks / G + 1));
-    const int64_t round = kStep * attend_waves(p.blocks), most = std::max<int64_t>((span + kLeastRounds * round - 1) / (kLeastRounds * round), 1);
-    const int64_t wanted = kWantedGroups / std::max<int64_t>(p.n_tiles * heads, 1);
-    p.n_splits = (int32_t)std::max<int64_t>(std::min<int64_t>(std::min(wanted, most), kMostSplits), 1);
-    p.split_tokens = (int32_t)((span + p.n_splits * round - 1) / (p.n_splits * round) * round);
-    p.n_splits = (int32_t)std::max<int64_t>((span + p.split_tokens - 1) / p.split_tokens, 1);
+    const int64_t groups = p.n_tiles * heads, round = kStep * attend_waves(p.blocks);
+    int64_t splits = 1;
+    if (groups < kUnits) {
+        splits = std::max<int64_t>(kUnits / groups, std::min<int64_t>(2 * kUnits / groups, kFewSplits));
+        splits = std::min({splits, (span + kLeastRounds * round - 1) / (kLeastRounds * round), (int64_t)kMostSplits});
+    }
+    p.split_tokens = (int32_t)((span + splits * round - 1) / (splits * round) * round);
+    p.n_splits = (int32_t)((span + p.split_tokens - 1) / p.split_tokens);
     p.ml_bytes = p.acc_bytes = 0;
     if (p.n_splits > 1) {
         const uint64_t parts = (uint64_t)b.n_rows * c.H * G * p.n_splits;
@@ -874,10 +917,14 @@ hipError_t launch_cache4_attend(const Cache4Attend &a, const Cache4Plan &plan, b
     if (err != hipSuccess || plan.n_splits == 1)
         return err;
     const dim3 rows((unsigned)std::min<int64_t>((int64_t)a.b.n_rows * a.c.H * a.G, 1 << 20));
-    if (bf16)
-        k_cache4_merge<true><<<rows, kMergeThreads, 0, stream>>>(args);
-    else
-        k_cache4_merge<false><<<rows, kMergeThreads, 0, stream>>>(args);
+    switch (a.c.NG) {
+    case 1: (bf16 ? k_cache4_merge<1, true> : k_cache4_merge<1, false>)<<<rows, kMergeThreads, 0, stream>>>(args); break;
+    case 2: (bf16 ? k_cache4_merge<2, true> : k_cache4_merge<2, false>)<<<rows, kMergeThreads, 0, stream>>>(args); break;
+    case 3: (bf16 ? k_cache4_merge<3, true> : k_cache4_merge<3, false>)<<<rows, kMergeThreads, 0, stream>>>(args); break;
+    case 4: (bf16 ? k_cache4_merge<4, true> : k_cache4_merge<4, false>)<<<rows, kMergeThreads, 0, stream>>>(args); break;
+    case 6: (bf16 ? k_cache4_merge<6, true> : k_cache4_merge<6, false>)<<<rows, kMergeThreads, 0, stream>>>(args); break;
+    default: (bf16 ? k_cache4_merge<8, true> : k_cache4_merge<8, false>)<<<rows, kMergeThreads, 0, stream>>>(args); break;
+    }
     return hipGetLastError();
 }
 
