@@ -235,7 +235,7 @@ __device__ __forceinline__ void blank_v(VStage<kFormat, NG> &s, int end)
     }
 }
 
-// The operand of channels 8 w .. 8 w + 7 of the lane's run, in their order (float) or in that of kIntOrder (int).
+// The operand of channels 8 w .. 8 w + 7 of the lane's run, in their order (float) or as 0 2 4 6 1 3 5 7 (int).
 template <int kFormat, int NG>
 __device__ __forceinline__ half8_t k_operand(const KStage<kFormat, NG> &s, int w, int lane)
 {
@@ -253,9 +253,11 @@ __device__ __forceinline__ half8_t k_operand(const KStage<kFormat, NG> &s, int w
         y[3] = e2m1_pair<3>(code, unit);
     } else {
         const half2_t sm = __builtin_bit_cast(half2_t, (uint32_t)scale), ss = {sm[0], sm[0]}, mm = {sm[1], sm[1]};
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            y[e] = int4_pair(code >> (4 * e), ss, mm);
+        const uint32_t even = code & 0x0f0f0f0fu, odd = code >> 4 & 0x0f0f0f0fu;
+        y[0] = int4_pair<false>(even, ss, mm);
+        y[1] = int4_pair<true>(even, ss, mm);
+        y[2] = int4_pair<false>(odd, ss, mm);
+        y[3] = int4_pair<true>(odd, ss, mm);
     }
     return __builtin_bit_cast(half8_t, uint4v{__builtin_bit_cast(uint32_t, y[0]), __builtin_bit_cast(uint32_t, y[1]),
                                               __builtin_bit_cast(uint32_t, y[2]), __builtin_bit_cast(uint32_t, y[3])});
@@ -294,15 +296,21 @@ __device__ __forceinline__ void v_operands(const VStage<kFormat, NG> (&s)[2], ha
                 const uint32_t a = s[x].scale[kPart].w[(2 * i) % VStage<kFormat, NG>::kWords], b = s[x].scale[kPart].w[(2 * i + 1) % VStage<kFormat, NG>::kWords];
                 const half2_t step = __builtin_bit_cast(half2_t, __builtin_amdgcn_perm(b, a, 0x05040100u));
                 const half2_t least = __builtin_bit_cast(half2_t, __builtin_amdgcn_perm(b, a, 0x07060302u));
-                uint32_t both;  // the byte of token 2 i at bits 0..7, that of token 2 i + 1 at 16..23
-                if (groups == 4)
-                    both = __builtin_amdgcn_perm(code[(2 * i + 1) % NG], code[(2 * i) % NG], 0x0c040c00u + 0x00010001u * kByte);
+                uint32_t both;  // bytes of the tokens 2 i and 2 i + 1 side by side
+                if (groups == 4)  // of two pairs of channels, and this one's half
+                    both = __builtin_amdgcn_perm(code[(2 * i + 1) % NG], code[(2 * i) % NG], kByte < 2 ? 0x05010400u : 0x07030602u);
                 else if (groups == 2)
-                    both = code[i % NG] >> (8 * kByte);
-                else
-                    both = __builtin_amdgcn_perm(0u, code[0], 0x0c010c00u + 0x00020002u * i);
-                e[2 * x + i] = __builtin_bit_cast(uint32_t, int4_pair(both, step, least));
-                o[2 * x + i] = __builtin_bit_cast(uint32_t, int4_pair(both >> 4, step, least));
+                    both = __builtin_amdgcn_perm(0u, code[i % NG], 0x03010200u);
+                else  // of both pairs of tokens
+                    both = code[0];
+                const uint32_t low = both & 0x0f0f0f0fu, high = both >> 4 & 0x0f0f0f0fu;
+                if (groups > 1 ? kByte & 1 : i) {
+                    e[2 * x + i] = __builtin_bit_cast(uint32_t, int4_pair<true>(low, step, least));
+                    o[2 * x + i] = __builtin_bit_cast(uint32_t, int4_pair<true>(high, step, least));
+                } else {
+                    e[2 * x + i] = __builtin_bit_cast(uint32_t, int4_pair<false>(low, step, least));
+                    o[2 * x + i] = __builtin_bit_cast(uint32_t, int4_pair<false>(high, step, least));
+                }
             }
         }
     }
@@ -486,9 +494,9 @@ __global__ __launch_bounds__(64 * attend_waves(kBlocks), attend_occupancy(NG, kB
 #pragma unroll
             for (int w = 0; w < NG; ++w) {
                 uint4v x = bits[w] ^ uint4v{flip, flip, flip, flip};
-                if (kFormat == HQMQ_CACHE4_INT)  // channels 0 4 1 5 2 6 3 7
-                    x = uint4v{__builtin_amdgcn_perm(x[2], x[0], 0x05040100u), __builtin_amdgcn_perm(x[2], x[0], 0x07060302u),
-                               __builtin_amdgcn_perm(x[3], x[1], 0x05040100u), __builtin_amdgcn_perm(x[3], x[1], 0x07060302u)};
+                if (kFormat == HQMQ_CACHE4_INT)  // channels 0 2 4 6 1 3 5 7
+                    x = uint4v{__builtin_amdgcn_perm(x[1], x[0], 0x05040100u), __builtin_amdgcn_perm(x[3], x[2], 0x05040100u),
+                               __builtin_amdgcn_perm(x[1], x[0], 0x07060302u), __builtin_amdgcn_perm(x[3], x[2], 0x07060302u)};
                 queries[(wave * NG + w) * 64 + lane] = __builtin_bit_cast(half8_t, x);
             }
             if (quarter == 0) {
@@ -821,11 +829,13 @@ __global__ __launch_bounds__(kMergeThreads) void k_cache4_merge(Cache4Attend a)
 //   - Tokens are split only where there are fewer workgroups than compute units, which the second kernel costs 4 us and more for many
 //     rows (32 sequences of 4000 tokens, 2 x 16 rows, 4 heads: 22 us as they are, 29 in two): into enough for two workgroups a unit
 //     (6 sequences of up to 12345 tokens, 5 rows x 8 query heads, 4 heads x 96 integers: 28 us, with one a unit 31), but no more than
-//     32 where that is enough for one (one sequence of 32768 tokens: 64 parts 16.0 us, 32 14.9), and of two steps of each wave at
-//     least (two of 8000: 13.3 us, with one step 14.4, with four 14.8).
+//     32 where that is enough for one (one sequence of 32768 tokens: 64 parts 16.0 us, 32 14.9), of two steps of each wave at least
+//     (two sequences of 8000: 13.5 us, with one step 14.4, with four 14.9) or of one, if that makes 16 at most (one of 4000: 10.5 us,
+//     with two steps 11.4).  Four steps are not split (8 sequences of up to 1500 tokens, 5 rows: 13.1 us, in two 14.9).
 constexpr int kUnits = 256;  // compute units
 constexpr int kFewSplits = 32;
-constexpr int kLeastRounds = 2;
+constexpr int kOneStepSplits = 16;
+constexpr int kWholeRounds = 4;
 
 Cache4Plan plan_cache4_attend(const Cache4 &c, const Cache4Seqs &b, int max_rows, int max_length, int G, int window)
 {
@@ -841,9 +851,10 @@ Cache4Plan plan_cache4_attend(const Cache4 &c, const Cache4Seqs &b, int max_rows
         span = std::min(span, (int64_t)window + std::min<int64_t>(max_rows, 16 * p.blocks / G + 1));
     const int64_t groups = p.n_tiles * heads, round = kStep * attend_waves(p.blocks);
     int64_t splits = 1;
-    if (groups < kUnits) {
+    const int64_t rounds = (span + round - 1) / round;
+    if (groups < kUnits && rounds > kWholeRounds) {
         splits = std::max<int64_t>(kUnits / groups, std::min<int64_t>(2 * kUnits / groups, kFewSplits));
-        splits = std::min({splits, (span + kLeastRounds * round - 1) / (kLeastRounds * round), (int64_t)kMostSplits});
+        splits = std::min({splits, std::max<int64_t>((rounds + 1) / 2, std::min<int64_t>(rounds, kOneStepSplits)), (int64_t)kMostSplits});
     }
     p.split_tokens = (int32_t)((span + splits * round - 1) / (splits * round) * round);
     p.n_splits = (int32_t)((span + p.split_tokens - 1) / p.split_tokens);

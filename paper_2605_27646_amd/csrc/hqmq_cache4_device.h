@@ -87,14 +87,13 @@ __device__ __forceinline__ cache4_h2 e2m1_pair(uint32_t word, float scale)
     return __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(word, scale, kByte);
 }
 
-// Integer codes, one at bits 0..3 and one at bits 16..19 (the others are ignored), times s plus m, rounded once: 1024 + c is the
-// fp16 number 0x6400 | c, and the difference is exact.
-__device__ __forceinline__ cache4_h2 int4_pair(uint32_t word, cache4_h2 s, cache4_h2 m)
+// Integer codes c in the two low (kHigh: high) bytes of a word times s plus m, rounded once.  A byte 0 .. 15 read as an fp8 number
+// (4 bits of exponent, 3 of mantissa, the smallest ones denormal) is c 2^-9 for each of them, so one conversion with a scale of
+// 2^9 gives both codes as fp16 numbers.
+template <bool kHigh>
+__device__ __forceinline__ cache4_h2 int4_pair(uint32_t bytes, cache4_h2 s, cache4_h2 m)
 {
-    uint32_t magic = 0x64006400u;
-    asm("" : "+v"(magic));  // in a vector register: one instruction masks and adds it, which takes one scalar operand only
-    const cache4_h2 big = __builtin_bit_cast(cache4_h2, (word & 0x000f000fu) | magic);
-    return __builtin_elementwise_fma(big - cache4_h2{(_Float16)1024.f, (_Float16)1024.f}, s, m);
+    return __builtin_elementwise_fma(__builtin_bit_cast(cache4_h2, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(bytes, 512.f, kHigh)), s, m);
 }
 
 __device__ __forceinline__ float e8m0(uint32_t byte) { return __uint_as_float(byte << 23); }

@@ -154,11 +154,12 @@ __device__ __forceinline__ uint4v values(uint32_t code, uint32_t scale)
         y[3] = e2m1_pair<3>(code, unit);
     } else {
         const cache4_h2 sm = __builtin_bit_cast(cache4_h2, scale), ss = {sm[0], sm[0]}, mm = {sm[1], sm[1]};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const uint32_t two = code >> (8 * e);
-            y[e] = int4_pair((two & 0xfu) | (two & 0xf0u) << 12, ss, mm);
-        }
+        const uint32_t even = code & 0x0f0f0f0fu, odd = code >> 4 & 0x0f0f0f0fu;
+        const uint32_t lo = __builtin_amdgcn_perm(odd, even, 0x05010400u), hi = __builtin_amdgcn_perm(odd, even, 0x07030602u);  // a code a byte
+        y[0] = int4_pair<false>(lo, ss, mm);
+        y[1] = int4_pair<true>(lo, ss, mm);
+        y[2] = int4_pair<false>(hi, ss, mm);
+        y[3] = int4_pair<true>(hi, ss, mm);
     }
     uint4v bits;
 #pragma unroll
