@@ -47,7 +47,7 @@ constexpr size_t attend_shared_bytes(int NG, int blocks)  // queries, then the w
 }
 constexpr size_t attend_lds_bytes(int NG, int blocks)
 {
-    return attend_shared_bytes(NG, blocks) + (size_t)blocks * 16 * 8 + (size_t)attend_waves(blocks) * blocks * 16 * 2 * 4;
+    return attend_shared_bytes(NG, blocks) + (size_t)blocks * 16 * (8 + 12 * attend_waves(blocks) + 8);
 }
 
 // Maximum or sum over the four lanes that hold a query's column.
@@ -332,24 +332,21 @@ constexpr int attend_occupancy(int NG, int blocks) { return blocks == 1 && NG <=
 
 }  // namespace
 
-// Four channels of a result: the weighted sum divided by the weights' sum l, relative to 2^m.
+// Four channels of a result, or the n of them that there are (any number).
 template <bool kBf16>
-__device__ __forceinline__ void store_row(const Cache4Attend &a, int row, int head, int ch, f4 total, float m, float l, int64_t row_at)
+__device__ __forceinline__ void store_four(uint16_t *dst, f4 y, int n)
 {
-    const float inverse = l > 0.f ? 1.f / l : 0.f;
     uint32_t bits[2];
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-        const float u = total[2 * e] * inverse, v = total[2 * e + 1] * inverse;
         if (kBf16) {
             typedef __bf16 b2 __attribute__((ext_vector_type(2)));
-            bits[e] = __builtin_bit_cast(uint32_t, b2{(__bf16)u, (__bf16)v});
+            bits[e] = __builtin_bit_cast(uint32_t, b2{(__bf16)y[2 * e], (__bf16)y[2 * e + 1]});
         } else {
-            bits[e] = __builtin_bit_cast(uint32_t, half2_t{(_Float16)u, (_Float16)v});
+            bits[e] = __builtin_bit_cast(uint32_t, half2_t{(_Float16)y[2 * e], (_Float16)y[2 * e + 1]});
         }
     }
-    uint16_t *dst = a.out.data + (int64_t)row * a.out.row + (int64_t)head * a.out.head + ch;
-    if (ch + 4 <= a.c.D) {
+    if (n >= 4) {
         struct __attribute__((packed, aligned(2))) Four {
             uint64_t bits;
         };
@@ -357,12 +354,12 @@ __device__ __forceinline__ void store_row(const Cache4Attend &a, int row, int he
     } else {
 #pragma unroll
         for (int e = 0; e < 3; ++e)
-            if (ch + e < a.c.D)
+            if (e < n)
                 dst[e] = (uint16_t)(bits[e / 2] >> (16 * (e & 1)));
     }
-    if (a.lse && ch == 0)
-        a.lse[row_at] = l > 0.f ? kLn2 * (m + __builtin_amdgcn_logf(l)) : -__builtin_inff();
 }
+// The logarithm of a sum of weights l relative to 2^m.
+__device__ __forceinline__ float lse_of(float m, float l) { return l > 0.f ? kLn2 * (m + __builtin_amdgcn_logf(l)) : -__builtin_inff(); }
 
 template <int kFormat, int NG, int kBlocks, bool kBf16>
 __global__ __launch_bounds__(64 * attend_waves(kBlocks), attend_occupancy(NG, kBlocks)) void k_cache4_attend(Cache4Attend a)
@@ -379,6 +376,8 @@ __global__ __launch_bounds__(64 * attend_waves(kBlocks), attend_occupancy(NG, kB
     float *const factor = reinterpret_cast<float *>(lds + kShared);      // [kRows]: from products to exponents of 2
     int *const position = reinterpret_cast<int *>(factor + kRows);       // [kRows]: -1 - 2^30 and less: no row
     float *const stats = reinterpret_cast<float *>(position + kRows);    // [kWaves][kRows][2]
+    float *const row_factors = stats + kWaves * kRows * 2;               // [kRows][kWaves]
+    int64_t *const row_at_lds = reinterpret_cast<int64_t *>(row_factors + kWaves * kRows);  // [kRows]
 
     const int tid = threadIdx.x;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -652,6 +651,42 @@ __global__ __launch_bounds__(64 * attend_waves(kBlocks), attend_occupancy(NG, kB
                 *reinterpret_cast<float2 *>(stats + (wave * kRows + 16 * nb + col_now) * 2) = make_float2(ref[nb], total);
         }
         __syncthreads();  // the queries are done with
+        if (thread < kRows) {  // what a row's channels have in common: the waves' factors, and where they go; -1: nowhere
+            float2 part[kWaves];
+            float m = kNothing, l = 0.f, f[kWaves];
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) {
+                part[w] = *reinterpret_cast<const float2 *>(stats + (w * kRows + thread) * 2);
+                m = fmaxf(m, part[w].x);
+            }
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) {
+                f[w] = __builtin_amdgcn_exp2f(part[w].x - m);
+                l = fmaf(part[w].y, f[w], l);
+            }
+            const int r = r0 + thread, j = divided(r, a.by_G), in_head = h * a.G + (r - j * a.G);
+            const int64_t row_at = (int64_t)(s.first_row + j) * n_heads + in_head;
+            int64_t at = -1;
+            if (r < n_rows) {
+                if (a.n_splits > 1) {
+                    const int64_t part_at = row_at * a.n_splits + split;
+                    *reinterpret_cast<float2 *>(a.part_ml + 2 * part_at) = make_float2(m, l);
+                    at = l > 0.f ? part_at * (32 * NG) : -1;
+                } else {
+                    const float inverse = l > 0.f ? 1.f / l : 0.f;
+#pragma unroll
+                    for (int w = 0; w < kWaves; ++w)
+                        f[w] *= inverse;
+                    at = (int64_t)(s.first_row + j) * a.out.row + (int64_t)in_head * a.out.head;
+                    if (a.lse)
+                        a.lse[row_at] = lse_of(m, l);
+                }
+            }
+#pragma unroll
+            for (int w = 0; w < kWaves; w += 4)
+                *reinterpret_cast<f4 *>(row_factors + thread * kWaves + w) = f4{f[w], f[w + 1], f[w + 2], f[w + 3]};
+            row_at_lds[thread] = at;
+        }
         constexpr int kPass = attend_pass(NG, kBlocks), kUnits = 8 * NG;  // a thread takes 4 channels of a row
 #pragma unroll 1
         for (int first = 0; first < kBlocks; first += kPass) {
@@ -676,42 +711,25 @@ __global__ __launch_bounds__(64 * attend_waves(kBlocks), attend_occupancy(NG, kB
                 }
             });
             __syncthreads();
-#pragma unroll 1
+#pragma unroll 2
             for (int unit = thread; unit < kPass * 16 * kUnits; unit += 64 * kWaves) {
-                const int row = unit / kUnits, ch = 4 * (unit - row * kUnits), r = r0 + 16 * first + row;
-                if (r >= n_rows)
-                    break;
-                float2 part[kWaves];
-                f4 y[kWaves];
-#pragma unroll
-                for (int w = 0; w < kWaves; ++w) {
-                    part[w] = *reinterpret_cast<const float2 *>(stats + (w * kRows + 16 * first + row) * 2);
-                    y[w] = *reinterpret_cast<const f4 *>(join + (w * kPass * 16 + row) * kPitch + ch);
-                }
-                float m = kNothing, l = 0.f;
-#pragma unroll
-                for (int w = 0; w < kWaves; ++w)
-                    m = fmaxf(m, part[w].x);
+                const int row = (int)((uint32_t)unit / kUnits), ch = 4 * (unit - row * kUnits);
+                const int64_t at = row_at_lds[16 * first + row];
                 f4 total = f4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int w = 0; w < kWaves; ++w) {
-                    const float f = __builtin_amdgcn_exp2f(part[w].x - m);
-                    l = fmaf(part[w].y, f, l);
+                    const float f = row_factors[(16 * first + row) * kWaves + w];
+                    const f4 y = *reinterpret_cast<const f4 *>(join + (w * kPass * 16 + row) * kPitch + ch);
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        total[e] = fmaf(f, y[w][e], total[e]);
+                        total[e] = fmaf(f, y[e], total[e]);
                 }
-                const int j = divided(r, a.by_G), in_head = h * a.G + (r - j * a.G);
-                const int64_t row_at = (int64_t)(s.first_row + j) * n_heads + in_head;
-                if (a.n_splits > 1) {
-                    const int64_t at = row_at * a.n_splits + split;
-                    if (l > 0.f)
-                        *reinterpret_cast<f4 *>(a.part_acc + at * (32 * NG) + ch) = total;
-                    if (ch == 0)
-                        *reinterpret_cast<float2 *>(a.part_ml + 2 * at) = make_float2(m, l);
-                } else {
-                    store_row<kBf16>(a, s.first_row + j, in_head, ch, total, m, l, row_at);
-                }
+                if (at < 0)
+                    continue;
+                if (a.n_splits > 1)
+                    *reinterpret_cast<f4 *>(a.part_acc + at + ch) = total;
+                else
+                    store_four<kBf16>(a.out.data + at + ch, total, c.D - ch);
             }
             __syncthreads();
         }
@@ -815,7 +833,11 @@ __global__ __launch_bounds__(kMergeThreads) void k_cache4_merge(Cache4Attend a)
 #pragma unroll
             for (int i = 1; i < kAtOnce; ++i)
                 total += partial[i][tid];
-            store_row<kBf16>(a, row, head, 4 * tid, total, m, l, row_at);
+            const float inverse = l > 0.f ? 1.f / l : 0.f;
+            store_four<kBf16>(a.out.data + (int64_t)row * a.out.row + (int64_t)head * a.out.head + 4 * tid, total * f4{inverse, inverse, inverse, inverse},
+                              a.c.D - 4 * tid);
+            if (a.lse && tid == 0)
+                a.lse[row_at] = lse_of(m, l);
         }
         __syncthreads();
     }
@@ -845,7 +867,8 @@ Cache4Plan plan_cache4_attend(const Cache4 &c, const Cache4Seqs &b, int max_rows
     p.blocks = 1;
     while (p.blocks < (c.NG > 4 ? 2 : 4) && tiles_of(p.blocks) > 1 && tiles_of(p.blocks) * heads > kUnits * p.blocks)
         p.blocks *= 2;
-    p.n_tiles = (int32_t)std::min<int64_t>(tiles_of(p.blocks), 512);  // more take turns
+    // More take turns, so that what the host believes of the rows never makes more workgroups than work could fill.
+    p.n_tiles = (int32_t)std::min(tiles_of(p.blocks), std::max<int64_t>(std::min<int64_t>(512, ((int64_t)1 << 20) / heads), 1));
     int64_t span = max_length;
     if (window)
         span = std::min(span, (int64_t)window + std::min<int64_t>(max_rows, 16 * p.blocks / G + 1));

@@ -15,7 +15,7 @@ namespace hqmq {
 namespace {
 
 constexpr int kRowThreads = 256;
-constexpr int kMostBlocks = 1 << 16;  // of a grid along the positions
+constexpr int64_t kMostGroups = 1 << 22;
 typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
 
 // Maximum over the four lanes of a group.
@@ -326,11 +326,13 @@ __global__ __launch_bounds__(kRowThreads) void k_cache4_read(Cache4 c, Cache4Seq
 
 namespace {
 
+// Blocks of four positions: as many as the largest sequence needs, wherever in one of them its first position lies; beyond
+// kMostGroups workgroups in all they take turns.
 dim3 rows_grid(const Cache4 &c, const Cache4Seqs &b, int max_rows)
 {
-    const int blocks = max_rows == 1 ? 1 : (max_rows - 1) / 4 + 2;  // wherever in a block of four the first position lies
-    return dim3((unsigned)(blocks < kMostBlocks ? blocks : kMostBlocks), (unsigned)((2 * c.H * 4 * c.NG + kRowThreads - 1) / kRowThreads),
-                (unsigned)b.n_seqs);
+    const int64_t per_block = ((int64_t)2 * c.H * 4 * c.NG + kRowThreads - 1) / kRowThreads;
+    const int64_t blocks = max_rows == 1 ? 1 : (max_rows - 1) / 4 + 2, room = kMostGroups / (per_block * b.n_seqs);
+    return dim3((unsigned)(blocks < room ? blocks : room < 1 ? 1 : room), (unsigned)per_block, (unsigned)b.n_seqs);
 }
 
 }  // namespace
