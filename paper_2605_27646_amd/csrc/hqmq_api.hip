@@ -1490,6 +1490,7 @@ extern "C" int32_t hqmq_cache4_attend(const hqmq_cache4_params *params, const hq
     a.window = std::min(window, 1 << 30);
     a.by_G = make_divisor((uint32_t)a.G);
     a.by_splits = make_divisor((uint32_t)plan.n_splits);
+    a.flat = plan.flat;
     a.n_tiles = plan.n_tiles;
     a.n_splits = plan.n_splits;
     a.split_tokens = plan.split_tokens;

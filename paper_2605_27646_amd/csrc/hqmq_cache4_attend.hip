@@ -382,7 +382,16 @@ __global__ __launch_bounds__(64 * attend_waves(kBlocks), attend_occupancy(NG, kB
     const int tid = threadIdx.x;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const Cache4 &c = a.c;
-    const int h = blockIdx.x, seq = blockIdx.z, rest = divided((int)blockIdx.y, a.by_splits), split = (int)blockIdx.y - rest * a.n_splits;
+    const int h = blockIdx.x, rest = divided((int)blockIdx.y, a.by_splits), split = (int)blockIdx.y - rest * a.n_splits;
+    // the longest first: a causal prompt's last rows see the most
+    int seq = blockIdx.z, first_tile = a.n_tiles - 1 - rest;
+    if (a.flat.on) {
+        const int place = a.n_tiles - 1 - (rest + (int)(blockIdx.z * gridDim.y));  // z: only where nothing is split
+        seq = place < 0 ? -1 : cache4_seq_at(a.b, a.flat, place);
+        if (seq < 0)
+            return;
+        first_tile = place - cache4_first(a.b, a.flat, seq);
+    }
     const int page_mask = (1 << c.page_shift) - 1;
     const uint64_t head_rows = (uint64_t)h << c.page_shift;
     constexpr int kScale = kFormat == HQMQ_CACHE4_FLOAT ? 1 : 4;
@@ -392,8 +401,7 @@ __global__ __launch_bounds__(64 * attend_waves(kBlocks), attend_occupancy(NG, kB
     const Cache4Seq s = cache4_seq(a.b, c.page_shift, seq);
     const int n_rows = s.n * a.G, n_heads = c.H * a.G;
 
-    // the longest first: a causal prompt's last rows see the most
-    for (int tile = a.n_tiles - 1 - rest; tile * kRows < n_rows; tile += a.n_tiles) {
+    for (int tile = first_tile; (int64_t)tile * kRows < n_rows; tile += a.n_tiles) {  // a second one only with fewer places than tiles
         const int r0 = tile * kRows;
         int lane = tid & 63;
         asm volatile("" : "+v"(lane));  // what is made of it stays inside a tile's turn, of which there is one as a rule
@@ -864,6 +872,7 @@ __global__ __launch_bounds__(kMergeThreads) void k_cache4_merge(Cache4Attend a)
 //     with two steps 11.4).  Four steps are not split (8 sequences of up to 1500 tokens, 5 rows: 13.1 us, in two 14.9).
 constexpr int kUnits = 256;  // compute units
 constexpr int kFewSplits = 32;
+constexpr int kFewPlaces = 1024;
 constexpr int kOneStepSplits = 16;
 constexpr int kWholeRounds = 4;
 
@@ -872,15 +881,22 @@ Cache4Plan plan_cache4_attend(const Cache4 &c, const Cache4Seqs &b, int max_rows
     Cache4Plan p;
     const int64_t rows = (int64_t)max_rows * G, heads = (int64_t)c.H * b.n_seqs;
     const auto tiles_of = [&](int blocks) { return (rows + 16 * blocks - 1) / (16 * blocks); };
+    const auto flat_of = [&](int blocks) { return Cache4Flat{1, G, blocks == 1 ? 4 : blocks == 2 ? 5 : 6, 1}; };
+    const auto places_of = [&](int blocks) {  // of one head, as many as there can be work for
+        return b.starts ? std::min(tiles_of(blocks) * b.n_seqs, cache4_places(flat_of(blocks), b.n_rows, b.n_seqs)) : tiles_of(blocks) * b.n_seqs;
+    };
     p.blocks = 1;
-    while (p.blocks < (c.NG > 4 ? 2 : 4) && tiles_of(p.blocks) > 1 && tiles_of(p.blocks) * heads > kUnits * p.blocks)
+    while (p.blocks < (c.NG > 4 ? 2 : 4) && tiles_of(p.blocks) > 1 && places_of(p.blocks) * c.H > kUnits * p.blocks)
         p.blocks *= 2;
-    // More take turns, so that what the host believes of the rows never makes more workgroups than work could fill.
-    p.n_tiles = (int32_t)std::min(tiles_of(p.blocks), std::max<int64_t>(std::min<int64_t>(512, ((int64_t)1 << 20) / heads), 1));
+    p.flat = flat_of(p.blocks);
+    const int64_t places = places_of(p.blocks);
+    p.flat.on = b.starts && b.n_seqs > 1 && tiles_of(p.blocks) * heads > kFewPlaces && 2 * tiles_of(p.blocks) * b.n_seqs > 3 * places;
+    // More tiles than places take turns, so that what the host believes of the rows never makes more workgroups than work could fill.
+    p.n_tiles = (int32_t)(p.flat.on ? places : std::min(tiles_of(p.blocks), std::max<int64_t>(std::min<int64_t>(512, ((int64_t)1 << 20) / heads), 1)));
     int64_t span = max_length;
     if (window)
         span = std::min(span, (int64_t)window + std::min<int64_t>(max_rows, 16 * p.blocks / G + 1));
-    const int64_t groups = p.n_tiles * heads, round = kStep * attend_waves(p.blocks);
+    const int64_t groups = places * c.H, round = kStep * attend_waves(p.blocks);
     int64_t splits = 1;
     const int64_t rounds = (span + round - 1) / round;
     if (groups < kUnits && rounds > kWholeRounds) {
@@ -952,7 +968,11 @@ hipError_t prepare_cache4_kernels()
 hipError_t launch_cache4_attend(const Cache4Attend &a, const Cache4Plan &plan, bool bf16, hipStream_t stream)
 {
     const void *kernel = attend_kernel(a.c.format, bf16, a.c.NG, plan.blocks);
-    const dim3 grid((unsigned)a.c.H, (unsigned)(plan.n_tiles * plan.n_splits), (unsigned)a.b.n_seqs);
+    dim3 grid((unsigned)a.c.H, (unsigned)(plan.n_tiles * plan.n_splits), (unsigned)a.b.n_seqs);
+    if (plan.flat.on) {
+        grid.z = (grid.y + 32767) / 32768;
+        grid.y = (grid.y + grid.z - 1) / grid.z;
+    }
     Cache4Attend args = a;
     void *list[] = {&args};
     hipError_t err = hipLaunchKernel(kernel, grid, dim3(64 * attend_waves(plan.blocks)), list, attend_lds_bytes(a.c.NG, plan.blocks), stream);

@@ -76,6 +76,33 @@ __device__ __forceinline__ Cache4Seq cache4_seq(const Cache4Seqs &b, int page_sh
     return s;
 }
 
+// Places of a launch along the rows of all sequences, where a place for each of the largest sequence's tiles would leave most of them
+// empty: sequence i has those from first(i) = (starts[i] mul >> shift) + extra i on, at least mul n_i / 2^shift + extra of them.
+struct Cache4Flat {
+    int32_t on, mul, shift, extra;
+};
+__device__ __forceinline__ int cache4_first(const Cache4Seqs &b, const Cache4Flat &f, int i)
+{
+    return (int)((int64_t)min(max(const_ints(b.starts)[i], 0), b.n_rows) * f.mul >> f.shift) + f.extra * i;
+}
+// The sequence of a place, the last whose first place is not behind it, or -1: every lane of the wave asks for one of 64 in each round.
+__device__ __forceinline__ int cache4_seq_at(const Cache4Seqs &b, const Cache4Flat &f, int place)
+{
+    int from = 0, n = b.n_seqs;
+    const int lane = threadIdx.x & 63;
+    do {
+        const int step = (n + 63) / 64, i = lane * step;
+        const bool before = i < n && cache4_first(b, f, from + i) <= place;
+        const int count = __popcll(__builtin_amdgcn_ballot_w64(before));
+        if (count == 0)  // in the first round only
+            return -1;
+        from += (count - 1) * step;
+        n = min(step, n - (count - 1) * step);
+    } while (n > 1);
+    return __builtin_amdgcn_readfirstlane(from);
+}
+inline int64_t cache4_places(const Cache4Flat &f, int64_t n_rows, int64_t n_seqs) { return (n_rows * f.mul >> f.shift) + f.extra * n_seqs; }
+
 // ---- codes ------------------------------------------------------------------------------------------------------------
 
 typedef _Float16 cache4_h2 __attribute__((ext_vector_type(2)));
@@ -131,12 +158,14 @@ struct Cache4Attend {
     float scale;
     int32_t G, window;
     Divisor by_G, by_splits;
-    int32_t n_tiles, n_splits; // workgroups along the rows and along the tokens
+    Cache4Flat flat;
+    int32_t n_tiles, n_splits; // workgroups along the rows (of a sequence, or of all where flat.on) and along the tokens
     int32_t split_tokens;      // of each split but the last, which goes to the end
 };
 struct Cache4Plan {
     int32_t blocks;            // of 16 query rows that a workgroup takes at a time: 1, 2 or 4
     int32_t n_tiles, n_splits, split_tokens;
+    Cache4Flat flat;
     uint64_t ml_bytes, acc_bytes;
 };
 Cache4Plan plan_cache4_attend(const Cache4 &c, const Cache4Seqs &b, int max_rows, int max_length, int G, int window);

@@ -16,6 +16,8 @@ namespace {
 
 constexpr int kRowThreads = 256;
 constexpr int64_t kMostGroups = 1 << 22;
+constexpr int64_t kFewGroups = 1024;
+constexpr int kPastAll = 1 << 28;  // blocks of four positions that a sequence has at most
 typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
 
 // Maximum over the four lanes of a group.
@@ -49,6 +51,19 @@ __device__ __forceinline__ Unit unit_of(const Cache4 &c, Divisor by_row)
     u.w = i - u.h * words;
     u.there = u.h < c.H;
     return u;
+}
+
+// The sequence of this workgroup and which of its blocks of four positions is the first to take.
+__device__ __forceinline__ bool place_of(const Cache4Seqs &b, const Cache4Flat &flat, int &seq, int &turn)
+{
+    seq = blockIdx.z;
+    turn = blockIdx.x;
+    if (flat.on) {
+        const int place = (int)(blockIdx.x + gridDim.x * blockIdx.z);
+        seq = cache4_seq_at(b, flat, place);
+        turn = seq < 0 ? 0 : place - cache4_first(b, flat, seq);
+    }
+    return seq >= 0;
 }
 
 // The page of the block of four positions that begins at pos (0 or above), or -1: a page holds whole blocks.
@@ -177,10 +192,12 @@ __device__ __forceinline__ uint4v values(uint32_t code, uint32_t scale)
 }  // namespace
 
 template <int kFormat, bool kBf16>
-__global__ __launch_bounds__(kRowThreads) void k_cache4_write(Cache4 c, Cache4Seqs b, Cache4Rows k, Cache4Rows v, Divisor by_row)
+__global__ __launch_bounds__(kRowThreads) void k_cache4_write(Cache4 c, Cache4Seqs b, Cache4Rows k, Cache4Rows v, Divisor by_row, Cache4Flat flat)
 {
     typedef std::conditional_t<kFormat == HQMQ_CACHE4_FLOAT, uint8_t, uint32_t> Scale;
-    const int seq = blockIdx.z;
+    int seq, turn;
+    if (!place_of(b, flat, seq, turn))
+        return;
     const Cache4Seq s = cache4_seq(b, c.page_shift, seq);
     const Unit u = unit_of(c, by_row);
     const Cache4Rows rows = u.is_v ? v : k;
@@ -188,7 +205,7 @@ __global__ __launch_bounds__(kRowThreads) void k_cache4_write(Cache4 c, Cache4Se
     Scale *const scales = reinterpret_cast<Scale *>(u.is_v ? c.v_scales : c.k_scales);
     const int ch = 8 * u.w, row_bytes = 16 * c.NG, n_ch = min(max(c.D - ch, 0), 8);
     const uint16_t *const src = rows.data + u.h * rows.head + ch;
-    for (int block = (max(s.pos0, 0) >> 2) + (int)blockIdx.x; 4 * block < s.length && s.n > 0; block += (int)gridDim.x) {
+    for (int block = (max(s.pos0, 0) >> 2) + turn; 4 * (int64_t)block < s.length && s.n > 0; block += flat.on ? kPastAll : (int)gridDim.x) {
         const int pos = 4 * block, first = max(s.pos0 - pos, 0), end = min(s.length - pos, 4);  // the block's tokens first .. end - 1
         const int page = page_of(c, b, seq, pos);
         if (page < 0)  // uniform
@@ -266,10 +283,12 @@ __global__ __launch_bounds__(kRowThreads) void k_cache4_write(Cache4 c, Cache4Se
 }
 
 template <int kFormat, bool kBf16>
-__global__ __launch_bounds__(kRowThreads) void k_cache4_read(Cache4 c, Cache4Seqs b, Cache4Rows k, Cache4Rows v, Divisor by_row)
+__global__ __launch_bounds__(kRowThreads) void k_cache4_read(Cache4 c, Cache4Seqs b, Cache4Rows k, Cache4Rows v, Divisor by_row, Cache4Flat flat)
 {
     typedef std::conditional_t<kFormat == HQMQ_CACHE4_FLOAT, uint8_t, uint32_t> Scale;
-    const int seq = blockIdx.z;
+    int seq, turn;
+    if (!place_of(b, flat, seq, turn))
+        return;
     const Cache4Seq s = cache4_seq(b, c.page_shift, seq);
     const Unit u = unit_of(c, by_row);
     const Cache4Rows rows = u.is_v ? v : k;
@@ -279,7 +298,7 @@ __global__ __launch_bounds__(kRowThreads) void k_cache4_read(Cache4 c, Cache4Seq
     if (!u.there || ch >= c.D)
         return;
     uint16_t *const dst = rows.data + u.h * rows.head + ch;
-    for (int block = (s.pos0 >> 2) + (int)blockIdx.x; 4 * block < s.length; block += (int)gridDim.x) {
+    for (int block = (s.pos0 >> 2) + turn; 4 * (int64_t)block < s.length; block += flat.on ? kPastAll : (int)gridDim.x) {
         const int pos = 4 * block, first = max(s.pos0 - pos, 0), end = min(s.length - pos, 4);
         const int page = pos >= 0 ? page_of(c, b, seq, pos) : -1;
         uint4v code = uint4v{0u, 0u, 0u, 0u}, scale = code;
@@ -327,11 +346,18 @@ __global__ __launch_bounds__(kRowThreads) void k_cache4_read(Cache4 c, Cache4Seq
 namespace {
 
 // Blocks of four positions: as many as the largest sequence needs, wherever in one of them its first position lies; beyond
-// kMostGroups workgroups in all they take turns.
-dim3 rows_grid(const Cache4 &c, const Cache4Seqs &b, int max_rows)
+// kMostGroups workgroups in all they take turns.  Where that would leave most of many workgroups without rows, places along all rows.
+dim3 rows_grid(const Cache4 &c, const Cache4Seqs &b, int max_rows, Cache4Flat &flat)
 {
     const int64_t per_block = ((int64_t)2 * c.H * 4 * c.NG + kRowThreads - 1) / kRowThreads;
     const int64_t blocks = max_rows == 1 ? 1 : (max_rows - 1) / 4 + 2, room = kMostGroups / (per_block * b.n_seqs);
+    flat = Cache4Flat{0, 1, 2, 2};
+    const int64_t places = cache4_places(flat, b.n_rows, b.n_seqs);
+    if (b.starts && b.n_seqs > 1 && blocks * b.n_seqs > kFewGroups && 2 * blocks * b.n_seqs > 3 * places) {
+        flat.on = 1;
+        const int64_t z = (places + (1 << 22) - 1) >> 22;
+        return dim3((unsigned)((places + z - 1) / z), (unsigned)per_block, (unsigned)z);
+    }
     return dim3((unsigned)(blocks < room ? blocks : room < 1 ? 1 : room), (unsigned)per_block, (unsigned)b.n_seqs);
 }
 
@@ -342,7 +368,9 @@ hipError_t launch_cache4_write(const Cache4 &c, const Cache4Seqs &b, int max_row
 {
     const auto kernel = c.format == HQMQ_CACHE4_FLOAT ? (bf16 ? k_cache4_write<HQMQ_CACHE4_FLOAT, true> : k_cache4_write<HQMQ_CACHE4_FLOAT, false>)
                                                       : (bf16 ? k_cache4_write<HQMQ_CACHE4_INT, true> : k_cache4_write<HQMQ_CACHE4_INT, false>);
-    kernel<<<rows_grid(c, b, max_rows), kRowThreads, 0, stream>>>(c, b, k, v, make_divisor((uint32_t)(4 * c.NG)));
+    Cache4Flat flat;
+    const dim3 grid = rows_grid(c, b, max_rows, flat);
+    kernel<<<grid, kRowThreads, 0, stream>>>(c, b, k, v, make_divisor((uint32_t)(4 * c.NG)), flat);
     return hipGetLastError();
 }
 
@@ -351,7 +379,9 @@ hipError_t launch_cache4_read(const Cache4 &c, const Cache4Seqs &b, int max_rows
 {
     const auto kernel = c.format == HQMQ_CACHE4_FLOAT ? (bf16 ? k_cache4_read<HQMQ_CACHE4_FLOAT, true> : k_cache4_read<HQMQ_CACHE4_FLOAT, false>)
                                                       : (bf16 ? k_cache4_read<HQMQ_CACHE4_INT, true> : k_cache4_read<HQMQ_CACHE4_INT, false>);
-    kernel<<<rows_grid(c, b, max_rows), kRowThreads, 0, stream>>>(c, b, k, v, make_divisor((uint32_t)(4 * c.NG)));
+    Cache4Flat flat;
+    const dim3 grid = rows_grid(c, b, max_rows, flat);
+    kernel<<<grid, kRowThreads, 0, stream>>>(c, b, k, v, make_divisor((uint32_t)(4 * c.NG)), flat);
     return hipGetLastError();
 }
 

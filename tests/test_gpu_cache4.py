@@ -327,6 +327,49 @@ def test_steps_together():
     w.same_bytes()
 
 
+@pytest.mark.parametrize("fmt,dtype", [(hq.HQMQ_CACHE4_FLOAT, BF16), (hq.HQMQ_CACHE4_INT, F16)])
+def test_one_prompt_among_many_steps(fmt, dtype):
+    """A batch of which one sequence has nearly all rows: places along all rows instead of the largest sequence's for each."""
+    n = 70
+    w = World(55, fmt, 4, 64, 32, n, 20)
+    rows = [1] * n
+    rows[0], rows[13], rows[40], rows[69] = 0, 600, 37, 0
+    lengths = [int(x) for x in w.rng.integers(1, 90, n)]
+    lengths[13], lengths[40] = 640, 37
+    k, v = (w.values(sum(rows), dtype) for _ in range(2))
+    w.fill_random(lengths, dtype)
+    batch = w.batch(lengths, rows, max_rows=600)
+    hq.hqmq_cache4_write(w.params, w.cache, batch, k, v)
+    w.write_plain(lengths, rows, k, v)
+    w.same_bytes()
+    back = [torch.full_like(x, float("nan")) for x in (k, v)]
+    hq.hqmq_cache4_read(w.params, w.cache, batch, *back)
+    for row, i, pos in w.places(lengths, rows):
+        want = torch.tensor(w.plain.get(0, int(w.table[i, pos // 32]), pos % 32)).to(dtype)
+        assert torch.equal(back[0][row].cpu(), want), row
+    _check_attend(w, lengths, rows, dtype, 4, max_rows=600, max_length=640)
+    _check_attend(w, lengths, rows, dtype, 4, max_rows=1, max_length=640)
+
+
+def test_thousands_of_sequences():
+    """Most of them with one row, some with none, one with many: three rounds of the search for a place's sequence."""
+    n = 5000
+    w = World(57, hq.HQMQ_CACHE4_FLOAT, 1, 32, 16, n, 2)
+    rows = [int(x) for x in w.rng.integers(0, 2, n)]
+    rows[17], rows[4999] = 32, 5
+    lengths = [max(r, int(x)) for r, x in zip(rows, w.rng.integers(0, 33, n))]
+    k, v = (w.values(sum(rows), F16) for _ in range(2))
+    batch = w.batch(lengths, rows)  # what a sequence may have is not known: all rows
+    hq.hqmq_cache4_write(w.params, w.cache, batch, k, v)
+    w.write_plain(lengths, rows, k, v)
+    w.same_bytes()
+    for t in w.buffers[1::2]:  # unwritten scales are zeros from here on
+        t[t == 255] = 0
+    w.plain.ks[w.plain.ks == 255] = 0
+    w.plain.vs[w.plain.vs == 255] = 0
+    _check_attend(w, lengths, rows, F16, 2)
+
+
 def test_no_rows():
     w = World(61, hq.HQMQ_CACHE4_INT, 2, 64, 16, 2, 2)
     none = torch.empty(0, 2, 64, dtype=F16, device=DEV)
