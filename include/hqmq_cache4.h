@@ -67,7 +67,8 @@ typedef struct hqmq_cache4_buffers {
  *   starts      DEVICE, int32 [n_seqs + 1], ascending, or NULL: every sequence has n_rows / n_seqs rows.  Rows outside
  *               starts[0] .. starts[n_seqs] - 1 are no sequence's: they are not read, nor written.
  *   max_rows, max_length   the largest number of rows and length of a sequence as far as the host knows them: they shape
- *               the launch; results do not depend on them.  max_rows is ignored where starts is NULL.
+ *               the launch and, through it, the order of sums; every row and token counts whatever they say.  max_rows is
+ *               ignored where starts is NULL.
  * A page number outside 0 .. n_pages - 1, and a position below 0 (more rows than tokens), are no tokens: write leaves
  * them out, read gives zeros, attend does not see them. */
 typedef struct hqmq_cache4_batch {
@@ -80,7 +81,8 @@ typedef struct hqmq_cache4_batch {
 } hqmq_cache4_batch;
 
 /* Rows [n_rows][heads][D] with element strides, channels contiguous: HOST struct of a DEVICE pointer, aligned to 2 bytes.
- * Strides and addresses that are multiples of 8 elements, and such a D, are moved 16 bytes at a time. */
+ * Any alignment of 2 bytes does: rows are moved 8 channels at a time, the last D % 8 one by one (as are all of q's where D
+ * is no multiple of 8). */
 typedef struct hqmq_cache4_rows {
     void *data;
     int64_t stride_row, stride_head;

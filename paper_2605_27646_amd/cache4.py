@@ -105,8 +105,8 @@ def alloc_cache4(params: Cache4Params, device) -> Cache4Buffers:
 class Cache4Batch:
     """Which rows a call has and where their tokens lie: block_table (int32 [n_seqs, pages_per_seq]), lengths (int32 [n_seqs], the
     call's rows included), starts (int32 [n_seqs + 1], ascending; None: equal shares).  max_rows and max_length: the largest as
-    far as the host knows them, by default all rows (of starts) and all that the table has room for; they shape the launch, not
-    the results.  The tensors are read when the calls run, so that one batch serves many steps; they have to stay in place."""
+    far as the host knows them, by default all rows (of starts) and all that the table has room for; they shape the launch, and
+    every row and token counts whatever they say.  The tensors are read when the calls run, so that one batch serves many steps; they have to stay in place."""
 
     def __init__(self, block_table: torch.Tensor, lengths: torch.Tensor, starts: torch.Tensor | None = None, max_rows: int | None = None,
                  max_length: int | None = None):

@@ -10,6 +10,11 @@
 //   O^T = V^T P^T lane (run l % 16, l / 16) reads the codes of those eight tokens for a run of 8 (4, 2) channels, two blocks of four
 //                 tokens of the V layout, and product e takes channel e of every run.
 // A query's maximum and sum belong to one column, so every factor is one per lane.
+//
+// Bound by memory for generation steps of many long sequences (64 of up to 8192 tokens, 8 heads x 128: 70.7 us, 301 MB at 4.3 TB/s,
+// vector instructions issue for a third of the time), by a workgroup's start and the join for short ones (130 tokens 5.5 us, of which
+// one step is 1), and by issue for prompts (1024 tokens of two sequences behind 15000: 452 us, 1.15 PFLOP/s, vector instructions
+// 58 % and matrix instructions 40 % of the time; of the former 37 % are exponentials, 33 % the reconstruction for 64 rows).
 #include <algorithm>
 #include <type_traits>
 
@@ -870,11 +875,13 @@ __global__ __launch_bounds__(kMergeThreads) void k_cache4_merge(Cache4Attend a)
 //     32 where that is enough for one (one sequence of 32768 tokens: 64 parts 16.0 us, 32 14.9), of two steps of each wave at least
 //     (two sequences of 8000: 13.5 us, with one step 14.4, with four 14.9) or of one, if that makes 16 at most (one of 4000: 10.5 us,
 //     with two steps 11.4).  Four steps are not split (8 sequences of up to 1500 tokens, 5 rows: 13.1 us, in two 14.9).
+//   - Where a launch of the largest sequence's tiles for each would be mostly empty, places are dealt along all rows and a workgroup finds
+//     its sequence (2048 rows among 63 single ones: 192 us without, 93 with; among 255 360 and 116).
 constexpr int kUnits = 256;  // compute units
 constexpr int kFewSplits = 32;
-constexpr int kFewPlaces = 1024;
 constexpr int kOneStepSplits = 16;
 constexpr int kWholeRounds = 4;
+constexpr int kFewPlaces = 1024;
 
 Cache4Plan plan_cache4_attend(const Cache4 &c, const Cache4Seqs &b, int max_rows, int max_length, int G, int window)
 {
