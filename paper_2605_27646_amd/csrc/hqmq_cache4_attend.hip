@@ -215,14 +215,14 @@ __device__ __forceinline__ void load_v(VStage<kFormat, NG> &s, const Tile &tile,
     }
 }
 
-// Tokens of the lane's four at or behind `end` (of these four) become zeros, whatever lies there.
+// Of the lane's four tokens those before `first` and from `end` on become zeros, whatever lies there.
 template <int kFormat, int NG>
-__device__ __forceinline__ void blank_v(VStage<kFormat, NG> &s, int end)
+__device__ __forceinline__ void blank_v(VStage<kFormat, NG> &s, int first, int end)
 {
     using P = Parts<NG>;
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
-        const bool gone = t >= end;
+        const bool gone = t < first || t >= end;
 #pragma unroll
         for (int p = 0; p < P::n; ++p) {
             const int at = P::before(p);
@@ -623,11 +623,14 @@ __global__ __launch_bounds__(64 * attend_waves(kBlocks), attend_occupancy(NG, kB
                         }
                     }
             }
-            // ---- values: a token that is none of the sequence's may hold anything
-            if (token + kStep > s.length || bad_now[0] || bad_now[1]) {
+            // ---- values: a token that none of the sequence's rows sees may hold anything
+            const bool too_early = a.window && token < all_end - a.window;
+            if (token + kStep > s.length || too_early || bad_now[0] || bad_now[1]) {
 #pragma unroll
-                for (int i = 0; i < 2; ++i)
-                    blank_v(vs[i], bad_now[i] ? 0 : s.length - (token + 16 * i + 4 * quarter));
+                for (int i = 0; i < 2; ++i) {
+                    const int base = token + 16 * i + 4 * quarter;
+                    blank_v(vs[i], too_early ? all_end - a.window - base : 0, bad_now[i] ? 0 : s.length - base);
+                }
             }
             if (kBlocks > 2)
                 __builtin_amdgcn_s_setprio(1);

@@ -116,7 +116,7 @@ def _check_attend(w, lengths, rows, dtype, G, scale=None, window=0, starts=True,
         err = np.abs(got[idx] - o)
         assert np.isfinite(got[idx]).all(), (i, lengths[i])
         assert (err <= tol).all(), (i, lengths[i], rows[i], np.argwhere(err > tol)[:3], (err / tol).max())
-        worst = max(worst, float((err / tol).max()))
+        worst = max(worst, float((err / np.maximum(tol, 1e-300)).max()))
         seen = np.isfinite(l)
         assert (got_lse[idx][~seen] == -np.inf).all() and (got[idx][~seen] == 0).all()
         err = np.abs(got_lse[idx][seen] - l[seen])
@@ -250,6 +250,29 @@ def test_attend_windows(window, rows, G):
     lengths = [500, 333]
     w.fill_random(lengths, BF16)
     _check_attend(w, lengths, [rows, min(rows, 50)], BF16, G, window=window)
+
+
+@pytest.mark.parametrize("fmt", FMT)
+@pytest.mark.parametrize("rows,window", [(1, 33), (1, 100), (6, 50), (40, 17)])
+def test_what_no_row_sees_may_hold_anything(fmt, rows, window):
+    """Pages before the windows given back: none, or one that holds another's bytes, here NaN scales; the same behind the last row."""
+    w = World(rows + window, fmt, 2, 96, 16, 2, 24)
+    lengths = [300, 187]
+    w.fill_random(lengths, F16)
+    other = [p for p in range(w.params.n_pages) if p not in set(w.table.ravel())][0]  # never written
+    plain = w.table.copy()
+    for i, length in enumerate(lengths):
+        given_back = max(0, length - rows + 1 - window) // 16
+        w.table[i, :given_back:2], w.table[i, 1:given_back:2] = other, -1
+        w.table[i, -(-length // 16):] = other
+    out, lse, _ = _check_attend(w, lengths, [rows, rows], F16, 3, window=window)
+    w.table = plain
+    w.rng = np.random.default_rng(0)
+    want = _check_attend(w, lengths, [rows, rows], F16, 3, window=window)
+    w.table[:, :1] = other
+    w.rng = np.random.default_rng(0)
+    got = _check_attend(w, lengths, [rows, rows], F16, 3, window=window)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
 
 
 @pytest.mark.parametrize("hint", [1, 200, 1024, 2048, 2 ** 30])
