@@ -393,9 +393,9 @@ __global__ __launch_bounds__(64 * attend_waves(kBlocks), attend_occupancy(NG, kB
     if (a.flat.on) {
         const int place = a.n_tiles - 1 - (rest + (int)(blockIdx.z * gridDim.y));  // z: only where nothing is split
         seq = place < 0 ? -1 : cache4_seq_at(a.b, a.flat, place);
-        if (seq < 0)
+        first_tile = seq < 0 ? -1 : place - cache4_first(a.b, a.flat, seq);
+        if (first_tile < 0)  // starts that do not ascend have no tiles
             return;
-        first_tile = place - cache4_first(a.b, a.flat, seq);
     }
     const int page_mask = (1 << c.page_shift) - 1;
     const uint64_t head_rows = (uint64_t)h << c.page_shift;

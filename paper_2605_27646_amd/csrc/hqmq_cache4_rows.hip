@@ -61,9 +61,9 @@ __device__ __forceinline__ bool place_of(const Cache4Seqs &b, const Cache4Flat &
     if (flat.on) {
         const int place = (int)(blockIdx.x + gridDim.x * blockIdx.z);
         seq = cache4_seq_at(b, flat, place);
-        turn = seq < 0 ? 0 : place - cache4_first(b, flat, seq);
+        turn = seq < 0 ? -1 : place - cache4_first(b, flat, seq);
     }
-    return seq >= 0;
+    return turn >= 0;  // starts that do not ascend have no places
 }
 
 // The page of the block of four positions that begins at pos (0 or above), or -1: a page holds whole blocks.

@@ -275,6 +275,25 @@ def test_what_no_row_sees_may_hold_anything(fmt, rows, window):
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
 
 
+def test_starts_that_do_not_ascend():
+    """Rows are lost, or some are computed twice, but every access stays inside the tensors: both ways of dealing places."""
+    w = World(77, hq.HQMQ_CACHE4_FLOAT, 4, 64, 16, 80, 4)
+    w.fill_random([64] * 80, F16)
+    n = 700
+    k, v, q = w.values(n, F16), w.values(n, F16), w.values(n, F16, heads=16)
+    out, ws = torch.empty_like(q), torch.empty(1 << 24, dtype=torch.uint8, device=DEV)
+    for seed in range(4):
+        g = torch.Generator().manual_seed(seed)
+        starts = torch.randint(-50, n + 50, (81,), generator=g).to(torch.int32).to(DEV)
+        lengths = torch.randint(-5, 80, (80,), generator=g).to(torch.int32).to(DEV)
+        for hint in (1, n):
+            batch = hq.Cache4Batch(torch.tensor(w.table, device=DEV), lengths, starts, max_rows=hint)
+            hq.hqmq_cache4_write(w.params, w.cache, batch, k, v)
+            hq.hqmq_cache4_read(w.params, w.cache, batch, k.clone(), v.clone())
+            hq.hqmq_cache4_attend(w.params, w.cache, batch, q, 0.1, out, ws)
+    torch.cuda.synchronize()
+
+
 @pytest.mark.parametrize("hint", [1, 200, 1024, 2048, 2 ** 30])
 @pytest.mark.parametrize("rows", [1, 20])
 def test_attend_splits_and_hints(hint, rows):
