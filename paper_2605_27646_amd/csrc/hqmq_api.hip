@@ -1400,10 +1400,8 @@ static int32_t cache4_move(bool write, const hqmq_cache4_params *params, const h
         return HQMQ_ERR_INVALID_ARG;
     if (n_rows == 0)
         return HQMQ_OK;
-    const auto launch = write ? launch_cache4_write : launch_cache4_read;
-    const hipError_t err = launch(make_cache4(params, cache), make_cache4_seqs(batch, n_rows), cache4_most_rows(batch, n_rows),
-                                  type == HQMQ_TYPE_BF16, make_cache4_rows(k), make_cache4_rows(v),
-                                  static_cast<hipStream_t>(stream));
+    const hipError_t err = launch_cache4_rows(write, make_cache4(params, cache), make_cache4_seqs(batch, n_rows), cache4_most_rows(batch, n_rows),
+                                              type == HQMQ_TYPE_BF16, make_cache4_rows(k), make_cache4_rows(v), static_cast<hipStream_t>(stream));
     return err == hipSuccess ? HQMQ_OK : hip_failed(err);
 }
 

@@ -952,6 +952,23 @@ const void *attend_kernel(int NG, int blocks)
 
 }  // namespace
 
+template <int NG>
+static const void *merge_kernel(bool bf16)
+{
+    return bf16 ? reinterpret_cast<const void *>(&k_cache4_merge<NG, true>) : reinterpret_cast<const void *>(&k_cache4_merge<NG, false>);
+}
+static const void *merge_kernel(int NG, bool bf16)
+{
+    switch (NG) {
+    case 1: return merge_kernel<1>(bf16);
+    case 2: return merge_kernel<2>(bf16);
+    case 3: return merge_kernel<3>(bf16);
+    case 4: return merge_kernel<4>(bf16);
+    case 6: return merge_kernel<6>(bf16);
+    default: return merge_kernel<8>(bf16);
+    }
+}
+
 static const void *attend_kernel(int format, bool bf16, int NG, int blocks)
 {
     if (format == HQMQ_CACHE4_FLOAT)
@@ -989,15 +1006,7 @@ hipError_t launch_cache4_attend(const Cache4Attend &a, const Cache4Plan &plan, b
     if (err != hipSuccess || plan.n_splits == 1)
         return err;
     const dim3 rows((unsigned)std::min<int64_t>((int64_t)a.b.n_rows * a.c.H * a.G, 1 << 20));
-    switch (a.c.NG) {
-    case 1: (bf16 ? k_cache4_merge<1, true> : k_cache4_merge<1, false>)<<<rows, kMergeThreads, 0, stream>>>(args); break;
-    case 2: (bf16 ? k_cache4_merge<2, true> : k_cache4_merge<2, false>)<<<rows, kMergeThreads, 0, stream>>>(args); break;
-    case 3: (bf16 ? k_cache4_merge<3, true> : k_cache4_merge<3, false>)<<<rows, kMergeThreads, 0, stream>>>(args); break;
-    case 4: (bf16 ? k_cache4_merge<4, true> : k_cache4_merge<4, false>)<<<rows, kMergeThreads, 0, stream>>>(args); break;
-    case 6: (bf16 ? k_cache4_merge<6, true> : k_cache4_merge<6, false>)<<<rows, kMergeThreads, 0, stream>>>(args); break;
-    default: (bf16 ? k_cache4_merge<8, true> : k_cache4_merge<8, false>)<<<rows, kMergeThreads, 0, stream>>>(args); break;
-    }
-    return hipGetLastError();
+    return hipLaunchKernel(merge_kernel(a.c.NG, bf16), rows, dim3(kMergeThreads), list, 0, stream);
 }
 
 }  // namespace hqmq

@@ -143,9 +143,7 @@ __device__ __forceinline__ Cache4Place cache4_v_place(int NG, int w, int t)
 
 // ---- launches ---------------------------------------------------------------------------------------------------------
 
-hipError_t launch_cache4_write(const Cache4 &c, const Cache4Seqs &b, int max_rows, bool bf16, const Cache4Rows &k, const Cache4Rows &v,
-                               hipStream_t stream);
-hipError_t launch_cache4_read(const Cache4 &c, const Cache4Seqs &b, int max_rows, bool bf16, const Cache4Rows &k, const Cache4Rows &v,
+hipError_t launch_cache4_rows(bool write, const Cache4 &c, const Cache4Seqs &b, int max_rows, bool bf16, const Cache4Rows &k, const Cache4Rows &v,
                               hipStream_t stream);
 
 struct Cache4Attend {

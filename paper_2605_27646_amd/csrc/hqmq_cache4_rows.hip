@@ -364,26 +364,26 @@ dim3 rows_grid(const Cache4 &c, const Cache4Seqs &b, int max_rows, Cache4Flat &f
 
 }  // namespace
 
-hipError_t launch_cache4_write(const Cache4 &c, const Cache4Seqs &b, int max_rows, bool bf16, const Cache4Rows &k, const Cache4Rows &v,
-                               hipStream_t stream)
+template <int kFormat>
+static const void *rows_kernel(bool write, bool bf16)
 {
-    const auto kernel = c.format == HQMQ_CACHE4_FLOAT ? (bf16 ? k_cache4_write<HQMQ_CACHE4_FLOAT, true> : k_cache4_write<HQMQ_CACHE4_FLOAT, false>)
-                                                      : (bf16 ? k_cache4_write<HQMQ_CACHE4_INT, true> : k_cache4_write<HQMQ_CACHE4_INT, false>);
-    Cache4Flat flat;
-    const dim3 grid = rows_grid(c, b, max_rows, flat);
-    kernel<<<grid, kRowThreads, 0, stream>>>(c, b, k, v, make_divisor((uint32_t)(4 * c.NG)), flat);
-    return hipGetLastError();
+    if (write)
+        return bf16 ? reinterpret_cast<const void *>(&k_cache4_write<kFormat, true>) : reinterpret_cast<const void *>(&k_cache4_write<kFormat, false>);
+    return bf16 ? reinterpret_cast<const void *>(&k_cache4_read<kFormat, true>) : reinterpret_cast<const void *>(&k_cache4_read<kFormat, false>);
 }
 
-hipError_t launch_cache4_read(const Cache4 &c, const Cache4Seqs &b, int max_rows, bool bf16, const Cache4Rows &k, const Cache4Rows &v,
+hipError_t launch_cache4_rows(bool write, const Cache4 &c, const Cache4Seqs &b, int max_rows, bool bf16, const Cache4Rows &k, const Cache4Rows &v,
                               hipStream_t stream)
 {
-    const auto kernel = c.format == HQMQ_CACHE4_FLOAT ? (bf16 ? k_cache4_read<HQMQ_CACHE4_FLOAT, true> : k_cache4_read<HQMQ_CACHE4_FLOAT, false>)
-                                                      : (bf16 ? k_cache4_read<HQMQ_CACHE4_INT, true> : k_cache4_read<HQMQ_CACHE4_INT, false>);
+    Cache4 cc = c;
+    Cache4Seqs bc = b;
+    Cache4Rows kc = k, vc = v;
+    Divisor by_row = make_divisor((uint32_t)(4 * c.NG));
     Cache4Flat flat;
     const dim3 grid = rows_grid(c, b, max_rows, flat);
-    kernel<<<grid, kRowThreads, 0, stream>>>(c, b, k, v, make_divisor((uint32_t)(4 * c.NG)), flat);
-    return hipGetLastError();
+    void *args[] = {&cc, &bc, &kc, &vc, &by_row, &flat};
+    const void *kernel = c.format == HQMQ_CACHE4_FLOAT ? rows_kernel<HQMQ_CACHE4_FLOAT>(write, bf16) : rows_kernel<HQMQ_CACHE4_INT>(write, bf16);
+    return hipLaunchKernel(kernel, grid, dim3(kRowThreads), args, 0, stream);
 }
 
 }  // namespace hqmq

@@ -423,6 +423,26 @@ def test_no_rows():
     w.same_bytes()
 
 
+def test_an_error_that_another_call_left():
+    """A failed HIP call before ours is not reported as ours."""
+    from paper_2605_27646_amd import binding
+    hip = binding._load()  # its own dependencies' names resolve through it
+    w = World(78, hq.HQMQ_CACHE4_FLOAT, 2, 64, 16, 2, 40)
+    w.fill_random([600, 500], F16)
+    batch, k, v, q = w.batch([600, 500], [1, 1]), w.values(2, F16), w.values(2, F16), w.values(2, F16)
+    out, ws = torch.empty_like(q), torch.empty(1 << 22, dtype=torch.uint8, device=DEV)
+    torch.cuda.synchronize()
+    calls = [lambda: hq.hqmq_cache4_write(w.params, w.cache, batch, k, v), lambda: hq.hqmq_cache4_read(w.params, w.cache, batch, k, v),
+             lambda: hq.hqmq_cache4_attend(w.params, w.cache, batch, q, 0.1, out, ws)]
+    for call in calls:
+        assert hip.hipSetDevice(1 << 20) != 0
+        try:
+            call()
+        finally:
+            hip.hipGetLastError()  # the next library's call is not to see it either
+    torch.cuda.synchronize()
+
+
 def test_offsets_past_32_bits():
     """Pages behind 4 GiB of codes."""
     n_pages, page, H, D = 140000, 64, 8, 128
