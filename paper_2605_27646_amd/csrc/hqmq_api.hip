@@ -1463,6 +1463,8 @@ extern "C" int32_t hqmq_cache4_attend(const hqmq_cache4_params *params, const hq
         return rc;
     if (!std::isfinite(scale) || misaligned(lse_dev, 4) || misaligned(workspace_dev, 256))
         return HQMQ_ERR_INVALID_ARG;
+    if (std::fabs(scale) > 0x1p100f)
+        return HQMQ_ERR_UNSUPPORTED;
     if (n_rows == 0)
         return HQMQ_OK;
     const Cache4Plan plan = cache4_plan(params, batch, n_rows, n_q_heads, window);

@@ -31,9 +31,11 @@ typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
 
 constexpr int kStep = 32;             // tokens that a wave takes at a time
 constexpr int kMergeThreads = 256;
-constexpr float kNothing = -1.0e30f;  // "no token seen yet": finite, so that differences stay finite
+constexpr float kNothing = -3.0e38f;  // "no token seen yet": less than any exponent, finite, so that of two of them the difference is 0
 constexpr float kTop4 = 7.f;          // weights are taken relative to 2^-kTop4 of the largest score,
 constexpr float kRise4 = 15.f;        // and relative to a newer one once they would pass 2^kRise4 (fp16 ends at 2^16)
+constexpr int kFarOnly = 0x7fffffff;
+constexpr float kMost4 = 0x1p127f;    // exponents and factors end here
 constexpr float kLog2e4 = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
 // Waves of a workgroup.  For up to 16 rows eight, of which two workgroups fill a compute unit's registers.
@@ -62,6 +64,13 @@ __device__ __forceinline__ float column_max(float x)
     x = fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
     y = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
     return fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
+}
+__device__ __forceinline__ uint32_t column_max(uint32_t x)
+{
+    auto y = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    x = max((uint32_t)y[0], (uint32_t)y[1]);
+    y = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    return max((uint32_t)y[0], (uint32_t)y[1]);
 }
 __device__ __forceinline__ float column_sum(float x)
 {
@@ -415,7 +424,7 @@ __global__ __launch_bounds__(64 * attend_waves(kBlocks), attend_occupancy(NG, kB
         const int j_first = divided(r0, a.by_G), j_last = min(divided(r0 + kRows - 1, a.by_G), s.n - 1);
         const int end = s.pos0 + j_last + 1, all_end = s.pos0 + j_first + 1;  // all_end: every row sees what is before it,
         const int begin = a.window ? max(0, s.pos0 + j_first + 1 - a.window) & ~(kStep - 1) : 0;
-        const int all_begin = a.window ? s.pos0 + j_last + 1 - a.window : 0;  // and from here on
+        int all_begin = a.window ? s.pos0 + j_last + 1 - a.window : 0;  // and from here on
         // Without a window the first pages are looked up before the length is there: no length puts them past the table.
         const int64_t share = (int64_t)begin + (int64_t)split * a.split_tokens;
         const int from = (int)min(share, (int64_t)(a.b.pitch << c.page_shift));
@@ -484,18 +493,28 @@ __global__ __launch_bounds__(64 * attend_waves(kBlocks), attend_occupancy(NG, kB
             float f = fabsf(a.scale) * kLog2e4;
             uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;  // a negative scale goes into the queries' signs
             asm volatile("" : "+s"(flip));
-            if (kBf16) {
-                // A power of two brings the row's largest magnitude to 2^14 .. 2^15, where fp16 has all its bits down to 2^-28 of it.
-                uint32_t top = 0;
+            typedef unsigned short us2 __attribute__((ext_vector_type(2)));
+            us2 tops = {0, 0};
+#pragma unroll
+            for (int w = 0; w < NG; ++w)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    tops = __builtin_elementwise_max(tops, __builtin_bit_cast(us2, bits[w][e] & 0x7fff7fffu));
+            uint32_t top = max((uint32_t)tops[0], (uint32_t)tops[1]);
+            top = column_max(top);
+            // A query that holds an infinity or a NaN has no scores: its sums are formed of zeros, and what it gives is NaN.
+            const bool lost = top >= (kBf16 ? 0x7f80u : 0x7c00u);
+            if (lost) {
+                top = 0;
 #pragma unroll
                 for (int w = 0; w < NG; ++w)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        top = max(top, max(bits[w][e] & 0x7fffu, bits[w][e] >> 16 & 0x7fffu));
-                top = max(top, (uint32_t)__shfl_xor((int)top, 16));
-                top = max(top, (uint32_t)__shfl_xor((int)top, 32));
+                    bits[w] = uint4v{0u, 0u, 0u, 0u};
+            }
+            if (kBf16) {
+                // A power of two brings the row's largest magnitude to 2^14 .. 2^15, where fp16 has all its bits down to 2^-28 of it.
                 const int up = 141 - (int)(top >> 7);
                 f = ldexpf(f, -up);
+                top = 0x7800u;  // as fp16 from here on
 #pragma unroll
                 for (int w = 0; w < NG; ++w)
 #pragma unroll
@@ -512,8 +531,12 @@ __global__ __launch_bounds__(64 * attend_waves(kBlocks), attend_occupancy(NG, kB
                 queries[(wave * NG + w) * 64 + lane] = __builtin_bit_cast(half8_t, x);
             }
             if (quarter == 0) {
-                // Products stay below 2^40: with a factor this small they all become 0, but minus infinity stays what it is.
-                factor[16 * wave + col] = fmaxf(f, 0x1p-120f);
+                // Products stay below 2^40: with a factor as small as the first they all become 0, but minus infinity stays what it is.
+                f = fminf(fmaxf(f, 0x1p-120f), kMost4);
+                // A fused product differs from the rounded one in a reference by up to half a last place, and where exponents pass 2^27 weights
+                // would pass 2^15.  A row that can come there, with keys below 2^16, has the same rounded product in both: its factor is marked.
+                factor[16 * wave + col] = f * (float)__builtin_bit_cast(_Float16, (uint16_t)top) > 2048.f / (32 * NG) ? -f : f;
+                row_at_lds[16 * wave + col] = lost;
                 position[16 * wave + col] = there ? s.pos0 + query_j : -0x7fffffff;
             }
         }
@@ -522,6 +545,16 @@ __global__ __launch_bounds__(64 * attend_waves(kBlocks), attend_occupancy(NG, kB
 #pragma unroll
         for (int nb = 0; nb < kBlocks; ++nb)
             scale[nb] = factor[16 * nb + col];
+        bool far = false;
+#pragma unroll
+        for (int nb = 0; nb < kBlocks; ++nb)
+            far |= scale[nb] < 0.f;
+        if (__any(far)) {
+            all_begin = kFarOnly;  // no step is without a look at its products
+#pragma unroll
+            for (int nb = 0; nb < kBlocks; ++nb)
+                scale[nb] = 1.f;
+        }
 
         f4 o[kChannels][kBlocks];
         float ref[kBlocks], sum[kBlocks];
@@ -564,8 +597,19 @@ __global__ __launch_bounds__(64 * attend_waves(kBlocks), attend_occupancy(NG, kB
 #pragma unroll
             for (int i = 0; i < 2; ++i)
                 load_k(ks[i], tiles[i], places);
-            // ---- unseen tokens
+            // ---- unseen tokens, and products that are rounded
             if (token + kStep > all_end || token < all_begin || bad_now[0] || bad_now[1]) {
+                if (all_begin == kFarOnly) {
+#pragma unroll
+                    for (int nb = 0; nb < kBlocks; ++nb) {
+                        const float f = fabsf(factor[16 * nb + col]);
+#pragma unroll
+                        for (int i = 0; i < 2; ++i)
+#pragma unroll
+                            for (int r = 0; r < 4; ++r)
+                                x[i][nb][r] = fminf(x[i][nb][r] * f, kMost4);
+                    }
+                }
 #pragma unroll
                 for (int nb = 0; nb < kBlocks; ++nb) {
                     const int pos = position[16 * nb + col], low = a.window ? max(pos, -1) + 1 - a.window : 0;
@@ -688,22 +732,25 @@ __global__ __launch_bounds__(64 * attend_waves(kBlocks), attend_occupancy(NG, kB
                 f[w] = __builtin_amdgcn_exp2f(part[w].x - m);
                 l = fmaf(part[w].y, f[w], l);
             }
+            uint32_t nan = 0x7fc00000u;
+            asm volatile("" : "+v"(nan));  // its bits: the compiler is told that no float is one
+            const bool none = row_at_lds[thread] != 0 && l > 0.f;  // of a query without scores
             const int r = r0 + thread, j = divided(r, a.by_G), in_head = h * a.G + (r - j * a.G);
             const int64_t row_at = (int64_t)(s.first_row + j) * n_heads + in_head;
             int64_t at = -1;
             if (r < n_rows) {
                 if (a.n_splits > 1) {
                     const int64_t part_at = row_at * a.n_splits + split;
-                    *reinterpret_cast<float2 *>(a.part_ml + 2 * part_at) = make_float2(m, l);
+                    *reinterpret_cast<float2 *>(a.part_ml + 2 * part_at) = make_float2(m, none ? -1.f : l);
                     at = l > 0.f ? part_at * (32 * NG) : -1;
                 } else {
                     const float inverse = l > 0.f ? 1.f / l : 0.f;
 #pragma unroll
                     for (int w = 0; w < kWaves; ++w)
-                        f[w] *= inverse;
+                        f[w] = __uint_as_float(none ? nan : __float_as_uint(f[w] * inverse));
                     at = (int64_t)(s.first_row + j) * a.out.row + (int64_t)in_head * a.out.head;
                     if (a.lse)
-                        a.lse[row_at] = lse_of(m, l);
+                        reinterpret_cast<uint32_t *>(a.lse)[row_at] = none ? nan : __float_as_uint(lse_of(m, l));
                 }
             }
 #pragma unroll
@@ -820,6 +867,13 @@ __global__ __launch_bounds__(kMergeThreads) void k_cache4_merge(Cache4Attend a)
         for (int i = 0; i < kAhead; ++i)
             y[i] = load(mine + i * kAtOnce);
         float m = kNothing, l = 0.f, f[kMls];
+        bool none = false;
+#pragma unroll
+        for (int i = 0; i < kMls; ++i)
+            none |= z[i].y < 0.f;  // a query without scores
+        none = __any(none);
+        uint32_t nan = 0x7fc00000u;
+        asm volatile("" : "+v"(nan));
 #pragma unroll
         for (int i = 0; i < kMls; ++i)
             m = fmaxf(m, lane + 64 * i < a.n_splits && z[i].y > 0.f ? z[i].x : kNothing);
@@ -858,10 +912,12 @@ __global__ __launch_bounds__(kMergeThreads) void k_cache4_merge(Cache4Attend a)
             for (int i = 1; i < kAtOnce; ++i)
                 total += partial[i][tid];
             const float inverse = l > 0.f ? 1.f / l : 0.f;
-            store_four<kBf16>(a.out.data + (int64_t)row * a.out.row + (int64_t)head * a.out.head + 4 * tid, total * f4{inverse, inverse, inverse, inverse},
-                              a.c.D - 4 * tid);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                total[e] = __uint_as_float(none ? nan : __float_as_uint(total[e] * inverse));
+            store_four<kBf16>(a.out.data + (int64_t)row * a.out.row + (int64_t)head * a.out.head + 4 * tid, total, a.c.D - 4 * tid);
             if (a.lse && tid == 0)
-                a.lse[row_at] = lse_of(m, l);
+                reinterpret_cast<uint32_t *>(a.lse)[row_at] = none ? nan : __float_as_uint(lse_of(m, l));
         }
         __syncthreads();
     }

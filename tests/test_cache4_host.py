@@ -110,7 +110,7 @@ def test_read_refuses_one_place_for_both(lib):
 
 @pytest.mark.parametrize("want,kw", [
     (INVALID, dict(heads=0)), (INVALID, dict(heads=6)), (INVALID, dict(heads=-4)), (UNSUPPORTED, dict(heads=65536)), (INVALID, dict(window=-1)),
-    (INVALID, dict(scale=float("nan"))), (INVALID, dict(scale=float("inf"))), (INVALID, dict(lse=P + 2)), (INVALID, dict(ws=P + 128)),
+    (INVALID, dict(scale=float("nan"))), (INVALID, dict(scale=float("inf"))), (UNSUPPORTED, dict(scale=-2.0 ** 101)), (INVALID, dict(lse=P + 2)), (INVALID, dict(ws=P + 128)),
     (INVALID, dict(ws=None)), (SMALL, dict(ws_bytes=100)), (UNSUPPORTED, dict(n_rows=1 << 29)),
 ])
 def test_attend_refuses(lib, want, kw):

@@ -352,6 +352,75 @@ def test_attend_rising_scores():
         assert (np.abs(_np(out) - o) <= tol).all() and (np.abs(_np(lse) - l) <= tol_l).all()
 
 
+@pytest.mark.parametrize("fmt", FMT)
+@pytest.mark.parametrize("dtype,size", [(F16, 2.0 ** -6), (F16, 60000.0), (BF16, 2.0 ** -6), (BF16, 2.0 ** 90), (BF16, 2.0 ** 127)])
+@pytest.mark.parametrize("scale", [2.0 ** 24, -1.0, 2.0 ** 60, 2.0 ** 100])
+def test_scores_of_any_size(fmt, dtype, size, scale):
+    """A token whose score is far above the others' has all the weight, two that tie have halves, whatever the scores are."""
+    w = World(43, fmt, 1, 64, 16, 2, 40)
+    n = 600
+    k = torch.zeros(2 * n, 1, 64, dtype=dtype, device=DEV)
+    k[:, 0, 0] = -4 if scale < 0 else 4
+    k[torch.arange(0, 2 * n, 3), 0, 0] = -1
+    for token in (99, n + 7, n + 599):
+        k[token, 0, 0] = -6 if scale < 0 else 6
+    v = w.values(2 * n, dtype)
+    hq.hqmq_cache4_write(w.params, w.cache, w.batch([n, n], [n, n]), k, v)
+    w.write_plain([n, n], [n, n], k, v)
+    q = torch.zeros(4, 3, 64, dtype=dtype, device=DEV)
+    q[:, :, 0] = size
+    q[0, 1, 0], q[3, 1, 0] = 0.5, 0.25
+    for hint in (600, 1):  # split or not
+        batch = w.batch([n, n], [1, 3], max_length=hint)
+        out, lse = torch.empty_like(q), torch.empty(4, 3, device=DEV)
+        ws = torch.empty(1 << 22, dtype=torch.uint8, device=DEV)
+        hq.hqmq_cache4_attend(w.params, w.cache, batch, q, scale, out, ws, lse=lse)
+        got, got_lse = _np(out), _np(lse)
+        for row, (seq, tokens) in enumerate([(0, [99]), (1, [7]), (1, [7]), (1, [7, 599])]):
+            vv, _ = w.plain.sequence(1, w.table[seq], n)
+            kk, _ = w.plain.sequence(0, w.table[seq], n)
+            want = vv[tokens, 0].mean(0)
+            for head in range(3):
+                x = float(q[row, head, 0])
+                s = float(np.float32(scale)) * x * kk[tokens[0], 0, 0]
+                gap = s - float(np.float32(scale)) * x * kk[300 if seq else 100, 0, 0]
+                assert np.isfinite(got[row, head]).all()
+                if abs(gap) < 200 or max(abs(s), abs(float(np.float32(scale)) * x)) > 2.0 ** 126:  # others have weight as well
+                    continue
+                # 2^-20: sums of two weights, their reciprocal and what rounding the values leaves
+                assert (np.abs(got[row, head] - want) <= np.abs(want) * (HALF[dtype] + 2.0 ** -20) + 2.0 ** -25).all(), (row, head)
+                assert abs(got_lse[row, head] - s) <= abs(s) * 2.0 ** -21 + 1, (row, head)
+
+
+@pytest.mark.parametrize("fmt", FMT)
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("rows,hint", [(1, 600), (1, 1), (9, 600), (40, 1)])
+def test_queries_that_are_not_finite(fmt, dtype, rows, hint):
+    """They give NaN where they see a token, zeros where they see none, and nothing to other rows."""
+    w = World(44, fmt, 2, 64, 16, 3, 40)
+    lengths = [600, 300, 0]
+    w.fill_random(lengths, dtype)
+    q = w.values(3 * rows, dtype, heads=6)
+    batch = w.batch(lengths, [rows] * 3, max_length=hint)
+    ws = torch.full((1 << 24,), 0xFF, dtype=torch.uint8, device=DEV)
+    results = []
+    lost = torch.zeros(3 * rows, 6, dtype=torch.bool)
+    for turn in range(2):
+        out, lse = torch.empty_like(q), torch.empty(3 * rows, 6, device=DEV)
+        hq.hqmq_cache4_attend(w.params, w.cache, batch, q, 0.125, out, ws, lse=lse)
+        results.append((out.cpu(), lse.cpu()))
+        if turn == 0:
+            for row in range(0, 3 * rows, 2 if rows > 1 else 1):
+                value = [float("nan"), float("inf"), -float("inf")][row % 3]
+                q[row, row % 6, (7 * row) % 64] = value
+                lost[row, row % 6] = True
+    (a, la), (b, lb) = results
+    empty = torch.arange(3 * rows)[:, None].expand(-1, 6) >= 2 * rows
+    assert torch.equal(a[~lost], b[~lost]) and torch.equal(la[~lost], lb[~lost])
+    assert b[lost & ~empty].isnan().all() and lb[lost & ~empty].isnan().all()
+    assert (b[empty] == 0).all() and (lb[empty] == -float("inf")).all()
+
+
 def test_steps_together():
     """As a server runs them: prompts written in chunks and attended to, then token by token with drafts taken back; every step's
     attention and the cache's bytes the same as the plain form's."""
