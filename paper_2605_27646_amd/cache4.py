@@ -102,6 +102,10 @@ def alloc_cache4(params: Cache4Params, device) -> Cache4Buffers:
     return Cache4Buffers(*(torch.empty(n, dtype=torch.uint8, device=device) for n in (codes, scales, codes, scales)))
 
 
+def _count(n: int) -> int:  # an argument of 32 bits: what is larger means the same as 2^30
+    return max(-1, min(n, 2 ** 30))
+
+
 class Cache4Batch:
     """Which rows a call has and where their tokens lie: block_table (int32 [n_seqs, pages_per_seq]), lengths (int32 [n_seqs], the
     call's rows included), starts (int32 [n_seqs + 1], ascending; None: equal shares).  max_rows and max_length: the largest as
@@ -113,6 +117,8 @@ class Cache4Batch:
         if block_table.dim() != 2:
             raise ValueError("block_table must be [n_seqs, pages_per_seq]")
         n, pages = block_table.shape
+        if (n | pages) >> 31:
+            raise ValueError("block_table must have less than 2^31 rows and columns")
         _rows_of("block_table", block_table, torch.int32, (n, pages))
         _rows_of("lengths", lengths, torch.int32, (n,))
         if starts is not None:
@@ -121,7 +127,7 @@ class Cache4Batch:
         self._device = block_table.get_device()
         if any(t is not None and t.get_device() != self._device for t in self._tensors):
             raise ValueError("block_table, lengths and starts must be on one device")
-        self.struct = _Batch(n, pages, 2 ** 30 if max_rows is None else int(max_rows), 2 ** 30 if max_length is None else int(max_length),
+        self.struct = _Batch(n, pages, 2 ** 30 if max_rows is None else _count(int(max_rows)), 2 ** 30 if max_length is None else _count(int(max_length)),
                              block_table.data_ptr(), lengths.data_ptr(), None if starts is None else starts.data_ptr())
         self._argument = C.byref(self.struct)
 
@@ -134,6 +140,8 @@ def _rows(name: str, x: torch.Tensor, D: int) -> tuple:
     shape, stride, code = x.shape, x.stride(), _TYPES.get(x.dtype)
     if code is None or len(shape) != 3 or shape[2] != D or (stride[2] != 1 and D > 1 and x.numel()):
         raise ValueError(f"{name} must be fp16 or bf16 [n_rows, heads, {D}] with contiguous channels")
+    if (shape[0] | shape[1]) >> 31:  # a count that a 32-bit argument would lose bits of
+        raise ValueError(f"{name} must have less than 2^31 rows and heads")
     return C.byref(_Rows(x.data_ptr(), stride[0], stride[1])), shape, code
 
 
@@ -165,7 +173,7 @@ def hqmq_cache4_read(params: Cache4Params, cache: Cache4Buffers, batch: Cache4Ba
 
 
 def hqmq_cache4_attend_workspace_bytes(params: Cache4Params, batch: Cache4Batch, n_rows: int, n_q_heads: int, window: int = 0) -> int:
-    return int(_load().hqmq_cache4_attend_workspace_bytes(C.byref(params), C.byref(batch.struct), int(n_rows), int(n_q_heads), int(window)))
+    return int(_load().hqmq_cache4_attend_workspace_bytes(C.byref(params), C.byref(batch.struct), int(n_rows), int(n_q_heads), _count(window)))
 
 
 def hqmq_cache4_attend(params: Cache4Params, cache: Cache4Buffers, batch: Cache4Batch, q: torch.Tensor, scale: float, out: torch.Tensor,
@@ -184,7 +192,7 @@ def hqmq_cache4_attend(params: Cache4Params, cache: Cache4Buffers, batch: Cache4
     if (not (device == batch._device == q.get_device() == out.get_device() == torch.cuda.current_device())
             or (lse is not None and lse.get_device() != device) or (workspace is not None and workspace.get_device() != device)):
         raise ValueError(_ELSEWHERE)
-    rc = (_lib or _load()).hqmq_cache4_attend(params, buffers, batch._argument, shape[0], shape[1], code, q_rows, scale, window, out_rows,
+    rc = (_lib or _load()).hqmq_cache4_attend(params, buffers, batch._argument, shape[0], shape[1], code, q_rows, scale, _count(window), out_rows,
                                               None if lse is None else lse.data_ptr(), None if workspace is None else workspace.data_ptr(),
                                               0 if workspace is None else workspace.nbytes, _stream(stream, device))
     if rc:

@@ -165,6 +165,20 @@ def test_binding_refuses_shapes(lib):
             hq.hqmq_cache4_write(params, short, batch, k, k.clone())
 
 
+def test_binding_counts_of_more_than_32_bits(lib):
+    table, lengths = torch.zeros(1, 4096, dtype=torch.int32), torch.zeros(1, dtype=torch.int32)
+    params = _params(n_pages=4096, H=8)
+    bytes_of = lambda window=0, **hints: hq.hqmq_cache4_attend_workspace_bytes(params, hq.Cache4Batch(table, lengths, **hints), 1, 32, window=window)
+    assert bytes_of(window=2 ** 32 + 1) == bytes_of(window=2 ** 30) and bytes_of(max_rows=2 ** 32 + 1, max_length=2 ** 32 + 1) == bytes_of() > 0
+    assert bytes_of(window=-2 ** 32) == 0
+    cache, batch = hq.alloc_cache4(_params(), "cpu"), hq.Cache4Batch(table, lengths)
+    for many in (torch.zeros(1, 4, 128, dtype=torch.float16).expand(2 ** 32 + 1, 4, 128), torch.zeros(1, 1, 128, dtype=torch.float16).expand(1, 2 ** 32 + 4, 128)):
+        with pytest.raises(ValueError, match="2.31"):
+            hq.hqmq_cache4_write(_params(), cache, batch, many, many)
+        with pytest.raises(ValueError, match="2.31"):
+            hq.hqmq_cache4_attend(_params(), cache, batch, many, 1.0, many)
+
+
 PLACES = """
 #include <cstdio>
 #include <initializer_list>
