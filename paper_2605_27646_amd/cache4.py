@@ -4,6 +4,7 @@ from __future__ import annotations
 
 import ctypes as C
 import functools
+import struct
 
 import torch
 
@@ -34,6 +35,10 @@ class _Rows(C.Structure):
     _fields_ = [("data", C.c_void_p), ("stride_row", C.c_int64), ("stride_head", C.c_int64)]
 
 
+# The calls get their structs as bytes or addresses: objects of ctypes and the checks of their types are a fifth of a call's time here.
+_pack_rows, _pack_buffers = struct.Struct("@Pqq").pack, struct.Struct("@4P").pack
+
+
 _lib = None
 
 
@@ -41,15 +46,15 @@ def _load():
     global _lib
     if _lib is None:
         lib = binding._load()
-        P, B, S, R = C.POINTER(Cache4Params), C.POINTER(_Buffers), C.POINTER(_Batch), C.POINTER(_Rows)
+        P, S = C.POINTER(Cache4Params), C.POINTER(_Batch)
         I, V, U = C.c_int32, C.c_void_p, C.c_uint64
         lib.hqmq_cache4_sizes.restype = I
         lib.hqmq_cache4_sizes.argtypes = [P, C.POINTER(U), C.POINTER(U)]
         for name in ("hqmq_cache4_write", "hqmq_cache4_read"):
             getattr(lib, name).restype = I
-            getattr(lib, name).argtypes = [P, B, S, I, I, R, R, V]
+            getattr(lib, name).argtypes = [V, V, V, I, I, V, V, V]
         lib.hqmq_cache4_attend.restype = I
-        lib.hqmq_cache4_attend.argtypes = [P, B, S, I, I, I, R, C.c_float, I, R, V, V, U, V]
+        lib.hqmq_cache4_attend.argtypes = [V, V, V, I, I, I, V, C.c_float, I, V, V, V, U, V]
         lib.hqmq_cache4_attend_workspace_bytes.restype = U
         lib.hqmq_cache4_attend_workspace_bytes.argtypes = [P, S, I, I, I]
         _lib = lib
@@ -92,7 +97,7 @@ class Cache4Buffers:
             device = self.k_codes.get_device()
             if any(t.get_device() != device for t, _ in tensors):
                 raise ValueError("the cache's tensors must be on one device")
-            held = (key, (C.byref(self.as_struct()), device))
+            held = (key, (key, _pack_buffers(*(t.data_ptr() for t in (self.k_codes, self.k_scales, self.v_codes, self.v_scales))), device))
             object.__setattr__(self, "_held", held)
         return held[1]
 
@@ -129,7 +134,7 @@ class Cache4Batch:
             raise ValueError("block_table, lengths and starts must be on one device")
         self.struct = _Batch(n, pages, 2 ** 30 if max_rows is None else _count(int(max_rows)), 2 ** 30 if max_length is None else _count(int(max_length)),
                              block_table.data_ptr(), lengths.data_ptr(), None if starts is None else starts.data_ptr())
-        self._argument = C.byref(self.struct)
+        self._argument = C.addressof(self.struct)
 
 
 _ELSEWHERE = "every tensor must be on torch's current device"
@@ -142,7 +147,7 @@ def _rows(name: str, x: torch.Tensor, D: int) -> tuple:
         raise ValueError(f"{name} must be fp16 or bf16 [n_rows, heads, {D}] with contiguous channels")
     if (shape[0] | shape[1]) >> 31:  # a count that a 32-bit argument would lose bits of
         raise ValueError(f"{name} must have less than 2^31 rows and heads")
-    return C.byref(_Rows(x.data_ptr(), stride[0], stride[1])), shape, code
+    return _pack_rows(x.data_ptr(), stride[0], stride[1]), shape, code
 
 
 def _stream(stream, device: int) -> int:
@@ -154,7 +159,7 @@ def _move(name, params, cache, batch, k, v, stream) -> None:
     v_rows, v_shape, v_code = _rows("v", v, params.D)
     if shape[1] != params.H or v_shape != shape or v_code != code:
         raise ValueError(f"k and v must be of one type, [n_rows, {params.H}, {params.D}] both")
-    buffers, device = cache._argument(params)
+    params, buffers, device = cache._argument(params)
     if not (device == batch._device == k.get_device() == v.get_device() == torch.cuda.current_device()):
         raise ValueError(_ELSEWHERE)
     rc = getattr(_lib or _load(), name)(params, buffers, batch._argument, shape[0], code, k_rows, v_rows, _stream(stream, device))
@@ -188,7 +193,7 @@ def hqmq_cache4_attend(params: Cache4Params, cache: Cache4Buffers, batch: Cache4
         _rows_of("lse", lse, torch.float32, shape[:2])
     if workspace is not None and not workspace.is_contiguous():
         raise ValueError("workspace must be contiguous")
-    buffers, device = cache._argument(params)
+    params, buffers, device = cache._argument(params)
     if (not (device == batch._device == q.get_device() == out.get_device() == torch.cuda.current_device())
             or (lse is not None and lse.get_device() != device) or (workspace is not None and workspace.get_device() != device)):
         raise ValueError(_ELSEWHERE)
