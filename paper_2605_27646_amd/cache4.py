@@ -137,6 +137,7 @@ class Cache4Batch:
         self._argument = C.addressof(self.struct)
 
 
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device  # without asking whether the runtime is up
 _ELSEWHERE = "every tensor must be on torch's current device"
 
 
@@ -160,7 +161,7 @@ def _move(name, params, cache, batch, k, v, stream) -> None:
     if shape[1] != params.H or v_shape != shape or v_code != code:
         raise ValueError(f"k and v must be of one type, [n_rows, {params.H}, {params.D}] both")
     params, buffers, device = cache._argument(params)
-    if not (device == batch._device == k.get_device() == v.get_device() == torch.cuda.current_device()):
+    if not (device == batch._device == k.get_device() == v.get_device() == _current_device()):
         raise ValueError(_ELSEWHERE)
     rc = getattr(_lib or _load(), name)(params, buffers, batch._argument, shape[0], code, k_rows, v_rows, _stream(stream, device))
     if rc:
@@ -194,7 +195,7 @@ def hqmq_cache4_attend(params: Cache4Params, cache: Cache4Buffers, batch: Cache4
     if workspace is not None and not workspace.is_contiguous():
         raise ValueError("workspace must be contiguous")
     params, buffers, device = cache._argument(params)
-    if (not (device == batch._device == q.get_device() == out.get_device() == torch.cuda.current_device())
+    if (not (device == batch._device == q.get_device() == out.get_device() == _current_device())
             or (lse is not None and lse.get_device() != device) or (workspace is not None and workspace.get_device() != device)):
         raise ValueError(_ELSEWHERE)
     rc = (_lib or _load()).hqmq_cache4_attend(params, buffers, batch._argument, shape[0], shape[1], code, q_rows, scale, _count(window), out_rows,

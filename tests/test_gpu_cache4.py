@@ -492,6 +492,70 @@ def test_no_rows():
     w.same_bytes()
 
 
+def test_tensors_elsewhere_are_refused():
+    """Each tensor of the three calls in turn in host memory."""
+    w = World(79, hq.HQMQ_CACHE4_FLOAT, 2, 64, 16, 2, 40)
+    here = w.batch([600, 500])
+    host = hq.Cache4Batch(*(t.cpu() for t in here._tensors[:2]))
+    k, q = w.values(2, F16), w.values(2, F16)
+    args = dict(cache=w.cache, batch=here, k=k, v=k.clone(), q=q, out=torch.empty_like(q), ws=torch.empty(1 << 22, dtype=torch.uint8, device=DEV),
+                lse=torch.empty(2, 2, device=DEV))
+    elsewhere = {name: x.cpu() for name, x in args.items() if isinstance(x, torch.Tensor)}
+    elsewhere.update(batch=host, cache=hq.alloc_cache4(w.params, "cpu"))
+    for name, x in elsewhere.items():
+        a = dict(args, **{name: x})
+        if name not in ("q", "out", "ws", "lse"):
+            for call in (hq.hqmq_cache4_write, hq.hqmq_cache4_read):
+                with pytest.raises(ValueError, match="current device"):
+                    call(w.params, a["cache"], a["batch"], a["k"], a["v"])
+        if name not in ("k", "v"):
+            with pytest.raises(ValueError, match="current device"):
+                hq.hqmq_cache4_attend(w.params, a["cache"], a["batch"], a["q"], 0.1, a["out"], a["ws"], lse=a["lse"])
+    mixed = hq.alloc_cache4(w.params, DEV)
+    mixed.v_scales = mixed.v_scales.cpu()
+    with pytest.raises(ValueError, match="one device"):
+        hq.hqmq_cache4_write(w.params, mixed, here, k, k.clone())
+    with pytest.raises(ValueError, match="one device"):
+        hq.Cache4Batch(here._tensors[0], here._tensors[1].cpu())
+
+
+def test_buffers_set_anew():
+    """Calls follow a Cache4Buffers whose tensors are replaced, and other params of the same buffers."""
+    w, other = World(80, hq.HQMQ_CACHE4_FLOAT, 2, 64, 16, 1, 4), World(81, hq.HQMQ_CACHE4_FLOAT, 2, 64, 16, 1, 4)
+    k, v = w.values(20, F16), w.values(20, F16)
+    hq.hqmq_cache4_write(w.params, w.cache, w.batch([20], [20]), k, v)
+    w.write_plain([20], [20], k, v)
+    for name in ("k_codes", "k_scales", "v_codes", "v_scales"):
+        setattr(w.cache, name, getattr(other.cache, name))
+    k, v = w.values(30, F16), w.values(30, F16)
+    hq.hqmq_cache4_write(other.params, w.cache, other.batch([30], [30]), k, v)
+    other.write_plain([30], [30], k, v)
+    w.same_bytes()
+    other.same_bytes()
+    small = hq.Cache4Params(other.params.n_pages, 16, 1, 64, hq.HQMQ_CACHE4_FLOAT)  # half the heads
+    one = World(82, hq.HQMQ_CACHE4_FLOAT, 1, 64, 16, 1, 4)
+    other.cache.k_codes.fill_(0xFF), other.cache.k_scales.fill_(0xFF), other.cache.v_codes.fill_(0xFF), other.cache.v_scales.fill_(0xFF)
+    k, v = one.values(9, BF16), one.values(9, BF16)
+    hq.hqmq_cache4_write(small, w.cache, one.batch([9], [9]), k, v)
+    one.write_plain([9], [9], k, v)
+    one.buffers = tuple(t[:t.numel() // 2] for t in other.buffers)
+    one.same_bytes()
+
+
+def test_expanded_rows_are_read():
+    """One row for all tokens, one head for all heads: strides of 0."""
+    w = World(83, hq.HQMQ_CACHE4_INT, 4, 96, 16, 2, 4)
+    k = w.values(1, F16, heads=1).expand(50, 4, 96)
+    v = w.values(50, F16, heads=1).expand(50, 4, 96)
+    hq.hqmq_cache4_write(w.params, w.cache, w.batch([27, 23], [27, 23]), k, v)
+    w.write_plain([27, 23], [27, 23], k, v)
+    w.same_bytes()
+    with pytest.raises(hq.HqmqError):  # but not written
+        hq.hqmq_cache4_read(w.params, w.cache, w.batch([27, 23], [27, 23]), k, v)
+    with pytest.raises(hq.HqmqError):
+        hq.hqmq_cache4_attend(w.params, w.cache, w.batch([27, 23], [27, 23]), v, 0.1, v, torch.empty(1 << 20, dtype=torch.uint8, device=DEV))
+
+
 def test_an_error_that_another_call_left():
     """A failed HIP call before ours is not reported as ours."""
     from paper_2605_27646_amd import binding
