@@ -81,8 +81,7 @@ typedef struct hqmq_cache4_batch {
 } hqmq_cache4_batch;
 
 /* Rows [n_rows][heads][D] with element strides, channels contiguous: HOST struct of a DEVICE pointer, aligned to 2 bytes.
- * Any alignment of 2 bytes does: rows are moved 8 channels at a time, the last D % 8 one by one (as are all of q's where D
- * is no multiple of 8). */
+ * Any alignment of 2 bytes does: rows are moved 8 channels at a time, at any address. */
 typedef struct hqmq_cache4_rows {
     void *data;
     int64_t stride_row, stride_head;

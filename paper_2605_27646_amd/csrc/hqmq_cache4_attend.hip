@@ -462,20 +462,22 @@ __global__ __launch_bounds__(64 * attend_waves(kBlocks), attend_occupancy(NG, kB
             const uint16_t *src = a.q.data + (int64_t)(s.first_row + query_j) * a.q.row + (int64_t)(h * a.G + (query - query_j * a.G)) * a.q.head;
             int D = c.D;
             asm volatile("" : "+s"(D));  // what is compared with it is not kept in registers from tile to tile
-            if (D % 8 == 0) {
+            if (__builtin_expect(D % 8 == 0, 1)) {
 #pragma unroll
                 for (int w = 0; w < NG; ++w)
                     if (first_ch + 8 * w < D)
                         bits[w] = load8(src + (first_ch + 8 * w));
-            } else {  // element by element, through the lane's own places in LDS
-                uint16_t *const mine = reinterpret_cast<uint16_t *>(queries + wave * NG * 64 + lane);
-#pragma unroll 1
-                for (int e = 0; e < 8 * NG; ++e)
-                    mine[512 * (e >> 3) + (e & 7)] = first_ch + e < D ? src[first_ch + e] : (uint16_t)0;
-                asm volatile("" : : : "memory");
+            } else if (NG == 1 && D < 8) {
+                if (first_ch == 0)
+                    bits[0] = load_some(src, D);
+            } else {
 #pragma unroll
                 for (int w = 0; w < NG; ++w)
-                    bits[w] = *reinterpret_cast<const uint4v *>(mine + 512 * w);
+                    if (first_ch + 8 * w < D)
+                        bits[w] = load8(src + min(first_ch + 8 * w, D - 8));
+#pragma unroll
+                for (int w = 0; w < NG; ++w)
+                    bits[w] = first_ch + 8 * w > D - 8 && first_ch + 8 * w < D ? last_of(bits[w], D & 7) : bits[w];
             }
         }
         if (wave < n_steps) {
@@ -504,7 +506,7 @@ __global__ __launch_bounds__(64 * attend_waves(kBlocks), attend_occupancy(NG, kB
             top = column_max(top);
             // A query that holds an infinity or a NaN has no scores: its sums are formed of zeros, and what it gives is NaN.
             const bool lost = top >= (kBf16 ? 0x7f80u : 0x7c00u);
-            if (lost) {
+            if (__builtin_expect(lost, 0)) {
                 top = 0;
 #pragma unroll
                 for (int w = 0; w < NG; ++w)
@@ -549,7 +551,7 @@ __global__ __launch_bounds__(64 * attend_waves(kBlocks), attend_occupancy(NG, kB
 #pragma unroll
         for (int nb = 0; nb < kBlocks; ++nb)
             far |= scale[nb] < 0.f;
-        if (__any(far)) {
+        if (__builtin_expect(__any(far), 0)) {
             all_begin = kFarOnly;  // no step is without a look at its products
 #pragma unroll
             for (int nb = 0; nb < kBlocks; ++nb)
@@ -599,7 +601,7 @@ __global__ __launch_bounds__(64 * attend_waves(kBlocks), attend_occupancy(NG, kB
                 load_k(ks[i], tiles[i], places);
             // ---- unseen tokens, and products that are rounded
             if (token + kStep > all_end || token < all_begin || bad_now[0] || bad_now[1]) {
-                if (all_begin == kFarOnly) {
+                if (__builtin_expect(all_begin == kFarOnly, 0)) {
 #pragma unroll
                     for (int nb = 0; nb < kBlocks; ++nb) {
                         const float f = fabsf(factor[16 * nb + col]);
@@ -669,7 +671,7 @@ __global__ __launch_bounds__(64 * attend_waves(kBlocks), attend_occupancy(NG, kB
             }
             // ---- values: a token that none of the sequence's rows sees may hold anything
             const bool too_early = a.window && token < all_end - a.window;
-            if (token + kStep > s.length || too_early || bad_now[0] || bad_now[1]) {
+            if (__builtin_expect(token + kStep > s.length || too_early || bad_now[0] || bad_now[1], 0)) {
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     const int base = token + 16 * i + 4 * quarter;

@@ -38,6 +38,52 @@ struct __attribute__((packed, aligned(2))) Cache4Eight {
 __device__ __forceinline__ cache4_u4 load8(const uint16_t *p) { return reinterpret_cast<const Cache4Eight *>(p)->bits; }
 __device__ __forceinline__ void store8(uint16_t *p, cache4_u4 bits) { reinterpret_cast<Cache4Eight *>(p)->bits = bits; }
 
+// The last n of a head's channels, 1 .. 7 and the same for all lanes: in pieces of 4, 2 and 1, or, where 8 precede the head's end, these
+// without the first 8 - n of them (no lane waits for what another branch has loaded).
+struct __attribute__((packed, aligned(2))) Cache4Four {
+    uint64_t bits;
+};
+struct __attribute__((packed, aligned(2))) Cache4Two {
+    uint32_t bits;
+};
+__device__ __forceinline__ cache4_u4 load_some(const uint16_t *p, int n)
+{
+    uint64_t four = 0, rest = 0;
+    if (n & 4)
+        four = reinterpret_cast<const Cache4Four *>(p)->bits;
+    if (n & 1)
+        rest = (uint64_t)p[n - 1] << (16 * (n & 2));
+    if (n & 2)
+        rest |= reinterpret_cast<const Cache4Two *>(p + (n & 4))->bits;
+    const uint64_t low = n & 4 ? four : rest, high = n & 4 ? rest : 0;
+    return cache4_u4{(uint32_t)low, (uint32_t)(low >> 32), (uint32_t)high, (uint32_t)(high >> 32)};
+}
+__device__ __forceinline__ void store_some(uint16_t *p, cache4_u4 bits, int n)
+{
+    const uint64_t low = (uint64_t)bits[1] << 32 | bits[0];
+    uint64_t rest = low;
+    if (n & 4) {
+        reinterpret_cast<Cache4Four *>(p)->bits = low;
+        rest = (uint64_t)bits[3] << 32 | bits[2];
+    }
+    if (n & 2)
+        reinterpret_cast<Cache4Two *>(p + (n & 4))->bits = (uint32_t)rest;
+    if (n & 1)
+        p[n - 1] = (uint16_t)(rest >> (16 * (n & 2)));
+}
+__device__ __forceinline__ cache4_u4 last_of(cache4_u4 x, int n)
+{
+    const int back = 8 - n;
+    if (back & 4)
+        x = cache4_u4{x[2], x[3], 0u, 0u};
+    if (back & 2)
+        x = cache4_u4{x[1], x[2], x[3], 0u};
+    if (back & 1)
+        x = cache4_u4{__builtin_amdgcn_alignbit(x[1], x[0], 16), __builtin_amdgcn_alignbit(x[2], x[1], 16), __builtin_amdgcn_alignbit(x[3], x[2], 16),
+                      x[3] >> 16};
+    return x;
+}
+
 // Division of numbers below 2^30 by one that the host knows: with l = ceil(log2 d) and m = ceil(2^(30 + l) / d), which is at most 2^30 + 1,
 // n m / 2^(30 + l) exceeds n / d by less than 2^l / 2^(30 + l) * n < 1 / d, and so has the same whole part.
 struct Divisor {

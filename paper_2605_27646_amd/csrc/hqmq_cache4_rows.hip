@@ -204,7 +204,9 @@ __global__ __launch_bounds__(kRowThreads) void k_cache4_write(Cache4 c, Cache4Se
     uint8_t *const codes = u.is_v ? c.v_codes : c.k_codes;
     Scale *const scales = reinterpret_cast<Scale *>(u.is_v ? c.v_scales : c.k_scales);
     const int ch = 8 * u.w, row_bytes = 16 * c.NG, n_ch = min(max(c.D - ch, 0), 8);
-    const uint16_t *const src = rows.data + u.h * rows.head + ch;
+    const int tail = c.D & 7;
+    const bool short_head = c.D < 8, last = n_ch > 0 && n_ch < 8;
+    const uint16_t *const src = rows.data + u.h * rows.head + (last && !short_head ? c.D - 8 : ch);
     for (int block = (max(s.pos0, 0) >> 2) + turn; 4 * (int64_t)block < s.length && s.n > 0; block += flat.on ? kPastAll : (int)gridDim.x) {
         const int pos = 4 * block, first = max(s.pos0 - pos, 0), end = min(s.length - pos, 4);  // the block's tokens first .. end - 1
         const int page = page_of(c, b, seq, pos);
@@ -214,17 +216,18 @@ __global__ __launch_bounds__(kRowThreads) void k_cache4_write(Cache4 c, Cache4Se
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
             bits[t] = uint4v{0u, 0u, 0u, 0u};
-            if (t >= first && t < end && u.there && n_ch > 0) {
+            if (t >= first && t < end && u.there && n_ch > 0 && !short_head) {
                 const uint16_t *at = src + (int64_t)(s.first_row + (pos + t - s.pos0)) * rows.row;
-                if (n_ch == 8) {
-                    bits[t] = load8(at);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 7; ++e)
-                        if (e < n_ch)
-                            bits[t][e / 2] |= (uint32_t)at[e] << (16 * (e & 1));
-                }
+                bits[t] = load8(at);
             }
+        }
+        if (tail) {
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+                if (!short_head)
+                    bits[t] = last ? last_of(bits[t], tail) : bits[t];
+                else if (t >= first && t < end && u.there && n_ch > 0)
+                    bits[t] = load_some(src + (int64_t)(s.first_row + (pos + t - s.pos0)) * rows.row, tail);
         }
         uint4v code, scale;
 #pragma unroll
@@ -331,14 +334,10 @@ __global__ __launch_bounds__(kRowThreads) void k_cache4_read(Cache4 c, Cache4Seq
             if (page >= 0)
                 bits = values<kFormat, kBf16>(code[t], scale[t]);
             uint16_t *const at = dst + (int64_t)(s.first_row + (pos + t - s.pos0)) * rows.row;
-            if (ch + 8 <= c.D) {
+            if (ch + 8 <= c.D)
                 store8(at, bits);
-            } else {
-#pragma unroll
-                for (int e = 0; e < 7; ++e)
-                    if (ch + e < c.D)
-                        at[e] = (uint16_t)(bits[e / 2] >> (16 * (e & 1)));
-            }
+            else
+                store_some(at, bits, c.D & 7);
         }
     }
 }
