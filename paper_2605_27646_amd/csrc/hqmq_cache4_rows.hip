@@ -30,9 +30,33 @@ __device__ __forceinline__ float group_max(float x)
 template <bool kBf16>
 __device__ __forceinline__ float widened(uint32_t bits)
 {
-    bits = (bits & 0x7fffu) > (kBf16 ? 0x7f80u : 0x7c00u) ? 0u : bits;  // a NaN counts as 0
-    const float x = kBf16 ? __uint_as_float(bits << 16) : (float)__builtin_bit_cast(_Float16, (uint16_t)bits);
-    return __builtin_amdgcn_fmed3f(x, -49152.f, 49152.f);
+    return kBf16 ? __uint_as_float(bits << 16) : (float)__builtin_bit_cast(_Float16, (uint16_t)bits);
+}
+
+// The largest magnitude of 8 channels, as its bits.  NaN become 0 and what is larger than 49152 that, which is rare: found by integers, two
+// channels an instruction.
+template <bool kBf16>
+__device__ __forceinline__ uint32_t cleaned(uint4v &bits)
+{
+    typedef unsigned short us2 __attribute__((ext_vector_type(2)));
+    constexpr uint32_t kNan = kBf16 ? 0x7f80u : 0x7c00u, kMost = kBf16 ? 0x4740u : 0x7a00u;
+    const auto top_of = [&] {
+        us2 y = {0, 0};
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            y = __builtin_elementwise_max(y, __builtin_bit_cast(us2, bits[e] & 0x7fff7fffu));
+        return max((uint32_t)y[0], (uint32_t)y[1]);
+    };
+    uint32_t top = top_of();
+    if (__builtin_expect(top > kMost, 0)) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const auto clean = [&](uint32_t y) { return (y & 0x7fffu) > kNan ? 0u : (y & 0x8000u) | min(y & 0x7fffu, kMost); };
+            bits[e] = clean(bits[e] & 0xffffu) | clean(bits[e] >> 16) << 16;
+        }
+        top = top_of();
+    }
+    return top;
 }
 
 // What a thread works on: 8 channels of a kv head, the same for every block of positions that it goes through.
@@ -97,19 +121,16 @@ __device__ __forceinline__ uint4v separated(uint4v y, int bytes)
 template <int kFormat, bool kBf16>
 __device__ __forceinline__ uint2 quantised(uint4v bits, int n)  // n: how many of them there are, others are zeros
 {
+    const uint32_t top = cleaned<kBf16>(bits);
     float x[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e)
         x[e] = widened<kBf16>((bits[e / 2] >> (16 * (e & 1))) & 0xffffu);
     uint32_t code = 0;
     if (kFormat == HQMQ_CACHE4_FLOAT) {
-        float top = 0.f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            top = fmaxf(top, fabsf(x[e]));
-        top = group_max(top);
+        const float most = group_max(widened<kBf16>(top));
         // 7 / 4 has the fraction bits 0x600000: an exponent more for anything above
-        const int exponent = min(max((int)((__float_as_uint(top) + 0x1fffffu) >> 23) - 2, 127 - 23), 127 + 13);
+        const int exponent = min(max((int)((__float_as_uint(most) + 0x1fffffu) >> 23) - 2, 127 - 23), 127 + 13);
         const float unit = e8m0((uint32_t)exponent);
         code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x[0], x[1], unit, 0);
         code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x[2], x[3], unit, 1);
@@ -117,13 +138,21 @@ __device__ __forceinline__ uint2 quantised(uint4v bits, int n)  // n: how many o
         code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x[6], x[7], unit, 3);
         return make_uint2(code, (uint32_t)exponent);
     }
-    float high = -1.0e30f, low = 1.0e30f;
+    float high = x[0], low = x[0];
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-        if (e < n) {
-            high = fmaxf(high, x[e]);
-            low = fminf(low, x[e]);
-        }
+    for (int e = 1; e < 8; ++e) {
+        high = fmaxf(high, x[e]);
+        low = fminf(low, x[e]);
+    }
+    if (__builtin_expect(n < 8, 0)) {  // without the zeros past the head's last channel
+        high = -1.0e30f, low = 1.0e30f;
+#pragma unroll
+        for (int e = 0; e < 7; ++e)
+            if (e < n) {
+                high = fmaxf(high, x[e]);
+                low = fminf(low, x[e]);
+            }
+    }
     high = group_max(high);
     low = -group_max(-low);
     if (low > high)  // channels past the head's only
@@ -131,28 +160,31 @@ __device__ __forceinline__ uint2 quantised(uint4v bits, int n)  // n: how many o
     float fifteenth = (high - low) * (1.f / 15.f);
     asm("" : "+v"(fifteenth));  // rounded to fp32 before fp16: v_fma_mixlo_f16 would round the product once
     const _Float16 s16 = (_Float16)fifteenth, m16 = (_Float16)low;
-    const float step = (float)s16, least = (float)m16, inverse = step > 0.f ? 1.f / step : 0.f;
-    float r[8], near = 1.f;
+    const float step = (float)s16, least = (float)m16, inverse = step > 0.f ? __builtin_amdgcn_rcpf(step) : 0.f;
+    float r[8], far = 0.f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        const float q = (x[e] - least) * inverse;
+        const float q = __builtin_amdgcn_fmed3f((x[e] - least) * inverse, 0.f, 15.f);
         r[e] = rintf(q);
-        near = fminf(near, fabsf(fabsf(q - r[e]) - 0.5f));
+        far = fmaxf(far, fabsf(q - r[e]));
     }
-    // Three roundings put q up to 16 * 3 * 2^-24 off.  Next to the middle of two codes the exact difference d + rest from it decides:
-    // the middle has 5 bits and the step 11, and d is within a factor of two of their product.
-    if (near < 1.0e-5f) {
+    // Two roundings and a reciprocal that is good to one last place put q up to 16 * 4 * 2^-24 off.  Next to the middle of two codes the
+    // exact difference d + rest from it decides: the middle has 5 bits and the step 11, and d is within a factor of two of their product.
+    if (far > 0.5f - 1.0e-5f) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const float d = x[e] - least, back = d - x[e], rest = (x[e] - (d - back)) - (least + back);
             const float lower = floorf(d * inverse), over = (d - (lower + 0.5f) * step) + rest;
             const bool up = over > 0.f || (over == 0.f && ((int)lower & 1));
-            r[e] = step > 0.f ? lower + (up ? 1.f : 0.f) : 0.f;
+            r[e] = step > 0.f ? __builtin_amdgcn_fmed3f(lower + (up ? 1.f : 0.f), 0.f, 15.f) : 0.f;
         }
     }
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-        code |= (e < n ? (uint32_t)__builtin_amdgcn_fmed3f(r[e], 0.f, 15.f) : 0u) << (4 * e);
+    // four codes as one number, which fp32 holds, and both of these as integers
+    const float first = fmaf(4096.f, r[3], fmaf(256.f, r[2], fmaf(16.f, r[1], r[0])));
+    const float second = fmaf(4096.f, r[7], fmaf(256.f, r[6], fmaf(16.f, r[5], r[4])));
+    code = (uint32_t)second << 16 | (uint32_t)first;
+    if (__builtin_expect(n < 8, 0))
+        code &= (1u << (4 * max(n, 0))) - 1u;
     return make_uint2(code, __builtin_bit_cast(uint32_t, cache4_h2{s16, m16}));
 }
 
