@@ -11,10 +11,10 @@
 //                 tokens of the V layout, and product e takes channel e of every run.
 // A query's maximum and sum belong to one column, so every factor is one per lane.
 //
-// Bound by memory for generation steps of many long sequences (64 of up to 8192 tokens, 8 heads x 128: 68.5 us, 301 MB at 4.4 TB/s,
+// Bound by memory for generation steps of many long sequences (64 of up to 8192 tokens, 8 heads x 128: 69 to 73 us, 301 MB at 4.2 to 4.4 TB/s,
 // vector instructions issue for a third of the time), by a workgroup's start and the join for short ones (130 tokens 6 us, of which
-// one step is 1), and by issue for prompts (1024 tokens of two sequences behind 15000: 439 us, 1.19 PFLOP/s, vector instructions
-// 59 % and matrix instructions 41 % of the time; of the former 37 % are exponentials, 33 % the reconstruction for 64 rows).
+// one step is 1), and by issue for prompts (1024 tokens of two sequences behind 15000: 435 us, 1.20 PFLOP/s, vector instructions
+// 61 % and matrix instructions 42 % of the time; of the former 37 % are exponentials, 33 % the reconstruction for 64 rows).
 #include <algorithm>
 #include <type_traits>
 
