@@ -332,6 +332,35 @@ def test_attend_strides_and_groups(D, G, rows):
     _check_attend(w, lengths, [rows, 1, rows], F16, G, strided=True)
 
 
+@pytest.mark.parametrize("fmt", FMT)
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("D", [1, 2, 3, 4, 5, 6, 7, 9, 11, 31, 36, 63, 95, 125, 135, 190, 250, 255])
+def test_heads_that_end_anywhere(fmt, dtype, D):
+    """Every number of last channels, in every width: rows between others that are not read nor written, at odd addresses."""
+    w = World(D, fmt, 2, D, 16, 2, 3)
+    lengths, rows = [37, 18], [21, 18]
+    n = sum(rows)
+    wide = w.values(n + 2, dtype, heads=2 * (2 * D + 3))[:, :, 0].contiguous() * 1000  # [n + 2, 2 (2 D + 3)], channels beside the rows' own
+    k, v = ((wide[1:-1, 1 + i * D:] if i else wide[1:-1, 1:])[:, :2 * (D + 1)].unflatten(1, (2, D + 1))[:, :, :D] for i in range(2))
+    batch = w.batch(lengths, rows)
+    hq.hqmq_cache4_write(w.params, w.cache, batch, k, v)
+    w.write_plain(lengths, rows, k, v)
+    w.same_bytes()
+    back = [torch.full((n, 2, D + 3), 7.0, dtype=dtype, device=DEV) for _ in range(2)]
+    hq.hqmq_cache4_read(w.params, w.cache, batch, *(x[:, :, 1:D + 1] for x in back))
+    tight = [torch.empty(n, 2, D, dtype=dtype, device=DEV) for _ in range(2)]
+    hq.hqmq_cache4_read(w.params, w.cache, batch, *tight)
+    for role, (x, y) in enumerate(zip(back, tight)):
+        assert torch.equal(x[:, :, 1:D + 1], y) and (x[:, :, 0] == 7).all() and (x[:, :, D + 1:] == 7).all()
+        for i, (length, first) in enumerate(zip(lengths, (0, 21))):
+            z, there = w.plain.sequence(role, w.table[i], length)
+            z = torch.tensor(z[length - rows[i]:], dtype=torch.float64).to(dtype)
+            assert torch.equal(y[first:first + rows[i]].cpu(), z)
+    w = World(D + 1, fmt, 2, D, 16, 2, 3)
+    w.fill_random(lengths, dtype)
+    _check_attend(w, lengths, rows, dtype, 3, strided=True)
+
+
 def test_attend_rising_scores():
     """Keys whose scores grow along the sequence, so that the reference is renewed again and again."""
     w = World(41, hq.HQMQ_CACHE4_FLOAT, 1, 32, 16, 1, 64)
