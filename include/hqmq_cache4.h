@@ -68,7 +68,7 @@ typedef struct hqmq_cache4_buffers {
  *               starts[0] .. starts[n_seqs] - 1 are no sequence's: they are not read, nor written.
  *   max_rows, max_length   the largest number of rows and length of a sequence as far as the host knows them: they shape
  *               the launch and, through it, the order of sums; every row and token counts whatever they say.  max_rows is
- *               ignored where starts is NULL.
+ *               ignored where starts is NULL, and counts as n_rows / n_seqs, rounded up, where it is less.
  * A page number outside 0 .. n_pages - 1, and a position below 0 (more rows than tokens), are no tokens: write leaves
  * them out, read gives zeros, attend does not see them. */
 typedef struct hqmq_cache4_batch {

@@ -1370,9 +1370,12 @@ static Cache4Seqs make_cache4_seqs(const hqmq_cache4_batch *b, int32_t n_rows)
     return Cache4Seqs{b->block_table, b->lengths, b->starts, b->n_seqs, n_rows, b->pages_per_seq, n_rows / b->n_seqs};
 }
 
+// Rows of the largest sequence as far as the host knows: some one has the average at least.  A belief below it is no reason to cut a call for
+// fewer rows than there are (4096 rows of one sequence believed to be one: 32 parts of its tokens, 2 GiB of workspace, none this way).
 static int32_t cache4_most_rows(const hqmq_cache4_batch *b, int32_t n_rows)
 {
-    return std::max(1, b->starts ? std::min(b->max_rows, n_rows) : n_rows / b->n_seqs);
+    const int32_t average = (int32_t)(((int64_t)n_rows + b->n_seqs - 1) / b->n_seqs);
+    return std::max(1, b->starts ? std::min(std::max(b->max_rows, average), n_rows) : average);
 }
 
 static Cache4Rows make_cache4_rows(const hqmq_cache4_rows *r)

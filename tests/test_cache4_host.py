@@ -137,6 +137,24 @@ def test_attend_workspace(lib):
     assert hq.hqmq_cache4_attend_workspace_bytes(params, hq.Cache4Batch(table, lengths), 1, 32) == n
 
 
+@pytest.mark.parametrize("n_seqs,n_rows", [(1, 4096), (1, 100000), (3, 12000), (64, 4160), (5000, 9000), (2, 3)])
+@pytest.mark.parametrize("H,G,D", [(8, 4, 128), (1, 1, 256), (2, 16, 64), (32, 1, 200)])
+def test_attend_workspace_with_too_few_rows_believed(lib, n_seqs, n_rows, H, G, D):
+    """A batch of more rows than max_rows allows for is cut by the rows that there are.  Tokens are split for fewer workgroups than 256
+    compute units, into at most 512 / workgroups parts (or 256 / workgroups, if that is more), and a workgroup has at most 64 rows, so
+    there are 512 * 64 partial rows at most, of all channels in fp32, a reference and a sum."""
+    table, lengths, starts = (torch.zeros(shape, dtype=torch.int32) for shape in ((n_seqs, 2048), (n_seqs,), (n_seqs + 1,)))
+    params = _params(n_pages=4096, H=H, D=D)
+    width = ref.width_of(D)
+    bytes_of = lambda **hints: hq.hqmq_cache4_attend_workspace_bytes(params, hq.Cache4Batch(table, lengths, starts, **hints), n_rows, H * G)
+    for max_length in (300, 5000, 32768):
+        for max_rows in (1, 7, 100):
+            n = bytes_of(max_rows=max_rows, max_length=max_length)
+            assert n <= 512 * 64 * (4 * width + 8) + 256
+            if n_seqs == 1:  # all rows are its own, whatever is believed
+                assert n == bytes_of(max_rows=n_rows, max_length=max_length)
+
+
 def test_binding_refuses_shapes(lib):
     i32 = dict(dtype=torch.int32)
     table, lengths = torch.zeros(2, 5, **i32), torch.zeros(2, **i32)
