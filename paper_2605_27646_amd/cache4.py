@@ -92,8 +92,8 @@ class Cache4Buffers:
         if held is None or held[0] != key:
             codes, scales = hqmq_cache4_sizes(params)
             tensors = ((self.k_codes, codes), (self.v_codes, codes), (self.k_scales, scales), (self.v_scales, scales))
-            if any(t.nbytes < n or not t.is_contiguous() for t, n in tensors):
-                raise ValueError(f"the cache's codes must be contiguous and hold {codes} bytes, its scales {scales}")
+            if any(t.dtype is not torch.uint8 or t.nbytes < n or not t.is_contiguous() for t, n in tensors):
+                raise ValueError(f"the cache's codes must be contiguous uint8 and hold {codes} bytes, its scales {scales}")
             device = self.k_codes.get_device()
             if any(t.get_device() != device for t, _ in tensors):
                 raise ValueError("the cache's tensors must be on one device")

@@ -183,6 +183,21 @@ def test_binding_refuses_shapes(lib):
             hq.hqmq_cache4_write(params, short, batch, k, k.clone())
 
 
+@pytest.mark.parametrize("field", ["k_codes", "k_scales", "v_codes", "v_scales"])
+@pytest.mark.parametrize("dtype", [torch.int8, torch.float16, torch.int32])
+def test_buffers_are_bytes(lib, field, dtype):
+    """A tensor of another type, a key of 16-bit numbers say, is not taken for pages, however many bytes it has."""
+    params = _params()
+    k = torch.zeros(4, 4, 128, dtype=torch.float16)
+    batch = hq.Cache4Batch(torch.zeros(2, 5, dtype=torch.int32), torch.zeros(2, dtype=torch.int32))
+    cache = hq.alloc_cache4(params, "cpu")
+    setattr(cache, field, torch.zeros(1 << 20, dtype=dtype))
+    for call in (lambda: hq.hqmq_cache4_write(params, cache, batch, k, k.clone()), lambda: hq.hqmq_cache4_read(params, cache, batch, k, k.clone()),
+                 lambda: hq.hqmq_cache4_attend(params, cache, batch, k, 1.0, k.clone())):
+        with pytest.raises(ValueError, match="uint8"):
+            call()
+
+
 def test_binding_counts_of_more_than_32_bits(lib):
     table, lengths = torch.zeros(1, 4096, dtype=torch.int32), torch.zeros(1, dtype=torch.int32)
     params = _params(n_pages=4096, H=8)
