@@ -100,6 +100,7 @@ int32_t hqmq_cache4_write(const hqmq_cache4_params *params, const hqmq_cache4_bu
 
 /* Read the rows of the batch's positions back: the same positions that hqmq_cache4_write writes for the same batch (whole
  * sequences: n_i = length_i).  bf16 rows hold the cache's values rounded once more, which HQMQ_CACHE4_FLOAT's never need.
+ *   k, v  HOST; no element of both.  Beside each other in one memory (a fused projection's) they need the same strides.
  * Errors: INVALID_ARG, UNSUPPORTED, HIP. */
 int32_t hqmq_cache4_read(const hqmq_cache4_params *params, const hqmq_cache4_buffers *cache, const hqmq_cache4_batch *batch,
                          int32_t n_rows, int32_t type, const hqmq_cache4_rows *k, const hqmq_cache4_rows *v, void *stream);

@@ -1365,6 +1365,39 @@ static int32_t check_cache4_rows(const hqmq_cache4_rows *r, int32_t n_rows, int3
     return HQMQ_OK;
 }
 
+// Whether rows share an element with others that are written, each as check_cache4_rows lets them pass.  Beside each other in one memory
+// (K and V of a fused projection) they are told apart where their strides are the same: an element of both is a difference of
+// places, d = i outer + j inner + c with |i|, |j| and |c| below the counts; the last two make less than a step of the first, and the last less
+// than one of the second, so that two numbers can be i and two j.  With other strides in one memory they count as shared.
+static bool cache4_rows_share(const hqmq_cache4_rows *a, const hqmq_cache4_rows *b, int64_t n_rows, int64_t heads, int64_t D)
+{
+    const auto extent = [&](const hqmq_cache4_rows *r) { return 2 * (uint64_t)((n_rows - 1) * r->stride_row + (heads - 1) * r->stride_head + D); };
+    const uint64_t x = reinterpret_cast<uintptr_t>(a->data), y = reinterpret_cast<uintptr_t>(b->data);
+    if (x + extent(a) <= y || y + extent(b) <= x)
+        return false;
+    const bool same_rows = n_rows == 1 || a->stride_row == b->stride_row, same_heads = heads == 1 || a->stride_head == b->stride_head;
+    if (!same_rows || !same_heads)
+        return true;
+    const bool row_major = n_rows == 1 || b->stride_row >= (heads - 1) * b->stride_head + D;
+    const int64_t outer = row_major ? b->stride_row : b->stride_head, n_outer = row_major ? n_rows : heads;
+    const int64_t inner = row_major ? b->stride_head : b->stride_row, n_inner = row_major ? heads : n_rows;
+    const int64_t d = (int64_t)(x - y) / 2;
+    const auto steps = [](int64_t d, int64_t step, int64_t n, int64_t (&at)[2]) {  // the two numbers of steps next to d, 0 where there is one place
+        at[0] = n == 1 ? 0 : d / step - (d % step < 0);
+        at[1] = n == 1 ? 0 : at[0] + 1;
+    };
+    int64_t is[2], js[2];
+    steps(d, outer, n_outer, is);
+    for (const int64_t i : is) {
+        const int64_t rest = n_outer == 1 ? d : d - i * outer;
+        steps(rest, inner, n_inner, js);
+        for (const int64_t j : js)
+            if (std::abs(i) < n_outer && std::abs(j) < n_inner && std::abs(rest - (n_inner == 1 ? 0 : j * inner)) < D)
+                return true;
+    }
+    return false;
+}
+
 static Cache4Seqs make_cache4_seqs(const hqmq_cache4_batch *b, int32_t n_rows)
 {
     return Cache4Seqs{b->block_table, b->lengths, b->starts, b->n_seqs, n_rows, b->pages_per_seq, n_rows / b->n_seqs};
@@ -1399,10 +1432,10 @@ static int32_t cache4_move(bool write, const hqmq_cache4_params *params, const h
         rc = check_cache4_rows(v, n_rows, params->H, params->D, !write);
     if (rc != HQMQ_OK)
         return rc;
-    if (!write && n_rows > 0 && k->data == v->data)
-        return HQMQ_ERR_INVALID_ARG;
     if (n_rows == 0)
         return HQMQ_OK;
+    if (!write && cache4_rows_share(k, v, n_rows, params->H, params->D))
+        return HQMQ_ERR_INVALID_ARG;
     const hipError_t err = launch_cache4_rows(write, make_cache4(params, cache), make_cache4_seqs(batch, n_rows), cache4_most_rows(batch, n_rows),
                                               type == HQMQ_TYPE_BF16, make_cache4_rows(k), make_cache4_rows(v), static_cast<hipStream_t>(stream));
     return err == hipSuccess ? HQMQ_OK : hip_failed(err);

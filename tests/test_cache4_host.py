@@ -9,6 +9,7 @@ import numpy as np
 import pytest
 import torch
 
+import cache4_cpp
 import cache4_ref as ref
 import paper_2605_27646_amd as hq
 from paper_2605_27646_amd import cache4
@@ -106,6 +107,63 @@ def test_rows_that_share_elements_are_not_written(lib, what, row, head):
 
 def test_read_refuses_one_place_for_both(lib):
     assert _call(lib, "read", a=_rows(), b=_rows()) == INVALID
+
+
+@pytest.mark.parametrize("b", [
+    _rows(P + (5 << 30) + 2),                 # the second channel on
+    _rows(P + (5 << 30) + 2 * 512 * 23),      # the last row is the first
+    _rows(P + (5 << 30) - 2 * 512 * 5),       # shifted by some rows
+    _rows(P + (5 << 30) + 2 * 127),           # the last channel of a head
+    _rows(P + (5 << 30) + 2 * (512 + 64), row=1024),  # other strides in the same memory
+])
+def test_read_refuses_rows_that_share_elements(lib, b):
+    assert _call(lib, "read", a=_rows(), b=b) == INVALID
+    assert _call(lib, "read", a=b, b=_rows()) == INVALID
+
+
+SHARE = """
+extern "C" int share(uint64_t a, uint64_t b, int64_t a_row, int64_t a_head, int64_t b_row, int64_t b_head, int n, int heads, int D)
+{
+    const hqmq_cache4_rows x = {reinterpret_cast<void *>(a), a_row, a_head}, y = {reinterpret_cast<void *>(b), b_row, b_head};
+    return cache4_rows_share(&x, &y, n, heads, D);
+}
+"""
+
+
+def test_rows_that_share_elements_are_found(tmp_path):
+    """Against sets of elements: rows beside each other in one tensor share none, shifted ones do; never missed with other strides."""
+    code = cache4_cpp.between("hqmq_api.hip", "static bool cache4_rows_share", "\nstatic Cache4Seqs") + SHARE
+    host = cache4_cpp.compiled(tmp_path, code)
+    host.share.argtypes = [C.c_uint64] * 2 + [C.c_int64] * 4 + [C.c_int] * 3
+    rng = np.random.default_rng(0)
+    elements = lambda at, row, head, n, heads, D: {at + i * row + j * head + c for i in range(n) for j in range(heads) for c in range(D)}
+    seen = set()
+    for _ in range(4000):
+        n, heads, D = (int(x) for x in rng.integers(1, 5, 3))
+        strides = []
+        for _ in range(2):
+            inner = D + int(rng.integers(0, 2 * D + 2))
+            if rng.random() < 0.5:  # heads in rows, or rows in heads
+                head, row = inner, (heads - 1) * inner + D + int(rng.integers(0, 3 * D))
+            else:
+                row, head = inner, (n - 1) * inner + D + int(rng.integers(0, 3 * D))
+            strides.append((row, head))
+        if rng.random() < 0.8:
+            strides[1] = strides[0]
+        a, b = 1000, 1000 + int(rng.integers(-60, 60))
+        one, other = elements(a, *strides[0], n, heads, D), elements(b, *strides[1], n, heads, D)
+        got = bool(host.share(2 * a, 2 * b, *strides[0], *strides[1], n, heads, D))
+        shared, apart = bool(one & other), min(one) > max(other) or min(other) > max(one)
+        same = all(count == 1 or x == y for count, x, y in zip((n, heads), *strides))
+        if shared or apart or same:
+            assert got == shared, (n, heads, D, strides, b - a)
+        else:
+            assert got  # other strides in the same memory are not looked at one by one
+        seen.add((shared, apart, same))
+    assert len(seen) == 6  # what is apart shares nothing
+    far = 1 << 45  # the largest strides and counts
+    assert not host.share(far, far + 2 * 128, 1 << 30, 1 << 8, 1 << 30, 1 << 8, 1 << 30, 2, 128)
+    assert host.share(far, far + 2 * ((1 << 59) + 127), 1 << 30, 1 << 8, 1 << 30, 1 << 8, 1 << 30, 2, 128)
 
 
 @pytest.mark.parametrize("want,kw", [

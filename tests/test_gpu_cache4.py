@@ -585,6 +585,30 @@ def test_expanded_rows_are_read():
         hq.hqmq_cache4_attend(w.params, w.cache, w.batch([27, 23], [27, 23]), v, 0.1, v, torch.empty(1 << 20, dtype=torch.uint8, device=DEV))
 
 
+@pytest.mark.parametrize("fmt", FMT)
+def test_rows_beside_each_other(fmt):
+    """K and V read into one memory between each other: by rows, by heads, by channels, by role; into places that overlap they are not."""
+    w = World(84, fmt, 3, 40, 16, 2, 4)
+    lengths = [60, 21]
+    w.fill_random(lengths, F16)
+    n = sum(lengths)
+    want = [np.concatenate([w.plain.sequence(role, w.table[i], length)[0] for i, length in enumerate(lengths)]) for role in range(2)]
+    fused = lambda *shape: torch.full(shape, 7.0, dtype=F16, device=DEV)
+    a, b, c, d = fused(n, 2, 3, 40), fused(n, 3, 2, 40), fused(n, 3, 83), fused(2, 3, n, 40)
+    views = [(a[:, 0], a[:, 1]), (b[:, :, 1], b[:, :, 0]), (c[:, :, :40], c[:, :, 43:]), (d[0].transpose(0, 1), d[1].transpose(0, 1)),
+             (a.view(n, 6, 40)[:, ::2], a.view(n, 6, 40)[:, 1::2])]
+    for k, v in views:
+        hq.hqmq_cache4_read(w.params, w.cache, w.batch(lengths, lengths), k, v)
+        assert np.array_equal(_np(k), want[0]) and np.array_equal(_np(v), want[1])
+    assert (c[:, :, 40:43] == 7).all()
+    wide = fused(n + 1, 6, 41)
+    for k, v in ((wide[:-1, :3, :40], wide[1:, :3, :40]), (wide[:-1, :3, :40], wide[:-1, :3, 1:]), (wide[:-1, :3, :40], wide[:-1, 2:5, :40]),
+                 (wide[:-1, :3, :40], wide.view(-1)[:n * 3 * 40].view(n, 3, 40))):
+        with pytest.raises(hq.HqmqError):
+            hq.hqmq_cache4_read(w.params, w.cache, w.batch(lengths, lengths), k, v)
+    assert (wide == 7).all()
+
+
 def test_an_error_that_another_call_left():
     """A failed HIP call before ours is not reported as ours."""
     from paper_2605_27646_amd import binding
