@@ -81,7 +81,8 @@ typedef struct hqmq_cache4_batch {
 } hqmq_cache4_batch;
 
 /* Rows [n_rows][heads][D] with element strides, channels contiguous: HOST struct of a DEVICE pointer, aligned to 2 bytes.
- * Any alignment of 2 bytes does: rows are moved 8 channels at a time, at any address. */
+ * Any alignment of 2 bytes does: rows are moved 8 channels at a time, at any address.  Strides are 0 .. 2^30.  The memory from the
+ * first element to the last may hold anything of the caller's between the rows, but none of the cache. */
 typedef struct hqmq_cache4_rows {
     void *data;
     int64_t stride_row, stride_head;
@@ -93,7 +94,7 @@ int32_t hqmq_cache4_sizes(const hqmq_cache4_params *params, uint64_t *code_bytes
 
 /* Quantise n_rows rows of K and V (HQMQ_TYPE_*) into the pages of their sequences.  Every page that is written must be one
  * sequence's only, at one place of its table: of tokens that two of them hold in one place the result is a mixture.
- *   k, v  HOST; neither may overlap the cache.
+ *   k, v  HOST.
  * Errors: INVALID_ARG, UNSUPPORTED, HIP. */
 int32_t hqmq_cache4_write(const hqmq_cache4_params *params, const hqmq_cache4_buffers *cache, const hqmq_cache4_batch *batch,
                           int32_t n_rows, int32_t type, const hqmq_cache4_rows *k, const hqmq_cache4_rows *v, void *stream);

@@ -1365,15 +1365,29 @@ static int32_t check_cache4_rows(const hqmq_cache4_rows *r, int32_t n_rows, int3
     return HQMQ_OK;
 }
 
+// Bytes from the first element of rows to behind their last, strides and counts as check_cache4_rows lets them pass.
+static uint64_t cache4_extent(const hqmq_cache4_rows *r, int64_t n_rows, int64_t heads, int64_t D)
+{
+    return 2 * (uint64_t)((n_rows - 1) * r->stride_row + (heads - 1) * r->stride_head + D);
+}
+
+static bool cache4_rows_over_cache(const hqmq_cache4_params *p, const hqmq_cache4_buffers *c, const hqmq_cache4_rows *r, int32_t n_rows, int32_t heads)
+{
+    uint64_t codes = 0, scales = 0;
+    hqmq_cache4_sizes(p, &codes, &scales);
+    const uint64_t x = reinterpret_cast<uintptr_t>(r->data), end = x + cache4_extent(r, n_rows, heads, p->D);
+    const auto over = [&](const void *at, uint64_t bytes) { return x < reinterpret_cast<uintptr_t>(at) + bytes && reinterpret_cast<uintptr_t>(at) < end; };
+    return over(c->k_codes, codes) || over(c->v_codes, codes) || over(c->k_scales, scales) || over(c->v_scales, scales);
+}
+
 // Whether rows share an element with others that are written, each as check_cache4_rows lets them pass.  Beside each other in one memory
 // (K and V of a fused projection) they are told apart where their strides are the same: an element of both is a difference of
 // places, d = i outer + j inner + c with |i|, |j| and |c| below the counts; the last two make less than a step of the first, and the last less
 // than one of the second, so that two numbers can be i and two j.  With other strides in one memory they count as shared.
 static bool cache4_rows_share(const hqmq_cache4_rows *a, const hqmq_cache4_rows *b, int64_t n_rows, int64_t heads, int64_t D)
 {
-    const auto extent = [&](const hqmq_cache4_rows *r) { return 2 * (uint64_t)((n_rows - 1) * r->stride_row + (heads - 1) * r->stride_head + D); };
     const uint64_t x = reinterpret_cast<uintptr_t>(a->data), y = reinterpret_cast<uintptr_t>(b->data);
-    if (x + extent(a) <= y || y + extent(b) <= x)
+    if (x + cache4_extent(a, n_rows, heads, D) <= y || y + cache4_extent(b, n_rows, heads, D) <= x)
         return false;
     const bool same_rows = n_rows == 1 || a->stride_row == b->stride_row, same_heads = heads == 1 || a->stride_head == b->stride_head;
     if (!same_rows || !same_heads)
@@ -1434,7 +1448,8 @@ static int32_t cache4_move(bool write, const hqmq_cache4_params *params, const h
         return rc;
     if (n_rows == 0)
         return HQMQ_OK;
-    if (!write && cache4_rows_share(k, v, n_rows, params->H, params->D))
+    if (cache4_rows_over_cache(params, cache, k, n_rows, params->H) || cache4_rows_over_cache(params, cache, v, n_rows, params->H) ||
+        (!write && cache4_rows_share(k, v, n_rows, params->H, params->D)))
         return HQMQ_ERR_INVALID_ARG;
     const hipError_t err = launch_cache4_rows(write, make_cache4(params, cache), make_cache4_seqs(batch, n_rows), cache4_most_rows(batch, n_rows),
                                               type == HQMQ_TYPE_BF16, make_cache4_rows(k), make_cache4_rows(v), static_cast<hipStream_t>(stream));
@@ -1503,6 +1518,8 @@ extern "C" int32_t hqmq_cache4_attend(const hqmq_cache4_params *params, const hq
         return HQMQ_ERR_UNSUPPORTED;
     if (n_rows == 0)
         return HQMQ_OK;
+    if (cache4_rows_over_cache(params, cache, q, n_rows, n_q_heads) || cache4_rows_over_cache(params, cache, out, n_rows, n_q_heads))
+        return HQMQ_ERR_INVALID_ARG;
     const Cache4Plan plan = cache4_plan(params, batch, n_rows, n_q_heads, window);
     if (plan.ml_bytes + plan.acc_bytes > 0) {
         if (!workspace_dev)

@@ -121,6 +121,21 @@ def test_read_refuses_rows_that_share_elements(lib, b):
     assert _call(lib, "read", a=b, b=_rows()) == INVALID
 
 
+@pytest.mark.parametrize("what", ["write", "read", "attend"])
+@pytest.mark.parametrize("which", ["a", "b"])
+@pytest.mark.parametrize("buffer", range(4))
+@pytest.mark.parametrize("at", ["first", "last", "around"])
+def test_rows_over_the_cache_are_refused(lib, what, which, buffer, at):
+    """Rows that begin inside one of the cache's buffers, end inside it, or enclose it."""
+    sizes = hq.hqmq_cache4_sizes(_params())
+    base, n = P + (buffer << 30), sizes[buffer % 2]
+    row = 1024 if what == "attend" else 512
+    heads = 8 if what == "attend" else 4
+    extent = 2 * (23 * row + (heads - 1) * 128 + 128)
+    rows = {"first": _rows(base + n - 2, row=row), "last": _rows(base - extent + 2, row=row), "around": _rows(base - 4096, row=(n + 8192) // 2)}[at]
+    assert _call(lib, what, **{which: rows}) == INVALID
+
+
 SHARE = """
 extern "C" int share(uint64_t a, uint64_t b, int64_t a_row, int64_t a_head, int64_t b_row, int64_t b_head, int n, int heads, int D)
 {
@@ -132,7 +147,8 @@ extern "C" int share(uint64_t a, uint64_t b, int64_t a_row, int64_t a_head, int6
 
 def test_rows_that_share_elements_are_found(tmp_path):
     """Against sets of elements: rows beside each other in one tensor share none, shifted ones do; never missed with other strides."""
-    code = cache4_cpp.between("hqmq_api.hip", "static bool cache4_rows_share", "\nstatic Cache4Seqs") + SHARE
+    code = cache4_cpp.between("hqmq_api.hip", "static uint64_t cache4_extent", "static bool cache4_rows_over_cache")
+    code += cache4_cpp.between("hqmq_api.hip", "static bool cache4_rows_share", "\nstatic Cache4Seqs") + SHARE
     host = cache4_cpp.compiled(tmp_path, code)
     host.share.argtypes = [C.c_uint64] * 2 + [C.c_int64] * 4 + [C.c_int] * 3
     rng = np.random.default_rng(0)
