@@ -114,8 +114,8 @@ int32_t hqmq_cache4_read(const hqmq_cache4_params *params, const hqmq_cache4_buf
  * rows, whose results have 8.  Tokens that no row of a sequence sees (behind the last row, before the first one's window) may
  * hold anything, and their pages may be none, or another's.  A query that holds an infinity or a NaN gives NaN, in its own row.
  *   n_q_heads   a multiple of H, at most 65535.
- *   q, out      HOST; rows of type `type`, [n_rows][n_q_heads][D]; out may be q itself with the same strides only if no two
- *               rows share elements.  A row that sees nothing gets zeros.
+ *   q, out      HOST; rows of type `type`, [n_rows][n_q_heads][D]; out may be q itself with the same strides, and may share no
+ *               element with it otherwise (in one memory between each other they need the same strides).  A row that sees nothing gets zeros.
  *   scale       finite, at most 2^100 in magnitude; scale q_c and scores are to stay below 2^126 (behind it scores tie, or
  *               count as unseen).
  *   window      0: none; else the number of tokens that a row sees at most, its own included.

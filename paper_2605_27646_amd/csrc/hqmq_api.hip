@@ -1380,6 +1380,11 @@ static bool cache4_rows_over_cache(const hqmq_cache4_params *p, const hqmq_cache
     return over(c->k_codes, codes) || over(c->v_codes, codes) || over(c->k_scales, scales) || over(c->v_scales, scales);
 }
 
+static bool cache4_same_strides(const hqmq_cache4_rows *a, const hqmq_cache4_rows *b, int64_t n_rows, int64_t heads)
+{
+    return (n_rows == 1 || a->stride_row == b->stride_row) && (heads == 1 || a->stride_head == b->stride_head);
+}
+
 // Whether rows share an element with others that are written, each as check_cache4_rows lets them pass.  Beside each other in one memory
 // (K and V of a fused projection) they are told apart where their strides are the same: an element of both is a difference of
 // places, d = i outer + j inner + c with |i|, |j| and |c| below the counts; the last two make less than a step of the first, and the last less
@@ -1389,8 +1394,7 @@ static bool cache4_rows_share(const hqmq_cache4_rows *a, const hqmq_cache4_rows 
     const uint64_t x = reinterpret_cast<uintptr_t>(a->data), y = reinterpret_cast<uintptr_t>(b->data);
     if (x + cache4_extent(a, n_rows, heads, D) <= y || y + cache4_extent(b, n_rows, heads, D) <= x)
         return false;
-    const bool same_rows = n_rows == 1 || a->stride_row == b->stride_row, same_heads = heads == 1 || a->stride_head == b->stride_head;
-    if (!same_rows || !same_heads)
+    if (!cache4_same_strides(a, b, n_rows, heads))
         return true;
     const bool row_major = n_rows == 1 || b->stride_row >= (heads - 1) * b->stride_head + D;
     const int64_t outer = row_major ? b->stride_row : b->stride_head, n_outer = row_major ? n_rows : heads;
@@ -1519,6 +1523,10 @@ extern "C" int32_t hqmq_cache4_attend(const hqmq_cache4_params *params, const hq
     if (n_rows == 0)
         return HQMQ_OK;
     if (cache4_rows_over_cache(params, cache, q, n_rows, n_q_heads) || cache4_rows_over_cache(params, cache, out, n_rows, n_q_heads))
+        return HQMQ_ERR_INVALID_ARG;
+    // A workgroup has read its rows' queries before it writes their results, but not another's.
+    const bool in_place = q->data == out->data && cache4_same_strides(q, out, n_rows, n_q_heads);
+    if (!in_place && cache4_rows_share(q, out, n_rows, n_q_heads, params->D))
         return HQMQ_ERR_INVALID_ARG;
     const Cache4Plan plan = cache4_plan(params, batch, n_rows, n_q_heads, window);
     if (plan.ml_bytes + plan.acc_bytes > 0) {

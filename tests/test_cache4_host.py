@@ -136,6 +136,17 @@ def test_rows_over_the_cache_are_refused(lib, what, which, buffer, at):
     assert _call(lib, what, **{which: rows}) == INVALID
 
 
+@pytest.mark.parametrize("b", [
+    _rows(P + (5 << 30) + 2 * 1024, row=1024),          # the result of a row over the next row's queries
+    _rows(P + (5 << 30) - 2 * 1024 * 20, row=1024),
+    _rows(P + (5 << 30) + 2 * 128, row=1024),           # over the next head's
+    _rows(P + (5 << 30) + 2, row=1024),
+    _rows(P + (5 << 30), row=1024 + 128),               # from the same place on, with other strides
+])
+def test_attend_refuses_results_over_other_queries(lib, b):
+    assert _call(lib, "attend", a=_rows(row=1024), b=b) == INVALID
+
+
 SHARE = """
 extern "C" int share(uint64_t a, uint64_t b, int64_t a_row, int64_t a_head, int64_t b_row, int64_t b_head, int n, int heads, int D)
 {
@@ -148,7 +159,7 @@ extern "C" int share(uint64_t a, uint64_t b, int64_t a_row, int64_t a_head, int6
 def test_rows_that_share_elements_are_found(tmp_path):
     """Against sets of elements: rows beside each other in one tensor share none, shifted ones do; never missed with other strides."""
     code = cache4_cpp.between("hqmq_api.hip", "static uint64_t cache4_extent", "static bool cache4_rows_over_cache")
-    code += cache4_cpp.between("hqmq_api.hip", "static bool cache4_rows_share", "\nstatic Cache4Seqs") + SHARE
+    code += cache4_cpp.between("hqmq_api.hip", "static bool cache4_same_strides", "\nstatic Cache4Seqs") + SHARE
     host = cache4_cpp.compiled(tmp_path, code)
     host.share.argtypes = [C.c_uint64] * 2 + [C.c_int64] * 4 + [C.c_int] * 3
     rng = np.random.default_rng(0)

@@ -738,6 +738,28 @@ def test_result_over_the_queries():
         assert torch.equal(q, out)
 
 
+def test_result_beside_the_queries():
+    """In the place of a fused projection's other heads, whose strides the queries have; one row of any strides over itself."""
+    w = World(96, hq.HQMQ_CACHE4_FLOAT, 2, 64, 16, 2, 20)
+    lengths = [300, 120]
+    w.fill_random(lengths, F16)
+    fused = w.values(2, F16, heads=12)
+    q, out = fused[:, 4:8], torch.empty(2, 4, 64, dtype=F16, device=DEV)
+    others = fused[:, :4].clone(), q.clone()
+    ws = torch.empty(hq.hqmq_cache4_attend_workspace_bytes(w.params, w.batch(lengths), 2, 4) + 1, dtype=torch.uint8, device=DEV)
+    hq.hqmq_cache4_attend(w.params, w.cache, w.batch(lengths), q, 0.1, out, ws)
+    hq.hqmq_cache4_attend(w.params, w.cache, w.batch(lengths), q, 0.1, fused[:, 8:], ws)
+    assert torch.equal(fused[:, 8:], out) and torch.equal(fused[:, :4], others[0]) and torch.equal(q, others[1])
+    for bad in (fused[:, 5:9], fused[:, 2:6]):
+        with pytest.raises(hq.HqmqError):
+            hq.hqmq_cache4_attend(w.params, w.cache, w.batch(lengths), q, 0.1, bad, ws)
+    assert torch.equal(fused[:, 8:], out) and torch.equal(fused[:, :4], others[0]) and torch.equal(q, others[1])
+    w.table, w.n_seqs = w.table[:1], 1
+    one, single = q[:1].as_strided((1, 4, 64), (64, 768 // 12, 1)), out[:1]
+    hq.hqmq_cache4_attend(w.params, w.cache, w.batch(lengths[:1]), one, 0.1, one.as_strided((1, 4, 64), (999, 64, 1)), ws)
+    assert torch.equal(one, single)
+
+
 def test_rows_of_no_sequence_are_left():
     """Rows before the first and behind the last sequence, with and without splits of the tokens."""
     w = World(97, hq.HQMQ_CACHE4_FLOAT, 1, 64, 16, 2, 100)
