@@ -21,6 +21,11 @@ class Cache4Params(C.Structure):
     """n_pages, page_size (a power of two, 16 or more), H kv heads, D channels of a head, format (HQMQ_CACHE4_*)."""
     _fields_ = [("n_pages", C.c_int32), ("page_size", C.c_int32), ("H", C.c_int32), ("D", C.c_int32), ("format", C.c_int32)]
 
+    def __setattr__(self, name, value):
+        if not -2 ** 31 <= value < 2 ** 31:  # the field would keep the low bits
+            raise ValueError(f"{name} must fit 32 bits")
+        super().__setattr__(name, value)
+
 
 class _Buffers(C.Structure):
     _fields_ = [("k_codes", C.c_void_p), ("k_scales", C.c_void_p), ("v_codes", C.c_void_p), ("v_scales", C.c_void_p)]
@@ -179,7 +184,10 @@ def hqmq_cache4_read(params: Cache4Params, cache: Cache4Buffers, batch: Cache4Ba
 
 
 def hqmq_cache4_attend_workspace_bytes(params: Cache4Params, batch: Cache4Batch, n_rows: int, n_q_heads: int, window: int = 0) -> int:
-    return int(_load().hqmq_cache4_attend_workspace_bytes(C.byref(params), C.byref(batch.struct), int(n_rows), int(n_q_heads), _count(window)))
+    n_rows, n_q_heads = int(n_rows), int(n_q_heads)
+    if (n_rows | n_q_heads) >> 31:  # as every number of rows or heads that the calls refuse
+        return 0
+    return int(_load().hqmq_cache4_attend_workspace_bytes(C.byref(params), C.byref(batch.struct), n_rows, n_q_heads, _count(window)))
 
 
 def hqmq_cache4_attend(params: Cache4Params, cache: Cache4Buffers, batch: Cache4Batch, q: torch.Tensor, scale: float, out: torch.Tensor,

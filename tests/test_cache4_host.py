@@ -297,6 +297,24 @@ def test_binding_counts_of_more_than_32_bits(lib):
             hq.hqmq_cache4_attend(_params(), cache, batch, many, 1.0, many)
 
 
+def test_binding_sizes_of_more_than_32_bits(lib):
+    """A number of rows, heads, pages or anything else that 32 bits do not hold is no number that they would hold."""
+    table, lengths = torch.zeros(1, 4096, dtype=torch.int32), torch.zeros(1, dtype=torch.int32)
+    params, batch = _params(n_pages=4096, H=8), hq.Cache4Batch(table, lengths)
+    assert hq.hqmq_cache4_attend_workspace_bytes(params, batch, 1, 32) > 0
+    for rows, heads in ((2 ** 32 + 1, 32), (1, 2 ** 32 + 32), (1 - 2 ** 32, 32), (2 ** 31, 32)):
+        assert hq.hqmq_cache4_attend_workspace_bytes(params, batch, rows, heads) == 0
+    for name in ("n_pages", "page_size", "H", "D", "format"):
+        for value in (2 ** 32 + 16, -2 ** 32 + 16, 2 ** 31):
+            with pytest.raises(ValueError, match="32 bits"):
+                _params(**{name: value})
+            with pytest.raises(ValueError, match="32 bits"):
+                setattr(params, name, value)
+    assert hq.hqmq_cache4_sizes(params) == hq.hqmq_cache4_sizes(_params(n_pages=4096, H=8))
+    with pytest.raises(ValueError, match="32 bits"):
+        hq.Cache4Params(n_pages=2 ** 32 + 100, page_size=16, H=8, D=128, format=0)
+
+
 PLACES = """
 #include <cstdio>
 #include <initializer_list>
