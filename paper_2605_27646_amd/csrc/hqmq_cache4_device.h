@@ -84,8 +84,9 @@ __device__ __forceinline__ cache4_u4 last_of(cache4_u4 x, int n)
     return x;
 }
 
-// Division of numbers below 2^30 by one that the host knows: with l = ceil(log2 d) and m = ceil(2^(30 + l) / d), which is at most 2^30 + 1,
-// n m / 2^(30 + l) exceeds n / d by less than 2^l / 2^(30 + l) * n < 1 / d, and so has the same whole part.
+// Division of numbers below 2^30 by one that the host knows: with l = ceil(log2 d) and m = ceil(2^(30 + l) / d), which is at most 2^31
+// (2^l < 2 d) and makes products below 2^61, m is less than 1 above 2^(30 + l) / d.  So n m / 2^(30 + l) exceeds n / d by less than
+// n / 2^(30 + l) <= n / (2^30 d) < 1 / d, and has the same whole part: the next one is 1 / d away at least.
 struct Divisor {
     uint32_t mul, shift;
 };

@@ -315,6 +315,39 @@ def test_binding_sizes_of_more_than_32_bits(lib):
         hq.Cache4Params(n_pages=2 ** 32 + 100, page_size=16, H=8, D=128, format=0)
 
 
+DIVIDED = """
+// The first number that is divided wrongly, the largest factor, and the largest product with it; beside every multiple of d, and at the ends.
+extern "C" int64_t check(uint32_t from, uint32_t to, uint64_t *mul, uint64_t *product)
+{
+    constexpr uint64_t kEnd = 1ull << 30;
+    for (uint32_t d = from; d <= to; ++d) {
+        const Divisor by = make_divisor(d);
+        *mul = std::max<uint64_t>(*mul, by.mul);
+        *product = std::max(*product, (kEnd - 1) * by.mul);
+        const uint64_t multiples = (kEnd - 1) / d, stride = multiples / 3000 + 1;
+        for (uint64_t k = 0; k <= multiples; k += k < 64 || k + 64 > multiples ? 1 : stride)
+            for (uint64_t n = k * d == 0 ? 0 : k * d - 1; n <= k * d + 1 && n < kEnd; ++n)
+                if ((uint64_t)divided((int)n, by) != n / d)
+                    return (int64_t)n;
+        if ((uint64_t)divided((int)(kEnd - 1), by) != (kEnd - 1) / d)
+            return (int64_t)kEnd - 1;
+    }
+    return -1;
+}
+"""
+
+
+def test_division_by_multiplication(tmp_path):
+    """Every divisor that there is (query heads of a kv head, dwords of a row, parts of the tokens), numbers up to 2^30 - 1 where a quotient
+    changes; and the sizes that the proof names: a factor of at most 2^31, products below 2^61."""
+    host = cache4_cpp.compiled(tmp_path, cache4_cpp.between("hqmq_cache4_device.h", "struct Divisor {", "// What no kernel writes") + DIVIDED)
+    host.check.restype, host.check.argtypes = C.c_int64, [C.c_uint32, C.c_uint32, C.POINTER(C.c_uint64), C.POINTER(C.c_uint64)]
+    mul, product = C.c_uint64(), C.c_uint64()
+    for first, last in ((1, 300), (32767, 32770), (65000, 65535)):
+        assert host.check(first, last, C.byref(mul), C.byref(product)) == -1
+    assert 2 ** 30 + 1 < mul.value <= 2 ** 31 and product.value < 2 ** 61
+
+
 PLACES = """
 #include <cstdio>
 #include <initializer_list>
