@@ -11,6 +11,7 @@ import torch
 
 import cache4_cpp
 import cache4_ref as ref
+from cache4_plan import plan
 import paper_2605_27646_amd as hq
 from paper_2605_27646_amd import cache4
 
@@ -238,6 +239,17 @@ def test_attend_workspace_with_too_few_rows_believed(lib, n_seqs, n_rows, H, G, 
             assert n <= 512 * 64 * (4 * width + 8) + 256
             if n_seqs == 1:  # all rows are its own, whatever is believed
                 assert n == bytes_of(max_rows=n_rows, max_length=max_length)
+
+
+def test_attend_plan_of_too_few_rows_believed(lib):
+    """One sequence of 4096 rows is cut the same way whatever max_rows says; of several, by the rows that they have on average."""
+    right = plan(8, 128, 64, 1, 512, 4096, 32, max_rows=4096, max_length=32768)
+    assert (right.blocks, right.n_tiles, right.n_splits) == (4, 256, 1)
+    for believed in (1, 100, 4095):
+        assert plan(8, 128, 64, 1, 512, 4096, 32, max_rows=believed, max_length=32768) == right
+    assert plan(8, 128, 64, 4, 512, 4096, 32, max_rows=1) == plan(8, 128, 64, 4, 512, 4096, 32, max_rows=1024) == plan(8, 128, 64, 4, 512, 4096, 32, starts=False)
+    # what is believed rightly is left as it is: a step of 64 sequences, and one with a prompt
+    assert plan(8, 128, 16, 64, 512, 64, 32, max_rows=1)[:3] == (1, 1, 1) and plan(8, 128, 16, 64, 512, 63 + 2048, 32, max_rows=2048).blocks == 4
 
 
 def test_binding_refuses_shapes(lib):
