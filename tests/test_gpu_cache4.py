@@ -294,6 +294,60 @@ def test_starts_that_do_not_ascend():
     torch.cuda.synchronize()
 
 
+class Fenced:
+    """Tensors in the middle of larger ones; whole() says whether what lies around them is as it was."""
+
+    def __init__(self):
+        self.all = []
+
+    def tensor(self, *shape, dtype):
+        item = torch.empty(0, dtype=dtype).element_size()
+        n, margin = int(np.prod(shape)) * item, 1 << 16
+        whole = torch.full((n + 2 * margin,), 0xA5, dtype=torch.uint8, device=DEV)
+        self.all.append((whole, margin, n))
+        return whole[margin:margin + n].view(dtype).view(shape)
+
+    def whole(self):
+        return all(bool((t[:m] == 0xA5).all()) and bool((t[m + n:] == 0xA5).all()) for t, m, n in self.all)
+
+
+@pytest.mark.parametrize("fmt,dtype,D", [(hq.HQMQ_CACHE4_FLOAT, F16, 64), (hq.HQMQ_CACHE4_INT, BF16, 100)])
+@pytest.mark.parametrize("pages", [4, 80])
+def test_starts_that_do_not_ascend_reach_nothing_else(fmt, dtype, D, pages):
+    """Every tensor that the calls write lies between others: what is around them, and pages of no sequence, keep their bytes, with places of each
+    sequence and along all rows, with tokens in parts and whole."""
+    n_seqs, H, n, spare = 80 if pages == 4 else 6, 4, 700 if pages == 4 else 12, 3
+    rng = np.random.default_rng(pages)
+    params = hq.Cache4Params(n_seqs * pages + spare, 16, H, D, fmt)
+    fence = Fenced()
+    cache = hq.Cache4Buffers(*(fence.tensor(size, dtype=torch.uint8) for size in hq.hqmq_cache4_sizes(params) * 2))
+    buffers = (cache.k_codes, cache.k_scales, cache.v_codes, cache.v_scales)
+    order = rng.permutation(params.n_pages)
+    table, unused = torch.tensor(order[:-spare].reshape(n_seqs, pages).astype(np.int32), device=DEV), torch.tensor(order[-spare:], device=DEV)
+    for t in buffers:
+        t.zero_()
+        t.view(params.n_pages, -1)[unused] = 0x5A
+    out, back_k, back_v = (fence.tensor(n, heads, D, dtype=dtype) for heads in (16, H, H))
+    lse = fence.tensor(n, 16, dtype=torch.float32)
+    make = lambda heads: torch.tensor(rng.standard_normal((n, heads, D)), dtype=dtype, device=DEV)
+    k, v, q = make(H), make(H), make(16)
+    seen = set()
+    for seed in range(6):
+        g = torch.Generator().manual_seed(seed)
+        starts = torch.randint(-50, n + 50, (n_seqs + 1,), generator=g).to(torch.int32).to(DEV)
+        lengths = torch.randint(-5, 16 * pages + 16, (n_seqs,), generator=g).to(torch.int32).to(DEV)
+        for hint in (1, n):
+            batch = hq.Cache4Batch(table, lengths, starts, max_rows=hint)
+            ws = fence.tensor(max(256, hq.hqmq_cache4_attend_workspace_bytes(params, batch, n, 16)), dtype=torch.uint8)
+            seen.add(ws.numel() > 256)
+            hq.hqmq_cache4_write(params, cache, batch, k, v)
+            hq.hqmq_cache4_read(params, cache, batch, back_k, back_v)
+            hq.hqmq_cache4_attend(params, cache, batch, q, 0.1, out, ws, lse=lse)
+            assert fence.whole(), (seed, hint)
+            assert all(bool((t.view(params.n_pages, -1)[unused] == 0x5A).all()) for t in buffers), (seed, hint)
+    assert seen == {pages == 80}
+
+
 @pytest.mark.parametrize("hint", [1, 200, 1024, 2048, 2 ** 30])
 @pytest.mark.parametrize("rows", [1, 20])
 def test_attend_splits_and_hints(hint, rows):
@@ -489,6 +543,31 @@ def test_one_prompt_among_many_steps(fmt, dtype):
         assert torch.equal(back[0][row].cpu(), want), row
     _check_attend(w, lengths, rows, dtype, 4, max_rows=600, max_length=640)
     _check_attend(w, lengths, rows, dtype, 4, max_rows=1, max_length=640)
+
+
+@pytest.mark.parametrize("fmt,dtype", [(hq.HQMQ_CACHE4_FLOAT, BF16), (hq.HQMQ_CACHE4_INT, F16)])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("ragged", [False, True])
+def test_one_head_of_many_rows(fmt, dtype, D, ragged):
+    """A shard of a model: one kv head, thousands of rows, in one sequence or most of them in one of many."""
+    n = 40 if ragged else 1
+    w = World(D + n, fmt, 1, D, 64, n, 66)
+    rows = [3] * n
+    rows[n // 2] = 4101
+    lengths = [int(x) for x in w.rng.integers(3, 100, n)]
+    lengths[n // 2] = 4201
+    k, v = (w.values(sum(rows), dtype, hot=role == 0) for role in range(2))
+    batch = w.batch(lengths, rows)
+    hq.hqmq_cache4_write(w.params, w.cache, batch, k, v)
+    w.write_plain(lengths, rows, k, v)
+    w.same_bytes()
+    back = [torch.full_like(x, float("nan")) for x in (k, v)]
+    hq.hqmq_cache4_read(w.params, w.cache, batch, *back)
+    back = [_np(x) for x in back]
+    for row, i, pos in w.places(lengths, rows):
+        for role in range(2):
+            want = torch.tensor(w.plain.get(role, int(w.table[i, pos // 64]), pos % 64)).to(dtype).double().numpy()
+            assert np.array_equal(back[role][row], want), (row, role)
 
 
 def test_thousands_of_sequences():
