@@ -63,7 +63,9 @@ typedef struct hqmq_cache4_buffers {
 
 /* A batch: HOST struct.
  *   block_table DEVICE, int32 [n_seqs][pages_per_seq]; entries behind a sequence's last page are not used.
- *   lengths     DEVICE, int32 [n_seqs]: negative ones count as 0, larger ones as pages_per_seq * page_size.
+ *   lengths     DEVICE, int32 [n_seqs]: negative ones count as 0, larger ones as pages_per_seq * page_size.  Rows are placed by what
+ *               counts: of a sequence grown past its table's room the last places are written again, and what they held is lost.
+ *               The table needs the page of a step's tokens before the step is enqueued.
  *   starts      DEVICE, int32 [n_seqs + 1], ascending, or NULL: every sequence has n_rows / n_seqs rows.  Rows outside
  *               starts[0] .. starts[n_seqs] - 1 are no sequence's: they are not read, nor written.
  *   max_rows, max_length   the largest number of rows and length of a sequence as far as the host knows them: they shape
@@ -111,7 +113,8 @@ int32_t hqmq_cache4_read(const hqmq_cache4_params *params, const hqmq_cache4_buf
  *     o = sum_t e^{s_t - M} V_t / sum_t e^{s_t - M},  s_t = scale <q, K_t>
  * over the fp16 values of the cache.  Products are accumulated in fp32, the softmax subtracts a running reference, the
  * result is rounded once.  Weights enter the products with V with 22 significant bits for fp16 rows, and with 11 for bf16
- * rows, whose results have 8.  Tokens that no row of a sequence sees (behind the last row, before the first one's window) may
+ * rows, whose results have 8, none finer than 2^-31 of the row's largest; their sum and lse are of the weights as fp32 has them.  Queries
+ * of bf16 enter as fp16 behind a power of two per row, which rounds channels below 2^-28 of the row's largest.  Tokens that no row of a sequence sees (behind the last row, before the first one's window) may
  * hold anything, and their pages may be none, or another's.  A query that holds an infinity or a NaN gives NaN, in its own row.
  *   n_q_heads   a multiple of H, at most 65535.
  *   q, out      HOST; rows of type `type`, [n_rows][n_q_heads][D]; out may be q itself with the same strides, and may share no

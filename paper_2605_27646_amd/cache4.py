@@ -120,7 +120,8 @@ class Cache4Batch:
     """Which rows a call has and where their tokens lie: block_table (int32 [n_seqs, pages_per_seq]), lengths (int32 [n_seqs], the
     call's rows included), starts (int32 [n_seqs + 1], ascending; None: equal shares).  max_rows and max_length: the largest as
     far as the host knows them, by default all rows (of starts) and all that the table has room for; they shape the launch, and
-    every row and token counts whatever they say.  The tensors are read when the calls run, so that one batch serves many steps; they have to stay in place."""
+    every row and token counts whatever they say.  A max_length near the lengths makes short steps fast.  A length past the table's room
+    counts as that room, so that write replaces the last tokens kept: give the table its next page before the step that needs it.  The tensors are read when the calls run, so that one batch serves many steps; they have to stay in place."""
 
     def __init__(self, block_table: torch.Tensor, lengths: torch.Tensor, starts: torch.Tensor | None = None, max_rows: int | None = None,
                  max_length: int | None = None):

@@ -13,8 +13,12 @@
 //
 // Bound by memory for generation steps of many long sequences (64 of up to 8192 tokens, 8 heads x 128: 69 to 73 us, 301 MB at 4.2 to 4.4 TB/s,
 // vector instructions issue for a third of the time), by a workgroup's start and the join for short ones (130 tokens 6 us, of which
-// one step is 1), and by issue for prompts (1024 tokens of two sequences behind 15000: 435 us, 1.20 PFLOP/s, vector instructions
-// 61 % and matrix instructions 42 % of the time; of the former 37 % are exponentials, 33 % the reconstruction for 64 rows).
+// one step is 1), and by issue for prompts (1024 tokens of two sequences behind 15000, bf16: 437 us, 1.19 PFLOP/s, 425 to 450 over inputs
+// and machines; of the kernel's 428 us in a trace vector instructions are 70 % and matrix instructions 48 %; of the former 37 % are exponentials,
+// 33 % the reconstruction for 64 rows).  With fp16 rows the second product runs twice: 629 us.
+//
+// Registers: 64 rows of 128 channels and 32 of 256 need all 256, and 8 to 25 more that are kept in scratch (28 to 72 bytes a lane).  A step
+// reads 2 to 9 words of them back and writes 2 at most, beside its 64 to 128 matrix instructions.
 #include <algorithm>
 #include <type_traits>
 
@@ -382,6 +386,9 @@ __global__ __launch_bounds__(64 * attend_waves(kBlocks), attend_occupancy(NG, kB
     constexpr int kRows = 16 * kBlocks, kChannels = 2 * NG;  // of a lane
     constexpr int kWaves = attend_waves(kBlocks), kPitch = attend_pitch(NG);
     static_assert(kBlocks <= kWaves, "a wave stages a block of queries");
+    // fp16 rows take weights in two parts.  bf16 rows take the first alone, 11 bits for results of 8: it moves a tenth of the results to the
+    // neighbouring bf16 number, the error against 64 bits is 0.5 to 0.7 % above that of rounding alone, and two parts take half as much matrix
+    // work again (the chunk above: 629 us with fp16 rows).  The sum stays that of the fp32 weights, because lse has 24 bits.
     constexpr bool kFine = !kBf16;
     extern __shared__ __align__(16) unsigned char lds[];
     constexpr size_t kShared = attend_shared_bytes(NG, kBlocks);
@@ -925,7 +932,9 @@ __global__ __launch_bounds__(kMergeThreads) void k_cache4_merge(Cache4Attend a)
     }
 }
 
-// How a call is cut.  Times are of 8 kv heads x 128 channels in the float format, 4 query heads a kv head, unless said otherwise.
+// How a call is cut.  Times are of 8 kv heads x 128 channels in the float format, 4 query heads a kv head, unless said otherwise, and of
+// calls whose max_length is the longest length.  Tokens are shared out by max_length, so that shorter sequences leave parts without
+// tokens: with room for 131072, one step of one sequence of 8192 tokens 21 us for 10, of eight 55 for 19.
 //   - Rows of a workgroup: 16 as long as that makes no more than a workgroup for each compute unit, 32 up to twice that many, then 64;
 //     never so many that a smaller form would hold all rows of a sequence.  More rows share the reconstruction, fewer keep more units
 //     at work.  16 / 32 / 64 rows: 20 new tokens behind 2000 12.7 / 14.3 / 17.7 us, 128 behind 8000 38 / 41 / 43, 512 behind 8000
@@ -937,7 +946,7 @@ __global__ __launch_bounds__(kMergeThreads) void k_cache4_merge(Cache4Attend a)
 //     (two sequences of 8000: 13.5 us, with one step 14.4, with four 14.9) or of one, if that makes 16 at most (one of 4000: 10.5 us,
 //     with two steps 11.4).  Four steps are not split (8 sequences of up to 1500 tokens, 5 rows: 13.1 us, in two 14.9).
 //   - Where a launch of the largest sequence's tiles for each would be mostly empty, places are dealt along all rows and a workgroup finds
-//     its sequence (2048 rows among 63 single ones: 192 us without, 93 with; among 255 360 and 116).
+//     its sequence (2048 rows among 63 single ones: 192 us without, 93 with; among 255 360 and 116; later steps brought these to 76 and 103).
 constexpr int kUnits = 256;  // compute units
 constexpr int kFewSplits = 32;
 constexpr int kOneStepSplits = 16;
