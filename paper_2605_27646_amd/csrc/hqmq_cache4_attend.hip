@@ -13,7 +13,7 @@
 //
 // Bound by memory for generation steps of many long sequences (64 of up to 8192 tokens, 8 heads x 128: 69 to 73 us, 301 MB at 4.2 to 4.4 TB/s,
 // vector instructions issue for a third of the time), by a workgroup's start and the join for short ones (130 tokens 6 us, of which
-// one step is 1), and by issue for prompts (1024 tokens of two sequences behind 15000, bf16: 437 us, 1.19 PFLOP/s, 425 to 450 over inputs
+// one step is 1), and by issue for prompts (1024 tokens of two sequences behind 15000, bf16: 437 us, 1.19 PFLOP/s, 425 to 455 over inputs
 // and machines; of the kernel's 428 us in a trace vector instructions are 70 % and matrix instructions 48 %; of the former 37 % are exponentials,
 // 33 % the reconstruction for 64 rows).  With fp16 rows the second product runs twice: 629 us.
 //
